@@ -31,6 +31,9 @@ EXPORTS = [
     "slim_sba_allocate", "slim_sba_prepare", "slim_sqc_calibrate", "slim_gptq_quantize", "slim_pack", "slim_dequant_matmul",
     "slim_dequant_matmul_noalloc", "slim_dequant_matmul_zp", "slim_dequant_matmul_handover",
     "slim_transpose_16", "slim_pack_zeros", "slim_unpack_zeros", "slim_lwc_quantize",
+    "slim_fp8_quantize_weights", "slim_fp8_linear_workspace", "slim_fp8_linear", "slim_fp8_linear_backward_workspace",
+    "slim_fp8_linear_backward", "slim_layer_norm", "slim_layer_norm_backward_workspace", "slim_layer_norm_backward",
+    "slim_distill_loss", "slim_distill_loss_grad",
     "slim_profile_enable", "slim_profile_collect", "slim_profile_entry", "slim_profile_reset",
 ]
 
@@ -122,6 +125,24 @@ def load() -> ctypes.CDLL:
     lib.slim_lwc_quantize.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_i64, c_void_p, c_i64, c_i64, c_void_p,
                                       c_int, c_int, c_double, c_double, c_double, c_double, c_double, c_void_p, c_void_p,
                                       c_void_p, c_void_p, c_int, P(c_double)]
+    c_size_t = ctypes.c_size_t
+    lib.slim_fp8_quantize_weights.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_i64] + [c_void_p, c_i64] * 4
+    lib.slim_fp8_linear_workspace.argtypes = [c_int] * 5
+    lib.slim_fp8_linear.argtypes = [c_void_p, c_void_p, c_int, c_int, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_int, c_int, c_void_p,
+                                    c_int, c_i64]
+    lib.slim_fp8_linear_backward_workspace.argtypes = [c_int] * 7
+    lib.slim_fp8_linear_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_i64, c_i64, c_void_p, c_i64, c_void_p, c_i64,
+                                             c_int, c_int, c_void_p, c_i64, c_void_p, c_int, c_i64]
+    lib.slim_layer_norm.argtypes = [c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_void_p, c_void_p, c_int, c_double, c_int, c_void_p,
+                                    c_i64, c_void_p, c_void_p]
+    lib.slim_layer_norm_backward_workspace.argtypes = [c_i64, c_int, c_int, c_int]
+    lib.slim_layer_norm_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_i64, c_void_p, c_int, c_void_p,
+                                             c_void_p, c_void_p, c_i64, c_void_p, c_void_p]
+    lib.slim_distill_loss.argtypes = [c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_void_p, c_int, c_void_p, c_int, c_int, c_i64,
+                                      c_void_p, c_double, c_void_p]
+    lib.slim_distill_loss_grad.argtypes = lib.slim_distill_loss.argtypes[:-1] + [c_void_p, c_void_p, c_void_p, c_i64]
+    for fn in (lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
+        fn.restype = c_size_t
     lib.slim_profile_enable.argtypes = [c_void_p, c_int]
     lib.slim_profile_collect.argtypes = [c_void_p]
     lib.slim_profile_collect.restype = c_int
@@ -130,7 +151,7 @@ def load() -> ctypes.CDLL:
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("slim_default_params", "slim_default_tau", "slim_last_error", "slim_workspace_bytes",
-                        "slim_workspace_query", "slim_profile_collect"):
+                        "slim_workspace_query", "slim_profile_collect") and not name.endswith("_workspace"):
             fn.restype = c_int
     _lib = lib
     return lib
@@ -148,8 +169,71 @@ def make_params(sqc_weight_mode: int = 0, mask_scope: int = 0, q1_mode: int = 0,
     return SlimParams(sqc_weight_mode, mask_scope, q1_mode, sal_mode)
 
 
+def _dtype(t: torch.Tensor) -> int:
+    try:
+        return _DT[t.dtype]
+    except KeyError:
+        raise ValueError("libslim has no %s" % t.dtype) from None
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+_E4M3 = torch.float8_e4m3fn
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def fp8_linear_workspace(n: int, m: int, t: int, dtype: torch.dtype = torch.bfloat16, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.fp8_linear (host only, no GPU needed)."""
+    return int(load().slim_fp8_linear_workspace(n, m, t, _DT[dtype], num_cus))
+
+
+def fp8_linear_backward_workspace(n: int, m: int, t: int, dx: bool = True, dw: bool = True,
+                                  dw_dtype: torch.dtype = torch.bfloat16, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.fp8_linear_backward (host only, no GPU needed)."""
+    return int(load().slim_fp8_linear_backward_workspace(n, m, t, int(dx), int(dw), _DT[dw_dtype], num_cus))
+
+
+def layer_norm_backward_workspace(rows: int, cols: int, bias: bool = True, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.layer_norm_backward (host only, no GPU needed)."""
+    return int(load().slim_layer_norm_backward_workspace(rows, cols, int(bias), num_cus))
+
+
+def _row_stride(x: torch.Tensor, what: str) -> int:
+    """The leading dimension of a matrix whose rows are contiguous."""
+    if x.dim() != 2:
+        raise ValueError("%s has to be a matrix, got %d dimensions" % (what, x.dim()))
+    if x.shape[0] <= 1 or x.shape[1] == 0:
+        if x.shape[1] > 1 and x.stride(1) != 1:
+            raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
+        return max(x.shape[1], 1)
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
+    ld = x.stride(0)
+    if ld < x.shape[1]:
+        raise ValueError("rows of %s overlap" % what)
+    return ld
+
+
+def _stored_strides(q: torch.Tensor, s: torch.Tensor, what: str):
+    """Leading dimensions of stored 8-bit weights; raises where they are not what Slim.fp8_quantize_weights makes."""
+    if q.dtype != _E4M3 or s.dtype != torch.uint8 or q.dim() != 2 or s.dim() != 2:
+        raise ValueError("%s has to be a float8_e4m3fn matrix, its scales a uint8 matrix" % what)
+    n, m = q.shape
+    nb, mb = (n + 127) // 128, (m + 127) // 128
+    if tuple(s.shape) != (nb, mb):
+        raise ValueError("%s (%d x %d) needs %d x %d scales, got %d x %d" % (what, n, m, nb, mb, s.shape[0], s.shape[1]))
+    ldq, lds = q.stride(0), s.stride(0)
+    if q.stride(1) != 1 and m > 1 or s.stride(1) != 1 and mb > 1:
+        raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
+    if ldq % 128 or lds % 4 or ldq < m or lds < mb:
+        raise ValueError("rows of %s have to be whole blocks of 128 and those of its scales whole words apart, got %d and %d" % (what, ldq, lds))
+    # rows are read to the end of their last block, and scales by the word: the padding of the last row has to be there as well
+    if (q.untyped_storage().nbytes() - q.storage_offset() < (n - 1) * ldq + mb * 128 or
+            s.untyped_storage().nbytes() - s.storage_offset() < (nb - 1) * lds + (mb + 3) // 4 * 4):
+        raise ValueError("the padding of the last row of %s or of its scales is missing" % what)
+    return ldq, lds
 
 
 def _need_cuda(*tensors):
@@ -421,6 +505,154 @@ class Slim:
         assert X.stride(1) == 1 and out.stride(1) == 1
         self._check(self.lib.slim_transpose_16(self.ctx, _ptr(X), X.shape[0], X.shape[1], X.stride(0), _ptr(out), out.stride(0)))
         return out
+
+    # ---- around a quantised layer: 8-bit linear layer, norms, divergence from a teacher
+    def _ready(self, *tensors):
+        """Tensors on the context's device, and the context's stream current: outputs are allocated on the current one."""
+        index = self.device.index or 0
+        for t in tensors:
+            if t is not None and t.get_device() != index:
+                raise ValueError("libslim takes tensors of the context's device")
+        if _current_stream(index) != self.stream.cuda_stream:
+            raise ValueError("the context is bound to another stream than the current one")
+
+    def fp8_quantize_weights(self, W: torch.Tensor, transposed: bool = True):
+        """W (n, m) float16 / bfloat16 / float32 as stored 8-bit weights: (q float8_e4m3fn (n, m), s uint8 (n / 128, m / 128 rounded up)),
+        and with `transposed` also those of W^T, which the backward pass reads.  Rows are padded: keep the tensors as they are."""
+        self._ready(W)
+        n, m = W.shape
+        nb, mb = (n + 127) // 128, (m + 127) // 128
+
+        def stored(rows, cols, rb, cb):
+            q = torch.empty((rows, cb * 128), dtype=_E4M3, device=W.device)[:, :cols]
+            return q, torch.zeros((rb, (cb + 3) // 4 * 4), dtype=torch.uint8, device=W.device)[:, :cb]
+
+        q, s = stored(n, m, nb, mb)
+        qt, st = stored(m, n, mb, nb) if transposed else (None, None)
+        self._check(self.lib.slim_fp8_quantize_weights(self.ctx, W.data_ptr(), _dtype(W), n, m, _row_stride(W, "W"), q.data_ptr(), mb * 128,
+                                                       s.data_ptr(), s.stride(0), _ptr(qt), nb * 128, _ptr(st),
+                                                       st.stride(0) if transposed else 0))
+        return (q, s, qt, st) if transposed else (q, s)
+
+    def fp8_linear(self, X: torch.Tensor, W: torch.Tensor, Ws: torch.Tensor, dtype: Optional[torch.dtype] = None):
+        """Y (t, n) = Q(X) W^T for X (t, m) float16 / bfloat16 and stored 8-bit weights W, Ws; `dtype`: of Y (default: X's)."""
+        self._ready(X, W, Ws)
+        ldq, lds = _stored_strides(W, Ws, "W")
+        n, m = W.shape
+        if X.dim() != 2 or X.shape[1] != m:
+            raise ValueError("X has to be (t, %d), got %s" % (m, tuple(X.shape)))
+        t = X.shape[0]
+        Y = torch.empty((t, n), dtype=dtype or X.dtype, device=X.device)
+        self._check(self.lib.slim_fp8_linear(self.ctx, X.data_ptr(), _dtype(X), t, _row_stride(X, "X"), W.data_ptr(), ldq, Ws.data_ptr(), lds,
+                                             n, m, Y.data_ptr(), _dtype(Y), n))
+        return Y
+
+    def fp8_linear_backward(self, dY: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[torch.Tensor], Wts: Optional[torch.Tensor],
+                            dw_dtype: Optional[torch.dtype] = None, dx: bool = True, dw: bool = True):
+        """(dX (t, m), dW (n, m)) for dY (t, n) and X (t, m) of one 16-bit type and the stored weights of W^T; dw_dtype: of dW (default:
+        X's).  Without `dx` Wt and Wts may be None, without `dw` X; the gradient that is not wanted is None."""
+        self._ready(dY, X, Wt, Wts)
+        if not (dx or dw):
+            raise ValueError("neither gradient is wanted")
+        if dY.dim() != 2:
+            raise ValueError("dY has to be a matrix")
+        t, n = dY.shape
+        ldqt = ldst = 0
+        if dw:
+            if X is None or X.dim() != 2 or X.shape[0] != t or X.dtype != dY.dtype:
+                raise ValueError("X has to be a matrix of dY's tokens and type")
+            m = X.shape[1]
+        if dx:
+            if Wt is None or Wts is None:
+                raise ValueError("dX needs the stored weights of W^T")
+            ldqt, ldst = _stored_strides(Wt, Wts, "Wt")
+            if Wt.shape[1] != n or dw and Wt.shape[0] != m:
+                raise ValueError("Wt has to be (m, n) = (%s, %d), got %s" % (m if dw else "m", n, tuple(Wt.shape)))
+            m = Wt.shape[0]
+        dX = torch.empty((t, m), dtype=dY.dtype, device=dY.device) if dx else None
+        dW = torch.empty((n, m), dtype=dw_dtype or dY.dtype, device=dY.device) if dw else None
+        self._check(self.lib.slim_fp8_linear_backward(self.ctx, dY.data_ptr(), X.data_ptr() if dw else None, _dtype(dY), t,
+                                                      _row_stride(dY, "dY"), _row_stride(X, "X") if dw else 0, Wt.data_ptr() if dx else None,
+                                                      ldqt, Wts.data_ptr() if dx else None, ldst, n, m, dX.data_ptr() if dx else None, m,
+                                                      dW.data_ptr() if dw else None, _dtype(dW) if dw else F32, m))
+        return dX, dW
+
+    def layer_norm(self, X: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor] = None, eps: float = 1e-5, rms: bool = False,
+                   stats: bool = False):
+        """Layer norm of the rows of X (rows, cols), without the mean with `rms`; w, b (cols,) of X's type or float32.  With `stats`
+        (Y, mean, rstd) for the backward pass (mean is None with `rms`)."""
+        self._ready(X, w, b)
+        rows, cols = self._norm_shape(X, w, b)
+        Y = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
+        mean = torch.empty(rows, dtype=torch.float32, device=X.device) if stats and not rms else None
+        rstd = torch.empty(rows, dtype=torch.float32, device=X.device) if stats else None
+        self._check(self.lib.slim_layer_norm(self.ctx, X.data_ptr(), _dtype(X), rows, cols, _row_stride(X, "X"), w.data_ptr(),
+                                             None if b is None else b.data_ptr(), _dtype(w), eps, int(rms), Y.data_ptr(), cols,
+                                             None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr()))
+        return (Y, mean, rstd) if stats else Y
+
+    @staticmethod
+    def _norm_shape(X, w, b):
+        if X.dim() != 2 or tuple(w.shape) != (X.shape[1],) or b is not None and (b.shape != w.shape or b.dtype != w.dtype):
+            raise ValueError("X has to be a matrix, w and b vectors of its columns and of one type")
+        if w.stride(0) != 1 and w.shape[0] > 1 or b is not None and b.stride(0) != 1 and b.shape[0] > 1:
+            raise ValueError("w and b have to be contiguous")
+        return X.shape[0], X.shape[1]
+
+    def layer_norm_backward(self, dY: torch.Tensor, X: torch.Tensor, w: torch.Tensor, mean: Optional[torch.Tensor], rstd: torch.Tensor,
+                            bias: bool = False):
+        """(dX, dw, db) from the gradient of the outputs and the statistics of layer_norm; db is None without `bias`."""
+        self._ready(dY, X, w, mean, rstd)
+        rows, cols = self._norm_shape(X, w, None)
+        if dY.shape != X.shape or dY.dtype != X.dtype:
+            raise ValueError("dY has to be of X's shape and type")
+        for v in (mean, rstd):
+            if v is not None and (v.dtype != torch.float32 or tuple(v.shape) != (rows,) or not v.is_contiguous()):
+                raise ValueError("mean and rstd have to be float32 vectors of X's rows")
+        dX = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
+        dw = torch.empty(cols, dtype=w.dtype, device=X.device)
+        db = torch.empty(cols, dtype=w.dtype, device=X.device) if bias else None
+        self._check(self.lib.slim_layer_norm_backward(self.ctx, dY.data_ptr(), X.data_ptr(), _dtype(X), rows, cols, _row_stride(dY, "dY"),
+                                                      _row_stride(X, "X"), w.data_ptr(), _dtype(w), None if mean is None else mean.data_ptr(),
+                                                      rstd.data_ptr(), dX.data_ptr(), cols, dw.data_ptr(), None if db is None else db.data_ptr()))
+        return dX, dw, db
+
+    def _distill_args(self, S, index, teacher, tau, lse):
+        if S.dim() != 2 or index.dim() != 2 or index.shape != teacher.shape or index.shape[0] != S.shape[0]:
+            raise ValueError("S has to be (rows, V), index and teacher (rows, K)")
+        if index.dtype not in (torch.int64, torch.int32):
+            raise ValueError("index has to be int64 or int32")
+        rows, V = S.shape
+        ldk = _row_stride(index, "index")
+        if _row_stride(teacher, "teacher") != ldk:
+            raise ValueError("index and teacher have to have one row stride")
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows,) or not lse.is_contiguous()):
+            raise ValueError("lse has to be a float32 vector of the rows")
+        return (self.ctx, S.data_ptr(), _dtype(S), rows, V, _row_stride(S, "S"), index.data_ptr(), int(index.dtype == torch.int64),
+                teacher.data_ptr(), _dtype(teacher), index.shape[1], ldk, None if lse is None else lse.data_ptr(), tau)
+
+    def distill_loss(self, S: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, tau: float = 1.0, lse: Optional[torch.Tensor] = None):
+        """loss float32 (rows,): the divergence of softmax(S / tau) from the teacher's top logits (rows, K) of the classes `index`."""
+        self._ready(S, index, teacher, lse)
+        args = self._distill_args(S, index, teacher, tau, lse)
+        loss = torch.empty(S.shape[0], dtype=torch.float32, device=S.device)
+        self._check(self.lib.slim_distill_loss(*args, loss.data_ptr()))
+        return loss
+
+    def distill_loss_grad(self, S: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, dloss: torch.Tensor, tau: float = 1.0,
+                          lse: Optional[torch.Tensor] = None, dS: Optional[torch.Tensor] = None):
+        """(loss, dS) with dS (rows, V) of S's type the gradient of sum(dloss * loss); dS may be given, S itself among others."""
+        self._ready(S, index, teacher, dloss, lse, dS)
+        args = self._distill_args(S, index, teacher, tau, lse)
+        if dloss.dtype != torch.float32 or tuple(dloss.shape) != (S.shape[0],) or not dloss.is_contiguous():
+            raise ValueError("dloss has to be a float32 vector of the rows")
+        if dS is None:
+            dS = torch.empty(S.shape, dtype=S.dtype, device=S.device)
+        elif dS.shape != S.shape or dS.dtype != S.dtype:
+            raise ValueError("dS has to be of S's shape and type")
+        loss = torch.empty(S.shape[0], dtype=torch.float32, device=S.device)
+        self._check(self.lib.slim_distill_loss_grad(*args, dloss.data_ptr(), loss.data_ptr(), dS.data_ptr(), _row_stride(dS, "dS")))
+        return loss, dS
 
     # ---- measurement aid
     def profile_enable(self, on: bool = True):

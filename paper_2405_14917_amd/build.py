@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libslim.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["ctx.hip", "util.hip", "dgemm.hip", "rgemm.hip", "gram.hip", "inverse.hip", "salience.hip", "sba.hip", "quant.hip",
-           "pack.hip", "dequant.hip", "dequant_few.hip", "dequant_gemm.hip", "handover.hip", "int8_products.hip", "lwc.hip"]
+           "pack.hip", "dequant.hip", "dequant_few.hip", "dequant_gemm.hip", "handover.hip", "int8_products.hip", "lwc.hip",
+           "fp8_quant.hip", "fp8_few.hip", "fp8_gemm.hip", "fp8_linear.hip", "norm.hip", "distill.hip"]
 
 # packed-fp32 code generation is switched off for all device code (a device-compiler option; the host
 # pass does not know the feature and says so, which is harmless)
@@ -38,7 +39,8 @@ EXTRA_FLAGS = {"dgemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                # gram.hip and dequant_gemm.hip set M0 in inline asm (destination of its direct-to-LDS loads) and say so in the clobber
                # list, which the compiler remarks on
                "rgemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"],
-               "gram.hip": ["-Wno-inline-asm"], "dequant_gemm.hip": ["-Wno-inline-asm"]}
+               "gram.hip": ["-Wno-inline-asm"], "dequant_gemm.hip": ["-Wno-inline-asm"],
+               "fp8_gemm.hip": ["-Wno-inline-asm"]}
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,499 @@
+// Layer norm and its form without the mean (RMS norm): outputs, and the gradients of inputs, weight and bias.
+//
+//   mu = mean x (0 without the mean), r = 1 / sqrt(mean (x - mu)^2 + eps), xh = (x - mu) r, y = xh w + b
+//   g = dy w:   dx = r (g - mean g - xh mean(g xh))   (no mean g without the mean);   dw = sum over rows of dy xh,  db = sum of dy
+//
+// Bound by memory: x is read and y written, dy and x are read and dx written, once each.  A row lives in the registers of a group of
+// wavefronts as it came (16-byte pieces of its own type), so that the deviations are taken from the mean itself and not from the
+// difference of two sums; means and deviations in fp32.  A workgroup goes through rows blockIdx, blockIdx + gridDim, ... with w and b kept in
+// registers, and sums its share of dw and db there: column sums of its rows, which a second kernel adds over the workgroups in a fixed
+// order.  Rows longer than 16 pieces per lane of 16 wavefronts are read again instead.
+#include "slim_device.h"
+#include "slim_internal.h"
+
+namespace {
+
+using namespace slimdev;
+
+struct NormArgs {
+  const void *X, *dY, *w, *b;
+  void *Y, *dX;
+  int64_t ldx, lddy, ldy, lddx;
+  float *mean, *rstd;                    // written by the forward pass (may be null), read by the backward pass
+  float *pw, *pb;                        // partial column sums: gridDim x cols
+  int64_t rows;
+  int cols;
+  float eps;
+  int rms;
+};
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__half> {
+  static __device__ __forceinline__ float widen(unsigned short v) { return (float)__builtin_bit_cast(_Float16, v); }
+  static __device__ __forceinline__ unsigned short narrow(float v) { return __builtin_bit_cast(unsigned short, (_Float16)v); }
+};
+template <>
+struct Elem<__hip_bfloat16> {
+  static __device__ __forceinline__ float widen(unsigned short v) { return __uint_as_float((unsigned)v << 16); }
+  static __device__ __forceinline__ unsigned short narrow(float v) { return __builtin_bit_cast(unsigned short, (__bf16)v); }
+};
+
+// A piece: 16 bytes of a row (4 or 8 elements)
+template <typename T>
+struct Piece {
+  static constexpr int E = 16 / sizeof(T);
+  unsigned v[4];
+  // from p on, of which `left` elements exist (the others are zero); p is aligned to its type only
+  __device__ __forceinline__ void load(const T* p, int left) {
+    if (left >= E) {
+      __builtin_memcpy(v, p, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = 0u;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i < left) v[i] = reinterpret_cast<const unsigned*>(p)[i];
+      } else {
+        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < left) v[i / 2] |= (unsigned)q[i] << (16 * (i & 1));
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
+    else return Elem<T>::widen((unsigned short)(v[i / 2] >> (16 * (i & 1))));
+  }
+  __device__ __forceinline__ void set(const float (&f)[E]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
+      else v[i] = (unsigned)Elem<T>::narrow(f[2 * i]) | (unsigned)Elem<T>::narrow(f[2 * i + 1]) << 16;
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int left) const {
+    if (left >= E) {
+      __builtin_memcpy(p, v, 16);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < left) reinterpret_cast<unsigned*>(p)[i] = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(v[i / 2] >> (16 * (i & 1)));
+    }
+  }
+};
+
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += __int_as_float(dpp_b32<DPP_XOR1>(__float_as_int(v)));
+  v += __int_as_float(dpp_b32<DPP_XOR2>(__float_as_int(v)));
+  v += __int_as_float(dpp_b32<DPP_HALF_MIRROR>(__float_as_int(v)));
+  v += __int_as_float(dpp_b32<DPP_MIRROR>(__float_as_int(v)));
+  const int i = __float_as_int(v);
+  return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
+         (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));
+}
+
+// Sums over the W wavefronts of a row.  `slot` alternates between calls, so that one barrier per call is enough.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[W][N], int& slot) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = wave_sum_f32(v[k]);
+  if constexpr (W > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < N; ++k) red[slot][wave][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) s += red[slot][i][k];
+      v[k] = s;
+    }
+    slot ^= 1;
+  }
+}
+
+// W wavefronts per row, P pieces per lane; W == 1: four rows per workgroup
+template <typename T, typename TW, int W, int P>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_forward(NormArgs a) {
+  constexpr int E = Piece<T>::E, LANES = 64 * W, RPW = W == 1 ? 4 : 1;
+  __shared__ float red[2][W][1];
+  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t row0 = (int64_t)blockIdx.x * RPW + (W == 1 ? threadIdx.x >> 6 : 0), step = (int64_t)gridDim.x * RPW;
+  const float inv_n = 1.f / (float)a.cols;
+  int slot = 0;
+  Piece<T> x[P];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = (i * LANES + lane) * E;
+      x[i].load(static_cast<const T*>(a.X) + row * a.ldx + c, a.cols - c);
+    }
+  };
+  if (row0 < a.rows) fetch(row0);
+  for (int64_t row = row0; row < a.rows; row += step) {
+    float s[1] = {0.f};
+    float mean = 0.f;
+    if (!a.rms) {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[0] += x[i].get(e);
+      row_sums<W, 1>(s, red, slot);
+      mean = s[0] * inv_n;
+      s[0] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int left = a.cols - (i * LANES + lane) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = e < left ? x[i].get(e) - mean : 0.f;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    }
+    row_sums<W, 1>(s, red, slot);
+    const float r = 1.f / sqrtf(fmaf(s[0], inv_n, a.eps));
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = (i * LANES + lane) * E;
+      if (c >= a.cols) break;
+      float y[E];
+#pragma unroll
+      for (int k = 0; k < E; k += Piece<TW>::E) {
+        Piece<TW> w, b;
+        w.load(static_cast<const TW*>(a.w) + c + k, a.cols - c - k);
+        if (a.b) b.load(static_cast<const TW*>(a.b) + c + k, a.cols - c - k);
+#pragma unroll
+        for (int e = 0; e < Piece<TW>::E; ++e) {
+          const float xh = (x[i].get(k + e) - mean) * r;
+          y[k + e] = a.b ? fmaf(xh, w.get(e), b.get(e)) : xh * w.get(e);
+        }
+      }
+      Piece<T> o;
+      o.set(y);
+      o.store(static_cast<T*>(a.Y) + row * a.ldy + c, a.cols - c);
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = r;
+    }
+    if (row + step < a.rows) fetch(row + step);
+  }
+}
+
+template <typename T, typename TW, int W, int P>
+__global__ __launch_bounds__(64 * W) void norm_backward(NormArgs a) {
+  constexpr int E = Piece<T>::E, LANES = 64 * W;
+  __shared__ float red[2][W][2];
+  const int lane = threadIdx.x;
+  const float inv_n = 1.f / (float)a.cols;
+  int slot = 0;
+  float w[P][E], dw[P][E], db[P][E];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int c = (i * LANES + lane) * E;
+#pragma unroll
+    for (int k = 0; k < E; k += Piece<TW>::E) {
+      Piece<TW> t;
+      t.load(static_cast<const TW*>(a.w) + min(c + k, a.cols - 1), a.cols - c - k);
+#pragma unroll
+      for (int e = 0; e < Piece<TW>::E; ++e) w[i][k + e] = t.get(e);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.f;
+  }
+  Piece<T> x[P], dy[P];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = (i * LANES + lane) * E;
+      x[i].load(static_cast<const T*>(a.X) + row * a.ldx + c, a.cols - c);
+      dy[i].load(static_cast<const T*>(a.dY) + row * a.lddy + c, a.cols - c);
+    }
+  };
+  if ((int64_t)blockIdx.x < a.rows) fetch(blockIdx.x);
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float mean = a.mean ? a.mean[row] : 0.f, r = a.rstd[row];
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = dy[i].get(e), xh = (x[i].get(e) - mean) * r, g = d * w[i][e];     // (behind the last column d is 0)
+        s[0] += g;
+        s[1] = fmaf(g, xh, s[1]);
+        dw[i][e] = fmaf(d, xh, dw[i][e]);
+        db[i][e] += d;
+      }
+    row_sums<W, 2>(s, red, slot);
+    const float mg = a.rms ? 0.f : s[0] * inv_n, mgx = s[1] * inv_n;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = (i * LANES + lane) * E;
+      if (c >= a.cols) break;
+      float o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float xh = (x[i].get(e) - mean) * r;
+        o[e] = r * (fmaf(dy[i].get(e), w[i][e], -mg) - xh * mgx);
+      }
+      Piece<T> p;
+      p.set(o);
+      p.store(static_cast<T*>(a.dX) + row * a.lddx + c, a.cols - c);
+    }
+    if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = (i * LANES + lane) * E + e;
+      if (c < a.cols) {
+        a.pw[(int64_t)blockIdx.x * a.cols + c] = dw[i][e];
+        if (a.pb) a.pb[(int64_t)blockIdx.x * a.cols + c] = db[i][e];
+      }
+    }
+}
+
+// Rows that no group of wavefronts holds: three passes over them, the column sums by a kernel of their own.
+template <typename T>
+__device__ __forceinline__ float value(const void* p, int64_t i) {
+  if constexpr (sizeof(T) == 4) return static_cast<const float*>(p)[i];
+  else return Elem<T>::widen(static_cast<const unsigned short*>(p)[i]);
+}
+template <typename T>
+__device__ __forceinline__ void put(void* p, int64_t i, float v) {
+  if constexpr (sizeof(T) == 4) static_cast<float*>(p)[i] = v;
+  else static_cast<unsigned short*>(p)[i] = Elem<T>::narrow(v);
+}
+
+template <typename T, typename TW>
+__global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
+  __shared__ float red[2][16][1];
+  int slot = 0;
+  const float inv_n = 1.f / (float)a.cols;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int64_t x0 = row * a.ldx;
+    float s[1] = {0.f};
+    float mean = 0.f;
+    if (!a.rms) {
+      for (int c = threadIdx.x; c < a.cols; c += 1024) s[0] += value<T>(a.X, x0 + c);
+      row_sums<16, 1>(s, red, slot);
+      mean = s[0] * inv_n;
+      s[0] = 0.f;
+    }
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float d = value<T>(a.X, x0 + c) - mean;
+      s[0] = fmaf(d, d, s[0]);
+    }
+    row_sums<16, 1>(s, red, slot);
+    const float r = 1.f / sqrtf(fmaf(s[0], inv_n, a.eps));
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float xh = (value<T>(a.X, x0 + c) - mean) * r, w = value<TW>(a.w, c);
+      put<T>(a.Y, row * a.ldy + c, a.b ? fmaf(xh, w, value<TW>(a.b, c)) : xh * w);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = r;
+    }
+  }
+}
+template <typename T, typename TW>
+__global__ __launch_bounds__(1024) void norm_backward_long(NormArgs a) {
+  __shared__ float red[2][16][2];
+  int slot = 0;
+  const float inv_n = 1.f / (float)a.cols;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float mean = a.mean ? a.mean[row] : 0.f, r = a.rstd[row];
+    float s[2] = {0.f, 0.f};
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float g = value<T>(a.dY, row * a.lddy + c) * value<TW>(a.w, c), xh = (value<T>(a.X, row * a.ldx + c) - mean) * r;
+      s[0] += g;
+      s[1] = fmaf(g, xh, s[1]);
+    }
+    row_sums<16, 2>(s, red, slot);
+    const float mg = a.rms ? 0.f : s[0] * inv_n, mgx = s[1] * inv_n;
+    for (int c = threadIdx.x; c < a.cols; c += 1024) {
+      const float g = value<T>(a.dY, row * a.lddy + c) * value<TW>(a.w, c), xh = (value<T>(a.X, row * a.ldx + c) - mean) * r;
+      put<T>(a.dX, row * a.lddx + c, r * (g - mg - xh * mgx));
+    }
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns(NormArgs a, int64_t per) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= a.cols) return;
+  const int64_t r0 = (int64_t)blockIdx.y * per, r1 = min(a.rows, r0 + per);
+  float dw = 0.f, db = 0.f;
+  for (int64_t row = r0; row < r1; ++row) {
+    const float d = value<T>(a.dY, row * a.lddy + c);
+    dw = fmaf(d, (value<T>(a.X, row * a.ldx + c) - (a.mean ? a.mean[row] : 0.f)) * a.rstd[row], dw);
+    db += d;
+  }
+  a.pw[(int64_t)blockIdx.y * a.cols + c] = dw;
+  if (a.pb) a.pb[(int64_t)blockIdx.y * a.cols + c] = db;
+}
+
+// dw, db: the sums of the workgroups' shares; 32 columns x 8 ranges of workgroups
+template <typename TW>
+__global__ __launch_bounds__(256) void norm_join(const float* __restrict__ pw, const float* __restrict__ pb, int parts, int cols,
+                                                 void* dw, void* db) {
+  __shared__ float red[8][32];
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+  const float* p = blockIdx.y ? pb : pw;
+  const int per = (parts + 7) / 8, i0 = k * per, i1 = min(parts, i0 + per);
+  float s = 0.f;
+  if (c < cols)
+    for (int i = i0; i < i1; ++i) s += p[(int64_t)i * cols + c];
+  red[k][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (k == 0 && c < cols) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += red[i][threadIdx.x & 31];
+    put<TW>(blockIdx.y ? db : dw, c, s);
+  }
+}
+
+constexpr int NB_PER_CU = 4;                   // workgroups per CU of the backward pass, and so partial sums
+
+// workgroups, and with them partial sums, of the backward pass
+int parts_of(int64_t rows, int ncu) { return (int)std::max<int64_t>(1, std::min<int64_t>(rows, (int64_t)NB_PER_CU * ncu)); }
+
+template <typename T, typename TW>
+slim_status forward(slim_ctx* ctx, const NormArgs& a) {
+  constexpr int E = Piece<T>::E;
+  const int pieces = slim_cdiv(a.cols, E);
+  const int64_t many = (int64_t)8 * ctx->num_cus;
+  const char* name = "norm_forward";
+  auto grid = [&](int64_t groups, int per_cu) { return dim3((unsigned)std::min<int64_t>(groups, (int64_t)per_cu * ctx->num_cus)); };
+  const bool few = a.rows < many;              // rows that do not fill the chip: more lanes per row
+  if (pieces <= 64) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 1, 1>), grid((a.rows + 3) / 4, 8), dim3(256), 0, a);
+  else if (pieces <= 256 && (few || pieces > 128)) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 4, 1>), grid(a.rows, 8), dim3(256), 0, a);
+  else if (pieces <= 128) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 1, 2>), grid((a.rows + 3) / 4, 8), dim3(256), 0, a);
+  else if (pieces <= 512) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 4, 2>), grid(a.rows, 8), dim3(256), 0, a);
+  else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 4, 4>), grid(a.rows, 8), dim3(256), 0, a);
+  else if (pieces <= 4096) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 16, 4>), grid(a.rows, 2), dim3(1024), 0, a);
+  else SLIM_LAUNCH(ctx, name, (norm_forward_long<T, TW>), grid(a.rows, 2), dim3(1024), 0, a);
+  return SLIM_OK;
+}
+
+template <typename T, typename TW>
+slim_status backward(slim_ctx* ctx, const NormArgs& a, void* dw, void* db, int parts) {
+  constexpr int E = Piece<T>::E;
+  const int pieces = slim_cdiv(a.cols, E);
+  const char* name = "norm_backward";
+  const dim3 grid(parts);
+  if (pieces <= 64) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1>), grid, dim3(64), 0, a);
+  else if (pieces <= 256) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1>), grid, dim3(256), 0, a);
+  else if (pieces <= 512) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2>), grid, dim3(256), 0, a);
+  else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2>), grid, dim3(512), 0, a);
+  else if (pieces <= 2048) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2>), grid, dim3(1024), 0, a);
+  else {
+    SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
+    SLIM_LAUNCH(ctx, "norm_columns", norm_columns<T>, dim3(slim_cdiv(a.cols, 256), parts), dim3(256), 0, a, (a.rows + parts - 1) / parts);
+  }
+  SLIM_LAUNCH(ctx, "norm_join", norm_join<TW>, dim3(slim_cdiv(a.cols, 32), db ? 2 : 1), dim3(256), 0, a.pw, a.pb, parts, a.cols, dw, db);
+  return SLIM_OK;
+}
+
+bool is_float(slim_dtype d) { return d == SLIM_F16 || d == SLIM_BF16 || d == SLIM_F32; }
+
+template <typename F>
+slim_status by_type(slim_dtype x, slim_dtype w, F f) {
+  if (x == SLIM_F32) return f(float(), float());
+  if (x == SLIM_F16) return w == SLIM_F32 ? f(__half(), float()) : f(__half(), __half());
+  return w == SLIM_F32 ? f(__hip_bfloat16(), float()) : f(__hip_bfloat16(), __hip_bfloat16());
+}
+
+slim_status check(slim_ctx* ctx, const char* fn, slim_dtype x, slim_dtype w, int64_t rows, int cols) {
+  if (!is_float(x)) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: X is F16, BF16 or F32", fn);
+  if (w != x && w != SLIM_F32) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: weight and bias are of the type of X or F32", fn);
+  SLIM_REQUIRE(ctx, rows >= 0 && cols > 0, "%s: rows = %lld, cols = %d", fn, (long long)rows, cols);
+  return SLIM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, int bias, int num_cus) {
+  if (rows <= 0 || cols <= 0) return 0;
+  const size_t one = slim_ws_round(sizeof(float) * (size_t)parts_of(rows, num_cus > 0 ? num_cus : 256) * cols);
+  return bias ? 2 * one : one;
+}
+
+slim_status slim_layer_norm(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int64_t rows, int cols, int64_t ldx, const void* w, const void* b,
+                            slim_dtype w_dtype, double eps, int rms, void* Y, int64_t ldy, float* mean, float* rstd) {
+  if (!ctx) return SLIM_ERR_INVALID_ARG;
+  const char* fn = "slim_layer_norm";
+  if (const slim_status st = check(ctx, fn, x_dtype, w_dtype, rows, cols); st != SLIM_OK) return st;
+  SLIM_REQUIRE(ctx, w, "%s: null weight", fn);
+  SLIM_REQUIRE(ctx, eps >= 0.0, "%s: eps = %g", fn, eps);
+  if (rows == 0) return SLIM_OK;
+  SLIM_REQUIRE(ctx, X && Y && ldx >= cols && ldy >= cols, "%s: null pointer, or rows shorter than cols (ldx = %lld, ldy = %lld)", fn,
+               (long long)ldx, (long long)ldy);
+  NormArgs a = {};
+  a.X = X;
+  a.w = w;
+  a.b = b;
+  a.Y = Y;
+  a.ldx = ldx;
+  a.ldy = ldy;
+  a.mean = rms ? nullptr : mean;
+  a.rstd = rstd;
+  a.rows = rows;
+  a.cols = cols;
+  a.eps = (float)eps;
+  a.rms = rms != 0;
+  return by_type(x_dtype, w_dtype, [&](auto x, auto wt) { return forward<decltype(x), decltype(wt)>(ctx, a); });
+}
+
+slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* X, slim_dtype x_dtype, int64_t rows, int cols, int64_t lddy,
+                                     int64_t ldx, const void* w, slim_dtype w_dtype, const float* mean, const float* rstd, void* dX,
+                                     int64_t lddx, void* dw, void* db) {
+  if (!ctx) return SLIM_ERR_INVALID_ARG;
+  const char* fn = "slim_layer_norm_backward";
+  if (const slim_status st = check(ctx, fn, x_dtype, w_dtype, rows, cols); st != SLIM_OK) return st;
+  SLIM_REQUIRE(ctx, w && dw, "%s: null weight or dw", fn);
+  SLIM_REQUIRE(ctx, rows == 0 || (dY && X && dX && rstd && lddy >= cols && ldx >= cols && lddx >= cols),
+               "%s: null pointer, or rows shorter than cols", fn);
+  const int parts = rows ? parts_of(rows, ctx->num_cus) : 0;
+  if (const slim_status st = slim_ws_reserve(ctx, slim_layer_norm_backward_workspace(rows, cols, db != nullptr, ctx->num_cus)); st != SLIM_OK)
+    return st;
+  NormArgs a = {};
+  a.X = X;
+  a.dY = dY;
+  a.w = w;
+  a.dX = dX;
+  a.ldx = ldx;
+  a.lddy = lddy;
+  a.lddx = lddx;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.rows = rows;
+  a.cols = cols;
+  a.rms = mean == nullptr;
+  if (parts > 0) {
+    a.pw = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols));
+    a.pb = db ? static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols)) : nullptr;
+    if (!a.pw || (db && !a.pb)) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
+    return by_type(x_dtype, w_dtype, [&](auto x, auto wt) { return backward<decltype(x), decltype(wt)>(ctx, a, dw, db, parts); });
+  }
+  // no rows: the sums are zero
+  return by_type(x_dtype, w_dtype, [&](auto, auto wt) {
+    SLIM_LAUNCH(ctx, "norm_join", norm_join<decltype(wt)>, dim3(slim_cdiv(cols, 32), db ? 2 : 1), dim3(256), 0, a.pw, a.pb, 0, cols, dw, db);
+    return SLIM_OK;
+  });
+}
+
+}  // extern "C"

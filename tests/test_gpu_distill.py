@@ -1,0 +1,231 @@
+"""The divergence from a teacher's top logits and its gradient, against their formulas in 64 bits.
+
+Tolerances (u = 2^-24).  An exponential of a difference d from the row's maximum, over tau, is off by about (|d| / tau + 4) u relatively (the
+argument's roundings, 2^-23 for the instruction); what counts in a sum of V of them has |d| / tau <= 30 (the rest is below 2^-43 of it), summed by a
+lane's 128 at most and a tree of 1024: the sum is off by (34 + 128 + 10) u = 172 u, its logarithm by that absolutely.  The loss adds 1 times that for the whole
+sum and rest / q_rest's logarithm, so 2 * 172 u absolutely, and half a step.  The gradient's elements are off by (|d| / tau + 4 + 172) u of q, twice
+that with a rest's factor, which is off by 2 * 172 u of rest q / q_rest."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+SUM = 172 * U
+HALF = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -140}
+
+
+@pytest.fixture(scope="module")
+def slim():
+    from paper_2405_14917_amd import binding
+    s = binding.Slim("cuda:0")
+    yield s
+    s.close()
+
+
+def data(rows, V, K, dtype, seed, tau, lse, pad=0, empty=True):
+    g = torch.Generator().manual_seed(seed)
+    S = torch.randn((rows, V), generator=g) * 2
+    S[torch.arange(rows), torch.randint(0, max(1, V - pad), (rows,), generator=g)] += 8
+    T = S + 0.5 * torch.randn((rows, V), generator=g)
+    if pad:
+        S[:, V - pad:] = -math.inf
+        T[:, V - pad:] = -math.inf
+    t, index = torch.topk(T, K, dim=1)
+    if empty and rows > 2:
+        used = torch.randint(0, K + 1, (rows,), generator=g)
+        used[0], used[1] = K, 0
+        index = torch.where(torch.arange(K)[None] < used[:, None], index, -1)
+    dloss = torch.rand(rows, generator=g) / rows
+    if rows > 3:
+        dloss[3] = 0.0
+    return S.to(dtype), index, t, dloss, torch.logsumexp(T.double() / tau, 1).float() if lse else None
+
+
+def formulas(S, index, teacher, dloss, tau, lse):
+    """loss, dS, and the bounds on what is off in fp32"""
+    z = S.double() / tau
+    rows, V = z.shape
+    used = (index >= 0) & (index < V)
+    t = torch.where(used, teacher.double() / tau, -math.inf)
+    p_slot = torch.nan_to_num(torch.softmax(t, 1), nan=0.0) if lse is None else torch.exp(t - lse.double()[:, None])
+    p = torch.zeros((rows, V + 1), dtype=torch.float64).scatter_(1, torch.where(used, index, V).long(), p_slot)[:, :V]
+    slot = torch.zeros((rows, V + 1), dtype=torch.bool).scatter_(1, torch.where(used, index, V).long(), True)[:, :V]
+    rest = torch.zeros(rows, dtype=torch.float64)
+    if lse is not None:
+        rest = 1 - p.sum(1)
+        rest = torch.where(rest < 2.0 ** -20, 0.0, rest)
+    live = p.sum(1) + rest > 0
+    lq = torch.log_softmax(z, 1)
+    lq_rest = torch.logsumexp(lq.masked_fill(slot, -math.inf), 1)
+    loss = torch.where(p > 0, torch.xlogy(p, p) - p * lq, 0.0).sum(1) + torch.where(rest > 0, torch.xlogy(rest, rest) - rest * lq_rest, 0.0)
+    q = torch.exp(lq)
+    share = torch.where((rest > 0) & (lq_rest > -math.inf), rest / torch.exp(lq_rest), 0.0)
+    d = torch.where(slot, q - p, q - q * share[:, None])
+    g = dloss.double() / tau
+    top = z.amax(1, keepdim=True)
+    e_q = torch.nan_to_num(q * ((top - z) + 4) * U, nan=0.0, posinf=0.0) + q * SUM
+    # (in a slot everything but the sum of the exponentials is of 64 bits)
+    e = torch.where(slot, q * SUM, e_q * (1 - share[:, None]).abs() + 2 * SUM * q * share[:, None])
+    z0 = lambda v: torch.where(live[:, None] if v.dim() == 2 else live, v, 0.0)
+    return z0(loss), z0(d * g[:, None]), z0(e * g[:, None].abs())
+
+
+def check(slim, S, index, teacher, dloss, tau, lse):
+    cu = lambda t: None if t is None else t.cuda()
+    args = cu(S), cu(index), cu(teacher)
+    loss = slim.distill_loss(*args, tau, lse=cu(lse))
+    loss2, dS = slim.distill_loss_grad(*args, cu(dloss), tau, lse=cu(lse))
+    want, dwant, e = formulas(S, index, teacher, dloss, tau, lse)
+    # the two entry points choose their kernels alike
+    assert torch.equal(loss, loss2)
+    got = loss.double().cpu()
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf])
+    bad = ~((got - want).abs() <= 2 * SUM + U * want.abs()) & ~inf
+    assert not bad.any(), (got[bad][:3], want[bad][:3])
+    h, tiny = HALF[S.dtype], TINY[S.dtype]
+    bad = ~((dS.double().cpu() - dwant).abs() <= e + 4 * U * dwant.abs() + h * (dwant.abs() + e) + tiny)
+    assert dS.dtype == S.dtype and not bad.any(), (int(bad.sum()), bad.nonzero()[:4], dS.cpu()[bad][:4], dwant[bad][:4])
+    return loss, dS
+
+
+@pytest.mark.parametrize("V,K", [(1, 1), (2, 1), (9, 4), (1000, 20), (1003, 256), (4099, 7), (8192, 64), (32000, 64), (50257, 20)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lse", [False, True])
+def test_every_size(slim, V, K, dtype, lse):
+    check(slim, *data(9, V, K, dtype, V + K, 1.0, lse, pad=V // 100)[:4], 1.0, data(9, V, K, dtype, V + K, 1.0, lse, pad=V // 100)[4])
+
+
+@pytest.mark.parametrize("V", [70001, 131072])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lse", [False, True])
+@pytest.mark.parametrize("rows", [1, 5])
+def test_rows_longer_than_registers_hold(slim, V, dtype, lse, rows):
+    S, index, t, dloss, l = data(rows, V, 33, dtype, V, 2.0, lse, pad=100)
+    check(slim, S, index, t, dloss, 2.0, l)
+
+
+@pytest.mark.parametrize("tau", [0.5, 0.7, 1.0, 4.0])
+@pytest.mark.parametrize("lse", [False, True])
+def test_temperatures(slim, tau, lse):
+    S, index, t, dloss, l = data(300, 777, 12, torch.bfloat16, 5, tau, lse)
+    check(slim, S, index, t, dloss, tau, l)
+
+
+@pytest.mark.parametrize("lse", [False, True])
+@pytest.mark.parametrize("V,dtype", [(517, torch.float16), (70001, torch.float32)])
+def test_slots_and_masks(slim, lse, V, dtype):
+    """No slots at all, as many slots as classes, slots far outside, infinite logits in and outside the slots, the type's lowest value as a mask."""
+    S, index, t, dloss, l = data(8, V, 16, dtype, 1, 1.0, lse, empty=False)
+    index[0] = -1
+    index[1, ::2] = 2 ** 40 + 3                                   # (beyond 32 bits, their low half a class)
+    index[2, 5] = V
+    S[3, 10:400] = -math.inf
+    S[4, 10:400] = torch.finfo(dtype).min
+    S[5, index[5, 3]] = -math.inf                                 # a class that the teacher wants and the student excludes: infinite loss
+    S[6] = 0.0
+    t[7] = -math.inf                                              # a teacher that says nothing
+    if lse:
+        l[7] = 0.0
+    loss, dS = check(slim, S, index, t, dloss, 1.0, l)
+    assert float(loss[0]) == 0.0 and not dS[0].any() and math.isinf(float(loss[5]))
+    assert not dS[3, 10:400][~torch.isin(torch.arange(10, 400), index[3])].any()
+    # int32 classes and narrower teachers
+    small = torch.where(index > V, -1, index).int()
+    a = slim.distill_loss(S.cuda(), small.cuda(), t.cuda(), 1.0, lse=None if l is None else l.cuda())
+    assert torch.equal(a, loss)
+    for narrow in (torch.float16, torch.bfloat16):
+        tn = t.to(narrow)
+        x = slim.distill_loss(S.cuda(), index.cuda(), tn.cuda(), 1.0, lse=None if l is None else l.cuda())
+        y = slim.distill_loss(S.cuda(), index.cuda(), tn.float().cuda(), 1.0, lse=None if l is None else l.cuda())
+        assert torch.equal(x, y)
+
+
+def test_a_rest_that_slots_nearly_cover(slim):
+    """The slots hold all but a few millionths of the student's mass: the sum outside them must not come from a difference."""
+    S, index, t, dloss, _ = data(16, 3000, 8, torch.float32, 2, 1.0, True, empty=False)
+    S.scatter_(1, index, 14.0)
+    l = torch.logsumexp(t.double(), 1).float() + 1e-4
+    check(slim, S, index, t, dloss, 1.0, l)
+
+
+def test_nothing_outside_the_slots(slim):
+    """A rest, and no class that could take it: the loss is infinite, the gradients stay numbers."""
+    S, index, t, dloss, _ = data(4, 64, 8, torch.float32, 3, 1.0, True, empty=False)
+    S = torch.full_like(S, -math.inf).scatter_(1, index, 1.0)
+    loss, dS = slim.distill_loss_grad(S.cuda(), index.cuda(), t.cuda(), dloss.cuda(), 1.0, lse=(torch.logsumexp(t, 1) + 1).cuda())
+    assert torch.isinf(loss).all() and torch.isfinite(dS).all()
+
+
+@pytest.mark.parametrize("V", [600, 70001])
+def test_what_is_not_a_number_stays_in_its_row(slim, V):
+    S, index, t, dloss, _ = data(6, V, 5, torch.float32, 4, 1.0, False, empty=False)
+    cu = lambda: (S.cuda(), index.cuda(), t.cuda(), dloss.cuda())
+    loss, dS = slim.distill_loss_grad(*cu())
+    S[2, V - 1], S[3, 0], S[4] = float("nan"), math.inf, -math.inf
+    bad, dB = slim.distill_loss_grad(*cu())
+    assert torch.isnan(bad[[2, 3, 4]]).all() and torch.isnan(dB[2]).any() and torch.isnan(dB[3]).any()
+    keep = [0, 1, 5]
+    assert torch.equal(bad[keep], loss[keep]) and torch.equal(dB[keep], dS[keep])
+
+
+def test_the_gradient_is_a_difference_of_the_loss(slim):
+    for tau, lse in ((1.0, False), (2.0, True)):
+        S, index, t, dloss, l = data(3, 40, 6, torch.float32, 8, tau, lse, empty=False)
+        _, dS = check(slim, S, index, t, dloss, tau, l)
+        h = 1e-5
+        for i, j in ((0, int(index[0, 0])), (1, 39), (2, int(index[2, 5])), (2, 0)):
+            f = lambda x: (formulas(x, index, t, dloss, tau, l)[0] * dloss.double()).sum()
+            up, down = S.double(), S.double()
+            up[i, j] += h
+            down[i, j] -= h
+            d = float(f(up) - f(down)) / (2 * h)
+            assert abs(float(dS[i, j]) - d) <= 1e-9 + 1e-6 * float(dloss[i])
+
+
+@pytest.mark.parametrize("V", [333, 70001])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_strides_alignment_and_in_place(slim, V, dtype):
+    S, index, t, dloss, l = data(12, V, 9, dtype, 6, 1.0, True)
+    loss, dS = check(slim, S, index, t, dloss, 1.0, l)
+    for first, gap in ((1, 1), (3, 8)):
+        wide = torch.full((12, V + gap), float("nan"), dtype=dtype, device="cuda")
+        v = wide[:, first:first + V]
+        v.copy_(S)
+        iw, tw = torch.full((12, 12), 10 ** 6), torch.full((12, 12), float("nan"))
+        iw[:, :9], tw[:, :9] = index, t
+        a, d = slim.distill_loss_grad(v, iw.cuda()[:, :9], tw.cuda()[:, :9], dloss.cuda(), 1.0, lse=l.cuda(), dS=v)
+        assert d is v and torch.equal(a, loss) and torch.equal(v, dS)
+        assert torch.isnan(wide[:, :first]).all() and torch.isnan(wide[:, first + V:]).all()
+
+
+def test_no_rows_and_no_slots(slim):
+    S = torch.randn(0, 50, device="cuda")
+    none = torch.empty((0, 3), device="cuda")
+    loss, dS = slim.distill_loss_grad(S, none.long(), none, torch.empty(0, device="cuda"))
+    assert loss.shape == (0,) and dS.shape == (0, 50)
+    S = torch.randn(2, 50, device="cuda")
+    none = torch.empty((2, 0), device="cuda")
+    loss, dS = slim.distill_loss_grad(S, none.long(), none, torch.ones(2, device="cuda"))
+    assert not loss.any() and not dS.any()
+
+
+def test_refusals(slim):
+    from paper_2405_14917_amd import binding
+    S, index, t, dloss, l = (None if v is None else v.cuda() for v in data(4, 50, 5, torch.float32, 7, 1.0, True))
+    for bad in (lambda: slim.distill_loss(S, index[:3], t), lambda: slim.distill_loss(S, index, t[:, :4]), lambda: slim.distill_loss(S, index.short(), t),
+                lambda: slim.distill_loss(S.t(), index, t), lambda: slim.distill_loss(S.cpu(), index, t), lambda: slim.distill_loss(S, index, t, lse=l.double()),
+                lambda: slim.distill_loss_grad(S, index, t, dloss.double()), lambda: slim.distill_loss_grad(S, index, t, dloss, dS=S.half())):
+        with pytest.raises(ValueError):
+            bad()
+    wide = torch.zeros((1, 1 << 20), device="cuda")
+    for bad, status in ((lambda: slim.distill_loss(S, index, t, 0.0), binding.ERR_INVALID_ARG), (lambda: slim.distill_loss(S, index, t, float("nan")), binding.ERR_INVALID_ARG),
+                        (lambda: slim.distill_loss(S.double(), index, t), binding.ERR_UNSUPPORTED),
+                        (lambda: slim.distill_loss(wide, index[:1], t[:1]), binding.ERR_UNSUPPORTED)):
+        with pytest.raises(binding.SlimError) as e:
+            bad()
+        assert e.value.status == status

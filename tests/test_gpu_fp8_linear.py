@@ -1,0 +1,260 @@
+"""The 8-bit linear layer with blocks of 128 against its definition in 64 bits (fp8_reference.py).
+
+Tolerances.  S = sum |a| |b| over the contraction.  Sums of 24 bits (fp32 outputs, and up to 16 tokens): the matrix cores add eight products
+at a time to the running sum with at most two roundings of 2^-23 of the largest term, and a part of the contraction is added by one more:
+(2 K / 8 + 16) 2^-23 S.  The e4m3 matrix cores (16-bit outputs of more tokens): each of eight products loses less than 2^-13 of the largest,
+so 2^-10 S.  Then half a step of the output's type."""
+import pytest
+import torch
+
+import fp8_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+HALF = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -140}
+
+
+@pytest.fixture(scope="module")
+def slim():
+    from paper_2405_14917_amd import binding
+    s = binding.Slim("cuda:0")
+    yield s
+    s.close()
+
+
+def numbers(rows, cols, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((rows, cols), generator=g) * torch.exp(spread * torch.randn((1, cols), generator=g)) * torch.exp(0.5 * torch.randn((rows, 1), generator=g))
+    if rows > 4:
+        x[rows // 2] = 0.0                                       # a token of nothing
+    return x.to(dtype)
+
+
+def close(Y, exact, size, K, few):
+    t = Y.dtype
+    got = Y.double().cpu()
+    tol = (2 * K / 8 + 16) * 2.0 ** -23 * size
+    if not few and t != torch.float32:
+        tol = tol + 2.0 ** -10 * size
+    tol = tol + HALF[t] * (exact.abs() + tol) + TINY[t]
+    bad = ~((got - exact).abs() <= tol)
+    assert not bad.any(), (int(bad.sum()), float(((got - exact).abs() / (size + 1e-300)).max()))
+
+
+def product(A, Bt, Y, few=False):
+    """Y against A Bt^T"""
+    close(Y, A @ Bt.t(), A.abs() @ Bt.abs().t(), A.shape[1], few)
+
+
+@pytest.mark.parametrize("n,m", [(1, 1), (128, 128), (130, 257), (257, 127), (96, 640), (515, 1100)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+def test_weights_are_stored_as_defined(slim, n, m, dtype):
+    W = numbers(n, m, torch.float32, n + m, 2.0) * 1e-2
+    W[n // 3] = 0.0
+    if n > 128:
+        W[128:] *= 2.0 ** -140                                  # scales at their smallest
+    if m > 200:
+        W[0, 150], W[1, 151], W[2, 152] = float("inf"), float("nan"), -float("inf")
+    W = W.to(dtype)
+    wide = torch.zeros((n, m + 3), dtype=dtype)
+    wide[:, 1:m + 1] = W
+    q, s, qt, st = slim.fp8_quantize_weights(wide.cuda()[:, 1:m + 1])
+    num, e, _ = ref.quantize(W, ref.B, ref.B)
+    same = lambda a, b: torch.equal(torch.nan_to_num(a, nan=1e9), torch.nan_to_num(b, nan=1e9))
+    assert same(q.cpu().double(), num) and torch.equal(s.cpu().double() - 127, e)
+    assert same(qt.cpu().double(), num.t()) and torch.equal(st.cpu().double() - 127, e.t())
+    for t, rows, cols in ((q, n, m), (qt, m, n)):               # the padding of every row is zero
+        whole = torch.as_strided(t, (rows, t.stride(0)), (t.stride(0), 1)).view(torch.uint8)
+        assert t.stride(0) % 128 == 0 and not whole[:, cols:].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("t", [1, 16, 17, 300])
+def test_activations_are_quantised_as_defined(slim, dtype, t):
+    """A layer that hands its inputs through shows Q(X) itself: every value there is, as numbers of a block and as its largest one."""
+    m = 384
+    bits = torch.arange(t * m, dtype=torch.int32) * 7919 % 65536
+    X = bits.to(torch.uint16).view(dtype).reshape(t, m).clone()
+    X[~torch.isfinite(X)] = 1.5
+    if dtype == torch.bfloat16:
+        X = (X.double().sign() * X.double().abs().clamp(2.0 ** -100, 2.0 ** 100)).to(dtype)     # exact through the identity
+    X[0, :128] = 448.0 if t % 2 else 449.0                       # the borders of a scale
+    X[0, 128:256] = 0.0
+    eye = torch.eye(m)
+    q, s = slim.fp8_quantize_weights(eye.cuda(), transposed=False)
+    Y = slim.fp8_linear(X.cuda(), q, s, torch.float32).cpu().double()
+    want = ref.q_rows(X)
+    # (a weight of one is 256 / 256: numbers of up to 2^8 times 2^8 in a scale's block)
+    assert torch.equal(Y, want)
+
+
+@pytest.mark.parametrize("t", [1, 5, 16, 17, 64, 200])
+def test_what_is_not_finite_stays_in_its_token(slim, t):
+    n, m = 64, 300
+    W = numbers(n, m, torch.float32, 1)
+    X = numbers(t, m, torch.bfloat16, 2)
+    q, s = slim.fp8_quantize_weights(W.cuda(), transposed=False)
+    clean = slim.fp8_linear(X.cuda(), q, s)
+    X[t - 1, 7], X[t - 1, 290] = float("inf"), float("nan")
+    Y = slim.fp8_linear(X.cuda(), q, s)
+    assert torch.isnan(Y[t - 1]).all() and torch.equal(Y[:t - 1], clean[:t - 1])
+
+
+SHAPES = [(1, 1), (16, 128), (127, 129), (130, 511), (300, 1024), (64, 4224), (700, 260)]
+
+
+@pytest.mark.parametrize("n,m", SHAPES)
+@pytest.mark.parametrize("t", [1, 2, 16, 17, 33, 130])
+@pytest.mark.parametrize("x,y", [(torch.float16, torch.float16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_forward(slim, n, m, t, x, y):
+    W, X = numbers(n, m, torch.float32, 3) * 0.02, numbers(t, m, x, 4)
+    q, s = slim.fp8_quantize_weights(W.cuda(), transposed=False)
+    s_pad = torch.as_strided(s, (s.shape[0], s.stride(0)), (s.stride(0), 1))
+    s_pad[:, s.shape[1]:] = 255                                  # (what pads a row of scales is not used)
+    Y = slim.fp8_linear(X.cuda(), q, s, y)
+    assert Y.dtype == y
+    product(ref.q_rows(X), ref.quantize(W, ref.B, ref.B)[2], Y, t <= 16)
+
+
+@pytest.mark.parametrize("n,m,t", [(1024, 512, 1100), (2304, 384, 2100), (4100, 1030, 70), (520, 9000, 96), (128, 20000, 40), (9000, 700, 16)])
+@pytest.mark.parametrize("y", [torch.bfloat16, torch.float32])
+def test_forward_of_every_tile(slim, n, m, t, y):
+    """Sizes that reach each tile and the parts of a long contraction; the layer's rows and the tokens end inside a tile."""
+    W, X = numbers(n, m, torch.float32, 5) * 0.02, numbers(t, m, torch.bfloat16, 6)
+    q, s = slim.fp8_quantize_weights(W.cuda(), transposed=False)
+    Y = slim.fp8_linear(X.cuda(), q, s, y)
+    again = slim.fp8_linear(X.cuda(), q, s, y)
+    product(ref.q_rows(X), ref.quantize(W, ref.B, ref.B)[2], Y, t <= 16)
+    assert torch.equal(Y, again)
+
+
+@pytest.mark.parametrize("n,m", [(1, 1), (127, 129), (300, 1024), (700, 260)])
+@pytest.mark.parametrize("t", [1, 17, 128, 301])
+@pytest.mark.parametrize("x,dw", [(torch.float16, torch.float16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float16, torch.float32)])
+def test_backward(slim, n, m, t, x, dw):
+    W, X, dY = numbers(n, m, torch.float32, 7) * 0.02, numbers(t, m, x, 8), numbers(t, n, x, 9) * 0.01
+    _, _, qt, st = slim.fp8_quantize_weights(W.cuda())
+    dX, dW = slim.fp8_linear_backward(dY.cuda(), X.cuda(), qt, st, dw)
+    assert dX.dtype == x and dW.dtype == dw
+    product(ref.q_rows(dY), ref.quantize(W, ref.B, ref.B)[2].t().contiguous(), dX)
+    product(ref.q_cols(dY).t().contiguous(), ref.q_cols(X).t().contiguous(), dW)
+    # one gradient alone: the same numbers as far as the sums are in the same order
+    only_x, none = slim.fp8_linear_backward(dY.cuda(), None, qt, st, dw=False)
+    assert none is None
+    product(ref.q_rows(dY), ref.quantize(W, ref.B, ref.B)[2].t().contiguous(), only_x)
+    none, only_w = slim.fp8_linear_backward(dY.cuda(), X.cuda(), None, None, dw, dx=False)
+    assert none is None
+    product(ref.q_cols(dY).t().contiguous(), ref.q_cols(X).t().contiguous(), only_w)
+
+
+@pytest.mark.parametrize("n,m,t,dw", [(2100, 1100, 1025, torch.bfloat16), (1090, 2200, 260, torch.float32), (300, 200, 5000, torch.float32)])
+def test_backward_of_large_tiles(slim, n, m, t, dw):
+    W, X, dY = numbers(n, m, torch.float32, 10) * 0.02, numbers(t, m, torch.bfloat16, 11), numbers(t, n, torch.bfloat16, 12) * 0.01
+    _, _, qt, st = slim.fp8_quantize_weights(W.cuda())
+    dX, dW = slim.fp8_linear_backward(dY.cuda(), X.cuda(), qt, st, dw)
+    product(ref.q_rows(dY), ref.quantize(W, ref.B, ref.B)[2].t().contiguous(), dX)
+    product(ref.q_cols(dY).t().contiguous(), ref.q_cols(X).t().contiguous(), dW)
+    again = slim.fp8_linear_backward(dY.cuda(), X.cuda(), qt, st, dw)
+    assert torch.equal(dX, again[0]) and torch.equal(dW, again[1])
+
+
+def test_gradients_are_those_of_the_forward_pass(slim):
+    """With numbers that the quantiser holds exactly the layer is linear: the gradients are its derivative, to the last bit of fp32, and
+    differences of the forward pass give them."""
+    g = torch.Generator().manual_seed(0)
+    small = lambda *shape: torch.randint(-3, 4, shape, generator=g).float()
+    n, m, t = 40, 200, 130
+    W, X, dY = small(n, m), small(t, m).bfloat16(), small(t, n).bfloat16()
+    q, s, qt, st = slim.fp8_quantize_weights(W.cuda())
+    dX, dW = slim.fp8_linear_backward(dY.cuda(), X.cuda(), qt, st, torch.float32)
+    f = lambda X_: (slim.fp8_linear(X_.cuda(), q, s, torch.float32).double().cpu() * dY.double()).sum()
+    assert torch.equal(dW.double().cpu(), dY.double().t() @ X.double())
+    for i, j in ((0, 0), (129, 199), (64, 77)):
+        up, down = X.clone(), X.clone()
+        up[i, j] += 1
+        down[i, j] -= 1
+        d = (f(up) - f(down)) / 2
+        assert abs(float(dX[i, j]) - float(d)) <= 2.0 ** -8 * abs(float(d))
+
+
+@pytest.mark.parametrize("t", [3, 40])
+def test_strides_and_alignment(slim, t):
+    """Rows that start anywhere, further apart than they are long; what lies between them is not read (it is NaN) or written."""
+    n, m = 150, 333
+    W, X, dY = numbers(n, m, torch.float32, 13) * 0.02, numbers(t, m, torch.float16, 14), numbers(t, n, torch.float16, 15)
+    q, s, qt, st = slim.fp8_quantize_weights(W.cuda())
+
+    def spread(v, first, gap):
+        wide = torch.full((v.shape[0] + 1, v.shape[1] + gap), float("nan"), dtype=v.dtype, device="cuda")
+        wide[:-1, first:first + v.shape[1]] = v.cuda()
+        return wide[:-1, first:first + v.shape[1]]
+
+    base = slim.fp8_linear(X.cuda(), q, s)
+    gx, gw = slim.fp8_linear_backward(dY.cuda(), X.cuda(), qt, st)
+    for first, gap in ((0, 1), (1, 2), (3, 6), (5, 8)):
+        assert torch.equal(slim.fp8_linear(spread(X, first, gap), q, s), base)
+        dX, dW = slim.fp8_linear_backward(spread(dY, first, gap), spread(X, first, gap + 1), qt, st)
+        assert torch.equal(dX, gx) and torch.equal(dW, gw)
+    # outputs in a wider matrix, through the C entry point
+    from paper_2405_14917_amd import binding as b
+    Y = torch.full((t, n + 5), 7.0, dtype=torch.float16, device="cuda")
+    Xc = X.cuda()
+    st_ = slim.lib.slim_fp8_linear(slim.ctx, Xc.data_ptr(), b.F16, t, m, q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), n, m,
+                                   Y.data_ptr() + 2, b.F16, n + 5)
+    assert st_ == b.SLIM_OK
+    assert torch.equal(Y[:, 1:n + 1], base) and bool((Y[:, 0] == 7).all()) and bool((Y[:, n + 1:] == 7).all())
+
+
+def test_no_tokens(slim):
+    q, s, qt, st = slim.fp8_quantize_weights(torch.randn(70, 200).cuda())
+    X, dY = torch.empty((0, 200), dtype=torch.float16, device="cuda"), torch.empty((0, 70), dtype=torch.float16, device="cuda")
+    assert slim.fp8_linear(X, q, s).shape == (0, 70)
+    dX, dW = slim.fp8_linear_backward(dY, X, qt, st)
+    assert dX.shape == (0, 200) and dW.shape == (70, 200) and not dW.any()
+
+
+@pytest.mark.parametrize("t", [20, 90])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_workspace_of_the_queried_size_is_enough(t, dtype):
+    from paper_2405_14917_amd import binding
+    n, m = 200, 5000
+    ncu = torch.cuda.get_device_properties(0).multi_processor_count
+    need = binding.fp8_linear_workspace(n, m, t, dtype, ncu), binding.fp8_linear_backward_workspace(n, m, t, dw_dtype=dtype, num_cus=ncu)
+    for size, ok in ((max(need), True), (min(need) - 256, False)):
+        s = binding.Slim("cuda:0", workspace_bytes=size)
+        try:
+            q, sc, qt, st = s.fp8_quantize_weights(torch.randn(n, m).cuda())
+            X, dY = torch.randn(t, m).bfloat16().cuda(), torch.randn(t, n).bfloat16().cuda()
+            for call in (lambda: s.fp8_linear(X, q, sc, dtype), lambda: s.fp8_linear_backward(dY, X, qt, st, dtype)):
+                if ok:
+                    call()
+                else:
+                    with pytest.raises(binding.SlimError) as e:
+                        call()
+                    assert e.value.status == binding.ERR_ALLOC
+            torch.cuda.synchronize()
+        finally:
+            s.close()
+
+
+def test_refusals(slim):
+    from paper_2405_14917_amd import binding
+    q, s, qt, st = slim.fp8_quantize_weights(torch.randn(70, 200).cuda())
+    X, dY = torch.randn(4, 200).half().cuda(), torch.randn(4, 70).half().cuda()
+    for bad in (lambda: slim.fp8_linear(X[:, :199], q, s), lambda: slim.fp8_linear(X.t(), q, s), lambda: slim.fp8_linear(X.cpu(), q, s),
+                lambda: slim.fp8_linear(X, q, s[:, :1]), lambda: slim.fp8_linear(X, q.contiguous(), s), lambda: slim.fp8_linear(X, s, s),
+                lambda: slim.fp8_linear(X.to(torch.int16), q, s), lambda: slim.fp8_linear(X, q, s, torch.int8),
+                lambda: slim.fp8_linear_backward(dY, X[:3], qt, st), lambda: slim.fp8_linear_backward(dY, X.bfloat16(), qt, st),
+                lambda: slim.fp8_linear_backward(dY, X, q, s), lambda: slim.fp8_linear_backward(dY, X, None, None),
+                lambda: slim.fp8_linear_backward(dY, X, qt, st, dx=False, dw=False)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: slim.fp8_linear(X.float(), q, s), lambda: slim.fp8_linear(X, q, s, torch.float64),
+                lambda: slim.fp8_quantize_weights(torch.randn(4, 4).double().cuda()),
+                lambda: slim.fp8_linear_backward(dY.float(), X.float(), qt, st)):
+        with pytest.raises(binding.SlimError) as e:
+            bad()
+        assert e.value.status == binding.ERR_UNSUPPORTED
+    with torch.cuda.stream(torch.cuda.Stream()), pytest.raises(ValueError):
+        slim.fp8_linear(X, q, s)

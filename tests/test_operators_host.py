@@ -1,0 +1,227 @@
+"""What needs no GPU of the 8-bit linear layer, the norms and the divergence from a teacher: the checks of arguments of the C entry points
+(their sources compiled for the host, with stand-ins for the HIP calls that count launches), those of the binding, and the workspace sizes."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2405_14917_amd import build
+
+PROGRAM = r"""
+#include <cstdlib>
+#include "slim_internal.h"
+
+static int launches;
+extern "C" {
+hipError_t hipMalloc(void** p, size_t bytes) { *p = malloc(bytes); return hipSuccess; }
+hipError_t hipFree(void* p) { free(p); return hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipGetLastError() { return hipSuccess; }
+const char* hipGetErrorString(hipError_t) { return ""; }
+hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
+hipError_t hipLaunchKernel(const void*, dim3 g, dim3 b, void**, size_t, hipStream_t) {
+  if (!g.x || !g.y || !g.z || b.x * b.y * b.z > 1024) printf("bad launch\n");
+  ++launches;
+  return hipSuccess;
+}
+hipError_t __hipPushCallConfiguration(dim3, dim3, size_t, hipStream_t) { return hipSuccess; }
+hipError_t __hipPopCallConfiguration(dim3* g, dim3* b, size_t* s, hipStream_t* st) { *g = *b = dim3(1, 1, 1); *s = 0; *st = nullptr; return hipSuccess; }
+void** __hipRegisterFatBinary(const void*) { static void* h; return &h; }
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void*, char*, const char*, unsigned, void*, void*, void*, void*, int*) {}
+void __hipRegisterVar(void**, void*, char*, char*, int, size_t, int, int) {}
+extern const unsigned long __hip_fatbin[1] = {0};
+}
+static void say(const char* what, int st) { printf("%s %d %d\n", what, st, launches); launches = 0; }
+
+int main() {
+  slim_ctx c;
+  c.num_cus = 256;
+  alignas(64) static char buf[1 << 16];
+  void* p = buf;
+  uint8_t* u = reinterpret_cast<uint8_t*>(buf);
+  float* f = reinterpret_cast<float*>(buf);
+  auto quantize = [&](int n, int m, int64_t ldw, int64_t ldq, int64_t lds, slim_dtype d, uint8_t* q, uint8_t* qt, uint8_t* st) {
+    return slim_fp8_quantize_weights(&c, p, d, n, m, ldw, q, ldq, u, lds, qt, 256, st, 4);
+  };
+  say("weights", quantize(130, 200, 200, 256, 4, SLIM_F32, u, u, u));
+  say("weights", quantize(130, 200, 200, 256, 4, SLIM_F32, u, nullptr, nullptr));
+  say("weights_bad", quantize(0, 200, 200, 256, 4, SLIM_F32, u, u, u));
+  say("weights_bad", quantize(130, 200, 199, 256, 4, SLIM_F32, u, u, u));
+  say("weights_bad", quantize(130, 200, 200, 200, 4, SLIM_F32, u, u, u));
+  say("weights_bad", quantize(130, 200, 200, 128, 4, SLIM_F32, u, u, u));
+  say("weights_bad", quantize(130, 200, 200, 256, 2, SLIM_F32, u, u, u));
+  say("weights_bad", quantize(130, 200, 200, 256, 4, SLIM_F32, u, u, nullptr));
+  say("weights_bad", quantize(130, 200, 200, 256, 4, SLIM_F32, u + 4, u, u));
+  say("weights_bad", quantize(130, 200, 200, 256, 4, SLIM_F32, nullptr, u, u));
+  say("weights_unsupported", quantize(130, 200, 200, 256, 4, SLIM_F64, u, u, u));
+  auto linear = [&](int t, int64_t ldx, int64_t ldq, int64_t lds, int n, int m, slim_dtype x, slim_dtype y, int64_t ldy, uint8_t* q, void* X) {
+    return slim_fp8_linear(&c, X, x, t, ldx, q, ldq, u, lds, n, m, p, y, ldy);
+  };
+  say("linear_few", linear(16, 200, 256, 4, 130, 200, SLIM_F16, SLIM_F32, 130, u, p));
+  say("linear", linear(17, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_none", linear(0, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, nullptr));
+  say("linear_bad", linear(-1, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_bad", linear(5, 199, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_bad", linear(5, 200, 255, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_bad", linear(5, 200, 256, 3, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_bad", linear(5, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 129, u, p));
+  say("linear_bad", linear(5, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, nullptr, p));
+  say("linear_bad", linear(5, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u + 8, p));
+  say("linear_bad", linear(5, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, nullptr));
+  say("linear_bad", linear(5, 200, 256, 4, 1 << 24, 200, SLIM_BF16, SLIM_BF16, 1 << 24, u, p));
+  say("linear_unsupported", linear(5, 200, 256, 4, 130, 200, SLIM_F32, SLIM_BF16, 130, u, p));
+  say("linear_unsupported", linear(5, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_F64, 130, u, p));
+  auto grad = [&](int t, void* dX, void* dW, uint8_t* qt, void* X, int64_t lddx, int64_t lddw, slim_dtype d) {
+    return slim_fp8_linear_backward(&c, p, X, SLIM_BF16, t, 130, 200, qt, 256, u, 4, 130, 200, dX, lddx, dW, d, lddw);
+  };
+  say("grad", grad(40, p, p, u, p, 200, 200, SLIM_BF16));
+  say("grad_mixed", grad(40, p, p, u, p, 200, 200, SLIM_F32));
+  say("grad_x", grad(40, p, nullptr, u, nullptr, 200, 0, SLIM_BF16));
+  say("grad_w", grad(40, nullptr, p, nullptr, p, 0, 200, SLIM_F32));
+  say("grad_none", grad(0, p, p, u, nullptr, 200, 200, SLIM_F32));
+  say("grad_bad", grad(40, nullptr, nullptr, u, p, 200, 200, SLIM_F32));
+  say("grad_bad", grad(40, p, p, nullptr, p, 200, 200, SLIM_F32));
+  say("grad_bad", grad(40, p, p, u, nullptr, 200, 200, SLIM_F32));
+  say("grad_bad", grad(40, p, p, u, p, 199, 200, SLIM_F32));
+  say("grad_bad", grad(40, p, p, u, p, 200, 199, SLIM_F32));
+  say("grad_unsupported", grad(40, p, p, u, p, 200, 200, SLIM_F64));
+  auto norm = [&](int64_t rows, int cols, int64_t ldx, void* X, void* w, slim_dtype wd, double eps) {
+    return slim_layer_norm(&c, X, SLIM_BF16, rows, cols, ldx, w, nullptr, wd, eps, 0, p, cols, f, f);
+  };
+  for (int cols : {1, 500, 1000, 2000, 4096, 8000, 30000, 70000}) say("norm", norm(9, cols, cols, p, p, SLIM_F32, 1e-5));
+  say("norm_none", norm(0, 32, 32, nullptr, p, SLIM_F32, 1e-5));
+  say("norm_bad", norm(9, 0, 32, p, p, SLIM_F32, 1e-5));
+  say("norm_bad", norm(-1, 32, 32, p, p, SLIM_F32, 1e-5));
+  say("norm_bad", norm(9, 32, 31, p, p, SLIM_F32, 1e-5));
+  say("norm_bad", norm(9, 32, 32, nullptr, p, SLIM_F32, 1e-5));
+  say("norm_bad", norm(9, 32, 32, p, nullptr, SLIM_F32, 1e-5));
+  say("norm_bad", norm(9, 32, 32, p, p, SLIM_F32, -1.0));
+  say("norm_unsupported", norm(9, 32, 32, p, p, SLIM_F16, 1e-5));
+  say("norm_unsupported", norm(9, 32, 32, p, p, SLIM_F64, 1e-5));
+  auto back = [&](int64_t rows, int cols, float* rstd, void* dw, int64_t lddx) {
+    return slim_layer_norm_backward(&c, p, p, SLIM_F32, rows, cols, cols, cols, p, SLIM_F32, nullptr, rstd, p, lddx, dw, nullptr);
+  };
+  for (int cols : {1, 500, 1000, 2000, 4096, 8000}) say("norm_back", back(9, cols, f, p, cols));
+  say("norm_back_long", back(9, 70000, f, p, 70000));
+  say("norm_back_none", back(0, 32, nullptr, p, 32));
+  say("norm_back_bad", back(9, 32, nullptr, p, 32));
+  say("norm_back_bad", back(9, 32, f, nullptr, 32));
+  say("norm_back_bad", back(9, 32, f, p, 31));
+  auto loss = [&](int64_t rows, int V, int64_t lds, int K, int64_t ldk, double tau, void* index, const float* lse, float* out) {
+    return slim_distill_loss(&c, p, SLIM_BF16, rows, V, lds, index, 1, p, SLIM_F32, K, ldk, lse, tau, out);
+  };
+  for (int V : {1, 1000, 9000, 32000, 131072, 524288}) say("distill", loss(3, V, V, 20, 20, 1.0, p, f, f));
+  say("distill", loss(3, 100, 100, 0, 0, 1.0, nullptr, nullptr, f));
+  say("distill_none", loss(0, 100, 100, 5, 5, 1.0, nullptr, nullptr, nullptr));
+  say("distill_bad", loss(3, 0, 100, 5, 5, 1.0, p, f, f));
+  say("distill_bad", loss(-1, 100, 100, 5, 5, 1.0, p, f, f));
+  say("distill_bad", loss(3, 100, 99, 5, 5, 1.0, p, f, f));
+  say("distill_bad", loss(3, 100, 100, 5, 4, 1.0, p, f, f));
+  say("distill_bad", loss(3, 100, 100, -1, 5, 1.0, p, f, f));
+  say("distill_bad", loss(3, 100, 100, 5, 5, 0.0, p, f, f));
+  say("distill_bad", loss(3, 100, 100, 5, 5, 0.0 / 0.0, p, f, f));
+  say("distill_bad", loss(3, 100, 100, 5, 5, 1.0, nullptr, f, f));
+  say("distill_bad", loss(3, 100, 100, 5, 5, 1.0, p, f, nullptr));
+  say("distill_unsupported", loss(3, 524289, 524289, 5, 5, 1.0, p, f, f));
+  say("distill_unsupported", loss(3, 100, 100, 2049, 2049, 1.0, p, f, f));
+  auto dgrad = [&](const float* dloss, void* dS, int64_t ldds) {
+    return slim_distill_loss_grad(&c, p, SLIM_F32, 3, 100, 100, p, 0, p, SLIM_BF16, 5, 5, nullptr, 2.0, dloss, f, dS, ldds);
+  };
+  say("dgrad", dgrad(f, p, 100));
+  say("dgrad_bad", dgrad(nullptr, p, 100));
+  say("dgrad_bad", dgrad(f, nullptr, 100));
+  say("dgrad_bad", dgrad(f, p, 99));
+  return 0;
+}
+"""
+
+# launches of a call that is right; a refused one has launched nothing
+EXPECTED = {"weights": (0, {1}), "linear_few": (0, {1}), "linear": (0, {2, 3}), "grad": (0, {2}), "grad_mixed": (0, {3}), "grad_x": (0, {2}), "grad_w": (0, {2}),
+            "grad_none": (0, {1}), "linear_none": (0, {0}), "norm": (0, {1}), "norm_none": (0, {0}), "norm_back": (0, {2}), "norm_back_long": (0, {3}),
+            "norm_back_none": (0, {1}), "distill": (0, {1, 2}), "distill_none": (0, {0}), "dgrad": (0, {1, 2})}
+
+
+def test_arguments_are_checked_before_anything_is_launched(tmp_path):
+    src, exe = tmp_path / "t.hip", tmp_path / "t"
+    src.write_text(PROGRAM)
+    jobs, objs = [], []
+    for f in [str(src)] + [os.path.join(build.CSRC, f) for f in build.SOURCES if f.startswith(("ctx", "fp8_", "norm", "distill"))]:
+        objs.append(str(tmp_path / (os.path.basename(f) + ".o")))
+        jobs.append(subprocess.Popen([build.hipcc(), "--offload-host-only", "-O0", "-fPIC", "-std=c++17", "-I" + build.INCLUDE, "-I" + build.CSRC, "-c", f,
+                                      "-o", objs[-1]], stderr=subprocess.DEVNULL))
+    assert not any(j.wait() for j in jobs)
+    subprocess.run(["g++", *objs, "-o", str(exe), "-pthread", "-Wl,--unresolved-symbols=ignore-in-object-files"], check=True)
+    out = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]
+    assert len(out) > 80
+    for line in out:
+        what, status, launches = line.split()
+        if what.endswith("_bad") or what.endswith("_unsupported"):
+            assert (int(status), int(launches)) == (-1 if what.endswith("_bad") else -5, 0), line
+        else:
+            want, counts = EXPECTED[what]
+            assert int(status) == want and int(launches) in counts, line
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2405_14917_amd import binding as b
+    if not os.path.exists(b.LIB_PATH):
+        build.build(verbose=False)
+    b.load()
+    return b
+
+
+def test_null_contexts_are_rejected(binding):
+    lib = binding.load()
+    for name in binding.EXPORTS:
+        if name.startswith(("slim_fp8", "slim_layer", "slim_distill")) and not name.endswith("_workspace"):
+            fn = getattr(lib, name)
+            zero = [None if a is ctypes.c_void_p else a(0).value for a in fn.argtypes]
+            assert fn(*zero) == binding.ERR_INVALID_ARG, name
+
+
+def test_the_binding_checks_strides(binding):
+    rs = binding._row_stride
+    x = torch.zeros(4, 10)
+    assert rs(x, "x") == 10 and rs(x[:, 2:7], "x") == 10 and rs(x[:1, 2:7], "x") == 5 and rs(torch.zeros(0, 7), "x") == 7
+    assert rs(torch.zeros(5, 1), "x") == 1 and rs(x[:, 3:4], "x") == 10
+    for bad in (x.t(), x[0], x[:, ::2], torch.zeros(1, 10).expand(4, 10), torch.zeros(4, 1).expand(4, 10)):
+        with pytest.raises(ValueError):
+            rs(bad, "x")
+
+
+def test_the_binding_checks_stored_weights(binding):
+    e4m3, check = torch.float8_e4m3fn, binding._stored_strides
+    q = lambda rows, ld, cols: torch.zeros(rows * ld, dtype=torch.uint8).view(e4m3).view(rows, ld)[:, :cols]
+    s = lambda rows, ld, cols: torch.zeros((rows, ld), dtype=torch.uint8)[:, :cols]
+    assert check(q(130, 256, 200), s(2, 4, 2), "W") == (256, 4)
+    short = torch.zeros(129 * 256 + 200, dtype=torch.uint8).view(e4m3)           # the last row's padding is missing
+    for a, b in ((q(130, 200, 200), s(2, 4, 2)), (q(130, 256, 200), s(2, 2, 2)), (q(130, 256, 200), s(2, 4, 3)), (q(130, 256, 200), s(1, 4, 2)),
+                 (q(130, 256, 200).view(torch.uint8), s(2, 4, 2)), (torch.as_strided(short, (130, 200), (256, 1)), s(2, 4, 2)),
+                 (q(130, 256, 200), torch.as_strided(torch.zeros(6, dtype=torch.uint8), (2, 2), (4, 1)))):
+        with pytest.raises(ValueError):
+            check(a, b, "W")
+
+
+def test_workspace_sizes_follow_the_entry_points(binding):
+    f16, f32 = torch.float16, torch.float32
+    assert binding.fp8_linear_workspace(4096, 4096, 16) == 0                     # one launch
+    t, n, m = 2048, 4096, 11008
+    assert binding.fp8_linear_workspace(n, m, t) >= t * m + t * m // 128
+    assert binding.fp8_linear_backward_workspace(n, m, t) >= t * n + n * t + m * t
+    assert binding.fp8_linear_backward_workspace(n, m, t, dw=False) < binding.fp8_linear_backward_workspace(n, m, t, dx=False)
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0)):
+        assert binding.fp8_linear_workspace(*bad) == 0 and binding.fp8_linear_backward_workspace(*bad) == 0
+    assert binding.layer_norm_backward_workspace(0, 10) == 0
+    assert binding.layer_norm_backward_workspace(9, 1000, True) == 2 * binding.layer_norm_backward_workspace(9, 1000, False) >= 2 * 4000
+    assert binding.fp8_linear_workspace(100, 100, 20, f16) <= binding.fp8_linear_workspace(100, 100, 20, f32)
+
+
+def test_head_tuning_asks_for_the_largest_workspace(binding):
+    from paper_2405_14917_amd import tuning
+    whole = tuning.workspace_query(32000, 4096, 2048)
+    assert whole >= max(binding.fp8_linear_workspace(32000, 4096, 2048), binding.layer_norm_backward_workspace(2048, 4096),
+                        binding.fp8_linear_backward_workspace(32000, 4096, 2048, dw_dtype=torch.float32))
