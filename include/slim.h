@@ -427,7 +427,9 @@ slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* 
  *            logits / tau: p = exp(t / tau - lse), and the rest 1 - sum p counts as one more class (none below 2^-20)
  *   loss     rows: sum p ln(p / q) with q = softmax(S / tau), the rest as rest ln(rest / q_rest); 0 for a row without p
  *   dS       rows x V of S's type (may be S): dloss / tau (q - p) in a slot, dloss / tau (q - rest q / q_rest) elsewhere
- * Logits of minus infinity (a padded vocabulary) have q = 0 and the gradient 0 outside the slots.  Up to 524288 classes, 2048 slots a row. */
+ * Logits of minus infinity (a padded vocabulary) have q = 0 and the gradient 0 outside the slots.  Up to 2048 slots a row.
+ * slim_distill_workspace: bytes of workspace of both (host only). */
+size_t slim_distill_workspace(int64_t rows, int V, slim_dtype s_dtype);
 slim_status slim_distill_loss(slim_ctx* ctx, const void* S, slim_dtype s_dtype, int64_t rows, int V, int64_t lds, const void* index,
                               int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                               float* loss);

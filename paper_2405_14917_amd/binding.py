@@ -33,7 +33,7 @@ EXPORTS = [
     "slim_transpose_16", "slim_pack_zeros", "slim_unpack_zeros", "slim_lwc_quantize",
     "slim_fp8_quantize_weights", "slim_fp8_linear_workspace", "slim_fp8_linear", "slim_fp8_linear_backward_workspace",
     "slim_fp8_linear_backward", "slim_layer_norm", "slim_layer_norm_backward_workspace", "slim_layer_norm_backward",
-    "slim_distill_loss", "slim_distill_loss_grad",
+    "slim_distill_workspace", "slim_distill_loss", "slim_distill_loss_grad",
     "slim_profile_enable", "slim_profile_collect", "slim_profile_entry", "slim_profile_reset",
 ]
 
@@ -141,7 +141,8 @@ def load() -> ctypes.CDLL:
     lib.slim_distill_loss.argtypes = [c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_void_p, c_int, c_void_p, c_int, c_int, c_i64,
                                       c_void_p, c_double, c_void_p]
     lib.slim_distill_loss_grad.argtypes = lib.slim_distill_loss.argtypes[:-1] + [c_void_p, c_void_p, c_void_p, c_i64]
-    for fn in (lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
+    lib.slim_distill_workspace.argtypes = [c_i64, c_int, c_int]
+    for fn in (lib.slim_distill_workspace, lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
         fn.restype = c_size_t
     lib.slim_profile_enable.argtypes = [c_void_p, c_int]
     lib.slim_profile_collect.argtypes = [c_void_p]
@@ -198,6 +199,11 @@ def fp8_linear_backward_workspace(n: int, m: int, t: int, dx: bool = True, dw: b
 def layer_norm_backward_workspace(rows: int, cols: int, bias: bool = True, num_cus: int = 0) -> int:
     """Bytes of workspace of Slim.layer_norm_backward (host only, no GPU needed)."""
     return int(load().slim_layer_norm_backward_workspace(rows, cols, int(bias), num_cus))
+
+
+def distill_workspace(rows: int, V: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes of workspace of Slim.distill_loss and Slim.distill_loss_grad for logits of `dtype` (host only, no GPU needed)."""
+    return int(load().slim_distill_workspace(rows, V, _DT[dtype]))
 
 
 def _row_stride(x: torch.Tensor, what: str) -> int:

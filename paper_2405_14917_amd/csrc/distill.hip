@@ -5,11 +5,13 @@
 //   dS = dloss / tau (q - p) in a slot, dloss / tau (q - rest q / q_rest) elsewhere (q without a rest);  rows of no p: zero
 //
 // Bound by memory: a row of logits is read once and its gradient written once.  One workgroup per row, which keeps it in registers as it
-// came: maximum, sum of exponentials, then the gradient, without a second read.  Rows that do not fit are read twice, the first time with a
-// running maximum and sum.  Outside the slots the gradient is one factor times the exponential; the slots are written over it
-// afterwards.  The sum outside the slots (with a rest) leaves them out by a bit per class in LDS: taking them from the whole sum would
-// cancel where they hold nearly all of it.  Sums over the vocabulary in fp32 (a lane's few, then a tree), exponentials of differences from
-// the maximum; whatever has one value per slot or row in fp64: the loss is a small difference of large terms.
+// came: maximum, sum of exponentials, then the gradient, without a second read.  Rows that do not fit, or are too few to fill the chip, are
+// cut into chunks of a workgroup each: one kernel leaves every chunk's maximum and sum, a second one joins them and writes the
+// gradient, its own read of the logits mostly from the cache behind the L2.  Outside the slots the gradient is one factor times the
+// exponential; the slots are written over it afterwards.  The sum outside the slots (with a rest) leaves them out by a bit per class in
+// LDS: taking them from the whole sum would cancel where they hold nearly all of it.  Sums over the vocabulary in fp32 (a lane's few,
+// then a tree; chunks in fp64), exponentials 2^(x log2(e) / tau - off) with one rounding of the argument; whatever has one value per slot
+// or row in fp64, relative to the same off: the loss is a small difference of large terms.
 #include "slim_device.h"
 #include "slim_internal.h"
 
@@ -17,8 +19,8 @@ namespace {
 
 using namespace slimdev;
 
-constexpr int DL_MAX_K = 2048, DL_MAX_V = 1 << 19;
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr int DL_MAX_K = 2048;
+constexpr double LOG2E = 1.44269504088896340736, LN2 = 0.693147180559945309417;
 
 struct DistillArgs {
   const void* S;
@@ -31,6 +33,10 @@ struct DistillArgs {
   int V, K;
   int index64, t_dtype;
   double tau;
+  // rows in chunks: `chunks` of them, their maxima and sums (rows x chunks), and the slots' sums (4 per row)
+  int chunks;
+  float2* part;
+  double* slots;
 };
 
 template <typename T>
@@ -55,29 +61,26 @@ __device__ __forceinline__ void put(void* p, int64_t i, float v) {
   else static_cast<unsigned short*>(p)[i] = narrow<T>(v);
 }
 
-// 16 bytes of a row; elements behind the row's end read as minus infinity, whose exponential is zero
+// 16 bytes of a row
 template <typename T>
 struct Piece {
   static constexpr int E = 16 / sizeof(T);
   unsigned v[4];
-  __device__ __forceinline__ void load(const T* p, int left) {
-    if (left >= E) {
-      __builtin_memcpy(v, p, 16);
-    } else if constexpr (sizeof(T) == 4) {
+  __device__ __forceinline__ void none() {                           // logits whose exponential is zero
+    constexpr unsigned NONE = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = i < left ? reinterpret_cast<const unsigned*>(p)[i] : 0xff800000u;
-    } else {
-      constexpr unsigned NONE = __is_same(T, __half) ? 0xfc00u : 0xff80u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
-        v[i] = (2 * i < left ? q[2 * i] : NONE) | (2 * i + 1 < left ? q[2 * i + 1] : NONE) << 16;
-      }
-    }
+    for (int i = 0; i < 4; ++i) v[i] = NONE;
   }
   __device__ __forceinline__ float get(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
     else return widen<T>((unsigned short)(v[i / 2] >> (16 * (i & 1))));
+  }
+  __device__ __forceinline__ void set(const float (&f)[E]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
+      else v[i] = (unsigned)narrow<T>(f[2 * i]) | (unsigned)narrow<T>(f[2 * i + 1]) << 16;
+    }
   }
   // The widened values are not kept from one use to the next: they would take twice the registers.
   __device__ __forceinline__ void narrow_again() {
@@ -85,154 +88,182 @@ struct Piece {
     asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]));
 #endif
   }
-  __device__ __forceinline__ float top() const {
-    float m = get(0);
+};
+
+__device__ __forceinline__ float exp_of(float v, float c, float off) { return __builtin_amdgcn_exp2f(fmaf(v, c, -off)); }
+
+// A range of a row in the registers of a workgroup: P pieces per thread, and the elements behind the last whole piece, one per thread.
+template <typename T, int THREADS, int P>
+struct Range {
+  static constexpr int E = Piece<T>::E;
+  Piece<T> x[P];
+  float last;
+  int pieces, rest, tid;
+  __device__ __forceinline__ void load(const T* S, int n, int t) {
+    tid = t;
+    pieces = n / E;
+    rest = n % E;
 #pragma unroll
-    for (int i = 1; i < E; ++i) m = fmaxf(m, get(i));
+    for (int i = 0; i < P; ++i) {
+      if (i * THREADS + tid < pieces) __builtin_memcpy(x[i].v, S + (i * THREADS + tid) * E, 16);
+      else x[i].none();
+    }
+    last = tid < rest ? value<T>(S, (int64_t)pieces * E + tid) : -INFINITY;
+  }
+  __device__ __forceinline__ float top() {
+    float m = last;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) m = fmaxf(m, x[i].get(e));
+      x[i].narrow_again();
+    }
     return m;
   }
-};
-template <typename T>
-__device__ __forceinline__ void store_piece(T* p, int left, const float (&f)[16 / sizeof(T)]) {
-  constexpr int E = 16 / sizeof(T);
-  unsigned v[4];
+  // sum of the exponentials; MASKED: without the classes whose bit is set
+  template <bool MASKED>
+  __device__ __forceinline__ float sum(float c, float off, const uint8_t* bits) {
+    float s = exp_of(last, c, off);
+    if (MASKED && tid < rest && (bits[(pieces * E + tid) >> 3] >> ((pieces * E + tid) & 7) & 1)) s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
-    else v[i] = (unsigned)narrow<T>(f[2 * i]) | (unsigned)narrow<T>(f[2 * i + 1]) << 16;
-  }
-  if (left >= E) {
-    __builtin_memcpy(p, v, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (i < left) {
-        if constexpr (sizeof(T) == 4) reinterpret_cast<unsigned*>(p)[i] = v[i];
-        else reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(v[i / 2] >> (16 * (i & 1)));
+    for (int i = 0; i < P; ++i) {
+      int mask = 0;
+      if constexpr (MASKED) {
+        const int at = min(i * THREADS + tid, max(pieces - 1, 0)) * E;
+        mask = (int)bits[at >> 3] >> (at & 7);
       }
+      float p = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float v = exp_of(x[i].get(e), c, off);
+        if constexpr (MASKED) v = __uint_as_float(__float_as_uint(v) & ~(unsigned)((mask << (31 - e)) >> 31));
+        p += v;
+      }
+      s += p;
+      x[i].narrow_again();
+    }
+    return s;
+  }
+  __device__ __forceinline__ void write(T* dS, float c, float off, float f) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (i * THREADS + tid < pieces) {
+        float o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = exp_of(x[i].get(e), c, off) * f;
+        Piece<T> p;
+        p.set(o);
+        store16_once(dS + (i * THREADS + tid) * E, p.v);
+      }
+    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, exp_of(last, c, off) * f);
+  }
+  __device__ __forceinline__ void write_zero(T* dS) {
+    Piece<T> p = {};
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (i * THREADS + tid < pieces) __builtin_memcpy(dS + (i * THREADS + tid) * E, p.v, 16);
+    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, 0.f);
+  }
+};
+
+// class of a slot, -1 for an empty one
+__device__ __forceinline__ int class_of(const DistillArgs& a, int64_t at) {
+  const int64_t c = a.index64 ? static_cast<const int64_t*>(a.index)[at] : (int64_t)static_cast<const int*>(a.index)[at];
+  return c >= 0 && c < a.V ? (int)c : -1;
+}
+__device__ __forceinline__ float teacher_of(const DistillArgs& a, int64_t at) {
+  return a.t_dtype == SLIM_F32 ? value<float>(a.teacher, at) : a.t_dtype == SLIM_F16 ? value<__half>(a.teacher, at) : value<__hip_bfloat16>(a.teacher, at);
+}
+
+// What a row's slots and sums make of it.  Slots: A = sum p (t - z), B = sum p (without a rest before its division by itself),
+// C = sum exp(z - z0); es: the vocabulary's sum of exp(z - z0), with a rest outside the slots.  All logits over tau.
+struct Row {
+  double total, rest, es, A, B, z0, t0;
+  bool live;
+  __device__ __forceinline__ Row(double A_, double B_, double C, double es_, double z0_, double t0_, bool with_rest)
+      : total(with_rest ? es_ + C : es_), rest(with_rest ? 1.0 - B_ : 0.0), es(es_), A(A_), B(B_), z0(z0_), t0(t0_) {
+    if (rest < 0x1p-20) rest = 0.0;
+    live = !(B + rest <= 0.0);
+  }
+  // the gradient outside the slots over the exponential
+  __device__ __forceinline__ float factor(double g) const {
+    const double other = rest > 0.0 && es > 0.0 ? 1.0 - rest * total / es : 1.0;
+    return (float)(g * other / total);
+  }
+  __device__ __forceinline__ float loss(bool with_rest) const {
+    const double lq = z0 + log(total);
+    double l = with_rest ? A + B * (lq - t0) : A / B + lq - (t0 + log(B));
+    if (rest > 0.0) l += rest * (log(rest) - log(es / total));
+    return live ? (float)l : 0.f;
+  }
+};
+
+// sums of N values over a workgroup of W wavefronts, in every thread
+template <int W, int N>
+__device__ __forceinline__ void group_sums(double (&d)[N], double (*red)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) d[i] = wave_sum(d[i]);
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[threadIdx.x >> 6][i] = d[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    d[i] = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) d[i] += red[w][i];
   }
 }
-
-__device__ __forceinline__ float wave_max_f32(float v) {
+template <int W>
+__device__ __forceinline__ float group_max(float m, float* red) {
+  m = wave_max_f32(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, WAVE));
-  return v;
-}
-__device__ __forceinline__ float wave_sum_f32(float v) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v += __shfl_xor(v, s, WAVE);
-  return v;
+  for (int w = 0; w < W; ++w) m = fmaxf(m, red[w]);
+  return m;
 }
 
-// P pieces of the row per thread in registers; P = 0: the row is read twice
+// ---- a row per workgroup --------------------------------------------------------------------------------------
 template <typename T, int THREADS, int P, bool REST, bool GRAD>
 __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
-  constexpr int E = Piece<T>::E, W = THREADS / 64;
+  constexpr int W = THREADS / 64;
   extern __shared__ __align__(16) char smem_dl[];
-  double* sp = reinterpret_cast<double*>(smem_dl);                 // p of a slot (without a rest: before its division by the sum)
-  double* se = sp + a.K;                                           // exp(z - top) of a slot
+  double* sp = reinterpret_cast<double*>(smem_dl);                 // p of a slot
+  double* se = sp + a.K;                                           // exp(z - z0) of a slot
   int* si = reinterpret_cast<int*>(se + a.K);                      // its class, or -1
   unsigned* bits = reinterpret_cast<unsigned*>(si + a.K);          // REST: a bit per class
-  __shared__ float red_m[W], red_t[W], red_e[W];
-  __shared__ double red_d[W][3];
-  __shared__ float share[2];
-  __shared__ double rows_[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ float red_m[W], red_t[W];
+  __shared__ double red_d[W][4];
+  const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
   const double itau = 1.0 / a.tau;
-  const float c = (float)(1.44269504088896340736 * itau);
+  const float c = (float)(LOG2E * itau);
 
-  Piece<T> x[P > 0 ? P : 1];
-  if constexpr (P > 0) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int at = (i * THREADS + tid) * E;
-      x[i].load(S + at, a.V - at);
-    }
-  }
-  if constexpr (REST)
+  Range<T, THREADS, P> x;
+  x.load(S, a.V, tid);
+  if constexpr (REST) {
     for (int i = tid; i < (a.V + 31) / 32; i += THREADS) bits[i] = 0u;
-  // slots
+    __syncthreads();
+  }
   float t_top = -INFINITY;
   for (int k = tid; k < a.K; k += THREADS) {
-    const int64_t at = row * a.ldk + k;
-    const int64_t cls = a.index64 ? static_cast<const int64_t*>(a.index)[at] : (int64_t)static_cast<const int*>(a.index)[at];
-    const bool used = cls >= 0 && cls < a.V;
-    si[k] = used ? (int)cls : -1;
-    if (used) {
-      const float t = a.t_dtype == SLIM_F32 ? value<float>(a.teacher, at) : a.t_dtype == SLIM_F16 ? value<__half>(a.teacher, at)
-                                                                                                  : value<__hip_bfloat16>(a.teacher, at);
+    const int cls = class_of(a, row * a.ldk + k);
+    si[k] = cls;
+    if (cls >= 0) {
+      const float t = teacher_of(a, row * a.ldk + k);
       sp[k] = (double)t;
       se[k] = (double)value<T>(S, cls);
       t_top = fmaxf(t_top, t);
+      if constexpr (REST) atomicOr(&bits[cls >> 5], 1u << (cls & 31));
     }
   }
-  // maximum (P = 0: with the sum relative to it)
-  float m = -INFINITY, e = 0.f;
-  if constexpr (P > 0) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      m = fmaxf(m, x[i].top());
-      x[i].narrow_again();
-    }
-  }
-  if constexpr (REST) {
-    __syncthreads();
-    for (int k = tid; k < a.K; k += THREADS)
-      if (si[k] >= 0) atomicOr(&bits[si[k] >> 5], 1u << (si[k] & 31));
-    __syncthreads();
-  }
-  auto sum_piece = [&](const Piece<T>& p, int at, float top) {
-    float s = 0.f;
-    int mask = 0;
-    if constexpr (REST) mask = at < a.V ? (int)reinterpret_cast<const uint8_t*>(bits)[at >> 3] >> (at & 7 & ~(E - 1)) : 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      float v = __builtin_amdgcn_exp2f((p.get(i) - top) * c);
-      if constexpr (REST) v = __uint_as_float(__float_as_uint(v) & ~(unsigned)((mask << (31 - i)) >> 31));
-      s += v;
-    }
-    return s;
-  };
-  if constexpr (P == 0) {
-    for (int at = tid * E; at < a.V; at += THREADS * E) {
-      Piece<T> p;
-      p.load(S + at, a.V - at);
-      const float mp = p.top();
-      if (mp > m) {
-        e *= __builtin_amdgcn_exp2f((m - mp) * c);
-        m = mp;
-      }
-      e += m > -INFINITY ? sum_piece(p, at, m) : (mp != mp ? mp : 0.f);
-    }
-  }
-  const float own_m = m;
-  m = wave_max_f32(m);
-  t_top = wave_max_f32(t_top);
-  if (lane == 0) {
-    red_m[wave] = m;
-    red_t[wave] = t_top;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    m = fmaxf(m, red_m[i]);
-    t_top = fmaxf(t_top, red_t[i]);
-  }
-  const float top = m;
-  if constexpr (P > 0) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      e += sum_piece(x[i], (i * THREADS + tid) * E, top);
-      x[i].narrow_again();
-    }
-  } else {
-    e = own_m > -INFINITY ? e * __builtin_amdgcn_exp2f((own_m - top) * c) : e;
-  }
-  // slots: A = sum p (t - z), B = sum p, C = sum exp(z - top); logits over tau
-  double d[3] = {0.0, 0.0, 0.0};
-  const double t0 = REST ? (double)a.lse[row] : (t_top > -INFINITY ? (double)t_top * itau : 0.0), z0 = (double)top * itau;
+  const float top = group_max<W>(x.top(), red_m);                  // (its barrier: the bits are set)
+  if constexpr (!REST) t_top = group_max<W>(t_top, red_t);
+  const float off = top * c;
+  double d[4] = {0.0, 0.0, 0.0, (double)x.template sum<REST>(c, off, reinterpret_cast<const uint8_t*>(bits))};
+  const double t0 = REST ? (double)a.lse[row] : (t_top > -INFINITY ? (double)t_top * itau : 0.0), z0 = (double)off * LN2;
   for (int k = tid; k < a.K; k += THREADS) {
     double p = 0.0, ez = 0.0;
     if (si[k] >= 0) {
@@ -246,92 +277,189 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     sp[k] = p;
     se[k] = ez;
   }
-  e = wave_sum_f32(e);
-#pragma unroll
-  for (int i = 0; i < 3; ++i) d[i] = wave_sum(d[i]);
-  if (lane == 0) {
-    red_e[wave] = e;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) red_d[wave][i] = d[i];
-  }
-  __syncthreads();
-  if (tid == 0) {
-    double es = 0.0, A = 0.0, B = 0.0, C = 0.0;
-    for (int i = 0; i < W; ++i) {
-      es += (double)red_e[i];
-      A += red_d[i][0];
-      B += red_d[i][1];
-      C += red_d[i][2];
-    }
-    const double total = REST ? es + C : es;
-    double rest = 0.0;
-    if (REST) {
-      rest = 1.0 - B;
-      if (rest < 0x1p-20) rest = 0.0;
-    }
-    const bool live = !(B + rest <= 0.0);
-    const double g = GRAD && live ? (double)a.dloss[row] * itau : 0.0;
-    const double other = rest > 0.0 && es > 0.0 ? 1.0 - rest * total / es : 1.0;
-    if (GRAD) {
-      share[0] = (float)(g * other / total);
-      share[1] = live ? 1.f : 0.f;
-      rows_[0] = g / total;
-      rows_[1] = REST ? g : g / B;
-    }
-    const double lq = z0 + log(total);
-    double l = REST ? A + B * (lq - t0) : A / B + lq - (t0 + log(B));
-    if (rest > 0.0) l += rest * (log(rest) - log(es / total));
-    a.loss[row] = live ? (float)l : 0.f;
-  }
+  group_sums<W, 4>(d, red_d);
+  const Row r(d[0], d[1], d[2], d[3], z0, t0, REST);
   if constexpr (GRAD) {
-    __syncthreads();
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
-    const float f = share[0];
-    const bool live = share[1] != 0.f;
-    auto write = [&](const Piece<T>& p, int at) {
-      float o[E];
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] = live ? __builtin_amdgcn_exp2f((p.get(i) - top) * c) * f : 0.f;
-      store_piece<T>(dS + at, a.V - at, o);
-    };
-    if constexpr (P > 0) {
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const int at = (i * THREADS + tid) * E;
-        if (at < a.V) write(x[i], at);
-      }
-    } else {
-      for (int at = tid * E; at < a.V; at += THREADS * E) {
-        Piece<T> p;
-        p.load(S + at, a.V - at);
-        write(p, at);
-      }
-    }
-    __syncthreads();
-    if (live)
+    const double g = (double)a.dloss[row] * itau;
+    if (r.live) {
+      x.write(dS, c, off, r.factor(g));
+      __syncthreads();
+      const double ge = g / r.total, gp = REST ? g : g / r.B;
       for (int k = tid; k < a.K; k += THREADS)
-        if (si[k] >= 0) put<T>(dS, si[k], (float)(se[k] * rows_[0] - sp[k] * rows_[1]));
+        if (si[k] >= 0) put<T>(dS, si[k], (float)(se[k] * ge - sp[k] * gp));
+    } else {
+      x.write_zero(dS);
+    }
   }
+  if (tid == THREADS - 64) a.loss[row] = r.loss(REST);                // (the last wavefront, whose share of the row is the smallest)
+}
+
+// ---- a chunk per workgroup --------------------------------------------------------------------------------------
+constexpr int CH_THREADS = 256, CH_P = 4;
+template <typename T>
+constexpr int CHUNK = CH_THREADS * CH_P * Piece<T>::E;            // elements
+
+// first kernel: a chunk's maximum and sum; the workgroup of the first chunk also the slots' sums
+template <typename T, bool REST>
+__global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
+  constexpr int W = CH_THREADS / 64;
+  __shared__ unsigned bits[CHUNK<T> / 32];
+  __shared__ float red_m[W], red_t[W], red_z[W];
+  __shared__ double red_d[W][3], red_e[W][1];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x / a.chunks;
+  const int chunk = (int)(blockIdx.x % a.chunks), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
+  const T* S = static_cast<const T*>(a.S) + row * a.lds;
+  const double itau = 1.0 / a.tau;
+  const float c = (float)(LOG2E * itau);
+  Range<T, CH_THREADS, CH_P> x;
+  x.load(S + c0, n, tid);
+  if constexpr (REST) {
+    for (int i = tid; i < CHUNK<T> / 32; i += CH_THREADS) bits[i] = 0u;
+    __syncthreads();
+    for (int k = tid; k < a.K; k += CH_THREADS) {
+      const int cls = class_of(a, row * a.ldk + k) - c0;
+      if (cls >= 0 && cls < n) atomicOr(&bits[cls >> 5], 1u << (cls & 31));
+    }
+  }
+  const float top = group_max<W>(x.top(), red_m);
+  // (a chunk of masked logits alone: a sum of zero, not of NaN)
+  double e[1] = {(double)x.template sum<REST>(c, top == -INFINITY ? 0.f : top * c, reinterpret_cast<const uint8_t*>(bits))};
+  group_sums<W, 1>(e, red_e);
+  if (tid == 0) a.part[row * a.chunks + chunk] = make_float2(top, (float)e[0]);
+  if (chunk != 0) return;
+  float t_top = -INFINITY, z_top = -INFINITY;
+  for (int k = tid; k < a.K; k += CH_THREADS) {
+    const int cls = class_of(a, row * a.ldk + k);
+    if (cls >= 0) {
+      t_top = fmaxf(t_top, teacher_of(a, row * a.ldk + k));
+      z_top = fmaxf(z_top, value<T>(S, cls));
+    }
+  }
+  t_top = group_max<W>(t_top, red_t);
+  z_top = group_max<W>(z_top, red_z);
+  const double t0 = REST ? (double)a.lse[row] : (t_top > -INFINITY ? (double)t_top * itau : 0.0);
+  const double zs = z_top > -INFINITY ? (double)z_top * itau : 0.0;
+  double d[3] = {0.0, 0.0, 0.0};
+  for (int k = tid; k < a.K; k += CH_THREADS) {
+    const int cls = class_of(a, row * a.ldk + k);
+    if (cls >= 0) {
+      const double t = (double)teacher_of(a, row * a.ldk + k) * itau, z = (double)value<T>(S, cls) * itau, p = exp(t - t0);
+      if (p != 0.0) d[0] += p * (t - z);
+      d[1] += p;
+      if constexpr (REST) d[2] += exp(z - zs);
+    }
+  }
+  group_sums<W, 3>(d, red_d);
+  if (tid == 0) {
+    double* s = a.slots + row * 5;
+    s[0] = d[0];
+    s[1] = d[1];
+    s[2] = d[2];
+    s[3] = zs;
+    s[4] = t0;
+  }
+}
+
+// second kernel: the row from its chunks, the gradient of a chunk; the workgroup of the first chunk also the loss.  Without the gradient one
+// wavefront per row.
+template <typename T, bool REST, bool GRAD>
+__global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillArgs a) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int per_row = GRAD ? a.chunks : 1;
+  const int64_t row = blockIdx.x / per_row;
+  const int chunk = (int)(blockIdx.x % per_row), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
+  const T* S = static_cast<const T*>(a.S) + row * a.lds;
+  const double itau = 1.0 / a.tau;
+  const float c = (float)(LOG2E * itau);
+  Range<T, CH_THREADS, CH_P> x;
+  if constexpr (GRAD) x.load(S + c0, n, tid);
+  const float2* part = a.part + row * a.chunks;
+  float top = -INFINITY;
+  for (int i = lane; i < a.chunks; i += 64) top = fmaxf(top, part[i].x);
+  top = wave_max_f32(top);
+  const float off = top * c;
+  double es = 0.0;
+  for (int i = lane; i < a.chunks; i += 64) {
+    const float2 v = part[i];
+    // (a chunk's sum is relative to the rounded product of its maximum)
+    es += v.x == -INFINITY ? (top == -INFINITY ? (double)NAN : (double)v.y) : (double)v.y * exp(((double)(v.x * c) - (double)off) * LN2);
+  }
+  es = wave_sum(es);
+  const double* s = a.slots + row * 5;
+  const double z0 = (double)off * LN2;
+  const Row r(s[0], s[1], REST && s[2] != 0.0 ? s[2] * exp(s[3] - z0) : 0.0, es, z0, s[4], REST);
+  if constexpr (GRAD) {
+    T* dS = static_cast<T*>(a.dS) + row * a.ldds;
+    const double g = (double)a.dloss[row] * itau;
+    if (r.live) {
+      // the gradients of the slots of this chunk, before their logits are written over (dS may be S)
+      extern __shared__ __align__(16) char smem_dl[];
+      float* sv = reinterpret_cast<float*>(smem_dl);
+      int* si = reinterpret_cast<int*>(sv + a.K);
+      const double ge = g / r.total, gp = REST ? g : g / r.B;
+      for (int k = tid; k < a.K; k += CH_THREADS) {
+        const int cls = class_of(a, row * a.ldk + k), at = cls - c0;
+        si[k] = cls >= 0 && at >= 0 && at < n ? at : -1;
+        if (si[k] >= 0)
+          sv[k] = (float)(exp((double)value<T>(S, cls) * itau - z0) * ge - exp((double)teacher_of(a, row * a.ldk + k) * itau - r.t0) * gp);
+      }
+      __syncthreads();
+      x.write(dS + c0, c, off, r.factor(g));
+      __syncthreads();
+      for (int k = tid; k < a.K; k += CH_THREADS)
+        if (si[k] >= 0) put<T>(dS, c0 + si[k], sv[k]);
+    } else {
+      x.write_zero(dS + c0);
+    }
+  }
+  if (chunk == 0 && tid == 0) a.loss[row] = r.loss(REST);
 }
 
 template <typename T, int THREADS, int P, bool REST, bool GRAD>
 slim_status launch(slim_ctx* ctx, const DistillArgs& a, int64_t rows) {
   const size_t smem = (size_t)a.K * 20 + (REST ? (size_t)(a.V + 31) / 32 * 4 : 0);
-  const char* name = GRAD ? "distill_grad" : "distill_loss";
-  if (smem > 48 * 1024)
-    SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&distill<T, THREADS, P, REST, GRAD>),
-                                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  SLIM_LAUNCH(ctx, name, (distill<T, THREADS, P, REST, GRAD>), dim3((unsigned)rows), dim3(THREADS), smem, a);
+  SLIM_LAUNCH(ctx, GRAD ? "distill_grad" : "distill_loss", (distill<T, THREADS, P, REST, GRAD>), dim3((unsigned)rows), dim3(THREADS), smem, a);
   return SLIM_OK;
 }
 
+// Rows as chunks: where a row does not fit a workgroup's registers (301 x 50257 fp32: 38 us; with 16 pieces in each of 1024 threads, one row
+// per CU, 88).
+constexpr int DL_ROW_PIECES = 4096;
+int chunks_of(int V, slim_dtype d) {
+  const int e = d == SLIM_F32 ? 4 : 8, chunk = CH_THREADS * CH_P * e;
+  return slim_cdiv(V, e) <= DL_ROW_PIECES ? 0 : slim_cdiv(V, chunk);
+}
+size_t part_bytes(int64_t rows, int chunks) { return slim_ws_round(sizeof(float2) * (size_t)rows * chunks); }
+size_t slot_bytes(int64_t rows) { return slim_ws_round(sizeof(double) * 5 * (size_t)rows); }
+size_t need(int64_t rows, int V, slim_dtype d) {
+  const int chunks = chunks_of(V, d);
+  return chunks ? part_bytes(rows, chunks) + slot_bytes(rows) : 0;
+}
+
 template <typename T, bool REST, bool GRAD>
-slim_status by_size(slim_ctx* ctx, const DistillArgs& a, int64_t rows) {
-  const int pieces = slim_cdiv(a.V, Piece<T>::E);
-  if (pieces <= 1024) return launch<T, 256, 4, REST, GRAD>(ctx, a, rows);
-  if (pieces <= 4096) return launch<T, 512, 8, REST, GRAD>(ctx, a, rows);
-  if (pieces <= 16384) return launch<T, 1024, 16, REST, GRAD>(ctx, a, rows);
-  return launch<T, 1024, 0, REST, GRAD>(ctx, a, rows);
+slim_status by_size(slim_ctx* ctx, DistillArgs a, int64_t rows) {
+  constexpr int E = Piece<T>::E;
+  const int pieces = a.V / E;
+  a.chunks = chunks_of(a.V, sizeof(T) == 4 ? SLIM_F32 : SLIM_BF16);
+  if (a.chunks) {
+    a.part = static_cast<float2*>(slim_ws_alloc(ctx, part_bytes(rows, a.chunks)));
+    a.slots = static_cast<double*>(slim_ws_alloc(ctx, slot_bytes(rows)));
+    if (!a.part || !a.slots) return slim_fail(ctx, SLIM_ERR_ALLOC, "slim_distill_loss: workspace");
+    SLIM_LAUNCH(ctx, "distill_chunks", (distill_chunks<T, REST>), dim3((unsigned)(rows * a.chunks)), dim3(CH_THREADS), 0, a);
+    SLIM_LAUNCH(ctx, GRAD ? "distill_join_grad" : "distill_join_loss", (distill_join<T, REST, GRAD>), dim3((unsigned)(GRAD ? rows * a.chunks : rows)),
+                dim3(GRAD ? CH_THREADS : 64), GRAD ? (size_t)a.K * 8 : 0, a);
+    return SLIM_OK;
+  }
+  // Eight pieces per thread up to 2048 pieces: of 4000 x 3000 bf16 one wavefront a row takes 19.9 us, four 24.9; 2048 x 12000 with four
+  // 26.6 us, with eight 38.0.  Beyond, many rows: four wavefronts of 16 pieces (2048 x 32000 bf16 61.5 us against 66.8 with eight of 8,
+  // 2048 x 16000 fp32 54.9 against 62.6); few rows, which take a round or two: eight of 8 (400 x 32000 16.8 us against 18.3).
+  if (pieces <= 512) return launch<T, 64, 8, REST, GRAD>(ctx, a, rows);
+  if (pieces <= 1024) return launch<T, 128, 8, REST, GRAD>(ctx, a, rows);
+  if (pieces <= 2048) return launch<T, 256, 8, REST, GRAD>(ctx, a, rows);
+  if (GRAD && rows > 6 * ctx->num_cus) return launch<T, 256, 16, REST, GRAD>(ctx, a, rows);
+  return launch<T, 512, 8, REST, GRAD>(ctx, a, rows);
 }
 
 template <typename T>
@@ -343,14 +471,17 @@ slim_status by_form(slim_ctx* ctx, const DistillArgs& a, int64_t rows, bool grad
 slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype, int64_t rows, slim_dtype t_dtype, bool grad) {
   auto is_float = [](slim_dtype d) { return d == SLIM_F16 || d == SLIM_BF16 || d == SLIM_F32; };
   if (!is_float(s_dtype) || !is_float(t_dtype)) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: logits are F16, BF16 or F32", fn);
-  SLIM_REQUIRE(ctx, rows >= 0 && rows < (1ll << 31) && a.V > 0 && a.K >= 0, "%s: rows = %lld, V = %d, K = %d", fn, (long long)rows, a.V, a.K);
-  if (a.V > DL_MAX_V || a.K > DL_MAX_K)
-    return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: up to %d classes and %d slots a row, got %d and %d", fn, DL_MAX_V, DL_MAX_K, a.V, a.K);
+  SLIM_REQUIRE(ctx, rows >= 0 && a.V > 0 && a.V < (1 << 30) && a.K >= 0, "%s: rows = %lld, V = %d, K = %d", fn, (long long)rows, a.V, a.K);
+  if (a.K > DL_MAX_K) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: up to %d slots a row, got %d", fn, DL_MAX_K, a.K);
+  if (rows * std::max(1, chunks_of(a.V, s_dtype)) >= (1ll << 31) || rows >= (1ll << 31))
+    return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: %lld rows of %d classes are too many for one call", fn, (long long)rows, a.V);
   SLIM_REQUIRE(ctx, a.tau > 0.0 && a.tau <= 1e30, "%s: tau = %g", fn, a.tau);
   if (rows == 0) return SLIM_OK;
   SLIM_REQUIRE(ctx, a.S && a.loss && (a.K == 0 || (a.index && a.teacher)), "%s: null pointer", fn);
   SLIM_REQUIRE(ctx, a.lds >= a.V && a.ldk >= a.K, "%s: rows shorter than V or K", fn);
   SLIM_REQUIRE(ctx, !grad || (a.dS && a.dloss && a.ldds >= a.V), "%s: null pointer, or rows shorter than V", fn);
+  if (const size_t bytes = need(rows, a.V, s_dtype))
+    if (const slim_status st = slim_ws_reserve(ctx, bytes); st != SLIM_OK) return st;
   a.t_dtype = (int)t_dtype;
   if (s_dtype == SLIM_F32) return by_form<float>(ctx, a, rows, grad);
   return s_dtype == SLIM_F16 ? by_form<__half>(ctx, a, rows, grad) : by_form<__hip_bfloat16>(ctx, a, rows, grad);
@@ -360,11 +491,13 @@ slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype
 
 extern "C" {
 
+size_t slim_distill_workspace(int64_t rows, int V, slim_dtype s_dtype) { return rows > 0 && V > 0 ? need(rows, V, s_dtype) : 0; }
+
 slim_status slim_distill_loss(slim_ctx* ctx, const void* S, slim_dtype s_dtype, int64_t rows, int V, int64_t lds, const void* index,
                               int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                               float* loss) {
   if (!ctx) return SLIM_ERR_INVALID_ARG;
-  DistillArgs a = {S, index, teacher, lse, nullptr, loss, nullptr, lds, ldk, 0, V, K, index64 != 0, 0, tau};
+  DistillArgs a = {S, index, teacher, lse, nullptr, loss, nullptr, lds, ldk, 0, V, K, index64 != 0, 0, tau, 0, nullptr, nullptr};
   return run(ctx, "slim_distill_loss", a, s_dtype, rows, t_dtype, false);
 }
 
@@ -372,7 +505,7 @@ slim_status slim_distill_loss_grad(slim_ctx* ctx, const void* S, slim_dtype s_dt
                                    int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                                    const float* dloss, float* loss, void* dS, int64_t ldds) {
   if (!ctx) return SLIM_ERR_INVALID_ARG;
-  DistillArgs a = {S, index, teacher, lse, dloss, loss, dS, lds, ldk, ldds, V, K, index64 != 0, 0, tau};
+  DistillArgs a = {S, index, teacher, lse, dloss, loss, dS, lds, ldk, ldds, V, K, index64 != 0, 0, tau, 0, nullptr, nullptr};
   return run(ctx, "slim_distill_loss_grad", a, s_dtype, rows, t_dtype, true);
 }
 

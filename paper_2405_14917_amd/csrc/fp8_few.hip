@@ -24,13 +24,13 @@ struct FewArgs {
 };
 
 template <typename T, int RT>
-__global__ __launch_bounds__(512) void fp8_few(FewArgs a) {
+__global__ __launch_bounds__(RT == 1 ? 1024 : 512) void fp8_few(FewArgs a) {
   constexpr int ROWS = 16 * RT, LD = ROWS + 4;                 // floats per token of a wavefront's sums
   extern __shared__ __align__(16) float part[];                // [wavefront][token][row]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), nw = blockDim.x >> 6;
   const int l16 = lane & 15, c = lane >> 4;
   const int row0 = blockIdx.x * ROWS;
-  const bool live = l16 < a.t;
+  // (tokens that do not exist are the last one again: their columns of the product are not stored)
   const T* xrow = static_cast<const T*>(a.X) + (int64_t)min(l16, a.t - 1) * a.ldx + c * 16;
   const uint8_t* wrow[RT];
 #pragma unroll
@@ -41,59 +41,84 @@ __global__ __launch_bounds__(512) void fp8_few(FewArgs a) {
   for (int r = 0; r < RT; ++r) acc[r] = v4f{0.f, 0.f, 0.f, 0.f};
 
   const int steps = (a.mb + 3) / 4;
-  for (int st = wave; st < steps; st += nw) {
-    unsigned x[4][2][8];
+  unsigned x[4][16];
+  uint4 w[4][RT][2];
+  int ws;
+  auto load_x = [&](int j, int st) {
+    const int ch = (st * 4 + j) * BLOCK;
+    if (ch + BLOCK <= a.m) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int h = 0; h < 4; ++h) __builtin_memcpy(&x[j][4 * h], xrow + ch + (h >> 1) * 64 + (h & 1) * 8, 16);
+    } else {                                                    // (behind the last channel everything reads as zero)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int ch = (st * 4 + j) * BLOCK + h * 64;          // (behind the last channel everything reads as zero)
-        unsigned (&v)[8] = x[j][h];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0u;
-        if (live) {
-          load8(xrow + ch, a.m - ch - c * 16, *reinterpret_cast<unsigned(*)[4]>(&v[0]));
-          load8(xrow + ch + 8, a.m - ch - c * 16 - 8, *reinterpret_cast<unsigned(*)[4]>(&v[4]));
-        }
+      for (int h = 0; h < 4; ++h) {
+        const int at = ch + (h >> 1) * 64 + (h & 1) * 8;
+        load8(xrow + at, a.m - at - c * 16, *reinterpret_cast<unsigned(*)[4]>(&x[j][4 * h]));
       }
-    uint4 w[4][RT][2];
+    }
+  };
+  auto load_w = [&](int j, int st) {
+    const int64_t at = (int64_t)min(st * 4 + j, a.mb - 1) * BLOCK;   // (a block behind the last: the last one again, times zeros)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)                            // (a block behind the last: the last one again, times zeros)
-          w[j][r][h] = *reinterpret_cast<const uint4*>(wrow[r] + (int64_t)min(st * 4 + j, a.mb - 1) * BLOCK + h * 64);
-    int ws = *reinterpret_cast<const int*>(srow + st * 4);
-    if (st * 4 + 4 > a.mb) ws &= (1 << (8 * (a.mb - st * 4))) - 1;      // (what pads a row of scales may be anything, a NaN's code too)
-    auto block = [&](auto index) {
-      constexpr int J = decltype(index)::value;
-      unsigned (&v)[16] = *reinterpret_cast<unsigned(*)[16]>(&x[J][0][0]);
-      unsigned mx = amax_x2(v);
+      for (int h = 0; h < 2; ++h) w[j][r][h] = *reinterpret_cast<const uint4*>(wrow[r] + at + h * 64);
+  };
+  auto load_s = [&](int st) {
+    int v = *reinterpret_cast<const int*>(srow + st * 4);
+    if (st * 4 + 4 > a.mb) v &= (1 << (8 * (a.mb - st * 4))) - 1;      // (what pads a row of scales may be anything, a NaN's code too)
+    return v;
+  };
+  auto block = [&](auto index) {
+    constexpr int J = decltype(index)::value;
+    unsigned mx = amax_x2(x[J]);
+    mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
+    mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
+    unsigned top = larger_half(mx);
+    if (__builtin_expect(__any(top >= Half16<T>::INF), 0)) {
+      mx = amax_finite_x2<T>(x[J]);
       mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
       mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
-      unsigned top = larger_half(mx);
-      if (__builtin_expect(__any(top >= Half16<T>::INF), 0)) {
-        mx = amax_finite_x2<T>(v);
-        mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
-        mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
-        top = larger_half(mx);
-      }
-      const float sx = __uint_as_float(scale_byte(Half16<T>::float_bits(top)) << 23), sw = scale_of<J>(ws);
+      top = larger_half(mx);
+    }
+    const float sx = __uint_as_float(scale_byte(Half16<T>::float_bits(top)) << 23), sw = scale_of<J>(ws);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const v8bf xb = dequantized((int)to_e4m3<T>(v[4 * i], v[4 * i + 1], sx), (int)to_e4m3<T>(v[4 * i + 2], v[4 * i + 3], sx), sx);
+    for (int i = 0; i < 4; ++i) {
+      const v8bf xb = dequantized((int)to_e4m3<T>(x[J][4 * i], x[J][4 * i + 1], sx), (int)to_e4m3<T>(x[J][4 * i + 2], x[J][4 * i + 3], sx), sx);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const uint4 wv = w[J][r][i >> 1];
-          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequantized((int)((i & 1) ? wv.z : wv.x), (int)((i & 1) ? wv.w : wv.y), sw), xb, acc[r], 0, 0, 0);
-        }
+      for (int r = 0; r < RT; ++r) {
+        const uint4 wv = w[J][r][i >> 1];
+        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequantized((int)((i & 1) ? wv.z : wv.x), (int)((i & 1) ? wv.w : wv.y), sw), xb, acc[r], 0, 0, 0);
       }
+    }
+  };
+  if (wave < steps) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      load_x(j, wave);
+      load_w(j, wave);
+    }
+    ws = load_s(wave);
+  }
+  for (int st = wave; st < steps; st += nw) {
+    const int next = st + nw;
+    const int ws_next = next < steps ? load_s(next) : 0;
+    auto refill = [&](int j) {                                  // a block that is used up makes room for the one four on
+      if (next < steps) {
+        load_x(j, next);
+        load_w(j, next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     };
     block(std::integral_constant<int, 0>());
+    refill(0);
     block(std::integral_constant<int, 1>());
+    refill(1);
     block(std::integral_constant<int, 2>());
+    refill(2);
     block(std::integral_constant<int, 3>());
+    refill(3);
+    ws = ws_next;
   }
   // a lane holds rows 4 c .. + 3 of its token
 #pragma unroll
@@ -112,20 +137,19 @@ __global__ __launch_bounds__(512) void fp8_few(FewArgs a) {
   }
 }
 
+template <typename T, int RT>
+slim_status launch(slim_ctx* ctx, const FewArgs& a, int nw) {
+  constexpr int ROWS = 16 * RT;
+  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT>), dim3(slim_cdiv(a.n, ROWS)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
+  return SLIM_OK;
+}
+
 template <typename T>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
-  // Wavefronts: one per 512 channels, eight at most.
-  const int steps = (a.mb + 3) / 4;
-  const int nw = std::min(8, steps);
-  const bool wide = slim_cdiv(a.n, 32) >= 2 * ctx->num_cus;
-  const int rows = wide ? 32 : 16;
-  const dim3 grid(slim_cdiv(a.n, rows)), block(64 * nw);
-  const size_t shmem = sizeof(float) * (size_t)nw * 16 * (rows + 4);
-  if (wide)
-    SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, 2>), grid, block, shmem, a);
-  else
-    SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, 1>), grid, block, shmem, a);
-  return SLIM_OK;
+  const int steps = (a.mb + 3) / 4, ncu = ctx->num_cus;
+  const int rt = slim_cdiv(a.n, 64) * 5 >= ncu * 3 ? 4 : slim_cdiv(a.n, 32) * 5 >= ncu * 3 ? 2 : 1;
+  const int nw = std::max(1, std::min(steps, std::max(2, std::min(rt == 1 ? 16 : 8, 8 * ncu / slim_cdiv(a.n, 16 * rt)))));
+  return rt == 4 ? launch<T, 4>(ctx, a, nw) : rt == 2 ? launch<T, 2>(ctx, a, nw) : launch<T, 1>(ctx, a, nw);
 }
 
 }  // namespace

@@ -53,6 +53,13 @@ __device__ __forceinline__ void load4<double>(const double* p, double out[4]) {
   out[3] = b.y;
 }
 
+// 16 bytes that nobody reads soon, to an address of any alignment of its 16-bit elements
+typedef unsigned uint4_unaligned __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store16_once(void* p, const unsigned (&v)[4]) {
+  const uint4_unaligned u = {v[0], v[1], v[2], v[3]};
+  __builtin_nontemporal_store(u, static_cast<uint4_unaligned*>(p));
+}
+
 // ---- wavefront (64 lanes) reductions: every lane ends up with the result ------------------------
 __device__ __forceinline__ double shfl_xor_f64(double v, int mask) {
   int lo = __double2loint(v), hi = __double2hiint(v);
@@ -97,6 +104,20 @@ __device__ __forceinline__ double wave_allreduce(double v) {
 __device__ __forceinline__ double wave_sum(double v) { return wave_allreduce<OpSum>(v); }
 __device__ __forceinline__ double wave_min(double v) { return wave_allreduce<OpMin>(v); }
 __device__ __forceinline__ double wave_max(double v) { return wave_allreduce<OpMax>(v); }
+struct OpSumF { __device__ static float f(float a, float b) { return a + b; } };
+struct OpMaxF { __device__ static float f(float a, float b) { return fmaxf(a, b); } };
+template <typename OP>
+__device__ __forceinline__ float wave_allreduce_f32(float v) {
+  v = OP::f(v, __int_as_float(dpp_b32<DPP_XOR1>(__float_as_int(v))));
+  v = OP::f(v, __int_as_float(dpp_b32<DPP_XOR2>(__float_as_int(v))));
+  v = OP::f(v, __int_as_float(dpp_b32<DPP_HALF_MIRROR>(__float_as_int(v))));
+  v = OP::f(v, __int_as_float(dpp_b32<DPP_MIRROR>(__float_as_int(v))));
+  const int i = __float_as_int(v);
+  return OP::f(OP::f(__int_as_float(__builtin_amdgcn_readlane(i, 0)), __int_as_float(__builtin_amdgcn_readlane(i, 16))),
+               OP::f(__int_as_float(__builtin_amdgcn_readlane(i, 32)), __int_as_float(__builtin_amdgcn_readlane(i, 48))));
+}
+__device__ __forceinline__ float wave_sum_f32(float v) { return wave_allreduce_f32<OpSumF>(v); }
+__device__ __forceinline__ float wave_max_f32(float v) { return wave_allreduce_f32<OpMaxF>(v); }
 __device__ __forceinline__ int wave_sum_int(int v) {
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) v += __shfl_xor(v, s, WAVE);

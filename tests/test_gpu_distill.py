@@ -203,6 +203,44 @@ def test_strides_alignment_and_in_place(slim, V, dtype):
         assert torch.isnan(wide[:, :first]).all() and torch.isnan(wide[:, first + V:]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_million_classes(slim, dtype):
+    S, index, t, dloss, l = data(2, 1000003, 50, dtype, 9, 1.0, True, pad=1000)
+    check(slim, S, index, t, dloss, 1.0, l)
+    check(slim, S, index, t, dloss, 1.0, None)
+
+
+@pytest.mark.parametrize("V,masked", [(70001, slice(0, 40000)), (131072, slice(8192, 131072))])
+def test_chunks_of_masked_logits(slim, V, masked):
+    """Whole chunks of minus infinity, before the first logit and behind the last."""
+    S, index, t, dloss, l = data(3, V, 8, torch.float32, 10, 1.0, True, empty=False)
+    S[:, masked] = -math.inf
+    keep = torch.isfinite(S)
+    t, index = torch.topk(torch.where(keep, S + 0.3, -math.inf), 8, dim=1)
+    l = torch.logsumexp(torch.where(keep, S.double() + 0.3, -math.inf), 1).float() + 0.5
+    check(slim, S, index, t, dloss, 1.0, l)
+    check(slim, S, index, t, dloss, 1.0, None)
+
+
+def test_a_workspace_of_the_queried_size_is_enough():
+    from paper_2405_14917_amd import binding
+    S, index, t, dloss, l = (v.cuda() for v in data(5, 70001, 9, torch.float32, 11, 1.0, True))
+    need = binding.distill_workspace(5, 70001, torch.float32)
+    for size, ok in ((need, True), (need - 256, False)):
+        s = binding.Slim("cuda:0", workspace_bytes=size)
+        try:
+            for call in (lambda: s.distill_loss(S, index, t, lse=l), lambda: s.distill_loss_grad(S, index, t, dloss)):
+                if ok:
+                    call()
+                else:
+                    with pytest.raises(binding.SlimError) as e:
+                        call()
+                    assert e.value.status == binding.ERR_ALLOC
+            torch.cuda.synchronize()
+        finally:
+            s.close()
+
+
 def test_no_rows_and_no_slots(slim):
     S = torch.randn(0, 50, device="cuda")
     none = torch.empty((0, 3), device="cuda")
@@ -222,10 +260,10 @@ def test_refusals(slim):
                 lambda: slim.distill_loss_grad(S, index, t, dloss.double()), lambda: slim.distill_loss_grad(S, index, t, dloss, dS=S.half())):
         with pytest.raises(ValueError):
             bad()
-    wide = torch.zeros((1, 1 << 20), device="cuda")
+    many = index.repeat(1, 410), t.repeat(1, 410)
     for bad, status in ((lambda: slim.distill_loss(S, index, t, 0.0), binding.ERR_INVALID_ARG), (lambda: slim.distill_loss(S, index, t, float("nan")), binding.ERR_INVALID_ARG),
                         (lambda: slim.distill_loss(S.double(), index, t), binding.ERR_UNSUPPORTED),
-                        (lambda: slim.distill_loss(wide, index[:1], t[:1]), binding.ERR_UNSUPPORTED)):
+                        (lambda: slim.distill_loss(S, *many), binding.ERR_UNSUPPORTED)):
         with pytest.raises(binding.SlimError) as e:
             bad()
         assert e.value.status == status

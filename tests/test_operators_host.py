@@ -113,7 +113,7 @@ int main() {
   auto loss = [&](int64_t rows, int V, int64_t lds, int K, int64_t ldk, double tau, void* index, const float* lse, float* out) {
     return slim_distill_loss(&c, p, SLIM_BF16, rows, V, lds, index, 1, p, SLIM_F32, K, ldk, lse, tau, out);
   };
-  for (int V : {1, 1000, 9000, 32000, 131072, 524288}) say("distill", loss(3, V, V, 20, 20, 1.0, p, f, f));
+  for (int V : {1, 1000, 9000, 32000, 131072, 524289}) say("distill", loss(3, V, V, 20, 20, 1.0, p, f, f));
   say("distill", loss(3, 100, 100, 0, 0, 1.0, nullptr, nullptr, f));
   say("distill_none", loss(0, 100, 100, 5, 5, 1.0, nullptr, nullptr, nullptr));
   say("distill_bad", loss(3, 0, 100, 5, 5, 1.0, p, f, f));
@@ -125,7 +125,7 @@ int main() {
   say("distill_bad", loss(3, 100, 100, 5, 5, 0.0 / 0.0, p, f, f));
   say("distill_bad", loss(3, 100, 100, 5, 5, 1.0, nullptr, f, f));
   say("distill_bad", loss(3, 100, 100, 5, 5, 1.0, p, f, nullptr));
-  say("distill_unsupported", loss(3, 524289, 524289, 5, 5, 1.0, p, f, f));
+  say("distill_unsupported", loss(1ll << 26, 1 << 20, 1 << 20, 5, 5, 1.0, p, f, f));
   say("distill_unsupported", loss(3, 100, 100, 2049, 2049, 1.0, p, f, f));
   auto dgrad = [&](const float* dloss, void* dS, int64_t ldds) {
     return slim_distill_loss_grad(&c, p, SLIM_F32, 3, 100, 100, p, 0, p, SLIM_BF16, 5, 5, nullptr, 2.0, dloss, f, dS, ldds);
@@ -217,6 +217,8 @@ def test_workspace_sizes_follow_the_entry_points(binding):
         assert binding.fp8_linear_workspace(*bad) == 0 and binding.fp8_linear_backward_workspace(*bad) == 0
     assert binding.layer_norm_backward_workspace(0, 10) == 0
     assert binding.layer_norm_backward_workspace(9, 1000, True) == 2 * binding.layer_norm_backward_workspace(9, 1000, False) >= 2 * 4000
+    assert binding.distill_workspace(0, 10) == binding.distill_workspace(10, 1000) == 0       # a row per workgroup
+    assert binding.distill_workspace(10, 131072, f32) >= 10 * (131072 // 4096) * 8
     assert binding.fp8_linear_workspace(100, 100, 20, f16) <= binding.fp8_linear_workspace(100, 100, 20, f32)
 
 
