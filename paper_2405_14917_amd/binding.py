@@ -210,14 +210,13 @@ def _row_stride(x: torch.Tensor, what: str) -> int:
     """The leading dimension of a matrix whose rows are contiguous."""
     if x.dim() != 2:
         raise ValueError("%s has to be a matrix, got %d dimensions" % (what, x.dim()))
-    if x.shape[0] <= 1 or x.shape[1] == 0:
-        if x.shape[1] > 1 and x.stride(1) != 1:
-            raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
-        return max(x.shape[1], 1)
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    rows, cols = x.shape
+    ld, step = x.stride()
+    if step != 1 and cols > 1:
         raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
-    ld = x.stride(0)
-    if ld < x.shape[1]:
+    if rows <= 1 or cols == 0:
+        return max(cols, 1)
+    if ld < cols:
         raise ValueError("rows of %s overlap" % what)
     return ld
 
@@ -228,16 +227,16 @@ def _stored_strides(q: torch.Tensor, s: torch.Tensor, what: str):
         raise ValueError("%s has to be a float8_e4m3fn matrix, its scales a uint8 matrix" % what)
     n, m = q.shape
     nb, mb = (n + 127) // 128, (m + 127) // 128
-    if tuple(s.shape) != (nb, mb):
+    if s.shape != (nb, mb):
         raise ValueError("%s (%d x %d) needs %d x %d scales, got %d x %d" % (what, n, m, nb, mb, s.shape[0], s.shape[1]))
-    ldq, lds = q.stride(0), s.stride(0)
-    if q.stride(1) != 1 and m > 1 or s.stride(1) != 1 and mb > 1:
+    (ldq, qstep), (lds, sstep) = q.stride(), s.stride()
+    if qstep != 1 and m > 1 or sstep != 1 and mb > 1:
         raise ValueError("libslim takes row-major tensors (last dimension contiguous): %s" % what)
     if ldq % 128 or lds % 4 or ldq < m or lds < mb:
         raise ValueError("rows of %s have to be whole blocks of 128 and those of its scales whole words apart, got %d and %d" % (what, ldq, lds))
     # rows are read to the end of their last block, and scales by the word: the padding of the last row has to be there as well
-    if (q.untyped_storage().nbytes() - q.storage_offset() < (n - 1) * ldq + mb * 128 or
-            s.untyped_storage().nbytes() - s.storage_offset() < (nb - 1) * lds + (mb + 3) // 4 * 4):
+    if (m % 128 and q.untyped_storage().nbytes() - q.storage_offset() < (n - 1) * ldq + mb * 128 or
+            mb % 4 and s.untyped_storage().nbytes() - s.storage_offset() < (nb - 1) * lds + (mb + 3) // 4 * 4):
         raise ValueError("the padding of the last row of %s or of its scales is missing" % what)
     return ldq, lds
 
@@ -262,6 +261,7 @@ class Slim:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = torch.cuda.current_stream(self.device)
+        self._index, self._raw_stream = self.device.index or 0, self.stream.cuda_stream
         self.workspace = (torch.empty(workspace_bytes + 256, dtype=torch.uint8, device=self.device)
                           if workspace_bytes > 0 else None)
         ws_ptr = None
@@ -515,11 +515,11 @@ class Slim:
     # ---- around a quantised layer: 8-bit linear layer, norms, divergence from a teacher
     def _ready(self, *tensors):
         """Tensors on the context's device, and the context's stream current: outputs are allocated on the current one."""
-        index = self.device.index or 0
+        index = self._index
         for t in tensors:
             if t is not None and t.get_device() != index:
                 raise ValueError("libslim takes tensors of the context's device")
-        if _current_stream(index) != self.stream.cuda_stream:
+        if _current_stream(index) != self._raw_stream:
             raise ValueError("the context is bound to another stream than the current one")
 
     def fp8_quantize_weights(self, W: torch.Tensor, transposed: bool = True):
@@ -548,9 +548,11 @@ class Slim:
         if X.dim() != 2 or X.shape[1] != m:
             raise ValueError("X has to be (t, %d), got %s" % (m, tuple(X.shape)))
         t = X.shape[0]
-        Y = torch.empty((t, n), dtype=dtype or X.dtype, device=X.device)
-        self._check(self.lib.slim_fp8_linear(self.ctx, X.data_ptr(), _dtype(X), t, _row_stride(X, "X"), W.data_ptr(), ldq, Ws.data_ptr(), lds,
-                                             n, m, Y.data_ptr(), _dtype(Y), n))
+        Y = X.new_empty((t, n), dtype=dtype)
+        st = self.lib.slim_fp8_linear(self.ctx, X.data_ptr(), _dtype(X), t, _row_stride(X, "X"), W.data_ptr(), ldq, Ws.data_ptr(), lds, n, m,
+                                      Y.data_ptr(), _dtype(Y), n)
+        if st:
+            self._check(st)
         return Y
 
     def fp8_linear_backward(self, dY: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[torch.Tensor], Wts: Optional[torch.Tensor],
@@ -589,21 +591,25 @@ class Slim:
         (Y, mean, rstd) for the backward pass (mean is None with `rms`)."""
         self._ready(X, w, b)
         rows, cols = self._norm_shape(X, w, b)
-        Y = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
-        mean = torch.empty(rows, dtype=torch.float32, device=X.device) if stats and not rms else None
-        rstd = torch.empty(rows, dtype=torch.float32, device=X.device) if stats else None
-        self._check(self.lib.slim_layer_norm(self.ctx, X.data_ptr(), _dtype(X), rows, cols, _row_stride(X, "X"), w.data_ptr(),
-                                             None if b is None else b.data_ptr(), _dtype(w), eps, int(rms), Y.data_ptr(), cols,
-                                             None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr()))
+        Y = X.new_empty((rows, cols))
+        mean = rstd = None
+        if stats:
+            mean = None if rms else X.new_empty(rows, dtype=torch.float32)
+            rstd = X.new_empty(rows, dtype=torch.float32)
+        st = self.lib.slim_layer_norm(self.ctx, X.data_ptr(), _dtype(X), rows, cols, _row_stride(X, "X"), w.data_ptr(),
+                                      None if b is None else b.data_ptr(), _dtype(w), eps, rms, Y.data_ptr(), cols,
+                                      None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr())
+        if st:
+            self._check(st)
         return (Y, mean, rstd) if stats else Y
 
     @staticmethod
     def _norm_shape(X, w, b):
-        if X.dim() != 2 or tuple(w.shape) != (X.shape[1],) or b is not None and (b.shape != w.shape or b.dtype != w.dtype):
+        if X.dim() != 2 or w.shape != X.shape[1:] or b is not None and (b.shape != w.shape or b.dtype != w.dtype):
             raise ValueError("X has to be a matrix, w and b vectors of its columns and of one type")
-        if w.stride(0) != 1 and w.shape[0] > 1 or b is not None and b.stride(0) != 1 and b.shape[0] > 1:
+        if not w.is_contiguous() or b is not None and not b.is_contiguous():
             raise ValueError("w and b have to be contiguous")
-        return X.shape[0], X.shape[1]
+        return X.shape
 
     def layer_norm_backward(self, dY: torch.Tensor, X: torch.Tensor, w: torch.Tensor, mean: Optional[torch.Tensor], rstd: torch.Tensor,
                             bias: bool = False):
@@ -615,9 +621,8 @@ class Slim:
         for v in (mean, rstd):
             if v is not None and (v.dtype != torch.float32 or tuple(v.shape) != (rows,) or not v.is_contiguous()):
                 raise ValueError("mean and rstd have to be float32 vectors of X's rows")
-        dX = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
-        dw = torch.empty(cols, dtype=w.dtype, device=X.device)
-        db = torch.empty(cols, dtype=w.dtype, device=X.device) if bias else None
+        dX, dw = X.new_empty((rows, cols)), w.new_empty(cols)
+        db = w.new_empty(cols) if bias else None
         self._check(self.lib.slim_layer_norm_backward(self.ctx, dY.data_ptr(), X.data_ptr(), _dtype(X), rows, cols, _row_stride(dY, "dY"),
                                                       _row_stride(X, "X"), w.data_ptr(), _dtype(w), None if mean is None else mean.data_ptr(),
                                                       rstd.data_ptr(), dX.data_ptr(), cols, dw.data_ptr(), None if db is None else db.data_ptr()))
@@ -641,8 +646,10 @@ class Slim:
         """loss float32 (rows,): the divergence of softmax(S / tau) from the teacher's top logits (rows, K) of the classes `index`."""
         self._ready(S, index, teacher, lse)
         args = self._distill_args(S, index, teacher, tau, lse)
-        loss = torch.empty(S.shape[0], dtype=torch.float32, device=S.device)
-        self._check(self.lib.slim_distill_loss(*args, loss.data_ptr()))
+        loss = S.new_empty(args[3], dtype=torch.float32)
+        st = self.lib.slim_distill_loss(*args, loss.data_ptr())
+        if st:
+            self._check(st)
         return loss
 
     def distill_loss_grad(self, S: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, dloss: torch.Tensor, tau: float = 1.0,
@@ -653,10 +660,10 @@ class Slim:
         if dloss.dtype != torch.float32 or tuple(dloss.shape) != (S.shape[0],) or not dloss.is_contiguous():
             raise ValueError("dloss has to be a float32 vector of the rows")
         if dS is None:
-            dS = torch.empty(S.shape, dtype=S.dtype, device=S.device)
+            dS = S.new_empty(S.shape)
         elif dS.shape != S.shape or dS.dtype != S.dtype:
             raise ValueError("dS has to be of S's shape and type")
-        loss = torch.empty(S.shape[0], dtype=torch.float32, device=S.device)
+        loss = S.new_empty(args[3], dtype=torch.float32)
         self._check(self.lib.slim_distill_loss_grad(*args, dloss.data_ptr(), loss.data_ptr(), dS.data_ptr(), _row_stride(dS, "dS")))
         return loss, dS
 

@@ -114,6 +114,13 @@ __device__ __forceinline__ void load8(const T* p, int left, unsigned (&v)[4]) {
   }
 }
 
+// The same, row_end_shift<8> pending (which with fewer than 8 columns has nothing to do).
+template <typename T>
+__device__ __forceinline__ void fetch8(const T* p, int left, int cols, unsigned (&v)[4]) {
+  if (cols >= 8) __builtin_memcpy(v, row_end_address<8>(p, left), 16);
+  else load8(p, left, v);
+}
+
 // ---- what fp8_gemm.hip offers the entry points ---------------------------------------------------------------
 // rows x K e4m3 numbers (whole blocks of K, ld bytes apart), and a scale for every block: that of row r is in row r >> shift
 struct Operand {

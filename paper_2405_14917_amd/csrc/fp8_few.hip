@@ -53,9 +53,15 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void fp8_few(FewArgs a) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const int at = ch + (h >> 1) * 64 + (h & 1) * 8;
-        load8(xrow + at, a.m - at - c * 16, *reinterpret_cast<unsigned(*)[4]>(&x[j][4 * h]));
+        fetch8(xrow + at, a.m - at - c * 16, a.m, *reinterpret_cast<unsigned(*)[4]>(&x[j][4 * h]));
       }
     }
+  };
+  auto end_x = [&](int j, int st) {
+    const int ch = (st * 4 + j) * BLOCK;
+    if (ch + BLOCK > a.m && a.m >= 8)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) row_end_shift<8>(*reinterpret_cast<unsigned(*)[4]>(&x[j][4 * h]), a.m - ch - (h >> 1) * 64 - (h & 1) * 8 - c * 16);
   };
   auto load_w = [&](int j, int st) {
     const int64_t at = (int64_t)min(st * 4 + j, a.mb - 1) * BLOCK;   // (a block behind the last: the last one again, times zeros)
@@ -69,8 +75,9 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void fp8_few(FewArgs a) {
     if (st * 4 + 4 > a.mb) v &= (1 << (8 * (a.mb - st * 4))) - 1;      // (what pads a row of scales may be anything, a NaN's code too)
     return v;
   };
-  auto block = [&](auto index) {
+  auto block = [&](auto index, int st) {
     constexpr int J = decltype(index)::value;
+    end_x(J, st);
     unsigned mx = amax_x2(x[J]);
     mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
     mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
@@ -110,13 +117,13 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void fp8_few(FewArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    block(std::integral_constant<int, 0>());
+    block(std::integral_constant<int, 0>(), st);
     refill(0);
-    block(std::integral_constant<int, 1>());
+    block(std::integral_constant<int, 1>(), st);
     refill(1);
-    block(std::integral_constant<int, 2>());
+    block(std::integral_constant<int, 2>(), st);
     refill(2);
-    block(std::integral_constant<int, 3>());
+    block(std::integral_constant<int, 3>(), st);
     refill(3);
     ws = ws_next;
   }

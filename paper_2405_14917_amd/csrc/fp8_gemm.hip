@@ -1,22 +1,30 @@
 // The scaled matrix product of the 8-bit linear layer: C[b][a] = sum over blocks of 128 of 2^(ea + eb - 254) A[a] . B[b], both operands
 // rows of e4m3 numbers along the contraction; forward A = weights, B = activations; gradients: fp8_linear.hip.
 //
-//  * v_mfma_scale_f32_32x32x64_f8f6f4 takes the scales themselves (one byte per row and 32 of the contraction, here the same for 128),
-//    so the fp32 sums stay in its registers from the first block to the last: no rescaling between blocks.
-//  * Workgroup tile TA x TB, contraction 128 bytes a step, from memory to LDS directly, two stages; one wait and one barrier a step.
-//    A row of a stage is 8 chunks of 16 bytes, chunk c at place c ^ (row / 2 % 8): 16 lanes that read one chunk of 16 rows hit sixteen
-//    different groups of four banks.  The scales of four steps (a word per row) come the same way.
+//  * 16-bit C: v_mfma_scale_f32_32x32x64_f8f6f4 takes the scales themselves (one byte per row and 32 of the contraction, here the same for
+//    128), so the fp32 sums stay in its registers from the first block to the last: no rescaling between blocks.  fp32 C: the numbers
+//    times their scales as bf16 (fp8_device.h: dequantized), converted in registers beside the products of v_mfma_f32_32x32x16_bf16.
+//  * Workgroup tile TA x TB, contraction 128 bytes a step, from memory to LDS directly, four loads to a word of M0 (the instruction's
+//    offset counts on both sides).  A row of a stage is 8 chunks of 16 bytes, chunk c at place c ^ (row / 2 % 8): 16 lanes that read one
+//    chunk of 16 rows hit sixteen different groups of four banks.  The scales of four steps (a word per row) come the same way.
+//  * Four wavefronts; the large tile is 128 x 128 of each, 256 accumulation registers, one wavefront per SIMD: 64 bytes of LDS per
+//    clock of matrix work in place of 96 with eight.  The operands of half a step are read beside the products of the half before, also
+//    across steps: the one barrier of a step is in its middle, behind it the step's stage is free for the loads of the step STAGES on.
 //  * The rows of A are the rows of an MFMA tile, so a lane ends up with 4 consecutive outputs of one row of C at a time; the tile goes through
 //    LDS, wavefront by wavefront, and leaves in rows.
-//  * Several products share a launch (the two gradients).  A product whose tiles do not fill the chip is cut along the contraction; the
-//    parts go to the workspace in fp32 and are added in a fixed order by a second kernel.
+//  * Several products share a launch (the two gradients, where their outputs are of one kind).  A product whose tiles do not fill the chip
+//    is cut along the contraction; the parts go to the workspace in fp32 and are added in a fixed order by a second kernel.
+//
+// What bounds it: the operands' way from L2 to LDS.  8192 x 28672 with 4096 tokens: 790 us (2430 TFLOP/s); without the loads the same
+// loop takes 517 us, with loads that all hit in the L2 661; the fp32 form 1415 us for as many products (1360 TFLOP/s, the bf16 matrix
+// cores at the clock the power allows).
 #include "fp8_device.h"
 
 namespace {
 
 using namespace slimfp8;
 
-constexpr int FG_BAND = 8;                 // tiles of A per band of the tile order
+constexpr int FG_BAND = 4;                 // tiles of A per band of the tile order
 
 struct ProductArgs {
   Operand a, b;
@@ -31,18 +39,34 @@ struct GemmArgs {
   int first;                               // workgroups of the first product
 };
 
-__device__ __forceinline__ void load_lds16(unsigned lds_addr, unsigned voff, const uint8_t* gbase) {
+// Direct loads, if step `k` is below `n` (the branch is in here so that the code around it stays one block for the scheduler).
+// load_lds16x4: four times 16 bytes per lane, to 4 KiB of LDS one after another, from gbase + off[i]; the instruction's offset counts
+// on both sides, so that off[i] is 1024 i less than what it means.
+__device__ __forceinline__ void load_lds16x4(unsigned lds_addr, const unsigned* off, const uint8_t* gbase, int k, int n) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(gbase) : "m0");
+  asm volatile("s_cmp_ge_i32 %6, %7\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+               "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072\n1:"
+               : : "s"(lds_addr), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(gbase), "s"(k), "s"(n) : "m0", "scc");
 #else
-  (void)lds_addr, (void)voff, (void)gbase;
+  (void)lds_addr, (void)off, (void)gbase, (void)k, (void)n;
 #endif
 }
-__device__ __forceinline__ void load_lds4(unsigned lds_addr, unsigned voff, const uint8_t* gbase) {
+__device__ __forceinline__ void load_lds4(unsigned lds_addr, unsigned voff, const uint8_t* gbase, int k, int n) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds_addr), "v"(voff), "s"(gbase) : "m0");
+  asm volatile("s_cmp_ge_i32 %3, %4\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n1:"
+               : : "s"(lds_addr), "v"(voff), "s"(gbase), "s"(k), "s"(n) : "m0", "scc");
 #else
-  (void)lds_addr, (void)voff, (void)gbase;
+  (void)lds_addr, (void)voff, (void)gbase, (void)k, (void)n;
+#endif
+}
+// waits until at most N of the wavefront's loads are outstanding (none, if k is above n), and for its reads of LDS
+template <int N>
+__device__ __forceinline__ void wait_loads(int k, int n) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  else asm volatile("s_cmp_le_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:\n\ts_waitcnt vmcnt(%2) lgkmcnt(0)" ::"s"(k), "s"(n), "n"(N) : "memory", "scc");
+#else
+  (void)k, (void)n;
 #endif
 }
 
@@ -53,15 +77,17 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
                           (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(u >> 32)) << 32);
 }
 
-template <int TA_, int TB_, int WA_, int WB_>
+template <int TA_, int TB_, int WA_, int WB_, int STAGES_>
 struct Tile {
-  static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
+  static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_, STAGES = STAGES_;
   static constexpr int WAVES = WA * WB, THREADS = 64 * WAVES, MA = TA / WA / 32, MB = TB / WB / 32;
-  static constexpr int STAGE = (TA + TB) * BLOCK, SCALES = (TA + TB) * 4;
-  static constexpr int LOADS = STAGE / 1024 / WAVES;           // direct loads of a wavefront per step
+  static constexpr int STAGE = (TA + TB) * BLOCK;              // bytes of operands per step
+  static constexpr int LOADS = STAGE / 1024 / WAVES, GROUPS = LOADS / 4;   // direct loads of a wavefront per step, four at a time
+  static constexpr int SLOADS = ((TA + TB) / 64 + WAVES - 1) / WAVES;      // and of scales per four steps
+  static constexpr int SCALES = 256 * WAVES * SLOADS;          // bytes of scales per four steps (a word per row)
   static constexpr int OUT_LD = MA * 32 + 4;                   // floats per row of C in the epilogue
   static constexpr int OUT = WAVES * 32 * OUT_LD * 4;
-  static constexpr int LDS = 2 * STAGE + 2 * SCALES > OUT ? 2 * STAGE + 2 * SCALES : OUT;
+  static constexpr int LDS = STAGES * STAGE + 2 * SCALES > OUT ? STAGES * STAGE + 2 * SCALES : OUT;
 };
 
 // four values of a row of C from column `col` on, of which `left` exist
@@ -89,9 +115,39 @@ __device__ __forceinline__ void store4(void* row, int dtype, int col, int left, 
   }
 }
 
+// The operands of half a step (64 of the contraction) in registers: 32 bytes per lane and 32 rows
+template <typename T>
+struct Half {
+  uint4 a[T::MA][2], b[T::MB][2];
+};
+// what a lane knows of its operands' places: chunk c of its rows of A and B (LDS bytes inside a stage)
+struct Places {
+  int a[4], b[4];
+};
+
+__device__ __forceinline__ v8i joined(const uint4 (&v)[2]) {
+  return v8i{(int)v[0].x, (int)v[0].y, (int)v[0].z, (int)v[0].w, (int)v[1].x, (int)v[1].y, (int)v[1].z, (int)v[1].w};
+}
+
+// read r of 2 (MA + MB) of half KK of the stage at `st`, in the order in which the products need them: the first rows of A, B, the other rows
+template <typename T, int KK>
+__device__ __forceinline__ void read_operand(Half<T>& f, const char* st, const Places& at, int r) {
+  const int o = r >> 1, c = r & 1;
+  if (o >= 1 && o <= T::MB) {
+    f.b[o - 1][c] = *reinterpret_cast<const uint4*>(st + at.b[KK * 2 + c] + (o - 1) * 32 * BLOCK);
+  } else {
+    const int i = o == 0 ? 0 : o - T::MB;
+    f.a[i][c] = *reinterpret_cast<const uint4*>(st + at.a[KK * 2 + c] + i * 32 * BLOCK);
+  }
+}
+// the share of n things that belongs beside product m of M, all of them beside the first half of the products
+template <int M>
+__device__ __forceinline__ constexpr int share_from(int m, int n) { return m * 2 >= M ? n : m * 2 * n / M; }
+
 // EXACT: products of the numbers in bf16 (fp32 outputs)
 template <typename T, bool EXACT>
-__global__ __launch_bounds__(T::THREADS) void fp8_gemm(GemmArgs ga) {
+__global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_gemm(GemmArgs ga) {
+  constexpr int MA = T::MA, MB = T::MB, M = MA * MB, READS = 2 * (MA + MB), S = T::STAGES;
   extern __shared__ __align__(16) char smem_fg[];
   const bool second = (int)blockIdx.x >= ga.first;
   const ProductArgs& p = ga.p[second];
@@ -103,110 +159,151 @@ __global__ __launch_bounds__(T::THREADS) void fp8_gemm(GemmArgs ga) {
   const int id0 = c8 * each + min(c8, rest8) + bid / 8, split = id0 / tiles, id = id0 - split * tiles;
   const int full = p.tiles_b * FG_BAND, band = id / full, inband = id - band * full, bw = min(FG_BAND, p.tiles_a - band * FG_BAND);
   const int a0 = (band * FG_BAND + inband % bw) * T::TA, b0 = (inband / bw) * T::TB;
-  const int k0 = split * p.per, nk = min(p.per, p.nk - k0);
+  const int k0 = split * p.per, nk = __builtin_amdgcn_readfirstlane(min(p.per, p.nk - k0));
   const int wa = wave % T::WA, wb = wave / T::WA;
 
-  // A direct load fills 1 KiB of a stage: 8 rows; the lane fetches the chunk that belongs at its place.  Rows behind the last one
-  // are the last one again (their sums are not stored).
+  // A direct load fills 1 KiB of a stage: 8 rows; the lane fetches the chunk that belongs at its place.  Four of a wavefront are 32 rows
+  // one after another, of A or of B.  Rows behind the last one are the last one again (their sums are not stored).
+  constexpr unsigned LOWER = 4096;          // what the bases are lowered by so that no offset is negative
   unsigned off[T::LOADS];
 #pragma unroll
   for (int i = 0; i < T::LOADS; ++i) {
-    const int r = (wave * T::LOADS + i) * 8 + (lane >> 3), ch = (lane & 7) ^ ((r >> 1) & 7);
-    off[i] = r < T::TA ? (unsigned)((int64_t)min(r, p.a.rows - 1 - a0) * p.a.ld) + ch * 16u
-                       : (unsigned)((int64_t)min(r - T::TA, p.b.rows - 1 - b0) * p.b.ld) + ch * 16u;
+    const int r = ((i / 4) * T::WAVES + wave) * 32 + (i % 4) * 8 + (lane >> 3), ch = (lane & 7) ^ ((r >> 1) & 7);
+    off[i] = LOWER - (i % 4) * 1024u + ch * 16u +
+             (r < T::TA ? (unsigned)((int64_t)min(r, p.a.rows - 1 - a0) * p.a.ld) : (unsigned)((int64_t)min(r - T::TA, p.b.rows - 1 - b0) * p.b.ld));
   }
-  const uint8_t* abase = uniform(p.a.q + (int64_t)a0 * p.a.ld + (int64_t)k0 * BLOCK);
-  const uint8_t* bbase = uniform(p.b.q + (int64_t)b0 * p.b.ld + (int64_t)k0 * BLOCK);
-  // scales: one load is the words of 64 rows
-  const bool scale_wave = wave < (T::TA + T::TB) / 64, scale_b = wave >= T::TA / 64;
-  unsigned soff = 0;
-  const uint8_t* sbase = nullptr;
-  if (scale_wave) {
-    const Operand& o = scale_b ? p.b : p.a;
-    const int r0 = scale_b ? b0 : a0, r = (scale_b ? wave - T::TA / 64 : wave) * 64 + lane;
-    soff = (unsigned)((int64_t)((min(r0 + r, o.rows - 1) >> o.shift) - (r0 >> o.shift)) * o.lds);
-    sbase = uniform(o.s + (int64_t)(r0 >> o.shift) * o.lds + k0);
+  const uint8_t* abase = uniform(p.a.q + (int64_t)a0 * p.a.ld + (int64_t)k0 * BLOCK - LOWER);
+  const uint8_t* bbase = uniform(p.b.q + (int64_t)b0 * p.b.ld + (int64_t)k0 * BLOCK - LOWER);
+  // scales: one load is the words of 64 rows (rows behind those of the tile: the last ones again, not used)
+  unsigned soff[T::SLOADS];
+  const uint8_t* sbase[T::SLOADS];
+#pragma unroll
+  for (int i = 0; i < T::SLOADS; ++i) {
+    const int r = min((i * T::WAVES + wave) * 64, T::TA + T::TB - 64);
+    const bool in_b = r >= T::TA;
+    const Operand& o = in_b ? p.b : p.a;
+    const int r0 = in_b ? b0 : a0, row = min(r0 + r - (in_b ? T::TA : 0) + lane, o.rows - 1);
+    soff[i] = (unsigned)((int64_t)((row >> o.shift) - (r0 >> o.shift)) * o.lds);
+    sbase[i] = uniform(o.s + (int64_t)(r0 >> o.shift) * o.lds + k0);
   }
   const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)((__attribute__((address_space(3))) char*)smem_fg));
-  auto issue = [&](int k) {
-    const unsigned st = lds0 + (unsigned)(k & 1) * T::STAGE + (unsigned)wave * T::LOADS * 1024u;
+  unsigned slot = 0;                        // of the next step to be loaded: LDS bytes of its stage
+  int loading = 0;                          // and its number
+  auto load_operands = [&](int g) {         // group g of this wavefront's loads
+    const int r0 = (g * T::WAVES + wave) * 32;
+    load_lds16x4(lds0 + slot + (unsigned)r0 * BLOCK, off + 4 * g, r0 < T::TA ? abase : bbase, loading, nk);
+  };
+  auto load_scales = [&]() {                // (first, so that they are not behind the operands of their step; one step in four)
 #pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) {
-      const bool in_a = (wave * T::LOADS + i) * 8 < T::TA;
-      load_lds16(st + i * 1024u, off[i], in_a ? abase : bbase);
-    }
+    for (int i = 0; i < T::SLOADS; ++i)
+      load_lds4(lds0 + (unsigned)(S * T::STAGE) + (unsigned)((loading >> 2) & 1) * T::SCALES + (unsigned)(i * T::WAVES + wave) * 256u, soff[i],
+                sbase[i] + loading, loading + ((loading & 3) << 20), nk);
+  };
+  auto loaded = [&]() {
     abase += BLOCK;
     bbase += BLOCK;
-    if ((k & 3) == 0 && scale_wave) {
-      load_lds4(lds0 + 2u * T::STAGE + (unsigned)((k >> 2) & 1) * T::SCALES + (unsigned)wave * 256u, soff, sbase);
-      sbase += 4;
-    }
+    slot = slot == (unsigned)((S - 1) * T::STAGE) ? 0u : slot + (unsigned)T::STAGE;
+    ++loading;
   };
 
-  v16f acc[T::MA][T::MB];
+  v16f acc[MA][MB];
 #pragma unroll
-  for (int i = 0; i < T::MA; ++i)
+  for (int i = 0; i < MA; ++i)
 #pragma unroll
-    for (int j = 0; j < T::MB; ++j)
+    for (int j = 0; j < MB; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 
   const int l32 = lane & 31, h = lane >> 5, sw = (l32 >> 1) & 7;
-  const int ra = wa * T::MA * 32 + l32, rb = T::TA + wb * T::MB * 32 + l32;
-  int sa[T::MA], sb[T::MB];
-  auto fragment = [&](const char* row, int kk) {
-    const uint4 lo = *reinterpret_cast<const uint4*>(row + (((kk * 4 + h * 2) ^ sw) * 16));
-    const uint4 hi = *reinterpret_cast<const uint4*>(row + (((kk * 4 + h * 2 + 1) ^ sw) * 16));
-    return v8i{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+  const int ra = wa * MA * 32 + l32, rb = T::TA + wb * MB * 32 + l32;
+  Places at;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int place = (((c >> 1) * 4 + h * 2 + (c & 1)) ^ sw) * 16;
+    at.a[c] = ra * BLOCK + place;
+    at.b[c] = rb * BLOCK + place;
+  }
+  Half<T> f[2];
+  int sa[MA], sb[MB];                       // scales of this step
+  auto read_scales = [&](int (&a)[MA], int (&b)[MB], int k) {
+    const uint8_t* sc = reinterpret_cast<const uint8_t*>(smem_fg) + S * T::STAGE + ((k >> 2) & 1) * T::SCALES + (k & 3);
+#pragma unroll
+    for (int i = 0; i < MA; ++i) a[i] = sc[(ra + i * 32) * 4];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) b[j] = sc[(rb + j * 32) * 4];
   };
-  if (nk > 0) issue(0);
-  auto step = [&](auto index, int k) {
-    constexpr int J = decltype(index)::value;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                       // everybody's loads of this step; everybody is done with the step before
-    if (k + 1 < nk) issue(k + 1);
-    const char* st = smem_fg + (J & 1) * T::STAGE;
-    if (J == 0) {
-      const int* sc = reinterpret_cast<const int*>(smem_fg + 2 * T::STAGE + ((k >> 2) & 1) * T::SCALES);
+  // Half a step: its products, and between them what `between(m)` has to do
+  auto half = [&](const Half<T>& g, auto between) {
+    if constexpr (EXACT) {
+      v8bf ba[2][MA], bb[2][MB];
+      auto convert = [&](int q, int r) {    // operand r of MA + MB, eighth q of its chunk pair
+        if (r < MA) ba[q & 1][r] = dequantized((int)((q & 1) ? g.a[r][q >> 1].z : g.a[r][q >> 1].x), (int)((q & 1) ? g.a[r][q >> 1].w : g.a[r][q >> 1].y), __uint_as_float((unsigned)sa[r] << 23));
+        else bb[q & 1][r - MA] = dequantized((int)((q & 1) ? g.b[r - MA][q >> 1].z : g.b[r - MA][q >> 1].x), (int)((q & 1) ? g.b[r - MA][q >> 1].w : g.b[r - MA][q >> 1].y), __uint_as_float((unsigned)sb[r - MA] << 23));
+      };
 #pragma unroll
-      for (int i = 0; i < T::MA; ++i) sa[i] = sc[ra + i * 32];
+      for (int r = 0; r < MA + MB; ++r) convert(0, r);
 #pragma unroll
-      for (int j = 0; j < T::MB; ++j) sb[j] = sc[rb + j * 32];
-    }
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      v8i fa[T::MA], fb[T::MB];
+        for (int m = 0; m < M; ++m) {
+          acc[m / MB][m % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ba[q & 1][m / MB], bb[q & 1][m % MB], acc[m / MB][m % MB], 0, 0, 0);
+          if (q < 3)
 #pragma unroll
-      for (int j = 0; j < T::MB; ++j) fb[j] = fragment(st + (rb + j * 32) * BLOCK, kk);
-#pragma unroll
-      for (int i = 0; i < T::MA; ++i) fa[i] = fragment(st + (ra + i * 32) * BLOCK, kk);
-      if constexpr (EXACT) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v8bf ba[T::MA], bb[T::MB];
-#pragma unroll
-          for (int j = 0; j < T::MB; ++j) bb[j] = dequantized(fb[j][2 * q], fb[j][2 * q + 1], scale_of<J>(sb[j]));
-#pragma unroll
-          for (int i = 0; i < T::MA; ++i) ba[i] = dequantized(fa[i][2 * q], fa[i][2 * q + 1], scale_of<J>(sa[i]));
-#pragma unroll
-          for (int i = 0; i < T::MA; ++i)
-#pragma unroll
-            for (int j = 0; j < T::MB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ba[i], bb[j], acc[i][j], 0, 0, 0);
+            for (int r = m * (MA + MB) / M; r < (m + 1) * (MA + MB) / M; ++r) convert(q + 1, r);
+          if ((q * M + m) % 4 == 0) between((q * M + m) / 4);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        continue;
+    } else {
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        acc[m / MB][m % MB] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(joined(g.a[m / MB]), joined(g.b[m % MB]), acc[m / MB][m % MB], 0, 0, 0,
+                                                                             sa[m / MB], 0, sb[m % MB]);
+        between(m);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int i = 0; i < T::MA; ++i)
-#pragma unroll
-        for (int j = 0; j < T::MB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 0, 0, J, sa[i], J, sb[j]);
     }
   };
-  for (int k = 0; k < nk; k += 4) {
-    step(std::integral_constant<int, 0>(), k);
-    if (k + 1 < nk) step(std::integral_constant<int, 1>(), k + 1);
-    if (k + 2 < nk) step(std::integral_constant<int, 2>(), k + 2);
-    if (k + 3 < nk) step(std::integral_constant<int, 3>(), k + 3);
+  if (nk > 0) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      load_scales();
+#pragma unroll
+      for (int g = 0; g < T::GROUPS; ++g) load_operands(g);
+      loaded();
+    }
+    // Loads complete in order: with those of S - 1 steps outstanding, the first one's have landed.
+    wait_loads<(S - 1) * T::LOADS>(S, nk);
+    __syncthreads();
+    read_scales(sa, sb, 0);
+#pragma unroll
+    for (int r = 0; r < READS; ++r) read_operand<T, 0>(f[0], smem_fg, at, r);
+  }
+  const char* stage = smem_fg;
+#pragma unroll 1
+  for (int k = 0; k < nk; ++k) {
+    // First half: the second half's operands are read.  Then the step's stage is free, and the step S on is loaded into it beside the
+    // second half, which reads the next step's first operands (behind the last step: what lies there, unused).
+    half(f[0], [&](int m) {
+#pragma unroll
+      for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 1>(f[1], stage, at, r);
+    });
+    wait_loads<(S - 2) * T::LOADS>(k + S, nk);
+    __syncthreads();                        // everybody's loads of the next step; everybody has read this one's stage
+    stage = stage == smem_fg + (S - 1) * T::STAGE ? smem_fg : stage + T::STAGE;
+    load_scales();
+    int na[MA], nb[MB];
+    read_scales(na, nb, k + 1);
+    half(f[1], [&](int m) {
+#pragma unroll
+      for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 0>(f[0], stage, at, r);
+#pragma unroll
+      for (int g = m * T::GROUPS / M; g < (m + 1) * T::GROUPS / M; ++g) load_operands(g);
+    });
+    loaded();
+#pragma unroll
+    for (int i = 0; i < MA; ++i) sa[i] = na[i];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) sb[j] = nb[j];
   }
 
   // A lane holds column b = lane % 32 of an MFMA tile and rows 8 (q / 4) + 4 h + q % 4.  32 rows of C at a time through a
@@ -254,30 +351,31 @@ __global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __re
 }
 
 enum { TILE_LARGE, TILE_MEDIUM, TILE_SMALL };
-typedef Tile<256, 256, 2, 4> Large;
-typedef Tile<128, 128, 2, 2> Medium;
-typedef Tile<64, 64, 2, 2> Small;
+typedef Tile<256, 256, 2, 2, 2> Large;
+typedef Tile<128, 128, 2, 2, 2> Medium;
+typedef Tile<64, 64, 2, 2, 4> Small;
 
 struct Plan {
   int tile, splits[2];
   int64_t ldp[2];
   size_t bytes;
 };
+constexpr int TILE_A[] = {Large::TA, Medium::TA, Small::TA}, TILE_B[] = {Large::TB, Medium::TB, Small::TB};
 
-template <typename T>
-int tiles_of(const Product& p) { return slim_cdiv(p.a.rows, T::TA) * slim_cdiv(p.b.rows, T::TB); }
+int tiles_of(const Product& p, int tile) { return slim_cdiv(p.a.rows, TILE_A[tile]) * slim_cdiv(p.b.rows, TILE_B[tile]); }
 
-// The tile: the largest of which there are enough to fill the chip; parts: where even the smallest do not.
+// The tile: the largest of which there are enough to fill the chip; parts: where even the smallest do not.  Medium from three quarters of
+// the CUs on (4096 x 1024, 1024 tokens, 256 tiles: 16.5 us, small ones 18.4; 2048 x 2048, 1024 tokens, 128 tiles: 26.1 and 16.7), but not
+// for up to 64 tokens, half of whose medium tile is empty (28672 x 8192, 64 tokens: 75.4 and 56.9).
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
-  int large = 0, medium = 0, small = 0;
+  int n[3] = {}, most = 0;
   for (int i = 0; i < count; ++i) {
-    large += tiles_of<Large>(p[i]);
-    medium += tiles_of<Medium>(p[i]);
-    small += tiles_of<Small>(p[i]);
+    for (int t = 0; t < 3; ++t) n[t] += tiles_of(p[i], t);
+    most = std::max(most, p[i].b.rows);
   }
-  pl.tile = large >= ncu ? TILE_LARGE : medium >= ncu / 2 ? TILE_MEDIUM : TILE_SMALL;
-  const int tiles = pl.tile == TILE_LARGE ? large : pl.tile == TILE_MEDIUM ? medium : small;
+  pl.tile = n[TILE_LARGE] >= ncu ? TILE_LARGE : most > Small::TB && 4 * n[TILE_MEDIUM] >= 3 * ncu ? TILE_MEDIUM : TILE_SMALL;
+  const int tiles = n[pl.tile];
   for (int i = 0; i < count; ++i) {
     int s = std::max(1, std::min(ncu / std::max(1, tiles), p[i].nk / 8));
     const int per = slim_cdiv(slim_cdiv(std::max(1, p[i].nk), s), 4) * 4;
@@ -298,8 +396,7 @@ slim_status launch(slim_ctx* ctx, const char* name, const GemmArgs& ga, int grid
 }
 template <bool EXACT>
 slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid) {
-  return tile == TILE_LARGE ? launch<Large, EXACT>(ctx, name, ga, grid)
-         : tile == TILE_MEDIUM ? launch<Medium, EXACT>(ctx, name, ga, grid) : launch<Small, EXACT>(ctx, name, ga, grid);
+  return tile == TILE_LARGE ? launch<Large, EXACT>(ctx, name, ga, grid) : tile == TILE_MEDIUM ? launch<Medium, EXACT>(ctx, name, ga, grid) : launch<Small, EXACT>(ctx, name, ga, grid);
 }
 
 // products of one launch: all, or one where they differ in their kind
@@ -317,10 +414,8 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
     q.nk = p[i].nk;
     q.splits = pl.splits[i];
     q.per = slim_cdiv(slim_cdiv(std::max(1, q.nk), q.splits), 4) * 4;
-    const int ta = pl.tile == TILE_LARGE ? Large::TA : pl.tile == TILE_MEDIUM ? Medium::TA : Small::TA;
-    const int tb = pl.tile == TILE_LARGE ? Large::TB : pl.tile == TILE_MEDIUM ? Medium::TB : Small::TB;
-    q.tiles_a = slim_cdiv(q.a.rows, ta);
-    q.tiles_b = slim_cdiv(q.b.rows, tb);
+    q.tiles_a = slim_cdiv(q.a.rows, TILE_A[pl.tile]);
+    q.tiles_b = slim_cdiv(q.b.rows, TILE_B[pl.tile]);
     q.c = p[i].c;
     q.ldc = p[i].ldc;
     q.c_dtype = p[i].c_dtype;

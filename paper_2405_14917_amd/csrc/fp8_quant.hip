@@ -38,13 +38,14 @@ __global__ __launch_bounds__(RQ_THREADS) void fp8_rows(const T* __restrict__ X, 
   for (int i = 0; i < RQ_UNITS; ++i) {
     const int64_t u = min(u0 + i, total - 1);
     const int r = (int)(u / units), c = (int)(u % units) * 512 + lane * 8;
-    load8(X + (int64_t)r * ldx + c, cols - c, v[i]);
+    fetch8(X + (int64_t)r * ldx + c, cols - c, cols, v[i]);
   }
 #pragma unroll
   for (int i = 0; i < RQ_UNITS; ++i) {
     const int64_t u = u0 + i;
     if (u >= total) break;
     const int r = (int)(u / units), c = (int)(u % units) * 512 + lane * 8;
+    row_end_shift<8>(v[i], cols < 8 ? 8 : cols - c);
     const unsigned b = block_scale<T>(v[i]);
     const float sc = __uint_as_float(b << 23);
     if (c < ldq) {
@@ -62,7 +63,7 @@ struct TileArgs {
 // Tiles of 128 x 128: thread t holds rows 8 (t / 16) .. + 7 of columns 8 (t % 16) .. + 7.
 template <typename T>
 __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
-  __shared__ unsigned colmax[4][64];                       // per wavefront, pairs of columns
+  __shared__ __align__(16) unsigned colmax[4][64];         // per wavefront, pairs of columns
   __shared__ __align__(16) uint8_t tile[BLOCK * BLOCK];    // [column][row], units of 8 bytes at unit ^ (column / 8)
   const int p = (int)blockIdx.x >= ta.tiles[0];
   const Activations& a = ta.a[p];
@@ -72,46 +73,73 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
   unsigned v[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0u;
-    if (r0 + i < a.rows) load8(static_cast<const T*>(a.X) + (int64_t)(r0 + i) * a.ldx + c0, a.cols - c0, v[i]);
+    fetch8(static_cast<const T*>(a.X) + (int64_t)min(r0 + i, a.rows - 1) * a.ldx + c0, a.cols - c0, a.cols, v[i]);
   }
-  if (a.rows_q) {
-    const int64_t ldq = (int64_t)(a.cols + BLOCK - 1) / BLOCK * BLOCK, lds = (int64_t)((a.cols + BLOCK - 1) / BLOCK + 3) / 4 * 4;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const unsigned b = block_scale<T>(v[i]);
-      const float sc = __uint_as_float(b << 23);
-      if (r0 + i < a.rows) {
-        *reinterpret_cast<uint2*>(a.rows_q + (int64_t)(r0 + i) * ldq + c0) =
-            make_uint2(to_e4m3<T>(v[i][0], v[i][1], sc), to_e4m3<T>(v[i][2], v[i][3], sc));
-        if (cg == 0) a.rows_s[(int64_t)(r0 + i) * lds + tc] = (uint8_t)b;
-      }
-    }
+  for (int i = 0; i < 8; ++i) {
+    row_end_shift<8>(v[i], a.cols < 8 ? 8 : a.cols - c0);
+    if (r0 + i >= a.rows) v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0u;
   }
-  // columns: the thread's eight rows, the four groups of 16 lanes, the four wavefronts
-  unsigned m[4];
-  auto column_max = [&](auto magnitude) {
+  // Largest magnitudes.  Rows: of the lane's eight numbers, two rows to a word, then over the 16 lanes of a row; columns: of the lane's
+  // eight rows, the four groups of 16 lanes, the four wavefronts.
+  unsigned rm[4], m[4];
+  auto maxima = [&](auto magnitude) {
+    unsigned r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned u = magnitude(v[i][j]);
+        r[i] = j ? max_u16x2(r[i], u) : u;
+        m[j] = i ? max_u16x2(m[j], u) : u;
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      rm[i] = row_max_x2(max_u16x2(__builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x05040100u), __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x07060302u)));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      m[j] = magnitude(v[0][j]);
-#pragma unroll
-      for (int i = 1; i < 8; ++i) m[j] = max_u16x2(m[j], magnitude(v[i][j]));
-      m[j] = max_u16x2(m[j], (unsigned)__shfl_xor((int)m[j], 16, 64));
-      m[j] = max_u16x2(m[j], (unsigned)__shfl_xor((int)m[j], 32, 64));
-      if (lane < 16) colmax[wave][cg * 4 + j] = m[j];
+      const auto a32 = __builtin_amdgcn_permlane32_swap(m[j], m[j], false, false);
+      const unsigned h = max_u16x2(a32[0], a32[1]);
+      const auto a16 = __builtin_amdgcn_permlane16_swap(h, h, false, false);
+      m[j] = max_u16x2(a16[0], a16[1]);
     }
+    if (lane < 16) *reinterpret_cast<uint4*>(&colmax[wave][cg * 4]) = make_uint4(m[0], m[1], m[2], m[3]);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      m[j] = max_u16x2(max_u16x2(colmax[0][cg * 4 + j], colmax[1][cg * 4 + j]), max_u16x2(colmax[2][cg * 4 + j], colmax[3][cg * 4 + j]));
+    for (int w = 0; w < 4; ++w) {
+      const uint4 o = *reinterpret_cast<const uint4*>(&colmax[w][cg * 4]);
+      m[0] = w ? max_u16x2(m[0], o.x) : o.x;
+      m[1] = w ? max_u16x2(m[1], o.y) : o.y;
+      m[2] = w ? max_u16x2(m[2], o.z) : o.z;
+      m[3] = w ? max_u16x2(m[3], o.w) : o.w;
+    }
   };
-  column_max([](unsigned u) { return u & 0x7fff7fffu; });
-  // (every thread of a column sees the same maxima, and all columns are seen by each wavefront: the branch is the workgroup's)
+  maxima([](unsigned u) { return u & 0x7fff7fffu; });
+  // (every wavefront sees the maxima of all columns: the branch is the workgroup's)
   const unsigned top = larger_half(max_u16x2(max_u16x2(m[0], m[1]), max_u16x2(m[2], m[3])));
   if (__builtin_expect(__any(top >= Half16<T>::INF), 0)) {
     __syncthreads();
-    column_max([](unsigned u) { return finite_x2<T>(u); });
+    maxima([](unsigned u) { return finite_x2<T>(u); });
   }
+  if (a.rows_q) {
+    const int64_t ldq = (int64_t)(a.cols + BLOCK - 1) / BLOCK * BLOCK, lds = (int64_t)((a.cols + BLOCK - 1) / BLOCK + 3) / 4 * 4;
+    uint8_t* q = a.rows_q + (int64_t)r0 * ldq + c0;
+    uint8_t* s = a.rows_s + (int64_t)r0 * lds + tc;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned b = scale_byte(Half16<T>::float_bits((i & 1) ? rm[i / 2] >> 16 : rm[i / 2] & 0xffffu));
+      const float sc = __uint_as_float(b << 23);
+      if (r0 + i < a.rows) {
+        *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3<T>(v[i][0], v[i][1], sc), to_e4m3<T>(v[i][2], v[i][3], sc));
+        if (cg == 0) *s = (uint8_t)b;
+      }
+      q += ldq;
+      s += lds;
+    }
+  }
+  if (!a.cols_q) return;
+  const int64_t lds = (int64_t)((a.rows + BLOCK - 1) / BLOCK + 3) / 4 * 4;
+  uint8_t* const tile0 = tile + cg * 8 * BLOCK + ((rg ^ cg) * 8);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -122,11 +150,8 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) pr[i] = __builtin_amdgcn_perm(v[2 * i + 1][j], v[2 * i][j], h ? 0x07060302u : 0x05040100u);
       const int c = cg * 8 + 2 * j + h;
-      *reinterpret_cast<uint2*>(tile + c * BLOCK + ((rg ^ cg) * 8)) = make_uint2(to_e4m3<T>(pr[0], pr[1], sc), to_e4m3<T>(pr[2], pr[3], sc));
-      if (rg == 0 && tc * BLOCK + c < a.cols) {
-        const int64_t lds = (int64_t)((a.rows + BLOCK - 1) / BLOCK + 3) / 4 * 4;
-        a.cols_s[(int64_t)(tc * BLOCK + c) * lds + tr] = (uint8_t)b;
-      }
+      *reinterpret_cast<uint2*>(tile0 + (2 * j + h) * BLOCK) = make_uint2(to_e4m3<T>(pr[0], pr[1], sc), to_e4m3<T>(pr[2], pr[3], sc));
+      if (rg == 0 && tc * BLOCK + c < a.cols) a.cols_s[(int64_t)(tc * BLOCK + c) * lds + tr] = (uint8_t)b;
     }
   }
   __syncthreads();

@@ -60,6 +60,31 @@ __device__ __forceinline__ void store16_once(void* p, const unsigned (&v)[4]) {
   __builtin_nontemporal_store(u, static_cast<uint4_unaligned*>(p));
 }
 
+// 16 bytes (E elements of a row) of which only the first `left` may exist, without a branch around the load: where fewer are left, the last
+// E of the row are loaded (the row has to have as many) and moved down afterwards, when they are used.
+template <int E>
+__device__ __forceinline__ const void* row_end_address(const void* p, int left) {
+  return left >= E ? p : static_cast<const char*>(p) + (left - E) * (16 / E);
+}
+template <int E>
+__device__ __forceinline__ void row_end_shift(unsigned (&v)[4], int left) {
+  if (left >= E) return;
+  const int s = E - max(left, 0);                    // elements to drop; zeros follow
+  if constexpr (E == 8) {
+    const bool odd = s & 1;
+    const unsigned a = __builtin_amdgcn_alignbit(v[1], v[0], 16), b = __builtin_amdgcn_alignbit(v[2], v[1], 16),
+                   c = __builtin_amdgcn_alignbit(v[3], v[2], 16), d = v[3] >> 16;
+    v[0] = odd ? a : v[0];
+    v[1] = odd ? b : v[1];
+    v[2] = odd ? c : v[2];
+    v[3] = odd ? d : v[3];
+  }
+  const int w = E == 8 ? s >> 1 : s;                 // words
+  if (w & 1) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; v[3] = 0u; }
+  if (w & 2) { v[0] = v[2]; v[1] = v[3]; v[2] = v[3] = 0u; }
+  if (w & 4) v[0] = v[1] = v[2] = v[3] = 0u;
+}
+
 // ---- wavefront (64 lanes) reductions: every lane ends up with the result ------------------------
 __device__ __forceinline__ double shfl_xor_f64(double v, int mask) {
   int lo = __double2loint(v), hi = __double2hiint(v);
