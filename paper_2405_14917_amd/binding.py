@@ -530,13 +530,14 @@ class Slim:
         nb, mb = (n + 127) // 128, (m + 127) // 128
 
         def stored(rows, cols, rb, cb):
-            q = torch.empty((rows, cb * 128), dtype=_E4M3, device=W.device)[:, :cols]
+            # (rows an odd number of blocks apart: they spread over the channels of the L2)
+            q = torch.zeros((rows, (cb | 1) * 128), dtype=torch.uint8, device=W.device).view(_E4M3)[:, :cols]
             return q, torch.zeros((rb, (cb + 3) // 4 * 4), dtype=torch.uint8, device=W.device)[:, :cb]
 
         q, s = stored(n, m, nb, mb)
         qt, st = stored(m, n, mb, nb) if transposed else (None, None)
-        self._check(self.lib.slim_fp8_quantize_weights(self.ctx, W.data_ptr(), _dtype(W), n, m, _row_stride(W, "W"), q.data_ptr(), mb * 128,
-                                                       s.data_ptr(), s.stride(0), _ptr(qt), nb * 128, _ptr(st),
+        self._check(self.lib.slim_fp8_quantize_weights(self.ctx, W.data_ptr(), _dtype(W), n, m, _row_stride(W, "W"), q.data_ptr(), q.stride(0),
+                                                       s.data_ptr(), s.stride(0), _ptr(qt), qt.stride(0) if transposed else 0, _ptr(st),
                                                        st.stride(0) if transposed else 0))
         return (q, s, qt, st) if transposed else (q, s)
 

@@ -223,7 +223,6 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
     at.a[c] = ra * BLOCK + place;
     at.b[c] = rb * BLOCK + place;
   }
-  Half<T> f[2];
   int sa[MA], sb[MB];                       // scales of this step
   auto read_scales = [&](int (&a)[MA], int (&b)[MB], int k) {
     const uint8_t* sc = reinterpret_cast<const uint8_t*>(smem_fg) + S * T::STAGE + ((k >> 2) & 1) * T::SCALES + (k & 3);
@@ -275,35 +274,74 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
     wait_loads<(S - 1) * T::LOADS>(S, nk);
     __syncthreads();
     read_scales(sa, sb, 0);
-#pragma unroll
-    for (int r = 0; r < READS; ++r) read_operand<T, 0>(f[0], smem_fg, at, r);
   }
   const char* stage = smem_fg;
-#pragma unroll 1
-  for (int k = 0; k < nk; ++k) {
-    // First half: the second half's operands are read.  Then the step's stage is free, and the step S on is loaded into it beside the
-    // second half, which reads the next step's first operands (behind the last step: what lies there, unused).
-    half(f[0], [&](int m) {
-#pragma unroll
-      for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 1>(f[1], stage, at, r);
-    });
-    wait_loads<(S - 2) * T::LOADS>(k + S, nk);
-    __syncthreads();                        // everybody's loads of the next step; everybody has read this one's stage
-    stage = stage == smem_fg + (S - 1) * T::STAGE ? smem_fg : stage + T::STAGE;
-    load_scales();
-    int na[MA], nb[MB];
-    read_scales(na, nb, k + 1);
-    half(f[1], [&](int m) {
-#pragma unroll
-      for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 0>(f[0], stage, at, r);
-#pragma unroll
-      for (int g = m * T::GROUPS / M; g < (m + 1) * T::GROUPS / M; ++g) load_operands(g);
-    });
-    loaded();
+  int na[MA], nb[MB];                       // scales of the next step
+  auto pass_scales = [&]() {
 #pragma unroll
     for (int i = 0; i < MA; ++i) sa[i] = na[i];
 #pragma unroll
     for (int j = 0; j < MB; ++j) sb[j] = nb[j];
+  };
+  if constexpr (M == 1) {
+    // One product per half: too few to read anything beside.  The whole next step is read beside this one's two.
+    Half<T> w[2][2];
+#pragma unroll
+    for (int r = 0; r < READS; ++r) {
+      read_operand<T, 0>(w[0][0], stage, at, r);
+      read_operand<T, 1>(w[0][1], stage, at, r);
+    }
+    auto step = [&](auto parity, int k) {
+      constexpr int P = decltype(parity)::value;
+      wait_loads<(S - 2) * T::LOADS>(k + S, nk);
+      __syncthreads();                      // everybody's loads of the next step; everybody has read this one's stage
+      stage = stage == smem_fg + (S - 1) * T::STAGE ? smem_fg : stage + T::STAGE;
+      read_scales(na, nb, k + 1);
+#pragma unroll
+      for (int r = 0; r < READS; ++r) {
+        read_operand<T, 0>(w[P ^ 1][0], stage, at, r);
+        read_operand<T, 1>(w[P ^ 1][1], stage, at, r);
+      }
+      load_scales();
+#pragma unroll
+      for (int g = 0; g < T::GROUPS; ++g) load_operands(g);
+      loaded();
+      __builtin_amdgcn_sched_barrier(0);
+      half(w[P][0], [](int) {});
+      half(w[P][1], [](int) {});
+      pass_scales();
+    };
+#pragma unroll 1
+    for (int k = 0; k < nk; k += 2) {
+      step(std::integral_constant<int, 0>(), k);
+      if (k + 1 < nk) step(std::integral_constant<int, 1>(), k + 1);
+    }
+  } else {
+    Half<T> f[2];
+#pragma unroll
+    for (int r = 0; r < READS; ++r) read_operand<T, 0>(f[0], stage, at, r);
+#pragma unroll 1
+    for (int k = 0; k < nk; ++k) {
+      // First half: the second half's operands are read.  Then the step's stage is free, and the step S on is loaded into it beside the
+      // second half, which reads the next step's first operands (behind the last step: what lies there, unused).
+      half(f[0], [&](int m) {
+#pragma unroll
+        for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 1>(f[1], stage, at, r);
+      });
+      wait_loads<(S - 2) * T::LOADS>(k + S, nk);
+      __syncthreads();                      // everybody's loads of the next step; everybody has read this one's stage
+      stage = stage == smem_fg + (S - 1) * T::STAGE ? smem_fg : stage + T::STAGE;
+      load_scales();
+      read_scales(na, nb, k + 1);
+      half(f[1], [&](int m) {
+#pragma unroll
+        for (int r = share_from<M>(m, READS); r < share_from<M>(m + 1, READS); ++r) read_operand<T, 0>(f[0], stage, at, r);
+#pragma unroll
+        for (int g = m * T::GROUPS / M; g < (m + 1) * T::GROUPS / M; ++g) load_operands(g);
+      });
+      loaded();
+      pass_scales();
+    }
   }
 
   // A lane holds column b = lane % 32 of an MFMA tile and rows 8 (q / 4) + 4 h + q % 4.  32 rows of C at a time through a

@@ -15,10 +15,10 @@ constexpr int FL_MAX = 1 << 23;            // rows and leading dimensions: offse
 bool is_16(slim_dtype d) { return d == SLIM_F16 || d == SLIM_BF16; }
 
 size_t activation_bytes(int64_t rows, int64_t contraction) {
-  return slim_ws_round((size_t)rows * padded(contraction)) + slim_ws_round((size_t)rows * scales_ld(contraction));
+  return slim_ws_round((size_t)rows * quantized_ld(contraction)) + slim_ws_round((size_t)rows * scales_ld(contraction));
 }
 bool carve(slim_ctx* ctx, int64_t rows, int64_t contraction, uint8_t*& q, uint8_t*& s) {
-  q = static_cast<uint8_t*>(slim_ws_alloc(ctx, (size_t)rows * padded(contraction)));
+  q = static_cast<uint8_t*>(slim_ws_alloc(ctx, (size_t)rows * quantized_ld(contraction)));
   s = static_cast<uint8_t*>(slim_ws_alloc(ctx, (size_t)rows * scales_ld(contraction)));
   return q && s;
 }
@@ -108,7 +108,7 @@ slim_status slim_fp8_linear(slim_ctx* ctx, const void* X, slim_dtype x_dtype, in
   if (const slim_status st = quantize(ctx, "fp8_quantize_x", x_dtype, &a, 1); st != SLIM_OK) return st;
   Product p = forward_product(n, m, t, y_dtype);
   p.a = w;
-  p.b = Operand{a.rows_q, a.rows_s, padded(m), scales_ld(m), t, 0};
+  p.b = Operand{a.rows_q, a.rows_s, quantized_ld(m), scales_ld(m), t, 0};
   p.c = Y;
   p.ldc = ldy;
   return gemm(ctx, "fp8_linear", &p, 1);
@@ -142,15 +142,15 @@ slim_status slim_fp8_linear_backward(slim_ctx* ctx, const void* dY, const void* 
   const int count = backward_products(n, m, t, dX != nullptr, dW != nullptr, dw_dtype, p);
   if (dX) {
     p[0].a = Operand{qt, st, ldqt, ldst, m, 7};
-    p[0].b = Operand{a[0].rows_q, a[0].rows_s, padded(n), scales_ld(n), t, 0};
+    p[0].b = Operand{a[0].rows_q, a[0].rows_s, quantized_ld(n), scales_ld(n), t, 0};
     p[0].c = dX;
     p[0].ldc = lddx;
     p[0].c_dtype = x_dtype;
   }
   if (dW) {
     Product& w = p[count - 1];
-    w.a = Operand{a[1].cols_q, a[1].cols_s, padded(t), scales_ld(t), m, 0};
-    w.b = Operand{a[0].cols_q, a[0].cols_s, padded(t), scales_ld(t), n, 0};
+    w.a = Operand{a[1].cols_q, a[1].cols_s, quantized_ld(t), scales_ld(t), m, 0};
+    w.b = Operand{a[0].cols_q, a[0].cols_s, quantized_ld(t), scales_ld(t), n, 0};
     w.c = dW;
     w.ldc = lddw;
   }

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(RQ_THREADS) void fp8_rows(const T* __restrict__ X, 
     row_end_shift<8>(v[i], cols < 8 ? 8 : cols - c);
     const unsigned b = block_scale<T>(v[i]);
     const float sc = __uint_as_float(b << 23);
-    if (c < ldq) {
+    if (c < (cols + BLOCK - 1) / BLOCK * BLOCK) {
       *reinterpret_cast<uint2*>(q + (int64_t)r * ldq + c) = make_uint2(to_e4m3<T>(v[i][0], v[i][1], sc), to_e4m3<T>(v[i][2], v[i][3], sc));
       if ((lane & 15) == 0) s[(int64_t)r * lds + c / BLOCK] = (uint8_t)b;
     }
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
     maxima([](unsigned u) { return finite_x2<T>(u); });
   }
   if (a.rows_q) {
-    const int64_t ldq = (int64_t)(a.cols + BLOCK - 1) / BLOCK * BLOCK, lds = (int64_t)((a.cols + BLOCK - 1) / BLOCK + 3) / 4 * 4;
+    const int64_t ldq = quantized_ld(a.cols), lds = (int64_t)((a.cols + BLOCK - 1) / BLOCK + 3) / 4 * 4;
     uint8_t* q = a.rows_q + (int64_t)r0 * ldq + c0;
     uint8_t* s = a.rows_s + (int64_t)r0 * lds + tc;
 #pragma unroll
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
     }
   }
   __syncthreads();
-  const int64_t ldq = (int64_t)(a.rows + BLOCK - 1) / BLOCK * BLOCK;
+  const int64_t ldq = quantized_ld(a.rows);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int c = i * 32 + (tid >> 3), u = tid & 7, x = c >> 3;      // 16 bytes: units 2 u and 2 u + 1
@@ -237,10 +237,10 @@ slim_status quantize(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const 
     const dim3 grid(slim_cdiv(waves, RQ_THREADS / 64));
     if (x_dtype == SLIM_F16)
       SLIM_LAUNCH(ctx, name, fp8_rows<__half>, grid, dim3(RQ_THREADS), 0, static_cast<const __half*>(a->X), a->ldx, a->rows, a->cols, units,
-                  a->rows_q, a->rows_s, padded(a->cols), scales_ld(a->cols));
+                  a->rows_q, a->rows_s, quantized_ld(a->cols), scales_ld(a->cols));
     else
       SLIM_LAUNCH(ctx, name, fp8_rows<__hip_bfloat16>, grid, dim3(RQ_THREADS), 0, static_cast<const __hip_bfloat16*>(a->X), a->ldx, a->rows,
-                  a->cols, units, a->rows_q, a->rows_s, padded(a->cols), scales_ld(a->cols));
+                  a->cols, units, a->rows_q, a->rows_s, quantized_ld(a->cols), scales_ld(a->cols));
     return SLIM_OK;
   }
   TileArgs ta = {};
