@@ -391,9 +391,11 @@ slim_status slim_fp8_quantize_weights(slim_ctx* ctx, const void* W, slim_dtype w
                                       int64_t ldq, uint8_t* s, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* st, int64_t ldst);
 
 /* Y (t x n; F16, BF16 or F32) = Q(X) W^T, X (t x m, F16 or BF16) in blocks of 128 channels.  Products of e4m3 numbers and scales on the
- * matrix cores, sums in fp32 in a fixed order (which follows the number of tokens), rounded once to Y's type.  For an fp32 Y, and up to 16
- * tokens, the sums keep 24 bits; for a 16-bit Y of more tokens the e4m3 matrix cores are used, at twice the rate, which of eight
- * products drop what lies some 13 bits below the largest: less than the rounding of Y.  Up to 16 tokens in one launch and without a workspace.  slim_fp8_linear_workspace: bytes of workspace (host only; num_cus as in slim_workspace_query). */
+ * matrix cores, sums in fp32 in a fixed order (which follows the number of tokens), rounded once to Y's type.  For an fp32 Y, up
+ * to 16 tokens, and where there is little to multiply, the sums keep 24 bits; for a 16-bit Y of larger calls the e4m3 matrix cores are
+ * used, at twice the rate, which of eight products drop what lies some 13 bits below the largest: less than the rounding of Y.  Up to 16
+ * tokens, and small calls, take one launch and no workspace.  slim_fp8_linear_workspace: bytes of workspace (host only;
+ * num_cus as in slim_workspace_query). */
 size_t slim_fp8_linear_workspace(int n, int m, int t, slim_dtype y_dtype, int num_cus);
 slim_status slim_fp8_linear(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq,
                             const uint8_t* s, int64_t lds, int n, int m, void* Y, slim_dtype y_dtype, int64_t ldy);

@@ -155,8 +155,8 @@ struct Activations {
 };
 slim_status quantize(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const Activations* a, int count);
 
-// ---- and fp8_few.hip: up to FEW_TOKENS tokens in one launch ------------------------------------------------------
-constexpr int FEW_TOKENS = 16;
+// ---- and fp8_few.hip: few tokens, or little work, in one launch -----------------------------------------------------
+bool takes_few_tokens(int n, int m, int t, int ncu);
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, void* Y,
                        slim_dtype y_dtype, int64_t ldy);
 

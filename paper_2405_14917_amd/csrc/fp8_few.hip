@@ -1,4 +1,4 @@
-// The 8-bit linear layer for the few tokens of a decoding step (up to 16), in one launch: Y = Q(X) W^T.
+// The 8-bit linear layer for the few tokens of a decoding step (16 to a workgroup), and for small layers, in one launch: Y = Q(X) W^T.
 //
 // Bound by reading the weights once.  A workgroup takes 16 RT output rows; its eight wavefronts share the blocks of channels and
 // their sums are joined in LDS in a fixed order.  The rows of W are the first operand of v_mfma_f32_16x16x32_bf16, the tokens the second,
@@ -33,9 +33,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   extern __shared__ __align__(16) float part[];                // [wavefront][token][row]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), nw = blockDim.x >> 6;
   const int l16 = lane & 15, c = lane >> 4;
-  const int row0 = blockIdx.x * ROWS;
+  const int row0 = blockIdx.x * ROWS, tok0 = blockIdx.y * 16, tn = min(16, a.t - tok0);
   // (tokens that do not exist are the last one again: their columns of the product are not stored)
-  const T* xrow = static_cast<const T*>(a.X) + (int64_t)min(l16, a.t - 1) * a.ldx + c * 16;
+  const T* xrow = static_cast<const T*>(a.X) + (int64_t)min(tok0 + l16, a.t - 1) * a.ldx + c * 16;
   const uint8_t* wrow[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) wrow[r] = a.q + (int64_t)min(row0 + r * 16 + l16, a.n - 1) * a.ldq + c * 16;
@@ -106,12 +106,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   for (int r = 0; r < RT; ++r) *reinterpret_cast<v4f*>(part + (wave * 16 + l16) * LD + r * 16 + c * 4) = acc[r];
   __syncthreads();
   const int last = min(ROWS, a.n - row0);
-  for (int e = threadIdx.x; e < a.t * ROWS; e += blockDim.x) {
+  for (int e = threadIdx.x; e < tn * ROWS; e += blockDim.x) {
     const int tok = e / ROWS, r = e % ROWS;
     float sum = 0.f;
     for (int i = 0; i < nw; ++i) sum += part[(i * 16 + tok) * LD + r];
     if (r < last) {
-      const int64_t at = (int64_t)tok * a.ldy + row0 + r;
+      const int64_t at = (int64_t)(tok0 + tok) * a.ldy + row0 + r;
       if (a.y_dtype == SLIM_F32) static_cast<float*>(a.Y)[at] = sum;
       else static_cast<unsigned short*>(a.Y)[at] = to_16(sum, a.y_dtype == SLIM_BF16);
     }
@@ -122,25 +122,31 @@ template <typename T, int RT>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
   constexpr int ROWS = 16 * RT;
   const int nw = std::min(FEW_WAVES, a.mb);
-  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT>), dim3(slim_cdiv(a.n, ROWS)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
+  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT>), dim3(slim_cdiv(a.n, ROWS), slim_cdiv(a.t, 16)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
   return SLIM_OK;
 }
 
+// Tiles of 16 x 16 outputs that the busiest CU gets with `rt` sixteens of rows per workgroup
+int busiest(int n, int t, int ncu, int rt) { return slim_cdiv((int64_t)slim_cdiv(n, 16 * rt) * slim_cdiv(t, 16), ncu) * rt; }
+int least_busiest(int n, int t, int ncu) {
+  int least = busiest(n, t, ncu, 1);
+  for (int r = 2; r <= FEW_RT; ++r) least = std::min(least, busiest(n, t, ncu, r));
+  return least;
+}
 // Sixteens of rows per workgroup: what the busiest CU gets is to be as small as it can (within 8 %), then as many as possible, since
 // every workgroup quantises the activations anew.  28672 x 8192, 16 tokens: seven (256 workgroups) 44 us, four (448) 53; 11008 x 4096: three
 // (230) 11.8, four 13.5; 32000 x 4096: four 30, eight (250, and one wavefront's registers fewer) 33.
-int sixteens(int n, int ncu) {
-  auto busiest = [&](int rt) { return slim_cdiv(slim_cdiv(n, 16 * rt), ncu) * rt; };
-  int least = busiest(1), rt = 1;
-  for (int r = 2; r <= FEW_RT; ++r) least = std::min(least, busiest(r));
+int sixteens(int n, int t, int ncu) {
+  const int least = least_busiest(n, t, ncu);
+  int rt = 1;
   for (int r = 2; r <= FEW_RT; ++r)
-    if (busiest(r) * 100 <= least * 108) rt = r;
+    if ((int64_t)busiest(n, t, ncu, r) * 100 <= (int64_t)least * 108) rt = r;
   return rt;
 }
 
 template <typename T>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
-  switch (sixteens(a.n, ctx->num_cus)) {
+  switch (sixteens(a.n, a.t, ctx->num_cus)) {
     case 1: return launch<T, 1>(ctx, a);
     case 2: return launch<T, 2>(ctx, a);
     case 3: return launch<T, 3>(ctx, a);
@@ -154,6 +160,13 @@ slim_status launch(slim_ctx* ctx, const FewArgs& a) {
 }  // namespace
 
 namespace slimfp8 {
+
+// Up to 16 tokens; more while the busiest CU has no more than 64 blocks of 16 x 16 x 128 to multiply, where the two launches of the other
+// way cost more than the work (host's share included: 1000 x 1504, 301 tokens, 60 blocks: 8.9 us and 11.7; 2048 x 2048, 128 tokens, 64 blocks: 8.5 and
+// 14.1; 700 x 700, 1000 tokens, 66 blocks: 14.0 and 12.2).
+bool takes_few_tokens(int n, int m, int t, int ncu) {
+  return t <= 16 || (t <= 65535 * 16 && (int64_t)least_busiest(n, t, ncu) * slim_cdiv(m, BLOCK) <= 64);
+}
 
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, void* Y,
                        slim_dtype y_dtype, int64_t ldy) {

@@ -394,7 +394,7 @@ typedef Tile<128, 128, 2, 2, 2> Medium;
 typedef Tile<64, 64, 2, 2, 4> Small;
 
 struct Plan {
-  int tile, splits[2];
+  int splits[2];
   int64_t ldp[2];
   size_t bytes;
 };
@@ -402,23 +402,44 @@ constexpr int TILE_A[] = {Large::TA, Medium::TA, Small::TA}, TILE_B[] = {Large::
 
 int tiles_of(const Product& p, int tile) { return slim_cdiv(p.a.rows, TILE_A[tile]) * slim_cdiv(p.b.rows, TILE_B[tile]); }
 
-// The tile: the largest of which there are enough to fill the chip; parts: where even the smallest do not.  Medium from three quarters of
-// the CUs on (4096 x 1024, 1024 tokens, 256 tiles: 16.5 us, small ones 18.4; 2048 x 2048, 1024 tokens, 128 tiles: 26.1 and 16.7), but not
-// for up to 64 tokens, half of whose medium tile is empty (28672 x 8192, 64 tokens: 75.4 and 56.9).
+// Parts along the contraction, where `tiles` do not fill the chip; eight steps a part at least.
+int parts_of(int tiles, int nk, int ncu) {
+  const int s = std::max(1, std::min(ncu / std::max(1, tiles), nk / 8));
+  const int per = slim_cdiv(slim_cdiv(std::max(1, nk), s), 4) * 4;
+  return std::max(1, slim_cdiv(nk, per));
+}
+
+// A product's tile: by what a round of workgroups costs, and a step of them.  Measured (us, 16-bit and fp32 C): a round of large tiles 15 +
+// 1.44 (2.6) a step, of two medium ones per CU 5.4 + 0.82 (1.42), of two small ones 2.7 + 0.34 (0.56), a medium one alone on its CU 0.6 of
+// that a step; 6 for the launch.  So 15872 x 128, 6139 tokens, takes medium tiles (81; large ones 110, small ones 147), as does 14666 x 2048, 2078 tokens,
+// whose 522 large ones are three rounds (78 and 102), 2048 x 2048, 1024 tokens, small ones (17; medium ones 26), and 8192 x 28672, 4096
+// tokens, large ones (790; medium ones above 900).
+double tile_cost(const Product& p, int tile, int ncu) {
+  static const double round[] = {15.0, 5.4, 2.7}, step[2][3] = {{1.44, 0.82, 0.34}, {2.6, 1.42, 0.56}};
+  const int tiles = tiles_of(p, tile), s = parts_of(tiles, p.nk, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
+  double one = step[p.c_dtype == SLIM_F32][tile];
+  if (tile == TILE_MEDIUM && tiles * s <= ncu) one *= 0.6;
+  const double join = s > 1 ? 4.0 + 8.0 * s * p.a.rows * (double)p.b.rows / 4.85e6 : 0.0;
+  return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + one * slim_cdiv(p.nk, s)) + join;
+}
+int tile_of(const Product& p, int ncu) {
+  int best = TILE_SMALL;
+  for (int t : {TILE_MEDIUM, TILE_LARGE})
+    if (tile_cost(p, t, ncu) < tile_cost(p, best, ncu)) best = t;
+  return best;
+}
+
+// Products of one launch: all, or one where they differ in their kind or tile (a gradient of long contraction and few tiles beside one of many).
+int in_one_launch(const Product* p, int count, int ncu) {
+  return count == 2 && ((p[0].c_dtype == SLIM_F32) != (p[1].c_dtype == SLIM_F32) || tile_of(p[0], ncu) != tile_of(p[1], ncu)) ? 1 : count;
+}
+
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
-  int n[3] = {}, most = 0;
+  int tiles = 0;
+  for (int i = 0; i < count; ++i) tiles += tiles_of(p[i], tile_of(p[i], ncu));
   for (int i = 0; i < count; ++i) {
-    for (int t = 0; t < 3; ++t) n[t] += tiles_of(p[i], t);
-    most = std::max(most, p[i].b.rows);
-  }
-  pl.tile = n[TILE_LARGE] >= ncu ? TILE_LARGE : most > Small::TB && 4 * n[TILE_MEDIUM] >= 3 * ncu ? TILE_MEDIUM : TILE_SMALL;
-  const int tiles = n[pl.tile];
-  for (int i = 0; i < count; ++i) {
-    int s = std::max(1, std::min(ncu / std::max(1, tiles), p[i].nk / 8));
-    const int per = slim_cdiv(slim_cdiv(std::max(1, p[i].nk), s), 4) * 4;
-    s = std::max(1, slim_cdiv(p[i].nk, per));
-    pl.splits[i] = s;
+    const int s = pl.splits[i] = parts_of(tiles, p[i].nk, ncu);
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
     if (s > 1) pl.bytes += slim_ws_round(sizeof(float) * (size_t)s * pl.ldp[i] * p[i].b.rows);
   }
@@ -437,11 +458,9 @@ slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga
   return tile == TILE_LARGE ? launch<Large, EXACT>(ctx, name, ga, grid) : tile == TILE_MEDIUM ? launch<Medium, EXACT>(ctx, name, ga, grid) : launch<Small, EXACT>(ctx, name, ga, grid);
 }
 
-// products of one launch: all, or one where they differ in their kind
-int in_one_launch(const Product* p, int count) { return count == 2 && (p[0].c_dtype == SLIM_F32) != (p[1].c_dtype == SLIM_F32) ? 1 : count; }
-
 slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count) {
   const Plan pl = make_plan(p, count, ctx->num_cus);
+  const int tile = tile_of(p[0], ctx->num_cus);
   GemmArgs ga = {};
   float* parts[2] = {};
   int grid = 0;
@@ -452,8 +471,8 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
     q.nk = p[i].nk;
     q.splits = pl.splits[i];
     q.per = slim_cdiv(slim_cdiv(std::max(1, q.nk), q.splits), 4) * 4;
-    q.tiles_a = slim_cdiv(q.a.rows, TILE_A[pl.tile]);
-    q.tiles_b = slim_cdiv(q.b.rows, TILE_B[pl.tile]);
+    q.tiles_a = slim_cdiv(q.a.rows, TILE_A[tile]);
+    q.tiles_b = slim_cdiv(q.b.rows, TILE_B[tile]);
     q.c = p[i].c;
     q.ldc = p[i].ldc;
     q.c_dtype = p[i].c_dtype;
@@ -468,7 +487,7 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
     if (i == 0) ga.first = q.tiles_a * q.tiles_b * q.splits;
     grid += q.tiles_a * q.tiles_b * q.splits;
   }
-  const slim_status st = p[0].c_dtype == SLIM_F32 ? launch<true>(ctx, name, pl.tile, ga, grid) : launch<false>(ctx, name, pl.tile, ga, grid);
+  const slim_status st = p[0].c_dtype == SLIM_F32 ? launch<true>(ctx, name, tile, ga, grid) : launch<false>(ctx, name, tile, ga, grid);
   if (st != SLIM_OK) return st;
   for (int i = 0; i < count; ++i)
     if (parts[i]) {
@@ -485,12 +504,12 @@ namespace slimfp8 {
 
 size_t gemm_workspace(const Product* p, int count, int num_cus) {
   size_t bytes = 0;
-  for (int i = 0, c = in_one_launch(p, count); i < count; i += c) bytes += make_plan(p + i, c, num_cus).bytes;
+  for (int i = 0, c = in_one_launch(p, count, num_cus); i < count; i += c) bytes += make_plan(p + i, c, num_cus).bytes;
   return bytes;
 }
 
 slim_status gemm(slim_ctx* ctx, const char* name, const Product* p, int count) {
-  for (int i = 0, c = in_one_launch(p, count); i < count; i += c)
+  for (int i = 0, c = in_one_launch(p, count, ctx->num_cus); i < count; i += c)
     if (const slim_status st = multiply(ctx, name, p + i, c); st != SLIM_OK) return st;
   return SLIM_OK;
 }

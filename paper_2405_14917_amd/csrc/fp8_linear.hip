@@ -1,4 +1,4 @@
-// Entry points of the 8-bit linear layer.  Forward: up to 16 tokens in one launch (fp8_few.hip), more as a launch that quantises the
+// Entry points of the 8-bit linear layer.  Forward: few tokens or little work in one launch (fp8_few.hip), more as a launch that quantises the
 // activations into the workspace and one that multiplies (fp8_gemm.hip).  Backward: one launch quantises the gradient of the
 // outputs in both directions (blocks of outputs for dX, blocks of tokens for dW) and the activations along the tokens, one multiplies:
 //   Y  (t x n) : A = W  (n rows),            B = Q(X)    (t rows),  contraction over m
@@ -52,7 +52,7 @@ int backward_products(int n, int m, int t, bool dx, bool dw, slim_dtype dw_dtype
   return count;
 }
 size_t forward_need(int n, int m, int t, slim_dtype y_dtype, int ncu) {
-  if (t <= FEW_TOKENS) return 0;
+  if (takes_few_tokens(n, m, t, ncu)) return 0;
   const Product p = forward_product(n, m, t, y_dtype);
   return activation_bytes(t, m) + gemm_workspace(&p, 1, ncu);
 }
@@ -101,7 +101,7 @@ slim_status slim_fp8_linear(slim_ctx* ctx, const void* X, slim_dtype x_dtype, in
   SLIM_REQUIRE(ctx, X && Y && ldx >= m && ldy >= n, "%s: null pointer, or rows shorter than the layer (ldx = %lld, ldy = %lld)", fn,
                (long long)ldx, (long long)ldy);
   const Operand w = {q, s, ldq, lds, n, 7};
-  if (t <= FEW_TOKENS) return few_tokens(ctx, X, x_dtype, t, ldx, w, m, Y, y_dtype, ldy);
+  if (takes_few_tokens(n, m, t, ctx->num_cus)) return few_tokens(ctx, X, x_dtype, t, ldx, w, m, Y, y_dtype, ldy);
   if (const slim_status st = slim_ws_reserve(ctx, forward_need(n, m, t, y_dtype, ctx->num_cus)); st != SLIM_OK) return st;
   Activations a = {X, ldx, t, m, nullptr, nullptr, nullptr, nullptr};
   if (!carve(ctx, t, m, a.rows_q, a.rows_s)) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);

@@ -61,7 +61,8 @@ int main() {
     return slim_fp8_linear(&c, X, x, t, ldx, q, ldq, u, lds, n, m, p, y, ldy);
   };
   say("linear_few", linear(16, 200, 256, 4, 130, 200, SLIM_F16, SLIM_F32, 130, u, p));
-  say("linear", linear(17, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear_few", linear(17, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
+  say("linear", linear(4000, 200, 256, 4, 4000, 200, SLIM_BF16, SLIM_BF16, 4000, u, p));
   say("linear_none", linear(0, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, nullptr));
   say("linear_bad", linear(-1, 200, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
   say("linear_bad", linear(5, 199, 256, 4, 130, 200, SLIM_BF16, SLIM_BF16, 130, u, p));
