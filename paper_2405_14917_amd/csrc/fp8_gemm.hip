@@ -434,12 +434,12 @@ int in_one_launch(const Product* p, int count, int ncu) {
   return count == 2 && ((p[0].c_dtype == SLIM_F32) != (p[1].c_dtype == SLIM_F32) || tile_of(p[0], ncu) != tile_of(p[1], ncu)) ? 1 : count;
 }
 
+// Each product's parts as if it were alone: beside another one of many tiles, few of long contraction would be what the launch waits for
+// (gradients of 14666 x 2078, 88 tokens: 17 tiles of 115 steps took 82 us beside 1955 of one).
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
-  int tiles = 0;
-  for (int i = 0; i < count; ++i) tiles += tiles_of(p[i], tile_of(p[i], ncu));
   for (int i = 0; i < count; ++i) {
-    const int s = pl.splits[i] = parts_of(tiles, p[i].nk, ncu);
+    const int s = pl.splits[i] = parts_of(tiles_of(p[i], tile_of(p[i], ncu)), p[i].nk, ncu);
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
     if (s > 1) pl.bytes += slim_ws_round(sizeof(float) * (size_t)s * pl.ldp[i] * p[i].b.rows);
   }
