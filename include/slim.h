@@ -416,7 +416,7 @@ slim_status slim_fp8_linear_backward(slim_ctx* ctx, const void* dY, const void* 
  * mean); dw = sum of dY xh and db (or NULL) = sum of dY over the rows, in fp32 in a fixed order, of w's type.  dX may be dY or X. */
 slim_status slim_layer_norm(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int64_t rows, int cols, int64_t ldx, const void* w,
                             const void* b, slim_dtype w_dtype, double eps, int rms, void* Y, int64_t ldy, float* mean, float* rstd);
-size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, int bias, int num_cus);
+size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, slim_dtype x_dtype, int bias, int num_cus);
 slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* X, slim_dtype x_dtype, int64_t rows, int cols, int64_t lddy,
                                      int64_t ldx, const void* w, slim_dtype w_dtype, const float* mean, const float* rstd, void* dX,
                                      int64_t lddx, void* dw, void* db);

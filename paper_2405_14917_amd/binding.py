@@ -135,7 +135,7 @@ def load() -> ctypes.CDLL:
                                              c_int, c_int, c_void_p, c_i64, c_void_p, c_int, c_i64]
     lib.slim_layer_norm.argtypes = [c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_void_p, c_void_p, c_int, c_double, c_int, c_void_p,
                                     c_i64, c_void_p, c_void_p]
-    lib.slim_layer_norm_backward_workspace.argtypes = [c_i64, c_int, c_int, c_int]
+    lib.slim_layer_norm_backward_workspace.argtypes = [c_i64, c_int, c_int, c_int, c_int]
     lib.slim_layer_norm_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_i64, c_void_p, c_int, c_void_p,
                                              c_void_p, c_void_p, c_i64, c_void_p, c_void_p]
     lib.slim_distill_loss.argtypes = [c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_void_p, c_int, c_void_p, c_int, c_int, c_i64,
@@ -196,9 +196,9 @@ def fp8_linear_backward_workspace(n: int, m: int, t: int, dx: bool = True, dw: b
     return int(load().slim_fp8_linear_backward_workspace(n, m, t, int(dx), int(dw), _DT[dw_dtype], num_cus))
 
 
-def layer_norm_backward_workspace(rows: int, cols: int, bias: bool = True, num_cus: int = 0) -> int:
+def layer_norm_backward_workspace(rows: int, cols: int, bias: bool = True, dtype: torch.dtype = torch.bfloat16, num_cus: int = 0) -> int:
     """Bytes of workspace of Slim.layer_norm_backward (host only, no GPU needed)."""
-    return int(load().slim_layer_norm_backward_workspace(rows, cols, int(bias), num_cus))
+    return int(load().slim_layer_norm_backward_workspace(rows, cols, _DT[dtype], int(bias), num_cus))
 
 
 def distill_workspace(rows: int, V: int, dtype: torch.dtype = torch.bfloat16) -> int:

@@ -7,7 +7,10 @@
 // wavefronts as it came (16-byte pieces of its own type), so that the deviations are taken from the mean itself and not from the
 // difference of two sums; means and deviations in fp32.  A workgroup goes through rows blockIdx, blockIdx + gridDim, ... with w and b kept in
 // registers, and sums its share of dw and db there: column sums of its rows, which a second kernel adds over the workgroups in a fixed
-// order.  Rows longer than 16 pieces per lane of 16 wavefronts are read again instead.
+// order.  Rows that the registers of 16 wavefronts do not hold are read again instead.
+//
+// 16384 x 4096 bf16 without the mean: forward 56 us (4.8 TB/s), backward 67 (6.0: a part of the inputs is still in the cache behind the
+// L2), the second kernel 3.
 #include "slim_device.h"
 #include "slim_internal.h"
 
@@ -90,13 +93,14 @@ struct Piece {
   }
 };
 
-// Sums over the W wavefronts of a row.  `slot` alternates between calls, so that one barrier per call is enough.
+// Sums over the W wavefronts of a row (of several rows of W each, with a `red` for each; the barrier is all of theirs).  `slot` alternates
+// between calls, so that one barrier per call is enough.
 template <int W, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[W][N], int& slot) {
 #pragma unroll
   for (int k = 0; k < N; ++k) v[k] = wave_sum_f32(v[k]);
   if constexpr (W > 1) {
-    const int wave = threadIdx.x >> 6;
+    const int wave = (threadIdx.x >> 6) % W;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int k = 0; k < N; ++k) red[slot][wave][k] = v[k];
@@ -182,11 +186,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_forward(NormArgs a
   }
 }
 
-template <typename T, typename TW, int W, int P>
-__global__ __launch_bounds__(64 * W) void norm_backward(NormArgs a) {
+// W wavefronts per row, P pieces per lane, G rows at a time; the G shares of dw and db are added in LDS (cols floats each, in turn)
+template <typename T, typename TW, int W, int P, int G>
+__global__ __launch_bounds__(64 * W * G) void norm_backward(NormArgs a) {
   constexpr int E = Piece<T>::E, LANES = 64 * W;
-  __shared__ float red[2][W][2];
-  const int lane = threadIdx.x;
+  __shared__ float red[G][2][W][2];
+  extern __shared__ float share[];
+  const int group = G == 1 ? 0 : threadIdx.x / LANES, lane = G == 1 ? threadIdx.x : threadIdx.x % LANES;
   const float inv_n = 1.f / (float)a.cols;
   int slot = 0;
   float w[P][E], dw[P][E], db[P][E];
@@ -212,26 +218,31 @@ __global__ __launch_bounds__(64 * W) void norm_backward(NormArgs a) {
       dy[i].load(static_cast<const T*>(a.dY) + row * a.lddy + c, a.cols - c);
     }
   };
-  if ((int64_t)blockIdx.x < a.rows) fetch(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const float mean = a.mean ? a.mean[row] : 0.f, r = a.rstd[row];
+  // (a group without a row in the last round goes through it with what it has, and keeps nothing of it)
+  const int64_t first = (int64_t)blockIdx.x * G + group, step = (int64_t)gridDim.x * G;
+  fetch(min(first, a.rows - 1));
+  for (int64_t row0 = (int64_t)blockIdx.x * G; row0 < a.rows; row0 += step) {
+    const int64_t row = row0 + group;
+    const bool live = G == 1 || row < a.rows;
+    const int64_t at = live ? row : a.rows - 1;
+    const float mean = a.mean ? a.mean[at] : 0.f, r = a.rstd[at];
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < P; ++i)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float d = dy[i].get(e), xh = (x[i].get(e) - mean) * r, g = d * w[i][e];     // (behind the last column d is 0)
+        const float d = live ? dy[i].get(e) : 0.f, xh = (x[i].get(e) - mean) * r, g = d * w[i][e];     // (behind the last column d is 0)
         s[0] += g;
         s[1] = fmaf(g, xh, s[1]);
-        dw[i][e] = fmaf(d, xh, dw[i][e]);
+        if (live) dw[i][e] = fmaf(d, xh, dw[i][e]);
         db[i][e] += d;
       }
-    row_sums<W, 2>(s, red, slot);
+    row_sums<W, 2>(s, red[group], slot);
     const float mg = a.rms ? 0.f : s[0] * inv_n, mgx = s[1] * inv_n;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int c = (i * LANES + lane) * E;
-      if (c >= a.cols) break;
+      if (c >= a.cols || !live) break;
       float o[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -242,18 +253,34 @@ __global__ __launch_bounds__(64 * W) void norm_backward(NormArgs a) {
       p.set(o);
       p.store(static_cast<T*>(a.dX) + row * a.lddx + c, a.cols - c);
     }
-    if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
+    if (row0 + step < a.rows) fetch(min(row + step, a.rows - 1));
   }
+  auto columns = [&](auto use) {
 #pragma unroll
-  for (int i = 0; i < P; ++i)
+    for (int i = 0; i < P; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (i * LANES + lane) * E + e;
-      if (c < a.cols) {
-        a.pw[(int64_t)blockIdx.x * a.cols + c] = dw[i][e];
-        if (a.pb) a.pb[(int64_t)blockIdx.x * a.cols + c] = db[i][e];
+      for (int e = 0; e < E; ++e) {
+        const int c = (i * LANES + lane) * E + e;
+        if (c < a.cols) use(c, dw[i][e], db[i][e]);
       }
-    }
+  };
+#pragma unroll
+  for (int g = 1; g < G; ++g) {
+    if (g > 1) __syncthreads();
+    if (group == g) columns([&](int c, float& p, float& q) {
+      share[c] = p;
+      if (a.pb) share[a.cols + c] = q;
+    });
+    __syncthreads();
+    if (group == 0) columns([&](int c, float& p, float& q) {
+      p += share[c];
+      if (a.pb) q += share[a.cols + c];
+    });
+  }
+  if (group == 0) columns([&](int c, float& p, float& q) {
+    a.pw[(int64_t)blockIdx.x * a.cols + c] = p;
+    if (a.pb) a.pb[(int64_t)blockIdx.x * a.cols + c] = q;
+  });
 }
 
 // Rows that no group of wavefronts holds: three passes over them, the column sums by a kernel of their own.
@@ -360,10 +387,28 @@ __global__ __launch_bounds__(1024) void norm_join(const float* __restrict__ pw, 
   }
 }
 
-constexpr int NB_PER_CU = 4;                   // workgroups per CU of the backward pass, and so partial sums
-
+// Wavefronts per row, pieces per lane, rows at a time, and workgroups per CU of the backward pass: as many wavefronts as hide the loads, and no
+// more partial sums than that takes.  With the forward pass: 16384 x 4096 bf16, one row at a time, three workgroups per CU 128 us, two 135,
+// two rows at a time 142 (too few registers); 3001 x 1501 fp32 the other way, 28.5 (four) and 26.0; 30000 x 640 bf16 one wavefront per row 52,
+// four 68.
+struct Shape {
+  int w, p, g, per_cu;
+};
+Shape shape_of(int cols, int e) {
+  const int pieces = slim_cdiv(cols, e);
+  if (pieces <= 64) return {1, 1, 4, 4};
+  if (pieces <= 128) return {1, 2, 4, 3};
+  if (pieces <= 256) return {4, 1, 2, 2};
+  if (pieces <= 512) return e == 8 ? Shape{4, 2, 1, 3} : Shape{4, 2, 2, 2};
+  if (pieces <= 1024) return {8, 2, 1, 2};
+  if (pieces <= 2048) return {16, 2, 1, 1};
+  return {0, 0, 1, 2};
+}
 // workgroups, and with them partial sums, of the backward pass
-int parts_of(int64_t rows, int ncu) { return (int)std::max<int64_t>(1, std::min<int64_t>(rows, (int64_t)NB_PER_CU * ncu)); }
+int parts_of(int64_t rows, int cols, slim_dtype d, int ncu) {
+  const Shape s = shape_of(cols, d == SLIM_F32 ? 4 : 8);
+  return (int)std::max<int64_t>(1, std::min<int64_t>((rows + s.g - 1) / s.g, (int64_t)s.per_cu * ncu));
+}
 
 template <typename T, typename TW>
 slim_status forward(slim_ctx* ctx, const NormArgs& a) {
@@ -385,18 +430,23 @@ slim_status forward(slim_ctx* ctx, const NormArgs& a) {
 
 template <typename T, typename TW>
 slim_status backward(slim_ctx* ctx, const NormArgs& a, void* dw, void* db, int parts) {
-  constexpr int E = Piece<T>::E;
-  const int pieces = slim_cdiv(a.cols, E);
+  const Shape s = shape_of(a.cols, Piece<T>::E);
   const char* name = "norm_backward";
-  const dim3 grid(parts);
-  if (pieces <= 64) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1>), grid, dim3(64), 0, a);
-  else if (pieces <= 256) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1>), grid, dim3(256), 0, a);
-  else if (pieces <= 512) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2>), grid, dim3(256), 0, a);
-  else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2>), grid, dim3(512), 0, a);
-  else if (pieces <= 2048) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2>), grid, dim3(1024), 0, a);
-  else {
-    SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
-    SLIM_LAUNCH(ctx, "norm_columns", norm_columns<T>, dim3(slim_cdiv(a.cols, 256), parts), dim3(256), 0, a, (a.rows + parts - 1) / parts);
+  const dim3 grid(parts), block(64 * s.w * s.g);
+  const size_t smem = s.g > 1 ? sizeof(float) * (db ? 2 : 1) * (size_t)a.cols : 0;
+  switch (s.w * 10 + s.p) {
+    case 11: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1, 4>), grid, block, smem, a); break;
+    case 12: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 2, 4>), grid, block, smem, a); break;
+    case 41: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1, 2>), grid, block, smem, a); break;
+    case 42:
+      if constexpr (Piece<T>::E == 8) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2, 1>), grid, block, smem, a);
+      else SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2, 2>), grid, block, smem, a);
+      break;
+    case 82: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2, 1>), grid, block, smem, a); break;
+    case 162: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2, 1>), grid, block, smem, a); break;
+    default:
+      SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
+      SLIM_LAUNCH(ctx, "norm_columns", norm_columns<T>, dim3(slim_cdiv(a.cols, 256), parts), dim3(256), 0, a, (a.rows + parts - 1) / parts);
   }
   SLIM_LAUNCH(ctx, "norm_join", norm_join<TW>, dim3(slim_cdiv(a.cols, 32), db ? 2 : 1), dim3(1024), 0, a.pw, a.pb, parts, a.cols, dw, db);
   return SLIM_OK;
@@ -422,9 +472,9 @@ slim_status check(slim_ctx* ctx, const char* fn, slim_dtype x, slim_dtype w, int
 
 extern "C" {
 
-size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, int bias, int num_cus) {
+size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, slim_dtype x_dtype, int bias, int num_cus) {
   if (rows <= 0 || cols <= 0) return 0;
-  const size_t one = slim_ws_round(sizeof(float) * (size_t)parts_of(rows, num_cus > 0 ? num_cus : 256) * cols);
+  const size_t one = slim_ws_round(sizeof(float) * (size_t)parts_of(rows, cols, x_dtype, num_cus > 0 ? num_cus : 256) * cols);
   return bias ? 2 * one : one;
 }
 
@@ -463,8 +513,8 @@ slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* 
   SLIM_REQUIRE(ctx, w && dw, "%s: null weight or dw", fn);
   SLIM_REQUIRE(ctx, rows == 0 || (dY && X && dX && rstd && lddy >= cols && ldx >= cols && lddx >= cols),
                "%s: null pointer, or rows shorter than cols", fn);
-  const int parts = rows ? parts_of(rows, ctx->num_cus) : 0;
-  if (const slim_status st = slim_ws_reserve(ctx, slim_layer_norm_backward_workspace(rows, cols, db != nullptr, ctx->num_cus)); st != SLIM_OK)
+  const int parts = rows ? parts_of(rows, cols, x_dtype, ctx->num_cus) : 0;
+  if (const slim_status st = slim_ws_reserve(ctx, slim_layer_norm_backward_workspace(rows, cols, x_dtype, db != nullptr, ctx->num_cus)); st != SLIM_OK)
     return st;
   NormArgs a = {};
   a.X = X;

@@ -15,7 +15,7 @@ def workspace_query(vocabulary: int, width: int, tokens: int, dtype: torch.dtype
     """Bytes of workspace of a HeadTuning with up to `tokens` tokens a call, for a context under graph capture."""
     return max(max(binding.fp8_linear_workspace(vocabulary, width, t, dtype, num_cus),
                    binding.fp8_linear_backward_workspace(vocabulary, width, t, True, head_grad, torch.float32, num_cus),
-                   binding.layer_norm_backward_workspace(t, width, bias, num_cus),
+                   binding.layer_norm_backward_workspace(t, width, bias, dtype, num_cus),
                    binding.distill_workspace(t, vocabulary, dtype)) for t in {tokens, min(tokens, 17)})
 
 

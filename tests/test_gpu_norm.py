@@ -204,7 +204,7 @@ def test_a_workspace_of_the_queried_size_is_enough():
     ncu = torch.cuda.get_device_properties(0).multi_processor_count
     X, dY, w, _ = (t.cuda() for t in data(2000, 999, torch.float32, torch.float32, 10))
     for bias in (False, True):
-        need = binding.layer_norm_backward_workspace(2000, 999, bias, ncu)
+        need = binding.layer_norm_backward_workspace(2000, 999, bias, torch.float32, ncu)
         for size, ok in ((need, True), (need - 256, False)):
             s = binding.Slim("cuda:0", workspace_bytes=size)
             try:
