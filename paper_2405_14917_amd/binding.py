@@ -206,6 +206,11 @@ def distill_workspace(rows: int, V: int, dtype: torch.dtype = torch.bfloat16) ->
     return int(load().slim_distill_workspace(rows, V, _DT[dtype]))
 
 
+def _empty_like(x: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of x's shape and type."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def _row_stride(x: torch.Tensor, what: str) -> int:
     """The leading dimension of a matrix whose rows are contiguous."""
     if x.dim() != 2:
@@ -578,12 +583,14 @@ class Slim:
             if Wt.shape[1] != n or dw and Wt.shape[0] != m:
                 raise ValueError("Wt has to be (m, n) = (%s, %d), got %s" % (m if dw else "m", n, tuple(Wt.shape)))
             m = Wt.shape[0]
-        dX = torch.empty((t, m), dtype=dY.dtype, device=dY.device) if dx else None
-        dW = torch.empty((n, m), dtype=dw_dtype or dY.dtype, device=dY.device) if dw else None
-        self._check(self.lib.slim_fp8_linear_backward(self.ctx, dY.data_ptr(), X.data_ptr() if dw else None, _dtype(dY), t,
-                                                      _row_stride(dY, "dY"), _row_stride(X, "X") if dw else 0, Wt.data_ptr() if dx else None,
-                                                      ldqt, Wts.data_ptr() if dx else None, ldst, n, m, dX.data_ptr() if dx else None, m,
-                                                      dW.data_ptr() if dw else None, _dtype(dW) if dw else F32, m))
+        dX = dY.new_empty((t, m)) if dx else None
+        dW = dY.new_empty((n, m), dtype=dw_dtype) if dw else None
+        st = self.lib.slim_fp8_linear_backward(self.ctx, dY.data_ptr(), X.data_ptr() if dw else None, _dtype(dY), t, _row_stride(dY, "dY"),
+                                               _row_stride(X, "X") if dw else 0, Wt.data_ptr() if dx else None, ldqt,
+                                               Wts.data_ptr() if dx else None, ldst, n, m, dX.data_ptr() if dx else None, m,
+                                               dW.data_ptr() if dw else None, _dtype(dW) if dw else F32, m)
+        if st:
+            self._check(st)
         return dX, dW
 
     def layer_norm(self, X: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor] = None, eps: float = 1e-5, rms: bool = False,
@@ -592,7 +599,7 @@ class Slim:
         (Y, mean, rstd) for the backward pass (mean is None with `rms`)."""
         self._ready(X, w, b)
         rows, cols = self._norm_shape(X, w, b)
-        Y = X.new_empty((rows, cols))
+        Y = _empty_like(X)
         mean = rstd = None
         if stats:
             mean = None if rms else X.new_empty(rows, dtype=torch.float32)
@@ -620,13 +627,15 @@ class Slim:
         if dY.shape != X.shape or dY.dtype != X.dtype:
             raise ValueError("dY has to be of X's shape and type")
         for v in (mean, rstd):
-            if v is not None and (v.dtype != torch.float32 or tuple(v.shape) != (rows,) or not v.is_contiguous()):
+            if v is not None and (v.dtype != torch.float32 or v.shape != (rows,) or not v.is_contiguous()):
                 raise ValueError("mean and rstd have to be float32 vectors of X's rows")
-        dX, dw = X.new_empty((rows, cols)), w.new_empty(cols)
-        db = w.new_empty(cols) if bias else None
-        self._check(self.lib.slim_layer_norm_backward(self.ctx, dY.data_ptr(), X.data_ptr(), _dtype(X), rows, cols, _row_stride(dY, "dY"),
-                                                      _row_stride(X, "X"), w.data_ptr(), _dtype(w), None if mean is None else mean.data_ptr(),
-                                                      rstd.data_ptr(), dX.data_ptr(), cols, dw.data_ptr(), None if db is None else db.data_ptr()))
+        dX, dw = _empty_like(X), torch.empty_like(w)
+        db = torch.empty_like(w) if bias else None
+        st = self.lib.slim_layer_norm_backward(self.ctx, dY.data_ptr(), X.data_ptr(), _dtype(X), rows, cols, _row_stride(dY, "dY"),
+                                               _row_stride(X, "X"), w.data_ptr(), _dtype(w), None if mean is None else mean.data_ptr(),
+                                               rstd.data_ptr(), dX.data_ptr(), cols, dw.data_ptr(), None if db is None else db.data_ptr())
+        if st:
+            self._check(st)
         return dX, dw, db
 
     def _distill_args(self, S, index, teacher, tau, lse):
@@ -638,7 +647,7 @@ class Slim:
         ldk = _row_stride(index, "index")
         if _row_stride(teacher, "teacher") != ldk:
             raise ValueError("index and teacher have to have one row stride")
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows,) or not lse.is_contiguous()):
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (rows,) or not lse.is_contiguous()):
             raise ValueError("lse has to be a float32 vector of the rows")
         return (self.ctx, S.data_ptr(), _dtype(S), rows, V, _row_stride(S, "S"), index.data_ptr(), int(index.dtype == torch.int64),
                 teacher.data_ptr(), _dtype(teacher), index.shape[1], ldk, None if lse is None else lse.data_ptr(), tau)
@@ -658,14 +667,16 @@ class Slim:
         """(loss, dS) with dS (rows, V) of S's type the gradient of sum(dloss * loss); dS may be given, S itself among others."""
         self._ready(S, index, teacher, dloss, lse, dS)
         args = self._distill_args(S, index, teacher, tau, lse)
-        if dloss.dtype != torch.float32 or tuple(dloss.shape) != (S.shape[0],) or not dloss.is_contiguous():
+        if dloss.dtype != torch.float32 or dloss.shape != (S.shape[0],) or not dloss.is_contiguous():
             raise ValueError("dloss has to be a float32 vector of the rows")
         if dS is None:
-            dS = S.new_empty(S.shape)
+            dS = _empty_like(S)
         elif dS.shape != S.shape or dS.dtype != S.dtype:
             raise ValueError("dS has to be of S's shape and type")
         loss = S.new_empty(args[3], dtype=torch.float32)
-        self._check(self.lib.slim_distill_loss_grad(*args, dloss.data_ptr(), loss.data_ptr(), dS.data_ptr(), _row_stride(dS, "dS")))
+        st = self.lib.slim_distill_loss_grad(*args, dloss.data_ptr(), loss.data_ptr(), dS.data_ptr(), _row_stride(dS, "dS"))
+        if st:
+            self._check(st)
         return loss, dS
 
     # ---- measurement aid

@@ -127,9 +127,9 @@ slim_status launch(slim_ctx* ctx, const FewArgs& a) {
 }
 
 // Tiles of 16 x 16 outputs that the busiest CU gets with `rt` sixteens of rows per workgroup
-int busiest(int n, int t, int ncu, int rt) { return slim_cdiv((int64_t)slim_cdiv(n, 16 * rt) * slim_cdiv(t, 16), ncu) * rt; }
-int least_busiest(int n, int t, int ncu) {
-  int least = busiest(n, t, ncu, 1);
+int64_t busiest(int n, int t, int ncu, int rt) { return ((int64_t)slim_cdiv(n, 16 * rt) * slim_cdiv(t, 16) + ncu - 1) / ncu * rt; }
+int64_t least_busiest(int n, int t, int ncu) {
+  int64_t least = busiest(n, t, ncu, 1);
   for (int r = 2; r <= FEW_RT; ++r) least = std::min(least, busiest(n, t, ncu, r));
   return least;
 }
@@ -137,10 +137,10 @@ int least_busiest(int n, int t, int ncu) {
 // every workgroup quantises the activations anew.  28672 x 8192, 16 tokens: seven (256 workgroups) 44 us, four (448) 53; 11008 x 4096: three
 // (230) 11.8, four 13.5; 32000 x 4096: four 30, eight (250, and one wavefront's registers fewer) 33.
 int sixteens(int n, int t, int ncu) {
-  const int least = least_busiest(n, t, ncu);
+  const int64_t least = least_busiest(n, t, ncu);
   int rt = 1;
   for (int r = 2; r <= FEW_RT; ++r)
-    if ((int64_t)busiest(n, t, ncu, r) * 100 <= (int64_t)least * 108) rt = r;
+    if (busiest(n, t, ncu, r) * 100 <= least * 108) rt = r;
   return rt;
 }
 
@@ -165,7 +165,7 @@ namespace slimfp8 {
 // way cost more than the work (host's share included: 1000 x 1504, 301 tokens, 60 blocks: 8.9 us and 11.7; 2048 x 2048, 128 tokens, 64 blocks: 8.5 and
 // 14.1; 700 x 700, 1000 tokens, 66 blocks: 14.0 and 12.2).
 bool takes_few_tokens(int n, int m, int t, int ncu) {
-  return t <= 16 || (t <= 65535 * 16 && (int64_t)least_busiest(n, t, ncu) * slim_cdiv(m, BLOCK) <= 64);
+  return t <= 16 || (t <= 65535 * 16 && least_busiest(n, t, ncu) * slim_cdiv(m, BLOCK) <= 64);
 }
 
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, void* Y,

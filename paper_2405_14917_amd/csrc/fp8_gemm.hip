@@ -18,6 +18,8 @@
 // What bounds it: the operands' way from L2 to LDS.  8192 x 28672 with 4096 tokens: 790 us (2430 TFLOP/s); without the loads the same
 // loop takes 517 us, with loads that all hit in the L2 661; the fp32 form 1415 us for as many products (1360 TFLOP/s, the bf16 matrix
 // cores at the clock the power allows).
+#include <atomic>
+
 #include "fp8_device.h"
 
 namespace {
@@ -448,8 +450,13 @@ Plan make_plan(const Product* p, int count, int ncu) {
 
 template <typename T, bool EXACT>
 slim_status launch(slim_ctx* ctx, const char* name, const GemmArgs& ga, int grid) {
-  if (T::LDS > 64 * 1024)
+  // (an attribute of the function on the device, asked for once: it costs a call as much as a third of the launch)
+  static std::atomic<uint64_t> allowed{0};
+  const uint64_t bit = ctx->device < 64 ? 1ull << ctx->device : 0;
+  if (T::LDS > 64 * 1024 && !(allowed.load(std::memory_order_relaxed) & bit)) {
     SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_gemm<T, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
   SLIM_LAUNCH(ctx, name, (fp8_gemm<T, EXACT>), dim3(grid), dim3(T::THREADS), T::LDS, ga);
   return SLIM_OK;
 }
