@@ -24,6 +24,7 @@ struct NormArgs {
   int64_t ldx, lddy, ldy, lddx;
   float *mean, *rstd;                    // written by the forward pass (may be null), read by the backward pass
   float *pw, *pb;                        // partial column sums: gridDim x cols
+  void *dw, *db;                         // of one workgroup for all rows: the sums themselves
   int64_t rows;
   int cols;
   float eps;
@@ -92,6 +93,17 @@ struct Piece {
     }
   }
 };
+
+template <typename T>
+__device__ __forceinline__ float value(const void* p, int64_t i) {
+  if constexpr (sizeof(T) == 4) return static_cast<const float*>(p)[i];
+  else return Elem<T>::widen(static_cast<const unsigned short*>(p)[i]);
+}
+template <typename T>
+__device__ __forceinline__ void put(void* p, int64_t i, float v) {
+  if constexpr (sizeof(T) == 4) static_cast<float*>(p)[i] = v;
+  else static_cast<unsigned short*>(p)[i] = Elem<T>::narrow(v);
+}
 
 // Sums over the W wavefronts of a row (of several rows of W each, with a `red` for each; the barrier is all of theirs).  `slot` alternates
 // between calls, so that one barrier per call is enough.
@@ -269,32 +281,25 @@ __global__ __launch_bounds__(64 * W * G) void norm_backward(NormArgs a) {
     if (g > 1) __syncthreads();
     if (group == g) columns([&](int c, float& p, float& q) {
       share[c] = p;
-      if (a.pb) share[a.cols + c] = q;
+      if (a.pb || a.db) share[a.cols + c] = q;
     });
     __syncthreads();
     if (group == 0) columns([&](int c, float& p, float& q) {
       p += share[c];
-      if (a.pb) q += share[a.cols + c];
+      if (a.pb || a.db) q += share[a.cols + c];
     });
   }
-  if (group == 0) columns([&](int c, float& p, float& q) {
+  if (group == 0 && a.dw) columns([&](int c, float& p, float& q) {
+    put<TW>(a.dw, c, p);
+    if (a.db) put<TW>(a.db, c, q);
+  });
+  if (group == 0 && !a.dw) columns([&](int c, float& p, float& q) {
     a.pw[(int64_t)blockIdx.x * a.cols + c] = p;
     if (a.pb) a.pb[(int64_t)blockIdx.x * a.cols + c] = q;
   });
 }
 
 // Rows that no group of wavefronts holds: three passes over them, the column sums by a kernel of their own.
-template <typename T>
-__device__ __forceinline__ float value(const void* p, int64_t i) {
-  if constexpr (sizeof(T) == 4) return static_cast<const float*>(p)[i];
-  else return Elem<T>::widen(static_cast<const unsigned short*>(p)[i]);
-}
-template <typename T>
-__device__ __forceinline__ void put(void* p, int64_t i, float v) {
-  if constexpr (sizeof(T) == 4) static_cast<float*>(p)[i] = v;
-  else static_cast<unsigned short*>(p)[i] = Elem<T>::narrow(v);
-}
-
 template <typename T, typename TW>
 __global__ __launch_bounds__(1024) void norm_forward_long(NormArgs a) {
   __shared__ float red[2][16][1];
@@ -391,23 +396,24 @@ __global__ __launch_bounds__(1024) void norm_join(const float* __restrict__ pw, 
 // more partial sums than that takes.  With the forward pass: 16384 x 4096 bf16, one row at a time, three workgroups per CU 128 us, two 135,
 // two rows at a time 142 (too few registers); 3001 x 1501 fp32 the other way, 28.5 (four) and 26.0; 30000 x 640 bf16 one wavefront per row 52,
 // four 68.
+// Up to four rounds of rows: one workgroup, which needs no second kernel (52 x 64: 24 -> 20 us with the forward pass, most of it the host's).
 struct Shape {
   int w, p, g, per_cu;
 };
-Shape shape_of(int cols, int e) {
+Shape shape_of(int64_t rows, int cols, int e) {
   const int pieces = slim_cdiv(cols, e);
-  if (pieces <= 64) return {1, 1, 4, 4};
-  if (pieces <= 128) return {1, 2, 4, 3};
-  if (pieces <= 256) return {4, 1, 2, 2};
-  if (pieces <= 512) return e == 8 ? Shape{4, 2, 1, 3} : Shape{4, 2, 2, 2};
-  if (pieces <= 1024) return {8, 2, 1, 2};
-  if (pieces <= 2048) return {16, 2, 1, 1};
+  if (pieces <= 64) return rows <= 64 ? Shape{1, 1, 16, 0} : Shape{1, 1, 4, 4};
+  if (pieces <= 128) return rows <= 32 ? Shape{1, 2, 8, 0} : Shape{1, 2, 4, 3};
+  if (pieces <= 256) return rows <= 16 ? Shape{4, 1, 4, 0} : Shape{4, 1, 2, 2};
+  if (pieces <= 512) return rows <= 8 ? Shape{4, 2, 2, 0} : e == 8 ? Shape{4, 2, 1, 3} : Shape{4, 2, 2, 2};
+  if (pieces <= 1024) return {8, 2, 1, rows <= 4 ? 0 : 2};
+  if (pieces <= 2048) return {16, 2, 1, rows <= 4 ? 0 : 1};
   return {0, 0, 1, 2};
 }
-// workgroups, and with them partial sums, of the backward pass
+// workgroups, and with them partial sums, of the backward pass; 0: one for all rows, without partial sums
 int parts_of(int64_t rows, int cols, slim_dtype d, int ncu) {
-  const Shape s = shape_of(cols, d == SLIM_F32 ? 4 : 8);
-  return (int)std::max<int64_t>(1, std::min<int64_t>((rows + s.g - 1) / s.g, (int64_t)s.per_cu * ncu));
+  const Shape s = shape_of(rows, cols, d == SLIM_F32 ? 4 : 8);
+  return (int)std::min<int64_t>((rows + s.g - 1) / s.g, (int64_t)s.per_cu * ncu);
 }
 
 template <typename T, typename TW>
@@ -430,24 +436,28 @@ slim_status forward(slim_ctx* ctx, const NormArgs& a) {
 
 template <typename T, typename TW>
 slim_status backward(slim_ctx* ctx, const NormArgs& a, void* dw, void* db, int parts) {
-  const Shape s = shape_of(a.cols, Piece<T>::E);
+  const Shape s = shape_of(a.rows, a.cols, Piece<T>::E);
   const char* name = "norm_backward";
-  const dim3 grid(parts), block(64 * s.w * s.g);
+  const dim3 grid(std::max(1, parts)), block(64 * s.w * s.g);
   const size_t smem = s.g > 1 ? sizeof(float) * (db ? 2 : 1) * (size_t)a.cols : 0;
-  switch (s.w * 10 + s.p) {
-    case 11: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1, 4>), grid, block, smem, a); break;
-    case 12: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 2, 4>), grid, block, smem, a); break;
-    case 41: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1, 2>), grid, block, smem, a); break;
-    case 42:
+  switch (s.w * 1000 + s.p * 100 + s.g) {
+    case 1104: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1, 4>), grid, block, smem, a); break;
+    case 1116: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 1, 16>), grid, block, smem, a); break;
+    case 1204: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 2, 4>), grid, block, smem, a); break;
+    case 1208: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 1, 2, 8>), grid, block, smem, a); break;
+    case 4102: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1, 2>), grid, block, smem, a); break;
+    case 4104: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 1, 4>), grid, block, smem, a); break;
+    case 4201:
       if constexpr (Piece<T>::E == 8) SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2, 1>), grid, block, smem, a);
-      else SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2, 2>), grid, block, smem, a);
       break;
-    case 82: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2, 1>), grid, block, smem, a); break;
-    case 162: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2, 1>), grid, block, smem, a); break;
+    case 4202: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 4, 2, 2>), grid, block, smem, a); break;
+    case 8201: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2, 1>), grid, block, smem, a); break;
+    case 16201: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2, 1>), grid, block, smem, a); break;
     default:
       SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
       SLIM_LAUNCH(ctx, "norm_columns", norm_columns<T>, dim3(slim_cdiv(a.cols, 256), parts), dim3(256), 0, a, (a.rows + parts - 1) / parts);
   }
+  if (parts == 0) return SLIM_OK;
   SLIM_LAUNCH(ctx, "norm_join", norm_join<TW>, dim3(slim_cdiv(a.cols, 32), db ? 2 : 1), dim3(1024), 0, a.pw, a.pb, parts, a.cols, dw, db);
   return SLIM_OK;
 }
@@ -529,10 +539,15 @@ slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* 
   a.rows = rows;
   a.cols = cols;
   a.rms = mean == nullptr;
-  if (parts > 0) {
-    a.pw = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols));
-    a.pb = db ? static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols)) : nullptr;
-    if (!a.pw || (db && !a.pb)) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
+  if (rows > 0) {
+    if (parts > 0) {
+      a.pw = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols));
+      a.pb = db ? static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)parts * cols)) : nullptr;
+      if (!a.pw || (db && !a.pb)) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
+    } else {
+      a.dw = dw;
+      a.db = db;
+    }
     return by_type(x_dtype, w_dtype, [&](auto x, auto wt) { return backward<decltype(x), decltype(wt)>(ctx, a, dw, db, parts); });
   }
   // no rows: the sums are zero

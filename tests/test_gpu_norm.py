@@ -98,8 +98,8 @@ def test_every_width(slim, cols, x, w, rms, bias):
     check(slim, X, dY, wt, b if bias else None, 1e-5, rms)
 
 
-@pytest.mark.parametrize("rows", [1, 2, 5, 1030, 5000])
-@pytest.mark.parametrize("cols", [96, 1000])
+@pytest.mark.parametrize("rows", [1, 2, 5, 16, 17, 64, 65, 1030, 5000])
+@pytest.mark.parametrize("cols", [96, 1000, 1500, 4000])
 @pytest.mark.parametrize("rms,bias", [(False, False), (True, True), (False, True)])
 def test_every_height(slim, rows, cols, rms, bias):
     X, dY, wt, b = data(rows, cols, torch.bfloat16, torch.float32, rows)
