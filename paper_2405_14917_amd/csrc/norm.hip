@@ -9,8 +9,8 @@
 // registers, and sums its share of dw and db there: column sums of its rows, which a second kernel adds over the workgroups in a fixed
 // order.  Rows that the registers of 16 wavefronts do not hold are read again instead.
 //
-// 16384 x 4096 bf16 without the mean: forward 56 us (4.8 TB/s), backward 67 (6.0: a part of the inputs is still in the cache behind the
-// L2), the second kernel 3.
+// 16384 x 4096 bf16 without the mean: forward 43 us (6.3 TB/s), backward 68 (5.9: a part of the inputs is still in the cache behind the
+// L2), the second kernel 5.
 #include "slim_device.h"
 #include "slim_internal.h"
 
@@ -165,7 +165,23 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_forward(NormArgs a
       x[i].load(static_cast<const T*>(a.X) + row * a.ldx + c, a.cols - c);
     }
   };
+  // w and b are kept where the registers hold them: read again for every row they made it 57 us in place of 43 (16384 x 4096 bf16 without
+  // the mean)
+  constexpr int Q = E / Piece<TW>::E;
+  constexpr bool KEEP = W < 16 || P * E <= 16;
+  Piece<TW> wk[KEEP ? P : 1][Q], bk[KEEP ? P : 1][Q];
+  auto affine = [&](Piece<TW> (&w)[Q], Piece<TW> (&b)[Q], int c) {
+#pragma unroll
+    for (int k = 0; k < Q; ++k) {
+      const int at = c + k * Piece<TW>::E;
+      w[k].load(static_cast<const TW*>(a.w) + at, a.cols - at);
+      if (a.b) b[k].load(static_cast<const TW*>(a.b) + at, a.cols - at);
+    }
+  };
   if (row0 < a.rows) fetch(row0);
+  if constexpr (KEEP)
+#pragma unroll
+    for (int i = 0; i < P; ++i) affine(wk[i], bk[i], (i * LANES + lane) * E);
   for (int64_t row = row0; row < a.rows; row += step) {
     float s[1] = {0.f};
     float mean = 0.f;
@@ -194,16 +210,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_forward(NormArgs a
       const int c = (i * LANES + lane) * E;
       if (c >= a.cols) break;
       float y[E];
+      if constexpr (!KEEP) affine(wk[0], bk[0], c);
+      const auto& w = wk[KEEP ? i : 0];
+      const auto& b = bk[KEEP ? i : 0];
 #pragma unroll
-      for (int k = 0; k < E; k += Piece<TW>::E) {
-        Piece<TW> w, b;
-        w.load(static_cast<const TW*>(a.w) + c + k, a.cols - c - k);
-        if (a.b) b.load(static_cast<const TW*>(a.b) + c + k, a.cols - c - k);
-#pragma unroll
-        for (int e = 0; e < Piece<TW>::E; ++e) {
-          const float xh = (x[i].get(k + e) - mean) * r;
-          y[k + e] = a.b ? fmaf(xh, w.get(e), b.get(e)) : xh * w.get(e);
-        }
+      for (int e = 0; e < E; ++e) {
+        constexpr int F = Piece<TW>::E;
+        const float xh = (x[i].get(e) - mean) * r;
+        y[e] = a.b ? fmaf(xh, w[e / F].get(e % F), b[e / F].get(e % F)) : xh * w[e / F].get(e % F);
       }
       Piece<T> o;
       o.set(y);
@@ -453,6 +467,7 @@ slim_status forward(slim_ctx* ctx, const NormArgs& a) {
   else if (pieces <= 128) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 1, 2>), grid((a.rows + 3) / 4, 8), dim3(256), 0, a);
   else if (pieces <= 512) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 4, 2>), grid(a.rows, 8), dim3(256), 0, a);
   else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 4, 4>), grid(a.rows, 8), dim3(256), 0, a);
+  else if (pieces <= 2048) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 16, 2>), grid(a.rows, 2), dim3(1024), 0, a);
   else if (pieces <= 4096) SLIM_LAUNCH(ctx, name, (norm_forward<T, TW, 16, 4>), grid(a.rows, 2), dim3(1024), 0, a);
   else SLIM_LAUNCH(ctx, name, (norm_forward_long<T, TW>), grid(a.rows, 2), dim3(1024), 0, a);
   return SLIM_OK;
