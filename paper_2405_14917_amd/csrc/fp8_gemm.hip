@@ -47,8 +47,9 @@ struct GemmArgs {
 __device__ __forceinline__ void load_lds16x4(unsigned lds_addr, const unsigned* off, const uint8_t* gbase, int k, int n) {
 #if defined(__HIP_DEVICE_COMPILE__)
   asm volatile("s_cmp_ge_i32 %6, %7\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-               "global_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072\n1:"
-               : : "s"(lds_addr), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(gbase), "s"(k), "s"(n) : "m0", "scc");
+               "global_load_lds_dwordx4 %2, %5 offset:%8\n\tglobal_load_lds_dwordx4 %3, %5 offset:%9\n\tglobal_load_lds_dwordx4 %4, %5 offset:%10\n1:"
+               : : "s"(lds_addr), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(gbase), "s"(k), "s"(n), "n"(1 << 10), "n"(2 << 10), "n"(3 << 10)
+               : "m0", "scc");
 #else
   (void)lds_addr, (void)off, (void)gbase, (void)k, (void)n;
 #endif
