@@ -493,8 +493,9 @@ slim_status backward(slim_ctx* ctx, const NormArgs& a, void* dw, void* db, int p
     case 8201: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 8, 2, 1>), grid, block, smem, a); break;
     case 16201: SLIM_LAUNCH(ctx, name, (norm_backward<T, TW, 16, 2, 1>), grid, block, smem, a); break;
     default:
-      SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
+      // (the columns first: dX may take the place of dY or X, which both kernels read)
       SLIM_LAUNCH(ctx, "norm_columns", norm_columns<T>, dim3(slim_cdiv(a.cols, 256), parts), dim3(256), 0, a, (a.rows + parts - 1) / parts);
+      SLIM_LAUNCH(ctx, name, (norm_backward_long<T, TW>), grid, dim3(1024), 0, a);
   }
   if (parts == 0) return SLIM_OK;
   SLIM_LAUNCH(ctx, "norm_join", norm_join<TW>, dim3(slim_cdiv(a.cols, 32), db ? 2 : 1), dim3(1024), 0, a.pw, a.pb, parts, a.cols, dw, db);

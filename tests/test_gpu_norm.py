@@ -235,3 +235,24 @@ def test_refusals(slim):
         with pytest.raises(binding.SlimError) as e:
             bad()
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("cols,x", [(20000, torch.bfloat16), (9000, torch.float32), (12288, torch.float32), (70001, torch.float32)])
+@pytest.mark.parametrize("rms,bias", [(False, True), (True, False)])
+def test_gradients_of_long_rows_may_take_the_place_of_inputs(slim, cols, x, rms, bias):
+    """Rows that the registers do not hold: the column sums are those of the inputs as they came, over dY as over X."""
+    from paper_2405_14917_amd import binding as B
+    rows = 40
+    X, dY, wt, _ = data(rows, cols, x, torch.float32, cols)
+    Xg, dYg, wg = X.cuda(), dY.cuda(), wt.cuda()
+    _, dX, dw, db = check(slim, X, dY, wt, torch.zeros_like(wt) if bias else None, 1e-5, rms)
+    _, mean, rstd = slim.layer_norm(Xg, wg, eps=1e-5, rms=rms, stats=True)
+    p = lambda t: None if t is None else t.data_ptr()
+    for over in ("dY", "X"):
+        x2, dy2 = Xg.clone(), dYg.clone()
+        out = dy2 if over == "dY" else x2
+        dw2, db2 = torch.empty_like(dw), None if db is None else torch.empty_like(db)
+        assert slim.lib.slim_layer_norm_backward(slim.ctx, p(dy2), p(x2), B.F32 if x == torch.float32 else B.BF16, rows, cols, cols, cols, p(wg), B.F32,
+                                                 p(mean), p(rstd), p(out), cols, p(dw2), p(db2)) == B.SLIM_OK
+        assert torch.equal(out, dX), over
+        assert torch.equal(dw2, dw) and (db is None or torch.equal(db2, db)), over
