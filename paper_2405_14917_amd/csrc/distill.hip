@@ -5,13 +5,15 @@
 //   dS = dloss / tau (q - p) in a slot, dloss / tau (q - rest q / q_rest) elsewhere (q without a rest);  rows of no p: zero
 //
 // Bound by memory: a row of logits is read once and its gradient written once.  One workgroup per row, which keeps it in registers as it
-// came: maximum, sum of exponentials, then the gradient, without a second read.  Rows that do not fit, or are too few to fill the chip, are
+// came: maximum, sum of exponentials, then the gradient, without a second read.  Rows that do not fit are
 // cut into chunks of a workgroup each: one kernel leaves every chunk's maximum and sum, a second one joins them and writes the
 // gradient, its own read of the logits mostly from the cache behind the L2.  Outside the slots the gradient is one factor times the
-// exponential; the slots are written over it afterwards.  The sum outside the slots (with a rest) leaves them out by a bit per class in
-// LDS: taking them from the whole sum would cancel where they hold nearly all of it.  Sums over the vocabulary in fp32 (a lane's few,
+// exponential; the slots are written over it afterwards.  With a rest, the classes outside the slots have a maximum and a sum of their own
+// (the slots are dropped from the row in registers by a bit per class in LDS): taken from the whole sum they would cancel where the slots
+// hold nearly all of it, and relative to the slots' maximum their exponentials would vanish where it leads them by more than fp32's range.
+// So the gradient there is r (q_rest - rest), r their softmax among themselves.  Sums over the vocabulary in fp32 (a lane's few,
 // then a tree; chunks in fp64), exponentials 2^(x log2(e) / tau - off) with one rounding of the argument; whatever has one value per slot
-// or row in fp64, relative to the same off: the loss is a small difference of large terms.
+// or row in fp64: the loss is a small difference of large terms.
 #include "slim_device.h"
 #include "slim_internal.h"
 
@@ -33,7 +35,7 @@ struct DistillArgs {
   int V, K;
   int index64, t_dtype;
   double tau;
-  // rows in chunks: `chunks` of them, their maxima and sums (rows x chunks), and the slots' sums (4 per row)
+  // rows in chunks: `chunks` of them, their maxima and sums (rows x chunks), and the slots' sums (5 per row)
   int chunks;
   float2* part;
   double* slots;
@@ -82,6 +84,10 @@ struct Piece {
       else v[i] = (unsigned)narrow<T>(f[2 * i]) | (unsigned)narrow<T>(f[2 * i + 1]) << 16;
     }
   }
+  __device__ __forceinline__ void drop(int i) {                      // element i becomes minus infinity
+    if constexpr (sizeof(T) == 4) v[i] = 0xff800000u;
+    else v[i / 2] = (v[i / 2] & (i & 1 ? 0xffffu : 0xffff0000u)) | (__is_same(T, __half) ? 0xfc00u : 0xff80u) << (16 * (i & 1));
+  }
   // The widened values are not kept from one use to the next: they would take twice the registers.
   __device__ __forceinline__ void narrow_again() {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -90,6 +96,10 @@ struct Piece {
   }
 };
 
+// Exponentials relative to the maximum less LIFT (powers of two): the instruction counts results below 2^-126 as zero, which lifted are below
+// 2^-186 of the largest, and 2^30 classes of 2^LIFT are no overflow.
+constexpr float LIFT = 60.f;
+__device__ __forceinline__ float off_of(float top, float c) { return top > -INFINITY ? fmaf(top, c, -LIFT) : 0.f; }
 __device__ __forceinline__ float exp_of(float v, float c, float off) { return __builtin_amdgcn_exp2f(fmaf(v, c, -off)); }
 
 // A range of a row in the registers of a workgroup: P pieces per thread, and the elements behind the last whole piece, one per thread.
@@ -120,25 +130,27 @@ struct Range {
     }
     return m;
   }
-  // sum of the exponentials; MASKED: without the classes whose bit is set
-  template <bool MASKED>
-  __device__ __forceinline__ float sum(float c, float off, const uint8_t* bits) {
-    float s = exp_of(last, c, off);
-    if (MASKED && tid < rest && (bits[(pieces * E + tid) >> 3] >> ((pieces * E + tid) & 7) & 1)) s = 0.f;
+  // the classes whose bit is set become minus infinity
+  __device__ __forceinline__ void drop(const uint8_t* bits) {
+    if (tid < rest && (bits[(pieces * E + tid) >> 3] >> ((pieces * E + tid) & 7) & 1)) last = -INFINITY;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      int mask = 0;
-      if constexpr (MASKED) {
-        const int at = min(i * THREADS + tid, max(pieces - 1, 0)) * E;
-        mask = (int)bits[at >> 3] >> (at & 7);
+      const int at = min(i * THREADS + tid, max(pieces - 1, 0)) * E, mask = (int)bits[at >> 3] >> (at & 7);
+      if (__builtin_expect(mask & ((1 << E) - 1), 0)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (mask >> e & 1) x[i].drop(e);
       }
+    }
+  }
+  // sum of the exponentials
+  __device__ __forceinline__ float sum(float c, float off) {
+    float s = exp_of(last, c, off);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
       float p = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float v = exp_of(x[i].get(e), c, off);
-        if constexpr (MASKED) v = __uint_as_float(__float_as_uint(v) & ~(unsigned)((mask << (31 - e)) >> 31));
-        p += v;
-      }
+      for (int e = 0; e < E; ++e) p += exp_of(x[i].get(e), c, off);
       s += p;
       x[i].narrow_again();
     }
@@ -175,25 +187,31 @@ __device__ __forceinline__ float teacher_of(const DistillArgs& a, int64_t at) {
   return a.t_dtype == SLIM_F32 ? value<float>(a.teacher, at) : a.t_dtype == SLIM_F16 ? value<__half>(a.teacher, at) : value<__hip_bfloat16>(a.teacher, at);
 }
 
-// What a row's slots and sums make of it.  Slots: A = sum p (t - z), B = sum p (without a rest before its division by itself),
-// C = sum exp(z - z0); es: the vocabulary's sum of exp(z - z0), with a rest outside the slots.  All logits over tau.
+// What a row's slots and sums make of it.  Slots, whose logits z are relative to a base zs: A = sum p (t - z), B = sum p (without a
+// rest before its division by itself), C = sum exp(z) (with a rest); es: the sum of the exponentials of the classes outside the slots (without
+// a rest: of all) relative to their maximum, gap: that less zs.  All logits over tau.
 struct Row {
-  double total, rest, es, A, B, z0, t0;
+  double rest, es, total, A, B, gap, q_rest, slot;               // slot: q of a slot over its exp(z)
   bool live;
-  __device__ __forceinline__ Row(double A_, double B_, double C, double es_, double z0_, double t0_, bool with_rest)
-      : total(with_rest ? es_ + C : es_), rest(with_rest ? 1.0 - B_ : 0.0), es(es_), A(A_), B(B_), z0(z0_), t0(t0_) {
+  __device__ __forceinline__ Row(double A_, double B_, double C, double es_, double gap_, bool with_rest)
+      : rest(with_rest ? 1.0 - B_ : 0.0), es(es_), total(es_), A(A_), B(B_), gap(gap_), q_rest(1.0), slot(1.0 / es_) {
     if (rest < 0x1p-20) rest = 0.0;
     live = !(B + rest <= 0.0);
+    if (with_rest) {
+      const double e = exp(-fabs(gap)), out = gap > 0.0 ? 1.0 : e, in = gap > 0.0 ? e : 1.0;
+      total = es * out + C * in;                                  // relative to the larger of the two maxima
+      q_rest = es * out / total;
+      slot = in / total;
+    }
   }
-  // the gradient outside the slots over the exponential
+  // the gradient outside the slots over the exponential; 0 where the slots leave no class with a probability, NaN where there is none at all
   __device__ __forceinline__ float factor(double g) const {
-    const double other = rest > 0.0 && es > 0.0 ? 1.0 - rest * total / es : 1.0;
-    return (float)(g * other / total);
+    return es == 0.0 ? (total == 0.0 ? NAN : 0.f) : (float)(g * (q_rest - rest) / es);
   }
   __device__ __forceinline__ float loss(bool with_rest) const {
-    const double lq = z0 + log(total);
-    double l = with_rest ? A + B * (lq - t0) : A / B + lq - (t0 + log(B));
-    if (rest > 0.0) l += rest * (log(rest) - log(es / total));
+    const double lt = with_rest ? fmax(gap, 0.0) + log(total) : log(es) + gap;      // of the sum over all classes, less zs
+    double l = with_rest ? A + B * lt : A / B + lt - log(B);
+    if (rest > 0.0) l += rest * (log(rest) - (log(es) + gap - lt));
     return live ? (float)l : 0.f;
   }
 };
@@ -230,7 +248,7 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
   constexpr int W = THREADS / 64;
   extern __shared__ __align__(16) char smem_dl[];
   double* sp = reinterpret_cast<double*>(smem_dl);                 // p of a slot
-  double* se = sp + a.K;                                           // exp(z - z0) of a slot
+  double* se = sp + a.K;                                           // exp(z) of a slot, relative to zs
   int* si = reinterpret_cast<int*>(se + a.K);                      // its class, or -1
   unsigned* bits = reinterpret_cast<unsigned*>(si + a.K);          // REST: a bit per class
   __shared__ float red_m[W], red_t[W];
@@ -247,29 +265,34 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     for (int i = tid; i < (a.V + 31) / 32; i += THREADS) bits[i] = 0u;
     __syncthreads();
   }
-  float t_top = -INFINITY;
+  float high = -INFINITY;                                          // of the slots: the student's logits, without a rest the teacher's
   for (int k = tid; k < a.K; k += THREADS) {
     const int cls = class_of(a, row * a.ldk + k);
     si[k] = cls;
     if (cls >= 0) {
-      const float t = teacher_of(a, row * a.ldk + k);
+      const float t = teacher_of(a, row * a.ldk + k), z = value<T>(S, cls);
       sp[k] = (double)t;
-      se[k] = (double)value<T>(S, cls);
-      t_top = fmaxf(t_top, t);
+      se[k] = (double)z;
+      high = fmaxf(high, REST ? z : t);
       if constexpr (REST) atomicOr(&bits[cls >> 5], 1u << (cls & 31));
     }
   }
-  const float top = group_max<W>(x.top(), red_m);                  // (its barrier: the bits are set)
-  if constexpr (!REST) t_top = group_max<W>(t_top, red_t);
-  const float off = top * c;
-  double d[4] = {0.0, 0.0, 0.0, (double)x.template sum<REST>(c, off, reinterpret_cast<const uint8_t*>(bits))};
-  const double t0 = REST ? (double)a.lse[row] : (t_top > -INFINITY ? (double)t_top * itau : 0.0), z0 = (double)off * LN2;
+  if constexpr (REST) {
+    __syncthreads();
+    x.drop(reinterpret_cast<const uint8_t*>(bits));
+  }
+  const float top = group_max<W>(x.top(), red_m);
+  high = group_max<W>(high, red_t);
+  const float off = off_of(top, c);
+  double d[4] = {0.0, 0.0, 0.0, (double)x.sum(c, off)};
+  const double zr = (double)off * LN2, zh = high > -INFINITY ? (double)high * itau : REST ? zr : 0.0;
+  const double t0 = REST ? (double)a.lse[row] : zh, zs = REST ? zh : zr;
   for (int k = tid; k < a.K; k += THREADS) {
     double p = 0.0, ez = 0.0;
     if (si[k] >= 0) {
-      const double t = sp[k] * itau, z = se[k] * itau;
-      p = exp(t - t0);
-      ez = exp(z - z0);
+      const double t = sp[k] * itau - t0, z = se[k] * itau - zs;
+      p = exp(t);
+      ez = exp(z);
       if (p != 0.0) d[0] += p * (t - z);
       d[1] += p;
       d[2] += ez;
@@ -278,14 +301,14 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     se[k] = ez;
   }
   group_sums<W, 4>(d, red_d);
-  const Row r(d[0], d[1], d[2], d[3], z0, t0, REST);
+  const Row r(d[0], d[1], d[2], d[3], zr - zs, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
     if (r.live) {
       x.write(dS, c, off, r.factor(g));
       __syncthreads();
-      const double ge = g / r.total, gp = REST ? g : g / r.B;
+      const double ge = g * r.slot, gp = REST ? g : g / r.B;
       for (int k = tid; k < a.K; k += THREADS)
         if (si[k] >= 0) put<T>(dS, si[k], (float)(se[k] * ge - sp[k] * gp));
     } else {
@@ -323,9 +346,13 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
       if (cls >= 0 && cls < n) atomicOr(&bits[cls >> 5], 1u << (cls & 31));
     }
   }
+  if constexpr (REST) {
+    __syncthreads();
+    x.drop(reinterpret_cast<const uint8_t*>(bits));
+  }
   const float top = group_max<W>(x.top(), red_m);
   // (a chunk of masked logits alone: a sum of zero, not of NaN)
-  double e[1] = {(double)x.template sum<REST>(c, top == -INFINITY ? 0.f : top * c, reinterpret_cast<const uint8_t*>(bits))};
+  double e[1] = {(double)x.sum(c, off_of(top, c))};
   group_sums<W, 1>(e, red_e);
   if (tid == 0) a.part[row * a.chunks + chunk] = make_float2(top, (float)e[0]);
   if (chunk != 0) return;
@@ -345,10 +372,10 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
   for (int k = tid; k < a.K; k += CH_THREADS) {
     const int cls = class_of(a, row * a.ldk + k);
     if (cls >= 0) {
-      const double t = (double)teacher_of(a, row * a.ldk + k) * itau, z = (double)value<T>(S, cls) * itau, p = exp(t - t0);
+      const double t = (double)teacher_of(a, row * a.ldk + k) * itau - t0, z = (double)value<T>(S, cls) * itau - zs, p = exp(t);
       if (p != 0.0) d[0] += p * (t - z);
       d[1] += p;
-      if constexpr (REST) d[2] += exp(z - zs);
+      if constexpr (REST) d[2] += exp(z);
     }
   }
   group_sums<W, 3>(d, red_d);
@@ -357,7 +384,7 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
     s[0] = d[0];
     s[1] = d[1];
     s[2] = d[2];
-    s[3] = zs;
+    s[3] = z_top > -INFINITY ? zs : -INFINITY;
     s[4] = t0;
   }
 }
@@ -379,17 +406,17 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
   float top = -INFINITY;
   for (int i = lane; i < a.chunks; i += 64) top = fmaxf(top, part[i].x);
   top = wave_max_f32(top);
-  const float off = top * c;
+  const float off = off_of(top, c);
   double es = 0.0;
   for (int i = lane; i < a.chunks; i += 64) {
     const float2 v = part[i];
-    // (a chunk's sum is relative to the rounded product of its maximum)
-    es += v.x == -INFINITY ? (top == -INFINITY ? (double)NAN : (double)v.y) : (double)v.y * exp(((double)(v.x * c) - (double)off) * LN2);
+    // (that of a chunk without a maximum is 0 or NaN)
+    es += v.x == -INFINITY ? (double)v.y : (double)v.y * exp(((double)off_of(v.x, c) - (double)off) * LN2);
   }
   es = wave_sum(es);
   const double* s = a.slots + row * 5;
-  const double z0 = (double)off * LN2;
-  const Row r(s[0], s[1], REST && s[2] != 0.0 ? s[2] * exp(s[3] - z0) : 0.0, es, z0, s[4], REST);
+  const double zr = (double)off * LN2, zs = s[3] > -INFINITY ? s[3] : zr, t0 = s[4];
+  const Row r(s[0], s[1], s[2], es, zr - zs, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
@@ -398,12 +425,12 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
       extern __shared__ __align__(16) char smem_dl[];
       float* sv = reinterpret_cast<float*>(smem_dl);
       int* si = reinterpret_cast<int*>(sv + a.K);
-      const double ge = g / r.total, gp = REST ? g : g / r.B;
+      const double ge = g * r.slot, gp = REST ? g : g / r.B, zb = REST ? zs : zr;
       for (int k = tid; k < a.K; k += CH_THREADS) {
         const int cls = class_of(a, row * a.ldk + k), at = cls - c0;
         si[k] = cls >= 0 && at >= 0 && at < n ? at : -1;
         if (si[k] >= 0)
-          sv[k] = (float)(exp((double)value<T>(S, cls) * itau - z0) * ge - exp((double)teacher_of(a, row * a.ldk + k) * itau - r.t0) * gp);
+          sv[k] = (float)(exp((double)value<T>(S, cls) * itau - zb) * ge - exp((double)teacher_of(a, row * a.ldk + k) * itau - t0) * gp);
       }
       __syncthreads();
       x.write(dS + c0, c, off, r.factor(g));

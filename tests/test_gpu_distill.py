@@ -267,3 +267,75 @@ def test_refusals(slim):
         with pytest.raises(binding.SlimError) as e:
             bad()
         assert e.value.status == status
+
+
+# Exponentials of a difference d from a maximum, over tau, times log2(e) / tau: three roundings of the argument, 2^-23 of the instruction, so
+# (3 |d| / tau + 4) u; the sums then (3 * 30 + 4 + 128 + 10) u = 232 u.
+SHIFTED = 232 * U
+
+
+def shifted_formulas(S, index, teacher, dloss, tau, lse):
+    """formulas() with every logarithm relative to the largest of its own classes, so that nothing under- or overflows however far apart the slots
+    and the others lie: the classes outside the slots hold r q_rest, r their softmax among themselves."""
+    x, rows, V = S.double(), *S.shape
+    used = (index >= 0) & (index < V)
+    t = teacher.double()
+    if lse is None:
+        lp = torch.where(used, (t - torch.where(used, t, -math.inf).amax(1, keepdim=True)) / tau, -math.inf)
+        lp = lp - torch.logsumexp(lp, 1, keepdim=True)
+    else:
+        lp = torch.where(used, t / tau - lse.double()[:, None], -math.inf)
+    p_slot = torch.exp(lp)
+    place = torch.where(used, index, V).long()
+    slot = torch.zeros((rows, V + 1), dtype=torch.bool).scatter_(1, place, True)[:, :V]
+    p = torch.zeros((rows, V + 1), dtype=torch.float64).scatter_(1, place, p_slot)[:, :V]
+    rest = torch.zeros(rows, dtype=torch.float64) if lse is None else 1 - p.sum(1)
+    rest = torch.where(rest < 2.0 ** -20, 0.0, rest)
+    top = x.amax(1, keepdim=True)
+    whole = torch.logsumexp((x - top) / tau, 1, keepdim=True)
+    lq = (x - top) / tau - whole
+    other = x.masked_fill(slot, -math.inf)
+    d = (other - other.amax(1, keepdim=True)) / tau
+    within = torch.logsumexp(d, 1, keepdim=True)
+    r = torch.exp(d - within)
+    lq_rest = within + (other.amax(1, keepdim=True) - top) / tau - whole
+    q_rest = torch.exp(lq_rest)
+    lq_slot = torch.where(used, lq.gather(1, torch.where(used, index, 0).long()), 0.0)
+    loss = torch.where(p_slot > 0, p_slot * (lp - lq_slot), 0.0).sum(1) + torch.where(rest > 0, torch.xlogy(rest, rest) - rest * lq_rest[:, 0], 0.0)
+    g = (dloss.double() / tau)[:, None]
+    grad = torch.where(slot, torch.exp(lq) - p, r * (q_rest - rest[:, None]))
+    e_r = torch.where(r > 0, r * ((3 * d.abs() + 4) * U + SHIFTED), 0.0)
+    e = torch.where(slot, torch.exp(lq) * SHIFTED, e_r * (q_rest - rest[:, None]).abs() + SHIFTED * r * q_rest)
+    return loss, grad * g, e * g.abs()
+
+
+def check_shifted(slim, S, index, teacher, dloss, tau, lse):
+    cu = lambda t: None if t is None else t.cuda()
+    loss = slim.distill_loss(cu(S), cu(index), cu(teacher), tau, lse=cu(lse))
+    loss2, dS = slim.distill_loss_grad(cu(S), cu(index), cu(teacher), cu(dloss), tau, lse=cu(lse))
+    assert torch.equal(loss, loss2)
+    want, dwant, e = shifted_formulas(S, index, teacher, dloss, tau, lse)
+    assert torch.isfinite(want).all()
+    got = loss.double().cpu()
+    bad = ~((got - want).abs() <= 2 * SHIFTED + 2 * U * want.abs())
+    assert not bad.any(), (got[bad][:3], want[bad][:3])
+    h, tiny = HALF[S.dtype], TINY[S.dtype]
+    bad = ~((dS.double().cpu() - dwant).abs() <= e + 4 * U * dwant.abs() + h * (dwant.abs() + e) + tiny)
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4], dS.cpu()[bad][:4], dwant[bad][:4])
+
+
+LONG = [(777, torch.float32), (3000, torch.bfloat16), (12000, torch.float16), (50257, torch.float32), (70001, torch.bfloat16)]
+
+
+@pytest.mark.parametrize("V,dtype", LONG)
+@pytest.mark.parametrize("gap", [60.0, 90.0, 120.0, 300.0, 1000.0])
+@pytest.mark.parametrize("tau", [1.0, 0.5])
+def test_slots_far_above_a_rest(slim, V, dtype, gap, tau):
+    """The student's logits of the slots lead all others by so much that fp32 exponentials relative to them vanish: the rest's share of the loss and
+    its gradient stay what they are."""
+    S, index, t, dloss, _ = data(6, V, 9, dtype, 21, tau, True, pad=V // 100, empty=False)
+    S.scatter_(1, index, S.float().gather(1, index).add(gap * tau).to(dtype))
+    index[4, 3:] = -1
+    used = index >= 0
+    lse = (torch.logsumexp(torch.where(used, t.double() / tau, -math.inf), 1) - math.log(0.9)).float()       # a rest of about a tenth
+    check_shifted(slim, S, index, t, dloss + 0.1, tau, lse)
