@@ -12,8 +12,9 @@
 // (the slots are dropped from the row in registers by a bit per class in LDS): taken from the whole sum they would cancel where the slots
 // hold nearly all of it, and relative to the slots' maximum their exponentials would vanish where it leads them by more than fp32's range.
 // So the gradient there is r (q_rest - rest), r their softmax among themselves.  Sums over the vocabulary in fp32 (a lane's few,
-// then a tree; chunks in fp64), exponentials 2^(x log2(e) / tau - off) with one rounding of the argument; whatever has one value per slot
-// or row in fp64: the loss is a small difference of large terms.
+// then a tree; chunks in fp64), exponentials of the difference from the maximum, 2^((x - top) log2(e) / tau): a common shift of a row's logits
+// changes nothing, and a row of nothing but the type's lowest value is one of zeros.  Whatever has one value per slot or row in fp64, differences
+// too: the loss is a small difference of large terms.
 #include "slim_device.h"
 #include "slim_internal.h"
 
@@ -22,7 +23,7 @@ namespace {
 using namespace slimdev;
 
 constexpr int DL_MAX_K = 2048;
-constexpr double LOG2E = 1.44269504088896340736, LN2 = 0.693147180559945309417;
+constexpr double LOG2E = 1.44269504088896340736;
 
 struct DistillArgs {
   const void* S;
@@ -96,11 +97,14 @@ struct Piece {
   }
 };
 
-// Exponentials relative to the maximum less LIFT (powers of two): the instruction counts results below 2^-126 as zero, which lifted are below
-// 2^-186 of the largest, and 2^30 classes of 2^LIFT are no overflow.
-constexpr float LIFT = 60.f;
-__device__ __forceinline__ float off_of(float top, float c) { return top > -INFINITY ? fmaf(top, c, -LIFT) : 0.f; }
-__device__ __forceinline__ float exp_of(float v, float c, float off) { return __builtin_amdgcn_exp2f(fmaf(v, c, -off)); }
+// Exponentials relative to the maximum `top`, times 2^LIFT: the instruction counts results below 2^-126 as zero, which lifted are below
+// 2^-150 of the largest, the least fp32 number; 2^30 classes of 2^LIFT are no overflow.
+constexpr int LIFT = 24;
+constexpr double UNLIFT = 1.0 / (1 << LIFT);
+__device__ __forceinline__ float exp_of(float v, float c, float top) { return __builtin_amdgcn_exp2f(fmaf(v - top, c, (float)LIFT)); }
+// log2(e) / tau; what a maximum is worth as a base (minus infinity, of nothing or of excluded classes alone: 0, against which they stay zero)
+__device__ __forceinline__ float per_tau(double itau) { return (float)fmin(LOG2E * itau, 3e38); }
+__device__ __forceinline__ float base_of(float top) { return top > -INFINITY ? top : 0.f; }
 
 // A range of a row in the registers of a workgroup: P pieces per thread, and the elements behind the last whole piece, one per thread.
 template <typename T, int THREADS, int P>
@@ -144,30 +148,30 @@ struct Range {
     }
   }
   // sum of the exponentials
-  __device__ __forceinline__ float sum(float c, float off) {
-    float s = exp_of(last, c, off);
+  __device__ __forceinline__ float sum(float c, float top) {
+    float s = exp_of(last, c, top);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       float p = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) p += exp_of(x[i].get(e), c, off);
+      for (int e = 0; e < E; ++e) p += exp_of(x[i].get(e), c, top);
       s += p;
       x[i].narrow_again();
     }
     return s;
   }
-  __device__ __forceinline__ void write(T* dS, float c, float off, float f) {
+  __device__ __forceinline__ void write(T* dS, float c, float top, float f) {
 #pragma unroll
     for (int i = 0; i < P; ++i)
       if (i * THREADS + tid < pieces) {
         float o[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = exp_of(x[i].get(e), c, off) * f;
+        for (int e = 0; e < E; ++e) o[e] = exp_of(x[i].get(e), c, top) * f;
         Piece<T> p;
         p.set(o);
         store16_once(dS + (i * THREADS + tid) * E, p.v);
       }
-    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, exp_of(last, c, off) * f);
+    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, exp_of(last, c, top) * f);
   }
   __device__ __forceinline__ void write_zero(T* dS) {
     Piece<T> p = {};
@@ -204,9 +208,9 @@ struct Row {
       slot = in / total;
     }
   }
-  // the gradient outside the slots over the exponential; 0 where the slots leave no class with a probability, NaN where there is none at all
+  // the gradient outside the slots over the lifted exponential; 0 where the slots leave no class with a probability, NaN where there is none at all
   __device__ __forceinline__ float factor(double g) const {
-    return es == 0.0 ? (total == 0.0 ? NAN : 0.f) : (float)(g * (q_rest - rest) / es);
+    return es == 0.0 ? (total == 0.0 ? NAN : 0.f) : (float)(g * UNLIFT * (q_rest - rest) / es);
   }
   __device__ __forceinline__ float loss(bool with_rest) const {
     const double lt = with_rest ? fmax(gap, 0.0) + log(total) : log(es) + gap;      // of the sum over all classes, less zs
@@ -257,7 +261,7 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
   const int64_t row = blockIdx.x;
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
   const double itau = 1.0 / a.tau;
-  const float c = (float)(LOG2E * itau);
+  const float c = per_tau(itau);
 
   Range<T, THREADS, P> x;
   x.load(S, a.V, tid);
@@ -281,16 +285,15 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     __syncthreads();
     x.drop(reinterpret_cast<const uint8_t*>(bits));
   }
-  const float top = group_max<W>(x.top(), red_m);
+  const float top = base_of(group_max<W>(x.top(), red_m));
   high = group_max<W>(high, red_t);
-  const float off = off_of(top, c);
-  double d[4] = {0.0, 0.0, 0.0, (double)x.sum(c, off)};
-  const double zr = (double)off * LN2, zh = high > -INFINITY ? (double)high * itau : REST ? zr : 0.0;
-  const double t0 = REST ? (double)a.lse[row] : zh, zs = REST ? zh : zr;
+  double d[4] = {0.0, 0.0, 0.0, (double)x.sum(c, top) * UNLIFT};
+  // (teacher: t / tau less its maximum, or less its log-sum-exp)
+  const double t0 = REST ? 0.0 : (double)base_of(high), tl = REST ? (double)a.lse[row] : 0.0, zs = REST && high > -INFINITY ? (double)high : (double)top;
   for (int k = tid; k < a.K; k += THREADS) {
     double p = 0.0, ez = 0.0;
     if (si[k] >= 0) {
-      const double t = sp[k] * itau - t0, z = se[k] * itau - zs;
+      const double t = (sp[k] - t0) * itau - tl, z = (se[k] - zs) * itau;
       p = exp(t);
       ez = exp(z);
       if (p != 0.0) d[0] += p * (t - z);
@@ -301,12 +304,12 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     se[k] = ez;
   }
   group_sums<W, 4>(d, red_d);
-  const Row r(d[0], d[1], d[2], d[3], zr - zs, REST);
+  const Row r(d[0], d[1], d[2], d[3], ((double)top - zs) * itau, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
     if (r.live) {
-      x.write(dS, c, off, r.factor(g));
+      x.write(dS, c, top, r.factor(g));
       __syncthreads();
       const double ge = g * r.slot, gp = REST ? g : g / r.B;
       for (int k = tid; k < a.K; k += THREADS)
@@ -335,7 +338,7 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
   const int chunk = (int)(blockIdx.x % a.chunks), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
   const double itau = 1.0 / a.tau;
-  const float c = (float)(LOG2E * itau);
+  const float c = per_tau(itau);
   Range<T, CH_THREADS, CH_P> x;
   x.load(S + c0, n, tid);
   if constexpr (REST) {
@@ -351,8 +354,7 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
     x.drop(reinterpret_cast<const uint8_t*>(bits));
   }
   const float top = group_max<W>(x.top(), red_m);
-  // (a chunk of masked logits alone: a sum of zero, not of NaN)
-  double e[1] = {(double)x.sum(c, off_of(top, c))};
+  double e[1] = {(double)x.sum(c, base_of(top)) * UNLIFT};
   group_sums<W, 1>(e, red_e);
   if (tid == 0) a.part[row * a.chunks + chunk] = make_float2(top, (float)e[0]);
   if (chunk != 0) return;
@@ -366,13 +368,12 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
   }
   t_top = group_max<W>(t_top, red_t);
   z_top = group_max<W>(z_top, red_z);
-  const double t0 = REST ? (double)a.lse[row] : (t_top > -INFINITY ? (double)t_top * itau : 0.0);
-  const double zs = z_top > -INFINITY ? (double)z_top * itau : 0.0;
+  const double t0 = REST ? 0.0 : (double)base_of(t_top), tl = REST ? (double)a.lse[row] : 0.0, zs = (double)base_of(z_top);
   double d[3] = {0.0, 0.0, 0.0};
   for (int k = tid; k < a.K; k += CH_THREADS) {
     const int cls = class_of(a, row * a.ldk + k);
     if (cls >= 0) {
-      const double t = (double)teacher_of(a, row * a.ldk + k) * itau - t0, z = (double)value<T>(S, cls) * itau - zs, p = exp(t);
+      const double t = ((double)teacher_of(a, row * a.ldk + k) - t0) * itau - tl, z = ((double)value<T>(S, cls) - zs) * itau, p = exp(t);
       if (p != 0.0) d[0] += p * (t - z);
       d[1] += p;
       if constexpr (REST) d[2] += exp(z);
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
     s[0] = d[0];
     s[1] = d[1];
     s[2] = d[2];
-    s[3] = z_top > -INFINITY ? zs : -INFINITY;
+    s[3] = (double)z_top;
     s[4] = t0;
   }
 }
@@ -399,24 +400,23 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
   const int chunk = (int)(blockIdx.x % per_row), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
   const double itau = 1.0 / a.tau;
-  const float c = (float)(LOG2E * itau);
+  const float c = per_tau(itau);
   Range<T, CH_THREADS, CH_P> x;
   if constexpr (GRAD) x.load(S + c0, n, tid);
   const float2* part = a.part + row * a.chunks;
   float top = -INFINITY;
   for (int i = lane; i < a.chunks; i += 64) top = fmaxf(top, part[i].x);
-  top = wave_max_f32(top);
-  const float off = off_of(top, c);
+  top = base_of(wave_max_f32(top));
   double es = 0.0;
   for (int i = lane; i < a.chunks; i += 64) {
     const float2 v = part[i];
     // (that of a chunk without a maximum is 0 or NaN)
-    es += v.x == -INFINITY ? (double)v.y : (double)v.y * exp(((double)off_of(v.x, c) - (double)off) * LN2);
+    es += v.x == -INFINITY ? (double)v.y : (double)v.y * exp(((double)v.x - (double)top) * itau);
   }
   es = wave_sum(es);
   const double* s = a.slots + row * 5;
-  const double zr = (double)off * LN2, zs = s[3] > -INFINITY ? s[3] : zr, t0 = s[4];
-  const Row r(s[0], s[1], s[2], es, zr - zs, REST);
+  const double zs = s[3] > -INFINITY ? s[3] : (double)top, t0 = s[4], tl = REST ? (double)a.lse[row] : 0.0;
+  const Row r(s[0], s[1], s[2], es, ((double)top - zs) * itau, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
@@ -425,15 +425,15 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
       extern __shared__ __align__(16) char smem_dl[];
       float* sv = reinterpret_cast<float*>(smem_dl);
       int* si = reinterpret_cast<int*>(sv + a.K);
-      const double ge = g * r.slot, gp = REST ? g : g / r.B, zb = REST ? zs : zr;
+      const double ge = g * r.slot, gp = REST ? g : g / r.B, zb = REST ? zs : (double)top;
       for (int k = tid; k < a.K; k += CH_THREADS) {
         const int cls = class_of(a, row * a.ldk + k), at = cls - c0;
         si[k] = cls >= 0 && at >= 0 && at < n ? at : -1;
         if (si[k] >= 0)
-          sv[k] = (float)(exp((double)value<T>(S, cls) * itau - zb) * ge - exp((double)teacher_of(a, row * a.ldk + k) * itau - t0) * gp);
+          sv[k] = (float)(exp(((double)value<T>(S, cls) - zb) * itau) * ge - exp(((double)teacher_of(a, row * a.ldk + k) - t0) * itau - tl) * gp);
       }
       __syncthreads();
-      x.write(dS + c0, c, off, r.factor(g));
+      x.write(dS + c0, c, top, r.factor(g));
       __syncthreads();
       for (int k = tid; k < a.K; k += CH_THREADS)
         if (si[k] >= 0) put<T>(dS, c0 + si[k], sv[k]);

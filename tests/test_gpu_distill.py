@@ -339,3 +339,28 @@ def test_slots_far_above_a_rest(slim, V, dtype, gap, tau):
     used = index >= 0
     lse = (torch.logsumexp(torch.where(used, t.double() / tau, -math.inf), 1) - math.log(0.9)).float()       # a rest of about a tenth
     check_shifted(slim, S, index, t, dloss + 0.1, tau, lse)
+    check_shifted(slim, S, index, t, dloss + 0.1, tau, None)
+
+
+@pytest.mark.parametrize("V,dtype", LONG)
+@pytest.mark.parametrize("lse", [False, True])
+def test_rows_of_nothing_but_the_types_lowest_value(slim, V, dtype, lse):
+    """A mask of the type's lowest value over the whole row, over all slots, over all others, over whole chunks: finite logits, and a softmax
+    among them."""
+    low = torch.finfo(dtype).min
+    S, index, t, dloss, l = data(5, V, 9, dtype, 22, 2.0, lse, empty=False)
+    S[0] = low
+    S[1].scatter_(0, index[1], low)
+    S[2] = torch.full((V,), low, dtype=dtype).scatter(0, index[2], S[2, index[2]])
+    S[3, : V // 2] = low
+    S[4] = torch.finfo(dtype).max
+    check_shifted(slim, S, index, t, dloss + 0.1, 2.0, l)
+
+
+@pytest.mark.parametrize("V,dtype", [(777, torch.float32), (3000, torch.float16), (50257, torch.float32)])
+@pytest.mark.parametrize("lse", [False, True])
+@pytest.mark.parametrize("shift", [-30000.0, -1000.0, 1000.0, 10000.0])
+def test_logits_may_be_shifted(slim, V, dtype, lse, shift):
+    """A number added to all logits of a row changes nothing but their own rounding."""
+    S, index, t, dloss, l = data(5, V, 9, dtype, 23, 0.7, lse, empty=False)
+    check_shifted(slim, (S.float() + shift).to(dtype), index, t, dloss + 0.1, 0.7, l)
