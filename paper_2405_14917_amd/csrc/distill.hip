@@ -465,6 +465,16 @@ size_t need(int64_t rows, int V, slim_dtype d) {
   return chunks ? part_bytes(rows, chunks) + slot_bytes(rows) : 0;
 }
 
+// Threads of a row in one workgroup.  Eight pieces per thread up to 2048 pieces: of 4000 x 3000 bf16 one wavefront a row takes 19.9 us, four
+// 24.9; 2048 x 12000 with four 26.6 us, with eight 38.0.  Beyond, many rows: four wavefronts of 16 pieces (2048 x 32000 bf16 61.5 us against
+// 66.8 with eight of 8, 2048 x 16000 fp32 54.9 against 62.6); few rows, which take a round or two: eight of 8 (400 x 32000 16.8 us against
+// 18.3).
+int threads_of(int pieces, int64_t rows, bool grad, int ncu) {
+  if (pieces <= 512) return 64;
+  if (pieces <= 1024) return 128;
+  return pieces <= 2048 || (grad && rows > 6 * ncu) ? 256 : 512;
+}
+
 template <typename T, bool REST, bool GRAD>
 slim_status by_size(slim_ctx* ctx, DistillArgs a, int64_t rows) {
   constexpr int E = Piece<T>::E;
@@ -479,14 +489,14 @@ slim_status by_size(slim_ctx* ctx, DistillArgs a, int64_t rows) {
                 dim3(GRAD ? CH_THREADS : 64), GRAD ? (size_t)a.K * 8 : 0, a);
     return SLIM_OK;
   }
-  // Eight pieces per thread up to 2048 pieces: of 4000 x 3000 bf16 one wavefront a row takes 19.9 us, four 24.9; 2048 x 12000 with four
-  // 26.6 us, with eight 38.0.  Beyond, many rows: four wavefronts of 16 pieces (2048 x 32000 bf16 61.5 us against 66.8 with eight of 8,
-  // 2048 x 16000 fp32 54.9 against 62.6); few rows, which take a round or two: eight of 8 (400 x 32000 16.8 us against 18.3).
-  if (pieces <= 512) return launch<T, 64, 8, REST, GRAD>(ctx, a, rows);
-  if (pieces <= 1024) return launch<T, 128, 8, REST, GRAD>(ctx, a, rows);
-  if (pieces <= 2048) return launch<T, 256, 8, REST, GRAD>(ctx, a, rows);
-  if (GRAD && rows > 6 * ctx->num_cus) return launch<T, 256, 16, REST, GRAD>(ctx, a, rows);
-  return launch<T, 512, 8, REST, GRAD>(ctx, a, rows);
+  switch (threads_of(pieces, rows, GRAD, ctx->num_cus)) {
+    case 64: return launch<T, 64, 8, REST, GRAD>(ctx, a, rows);
+    case 128: return launch<T, 128, 8, REST, GRAD>(ctx, a, rows);
+    case 512: return launch<T, 512, 8, REST, GRAD>(ctx, a, rows);
+  }
+  if constexpr (GRAD)
+    if (pieces > 2048) return launch<T, 256, 16, REST, GRAD>(ctx, a, rows);
+  return launch<T, 256, 8, REST, GRAD>(ctx, a, rows);
 }
 
 template <typename T>
@@ -500,7 +510,9 @@ slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype
   if (!is_float(s_dtype) || !is_float(t_dtype)) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: logits are F16, BF16 or F32", fn);
   SLIM_REQUIRE(ctx, rows >= 0 && a.V > 0 && a.V < (1 << 30) && a.K >= 0, "%s: rows = %lld, V = %d, K = %d", fn, (long long)rows, a.V, a.K);
   if (a.K > DL_MAX_K) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: up to %d slots a row, got %d", fn, DL_MAX_K, a.K);
-  if (rows * std::max(1, chunks_of(a.V, s_dtype)) >= (1ll << 31) || rows >= (1ll << 31))
+  // (a launch has fewer than 2^32 threads)
+  const int chunks = chunks_of(a.V, s_dtype), threads = threads_of(a.V / (s_dtype == SLIM_F32 ? 4 : 8), rows, grad, ctx->num_cus);
+  if (rows >= (1ll << 31) || rows * (chunks ? (int64_t)chunks * CH_THREADS : threads) >= (1ll << 32))
     return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: %lld rows of %d classes are too many for one call", fn, (long long)rows, a.V);
   SLIM_REQUIRE(ctx, a.tau > 0.0 && a.tau <= 1e30, "%s: tau = %g", fn, a.tau);
   if (rows == 0) return SLIM_OK;

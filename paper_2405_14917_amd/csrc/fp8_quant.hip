@@ -234,6 +234,8 @@ slim_status quantize(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const 
   if (count == 1 && !a->cols_q) {
     const int units = slim_cdiv(a->cols, 512);
     const int64_t waves = ((int64_t)a->rows * units + RQ_UNITS - 1) / RQ_UNITS;
+    if (waves > (1ll << 26) - 4)                                // (a launch has fewer than 2^32 threads)
+      return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: %d rows of %d channels are too many for one call", name, a->rows, a->cols);
     const dim3 grid(slim_cdiv(waves, RQ_THREADS / 64));
     if (x_dtype == SLIM_F16)
       SLIM_LAUNCH(ctx, name, fp8_rows<__half>, grid, dim3(RQ_THREADS), 0, static_cast<const __half*>(a->X), a->ldx, a->rows, a->cols, units,

@@ -229,3 +229,52 @@ def test_head_tuning_asks_for_the_largest_workspace(binding):
     whole = tuning.workspace_query(32000, 4096, 2048)
     assert whole >= max(binding.fp8_linear_workspace(32000, 4096, 2048), binding.layer_norm_backward_workspace(2048, 4096),
                         binding.fp8_linear_backward_workspace(32000, 4096, 2048, dw_dtype=torch.float32))
+
+
+# the same stand-ins, which count launches and those that are too large
+SIZES = PROGRAM[:PROGRAM.index("int main() {")].replace("static int launches;", "static int launches, calls, large;").replace(
+    "hipError_t __hipPushCallConfiguration(dim3, dim3, size_t, hipStream_t) { return hipSuccess; }",
+    """hipError_t __hipPushCallConfiguration(dim3 g, dim3 b, size_t, hipStream_t) {
+  ++calls;
+  large += (uint64_t)g.x * b.x >> 32 != 0 || (uint64_t)g.y * b.y >> 32 != 0;
+  return hipSuccess;
+}""") + r"""
+int main() {
+  slim_ctx c;
+  c.num_cus = 256;
+  c.ws_bytes = SIZE_MAX;           // (nothing is written: no launch runs)
+  c.ws_external = true;
+  alignas(64) static char buf[64];
+  c.ws = buf;
+  void* p = buf;
+  float* f = reinterpret_cast<float*>(buf);
+  uint8_t* u = reinterpret_cast<uint8_t*>(buf);
+  auto told = [&](int st) { printf("%d %d %d\n", st, calls, large); calls = large = 0; };
+  for (int64_t rows : {(1ll << 26) - 1, 1ll << 26}) told(slim_distill_loss(&c, p, SLIM_BF16, rows, 1000, 1000, p, 1, p, SLIM_F32, 5, 5, f, 1.0, f));
+  for (int64_t rows : {(1ll << 23) - 1, 1ll << 23}) told(slim_distill_loss(&c, p, SLIM_BF16, rows, 32000, 32000, p, 1, p, SLIM_F32, 5, 5, f, 1.0, f));
+  for (int64_t rows : {(1ll << 24) - 1, 1ll << 24})
+    told(slim_distill_loss_grad(&c, p, SLIM_BF16, rows, 32000, 32000, p, 1, p, SLIM_F32, 5, 5, f, 1.0, f, f, p, 32000));
+  for (int64_t rows : {(1ll << 20) - 1, 1ll << 20})
+    told(slim_distill_loss_grad(&c, p, SLIM_BF16, rows, 131072, 131072, p, 1, p, SLIM_F32, 5, 5, f, 1.0, f, f, p, 131072));
+  for (int t : {(1 << 23) - 1, 1 << 23}) told(slim_fp8_linear(&c, p, SLIM_BF16, t, 8192, u, 8192, u, 64, 128, 8192, p, SLIM_BF16, 128));
+  return 0;
+}
+"""
+
+
+def test_calls_too_large_for_a_launch_are_refused(tmp_path):
+    """A launch has fewer than 2^32 threads: what would need more is refused with nothing launched, the size below it is not."""
+    src, exe = tmp_path / "t.hip", tmp_path / "t"
+    src.write_text(SIZES)
+    jobs, objs = [], []
+    for f in [str(src)] + [os.path.join(build.CSRC, f) for f in build.SOURCES if f.startswith(("ctx", "fp8_", "distill"))]:
+        objs.append(str(tmp_path / (os.path.basename(f) + ".o")))
+        jobs.append(subprocess.Popen([build.hipcc(), "--offload-host-only", "-O0", "-fPIC", "-std=c++17", "-I" + build.INCLUDE, "-I" + build.CSRC, "-c", f,
+                                      "-o", objs[-1]], stderr=subprocess.DEVNULL))
+    assert not any(j.wait() for j in jobs)
+    subprocess.run(["g++", *objs, "-o", str(exe), "-pthread", "-Wl,--unresolved-symbols=ignore-in-object-files"], check=True)
+    out = [tuple(map(int, line.split())) for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]]
+    assert len(out) == 10
+    for fits, over in zip(out[::2], out[1::2]):
+        assert fits[0] == 0 and fits[1] > 0 and fits[2] == 0, out
+        assert over == (-5, 0, 0), out
