@@ -374,6 +374,7 @@ slim_status slim_dequant_matmul_noalloc(slim_ctx* ctx, const uint32_t* packed, i
  *  - rows may have any length, leading dimension and alignment of their type (only the stored 8-bit form asks for more, below);
  *  - a call enqueues its work and returns: no waits, no allocation once the workspace is large enough (a context that works under graph
  *    capture is created with its workspace: a call that has to grow the context's own one cannot be captured);
+ *  - the size that a query of workspace gives is enough for any smaller number of tokens or rows too;
  *  - zero tokens or rows are valid: outputs without rows are not touched, sums over no rows are zero.
  *
  * The 8-bit linear layer.  Quantiser Q: a block of 128 numbers with the largest finite magnitude a gets the scale s, the smallest power of

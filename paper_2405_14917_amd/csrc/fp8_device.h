@@ -140,7 +140,7 @@ struct Product {
   slim_dtype c_dtype;
   int nk;
 };
-// bytes of workspace of a set of products (they share one launch); 256-byte multiples
+// bytes of workspace of a set of products, enough too for those of fewer rows and shorter contractions; 256-byte multiples
 size_t gemm_workspace(const Product* p, int count, int num_cus);
 slim_status gemm(slim_ctx* ctx, const char* name, const Product* p, int count);
 

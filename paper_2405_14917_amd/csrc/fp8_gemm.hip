@@ -399,7 +399,6 @@ typedef Tile<64, 64, 2, 2, 4> Small;
 struct Plan {
   int splits[2];
   int64_t ldp[2];
-  size_t bytes;
 };
 constexpr int TILE_A[] = {Large::TA, Medium::TA, Small::TA}, TILE_B[] = {Large::TB, Medium::TB, Small::TB};
 
@@ -442,11 +441,19 @@ int in_one_launch(const Product* p, int count, int ncu) {
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
   for (int i = 0; i < count; ++i) {
-    const int s = pl.splits[i] = parts_of(tiles_of(p[i], tile_of(p[i], ncu)), p[i].nk, ncu);
+    pl.splits[i] = parts_of(tiles_of(p[i], tile_of(p[i], ncu)), p[i].nk, ncu);
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
-    if (s > 1) pl.bytes += slim_ws_round(sizeof(float) * (size_t)s * pl.ldp[i] * p[i].b.rows);
   }
   return pl;
+}
+
+// Bytes that a product's parts take at most, and those of one of fewer rows or a shorter contraction: with more than one part the tiles times
+// the parts are no more than the CUs (so the parts hold no more than a large tile for each), and the parts no more than an eighth of the
+// steps.  What the parts of the very product take is no bound for fewer tokens: they vanish once the tiles fill the chip (32000 x 4096: 34 MB
+// at 768 tokens, none at 769).
+size_t parts_bytes(const Product& p, int ncu) {
+  const int64_t most = std::min(ncu, p.nk / 8), ldp = (p.a.rows + 3) / 4 * 4;
+  return most < 2 ? 0 : slim_ws_round(sizeof(float) * (size_t)std::min((int64_t)ncu * Large::TA * Large::TB, most * ldp * p.b.rows));
 }
 
 template <typename T, bool EXACT>
@@ -512,7 +519,7 @@ namespace slimfp8 {
 
 size_t gemm_workspace(const Product* p, int count, int num_cus) {
   size_t bytes = 0;
-  for (int i = 0, c = in_one_launch(p, count, num_cus); i < count; i += c) bytes += make_plan(p + i, c, num_cus).bytes;
+  for (int i = 0; i < count; ++i) bytes += parts_bytes(p[i], num_cus);
   return bytes;
 }
 

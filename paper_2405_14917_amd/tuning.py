@@ -13,10 +13,10 @@ from . import binding
 def workspace_query(vocabulary: int, width: int, tokens: int, dtype: torch.dtype = torch.bfloat16, bias: bool = True,
                     head_grad: bool = True, num_cus: int = 0) -> int:
     """Bytes of workspace of a HeadTuning with up to `tokens` tokens a call, for a context under graph capture."""
-    return max(max(binding.fp8_linear_workspace(vocabulary, width, t, dtype, num_cus),
-                   binding.fp8_linear_backward_workspace(vocabulary, width, t, True, head_grad, torch.float32, num_cus),
-                   binding.layer_norm_backward_workspace(t, width, bias, dtype, num_cus),
-                   binding.distill_workspace(t, vocabulary, dtype)) for t in {tokens, min(tokens, 17)})
+    return max(binding.fp8_linear_workspace(vocabulary, width, tokens, dtype, num_cus),
+               binding.fp8_linear_backward_workspace(vocabulary, width, tokens, True, head_grad, torch.float32, num_cus),
+               binding.layer_norm_backward_workspace(tokens, width, bias, dtype, num_cus),
+               binding.distill_workspace(tokens, vocabulary, dtype))          # (each of them is enough for fewer tokens too)
 
 
 class HeadTuning:

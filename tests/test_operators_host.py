@@ -278,3 +278,65 @@ def test_calls_too_large_for_a_launch_are_refused(tmp_path):
     for fits, over in zip(out[::2], out[1::2]):
         assert fits[0] == 0 and fits[1] > 0 and fits[2] == 0, out
         assert over == (-5, 0, 0), out
+
+
+@pytest.mark.parametrize("V,m,tokens", [(32000, 4096, 769), (32000, 4096, 1024), (50257, 8192, 513), (1003, 384, 300), (128, 20000, 2000), (4096, 11008, 2500)])
+@pytest.mark.parametrize("head_grad", [False, True])
+def test_a_workspace_is_enough_for_fewer_tokens(binding, V, m, tokens, head_grad):
+    """What the queries give for a number of tokens covers every smaller one: of each entry point, and of the step that calls them."""
+    from paper_2405_14917_amd import tuning
+    bf16, f32 = torch.bfloat16, torch.float32
+    needs = lambda t: (binding.fp8_linear_workspace(V, m, t, bf16, 256), binding.fp8_linear_workspace(V, m, t, f32, 256),
+                       binding.fp8_linear_backward_workspace(V, m, t, True, head_grad, f32, 256),
+                       binding.fp8_linear_backward_workspace(V, m, t, True, head_grad, bf16, 256),
+                       binding.layer_norm_backward_workspace(t, m, True, bf16, 256), binding.distill_workspace(t, V, bf16))
+    whole, query = needs(tokens), tuning.workspace_query(V, m, tokens, bf16, True, head_grad, 256)
+    for t in range(1, tokens + 1):
+        now = needs(t)
+        assert all(a <= b for a, b in zip(now, whole)), (t, now, whole)
+        assert query >= max(now[0], now[2], now[4], now[5]), t
+
+
+ENOUGH = SIZES[:SIZES.index("int main() {")] + r"""
+#include <random>
+int main() {
+  slim_ctx c;
+  c.num_cus = 256;
+  c.ws_external = true;
+  alignas(256) static char buf[64];
+  c.ws = buf;                      // (nothing is written: no launch runs)
+  void* p = buf;
+  uint8_t* u = reinterpret_cast<uint8_t*>(buf);
+  std::mt19937 g(1);
+  auto size = [&](int hi) { return (int)std::exp(std::uniform_real_distribution<double>(0.0, std::log((double)hi))(g)); };
+  int bad = 0, parts = 0;
+  for (int i = 0; i < 40000; ++i) {
+    const int n = size(30000), m = size(30000), t = size(i % 2 ? 3000 : 30000), x = i % 3, w = i / 3 % 3;
+    const int64_t ld = 1 << 15;
+    const slim_dtype d = i % 4 < 2 ? SLIM_F32 : SLIM_BF16;
+    c.ws_bytes = slim_fp8_linear_workspace(n, m, t, d, 256);
+    calls = 0;
+    bad += slim_fp8_linear(&c, p, SLIM_BF16, t, ld, u, ld, u, 256, n, m, p, d, ld) != 0;
+    parts += calls > 2;
+    c.ws_bytes = slim_fp8_linear_backward_workspace(n, m, t, x != 0, w != 0 || x == 0, d, 256);
+    bad += slim_fp8_linear_backward(&c, p, p, SLIM_BF16, t, ld, ld, u, ld, u, 256, n, m, x != 0 ? p : nullptr, ld, w != 0 || x == 0 ? p : nullptr, d, ld) != 0;
+  }
+  printf("%d %d\n", bad, parts);
+  return 0;
+}
+"""
+
+
+def test_the_queried_workspace_holds_every_shapes_parts(tmp_path):
+    """40000 shapes of the forward and the backward pass in a workspace of exactly the queried size."""
+    src, exe = tmp_path / "t.hip", tmp_path / "t"
+    src.write_text("#include <cmath>\n" + ENOUGH)
+    jobs, objs = [], []
+    for f in [str(src)] + [os.path.join(build.CSRC, f) for f in build.SOURCES if f.startswith(("ctx", "fp8_"))]:
+        objs.append(str(tmp_path / (os.path.basename(f) + ".o")))
+        jobs.append(subprocess.Popen([build.hipcc(), "--offload-host-only", "-O1", "-fPIC", "-std=c++17", "-I" + build.INCLUDE, "-I" + build.CSRC, "-c", f,
+                                      "-o", objs[-1]], stderr=subprocess.DEVNULL))
+    assert not any(j.wait() for j in jobs)
+    subprocess.run(["g++", *objs, "-o", str(exe), "-pthread", "-Wl,--unresolved-symbols=ignore-in-object-files"], check=True)
+    bad, parts = map(int, subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split())
+    assert bad == 0 and parts > 1000, (bad, parts)
