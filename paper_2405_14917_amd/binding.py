@@ -246,6 +246,17 @@ def _stored_strides(q: torch.Tensor, s: torch.Tensor, what: str):
     return ldq, lds
 
 
+def _stored_out(out, n: int, m: int, transposed: bool):
+    """Stored weights given to be written over, checked: (q, s, qt, st), the last two None without `transposed`."""
+    if len(out) != (4 if transposed else 2):
+        raise ValueError("out has to be the %d tensors of an earlier call" % (4 if transposed else 2))
+    for q, s, shape in ((out[0], out[1], (n, m)),) + (((out[2], out[3], (m, n)),) if transposed else ()):
+        _stored_strides(q, s, "out")
+        if q.shape != shape:
+            raise ValueError("out holds weights of %d x %d, got %d x %d" % (*q.shape, *shape))
+    return (*out, None, None)[:4]
+
+
 def _need_cuda(*tensors):
     for t in tensors:
         if t is None:
@@ -527,10 +538,13 @@ class Slim:
         if _current_stream(index) != self._raw_stream:
             raise ValueError("the context is bound to another stream than the current one")
 
-    def fp8_quantize_weights(self, W: torch.Tensor, transposed: bool = True):
+    def fp8_quantize_weights(self, W: torch.Tensor, transposed: bool = True, out=None):
         """W (n, m) float16 / bfloat16 / float32 as stored 8-bit weights: (q float8_e4m3fn (n, m), s uint8 (n / 128, m / 128 rounded up)),
-        and with `transposed` also those of W^T, which the backward pass reads.  Rows are padded: keep the tensors as they are."""
-        self._ready(W)
+        and with `transposed` also those of W^T, which the backward pass reads.  Rows are padded: keep the tensors as they are.  `out`: the
+        tensors of an earlier call for weights of this shape, to be written over (what a captured graph reads has to stay in its place)."""
+        self._ready(W, *(out or ()))
+        if W.dim() != 2:
+            raise ValueError("W has to be a matrix")
         n, m = W.shape
         nb, mb = (n + 127) // 128, (m + 127) // 128
 
@@ -539,8 +553,11 @@ class Slim:
             q = torch.zeros((rows, (cb | 1) * 128), dtype=torch.uint8, device=W.device).view(_E4M3)[:, :cols]
             return q, torch.zeros((rb, (cb + 3) // 4 * 4), dtype=torch.uint8, device=W.device)[:, :cb]
 
-        q, s = stored(n, m, nb, mb)
-        qt, st = stored(m, n, mb, nb) if transposed else (None, None)
+        if out is not None:
+            q, s, qt, st = _stored_out(out, n, m, transposed)
+        else:
+            q, s = stored(n, m, nb, mb)
+            qt, st = stored(m, n, mb, nb) if transposed else (None, None)
         self._check(self.lib.slim_fp8_quantize_weights(self.ctx, W.data_ptr(), _dtype(W), n, m, _row_stride(W, "W"), q.data_ptr(), q.stride(0),
                                                        s.data_ptr(), s.stride(0), _ptr(qt), qt.stride(0) if transposed else 0, _ptr(st),
                                                        st.stride(0) if transposed else 0))

@@ -20,16 +20,17 @@ def workspace_query(vocabulary: int, width: int, tokens: int, dtype: torch.dtype
 
 
 class HeadTuning:
-    """Norm (weight, bias or None; without the mean with `rms`) and 8-bit head W (vocabulary x width, 16 bits or fp32) on hidden states."""
+    """Norm (weight, bias or None; without the mean with `rms`) and 8-bit head W (vocabulary x width, 16 bits or fp32) on hidden states.
+    Where a call is captured into a graph, change weight and bias in place between the replays; store() does so with the head."""
 
     def __init__(self, slim: binding.Slim, W: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                  rms: bool = False, tau: float = 1.0):
         self.slim, self.weight, self.bias, self.eps, self.rms, self.tau = slim, weight, bias, eps, rms, tau
-        self.store(W)
+        self.q, self.s, self.qt, self.st = slim.fp8_quantize_weights(W)
 
     def store(self, W: torch.Tensor):
-        """Takes (new) weights of the head into the stored 8-bit form."""
-        self.q, self.s, self.qt, self.st = self.slim.fp8_quantize_weights(W)
+        """Takes new weights of the head, of the same shape, into the stored 8-bit form: in its place, where a captured graph reads it."""
+        self.slim.fp8_quantize_weights(W, out=(self.q, self.s, self.qt, self.st))
 
     def logits(self, X: torch.Tensor) -> torch.Tensor:
         """Serving: the logits of hidden states X (t, width), one token or many."""

@@ -78,3 +78,46 @@ def test_captured_into_a_graph(t):
     torch.cuda.synchronize()
     slim.close()
     eager.slim.close()
+
+
+@pytest.mark.parametrize("t", [16, 200])
+def test_new_weights_between_replays(t):
+    """Captured gradients, an update of the head, other allocations, a replay: the loop of a tuning step."""
+    from paper_2405_14917_amd import binding, tuning
+    V, m = 1003, 384
+    W, X, w, b, index, teacher, lse = problem(t, V, m, torch.bfloat16)
+    ncu = torch.cuda.get_device_properties(0).multi_processor_count
+    dloss = torch.full((t,), 1.0 / t, device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        slim = binding.Slim("cuda:0", workspace_bytes=tuning.workspace_query(V, m, t, num_cus=ncu))
+        head = tuning.HeadTuning(slim, W, w, b)
+        head.gradients(X, index, teacher, dloss, lse)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        loss, g = head.gradients(X, index, teacher, dloss, lse)
+    place = [v.data_ptr() for v in (head.q, head.s, head.qt, head.st)]
+    for seed in range(1, 5):
+        W2 = problem(1, V, m, torch.bfloat16, seed)[0]
+        with torch.cuda.stream(stream):
+            head.store(W2)
+        stream.synchronize()
+        assert [v.data_ptr() for v in (head.q, head.s, head.qt, head.st)] == place
+        other = tuning.HeadTuning(binding.Slim("cuda:0"), W2, w, b)
+        want, gw = other.gradients(X, index, teacher, dloss, lse)
+        junk = [torch.full_like(v.view(torch.uint8), 0x7f) for v in (head.q, head.qt, other.q, other.qt)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want)
+        for k in gw:
+            assert torch.equal(g[k], gw[k]), k
+        other.slim.close()
+        del junk
+    with torch.cuda.stream(stream), pytest.raises(ValueError):
+        head.store(W[:1000])
+    del graph
+    torch.cuda.synchronize()
+    slim.close()

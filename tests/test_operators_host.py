@@ -340,3 +340,32 @@ def test_the_queried_workspace_holds_every_shapes_parts(tmp_path):
     subprocess.run(["g++", *objs, "-o", str(exe), "-pthread", "-Wl,--unresolved-symbols=ignore-in-object-files"], check=True)
     bad, parts = map(int, subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split())
     assert bad == 0 and parts > 1000, (bad, parts)
+
+
+def test_a_heads_new_weights_take_the_place_of_the_old(binding):
+    """A captured step reads the stored weights where they were: store() writes there, and takes no weights of another shape."""
+    from paper_2405_14917_amd import tuning
+
+    class Recorder:
+        """Stands in for the library: what it allocates and where it is told to write."""
+        def fp8_quantize_weights(self, W, transposed=True, out=None):
+            n, m = W.shape
+            if out is not None:
+                return binding._stored_out(out, n, m, transposed)[: 4 if transposed else 2]
+            q = lambda r, c: torch.zeros((r, (c + 127) // 128 * 128), dtype=torch.uint8).view(torch.float8_e4m3fn)[:, :c]
+            s = lambda r, c: torch.zeros(((r + 127) // 128, (c + 511) // 512 * 4), dtype=torch.uint8)[:, : (c + 127) // 128]
+            return q(n, m), s(n, m), q(m, n), s(m, n)
+
+    head = tuning.HeadTuning(Recorder(), torch.zeros(300, 200), torch.ones(200))
+    place = lambda: [t.data_ptr() for t in (head.q, head.s, head.qt, head.st)]
+    before = place()
+    head.store(torch.ones(300, 200))
+    assert place() == before
+    for W in (torch.zeros(300, 199), torch.zeros(301, 200), torch.zeros(200, 300)):
+        with pytest.raises(ValueError):
+            head.store(W)
+    out = head.q, head.s, head.qt, head.st
+    for bad in (out[:2], out[:3], (head.qt, head.st, head.q, head.s), (head.q.view(torch.uint8), *out[1:])):
+        with pytest.raises(ValueError):
+            binding._stored_out(bad, 300, 200, True)
+    assert binding._stored_out(out[:2], 300, 200, False)[2:] == (None, None)
