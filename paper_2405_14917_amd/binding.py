@@ -257,6 +257,14 @@ def _stored_out(out, n: int, m: int, transposed: bool):
     return (*out, None, None)[:4]
 
 
+def _no_graph(*tensors):
+    """Raises where autograd would expect a recorded call: these calls record none, and their outputs would silently carry no gradient."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("libslim records no graph: a tensor that requires a gradient is taken under torch.no_grad(), or detached")
+
+
 def _need_cuda(*tensors):
     for t in tensors:
         if t is None:
@@ -564,7 +572,9 @@ class Slim:
         return (q, s, qt, st) if transposed else (q, s)
 
     def fp8_linear(self, X: torch.Tensor, W: torch.Tensor, Ws: torch.Tensor, dtype: Optional[torch.dtype] = None):
-        """Y (t, n) = Q(X) W^T for X (t, m) float16 / bfloat16 and stored 8-bit weights W, Ws; `dtype`: of Y (default: X's)."""
+        """Y (t, n) = Q(X) W^T for X (t, m) float16 / bfloat16 and stored 8-bit weights W, Ws; `dtype`: of Y (default: X's).  Records no
+        graph: X that requires a gradient is refused outside torch.no_grad() (detach it, and call fp8_linear_backward)."""
+        _no_graph(X, W)
         self._ready(X, W, Ws)
         ldq, lds = _stored_strides(W, Ws, "W")
         n, m = W.shape
@@ -613,7 +623,10 @@ class Slim:
     def layer_norm(self, X: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor] = None, eps: float = 1e-5, rms: bool = False,
                    stats: bool = False):
         """Layer norm of the rows of X (rows, cols), without the mean with `rms`; w, b (cols,) of X's type or float32.  With `stats`
-        (Y, mean, rstd) for the backward pass (mean is None with `rms`)."""
+        (Y, mean, rstd) for the backward pass (mean is None with `rms`).  Records no graph: without `stats` tensors that require a gradient
+        are refused outside torch.no_grad()."""
+        if not stats:                        # (who asks for them calls layer_norm_backward)
+            _no_graph(X, w, b)
         self._ready(X, w, b)
         rows, cols = self._norm_shape(X, w, b)
         Y = _empty_like(X)
@@ -670,7 +683,9 @@ class Slim:
                 teacher.data_ptr(), _dtype(teacher), index.shape[1], ldk, None if lse is None else lse.data_ptr(), tau)
 
     def distill_loss(self, S: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, tau: float = 1.0, lse: Optional[torch.Tensor] = None):
-        """loss float32 (rows,): the divergence of softmax(S / tau) from the teacher's top logits (rows, K) of the classes `index`."""
+        """loss float32 (rows,): the divergence of softmax(S / tau) from the teacher's top logits (rows, K) of the classes `index`.  Records no
+        graph: S that requires a gradient is refused outside torch.no_grad() (distill_loss_grad gives it)."""
+        _no_graph(S, teacher)
         self._ready(S, index, teacher, lse)
         args = self._distill_args(S, index, teacher, tau, lse)
         loss = S.new_empty(args[3], dtype=torch.float32)

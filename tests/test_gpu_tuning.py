@@ -121,3 +121,25 @@ def test_new_weights_between_replays(t):
     del graph
     torch.cuda.synchronize()
     slim.close()
+
+
+def test_parameters():
+    """A norm's weight that requires a gradient: the step, whose gradients are its results, takes it; serving does under no_grad and refuses to lose the
+    gradient elsewhere."""
+    from paper_2405_14917_amd import binding, tuning
+    slim = binding.Slim("cuda:0")
+    W, X, w, b, index, teacher, lse = problem(5, 300, 256, torch.bfloat16)
+    dloss = torch.full((5,), 0.2, device="cuda")
+    plain = tuning.HeadTuning(slim, W, w, b)
+    head = tuning.HeadTuning(slim, torch.nn.Parameter(W), torch.nn.Parameter(w), torch.nn.Parameter(b))
+    loss, g = plain.gradients(X, index, teacher, dloss, lse)
+    loss2, g2 = head.gradients(X, index, teacher, dloss, lse)
+    assert torch.equal(loss, loss2) and all(torch.equal(g[k], g2[k]) for k in g)
+    with torch.no_grad():
+        assert torch.equal(head.validate(X, index, teacher, lse), loss)
+        head.store(torch.nn.Parameter(W))
+    for call in (lambda: head.logits(X), lambda: head.validate(X, index, teacher, lse), lambda: plain.logits(X.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="graph"):
+            call()
+    torch.cuda.synchronize()
+    slim.close()

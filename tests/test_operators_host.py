@@ -369,3 +369,20 @@ def test_a_heads_new_weights_take_the_place_of_the_old(binding):
         with pytest.raises(ValueError):
             binding._stored_out(bad, 300, 200, True)
     assert binding._stored_out(out[:2], 300, 200, False)[2:] == (None, None)
+
+
+def test_a_gradient_is_not_lost_silently(binding):
+    """Calls whose outputs carry no graph refuse inputs that require a gradient where autograd records, before anything else."""
+    slim = object.__new__(binding.Slim)                          # (no context: the check comes first)
+    slim.ctx = None
+    x, w = torch.ones(2, 8), torch.ones(8)
+    leaf = lambda t: t.clone().requires_grad_()
+    calls = [lambda: slim.layer_norm(leaf(x), w), lambda: slim.layer_norm(x, leaf(w)), lambda: slim.layer_norm(x, w, leaf(w)),
+             lambda: slim.fp8_linear(leaf(x), w, w), lambda: slim.distill_loss(leaf(x), w, x), lambda: slim.distill_loss(x, w, leaf(x) * 2)]
+    for call in calls:
+        with pytest.raises(ValueError, match="graph"):
+            call()
+    with torch.no_grad():
+        for t in (leaf(x), None):
+            binding._no_graph(t)
+    binding._no_graph(x, w, None)
