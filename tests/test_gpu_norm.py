@@ -256,3 +256,20 @@ def test_gradients_of_long_rows_may_take_the_place_of_inputs(slim, cols, x, rms,
                                                  p(mean), p(rstd), p(out), cols, p(dw2), p(db2)) == B.SLIM_OK
         assert torch.equal(out, dX), over
         assert torch.equal(dw2, dw) and (db is None or torch.equal(db2, db)), over
+
+
+@pytest.mark.parametrize("rows,cols,x", [(3001, 1501, torch.float32), (16384, 300, torch.bfloat16), (5000, 4096, torch.bfloat16), (700, 9000, torch.float32)])
+def test_column_sums_are_rounded_at_their_end(slim, rows, cols, x):
+    """Whole numbers whose sums over a workgroup's rows are exact in fp32 and over all rows are not: db is the exact sum, rounded once."""
+    g = torch.Generator().manual_seed(rows)
+    largest = 2 ** 17 if x == torch.float32 else 255                 # (all bits of the type)
+    dY = torch.randint(-largest, largest + 1, (rows, cols), generator=g).double()
+    if x == torch.bfloat16:
+        dY *= 2.0 ** torch.randint(0, 9, (rows, 1), generator=g)    # (17 bits over the rows)
+    dY += torch.where(dY > 0, largest, 0).double() * (x == torch.float32)      # sums that grow with the rows
+    assert torch.equal(dY.to(x).double(), dY)
+    X = torch.randn((rows, cols), generator=g).to(x)
+    w = torch.ones(cols)
+    _, mean, rstd = slim.layer_norm(X.cuda(), w.cuda(), stats=True)
+    db = slim.layer_norm_backward(dY.to(x).cuda(), X.cuda(), w.cuda(), mean, rstd, bias=True)[2]
+    assert torch.equal(db.cpu(), dY.sum(0).float())
