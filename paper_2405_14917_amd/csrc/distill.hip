@@ -466,13 +466,13 @@ size_t need(int64_t rows, int V, slim_dtype d) {
 }
 
 // Threads of a row in one workgroup.  Eight pieces per thread up to 2048 pieces: of 4000 x 3000 bf16 one wavefront a row takes 19.9 us, four
-// 24.9; 2048 x 12000 with four 26.6 us, with eight 38.0.  Beyond, many rows: four wavefronts of 16 pieces (2048 x 32000 bf16 61.5 us against
-// 66.8 with eight of 8, 2048 x 16000 fp32 54.9 against 62.6); few rows, which take a round or two: eight of 8 (400 x 32000 16.8 us against
-// 18.3).
+// 24.9; 2048 x 12000 with four 26.6 us, with eight 38.0.  Beyond, more than two rows per CU: four wavefronts of 16 pieces (2048 x 32000 bf16
+// 62.6 us against 66.1 with eight of 8, 2048 x 16000 fp32 56.1 and 60.8; 600 x 32000 22.0 and 22.5, 600 x 16000 16.3 and 19.4); fewer: eight of
+// 8 (400 x 32000 16.3 us against 17.7, 400 x 16000 12.3 and 13.5).
 int threads_of(int pieces, int64_t rows, bool grad, int ncu) {
   if (pieces <= 512) return 64;
   if (pieces <= 1024) return 128;
-  return pieces <= 2048 || (grad && rows > 6 * ncu) ? 256 : 512;
+  return pieces <= 2048 || (grad && rows > 2 * ncu) ? 256 : 512;
 }
 
 template <typename T, bool REST, bool GRAD>
