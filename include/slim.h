@@ -394,7 +394,10 @@ slim_status slim_fp8_quantize_weights(slim_ctx* ctx, const void* W, slim_dtype w
 /* Y (t x n; F16, BF16 or F32) = Q(X) W^T, X (t x m, F16 or BF16) in blocks of 128 channels.  Products of e4m3 numbers and scales on the
  * matrix cores, sums in fp32 in a fixed order (which follows the number of tokens), rounded once to Y's type.  For an fp32 Y, up
  * to 16 tokens, and where there is little to multiply, the sums keep 24 bits; for a 16-bit Y of larger calls the e4m3 matrix cores are
- * used, at twice the rate, which of eight products drop what lies some 13 bits below the largest: less than the rounding of Y.  Up to 16
+ * used, at twice the rate, which of eight products drop what lies some 13 bits below the largest.  That is up to 2^-10 of the sum of the
+ * products' magnitudes (2^-11.5 was seen), without a bias, and 1.5e-5 (normal data) to 7e-5 (channels of very different size) of the norm of Y: 4 %
+ * of the rounding to bf16 and up to a third of that to fp16.  It does not shrink with an element whose products cancel: 0.5 % of bf16 and 4 % of
+ * fp16 outputs are more than one and a half of their own half steps off.  Who needs their bits asks for an fp32 Y.  Up to 16
  * tokens, and small calls, take one launch and no workspace.  slim_fp8_linear_workspace: bytes of workspace (host only;
  * num_cus as in slim_workspace_query). */
 size_t slim_fp8_linear_workspace(int n, int m, int t, slim_dtype y_dtype, int num_cus);
@@ -403,7 +406,7 @@ slim_status slim_fp8_linear(slim_ctx* ctx, const void* X, slim_dtype x_dtype, in
 
 /* Its backward pass: dX (t x m, the type of dY and X, or NULL) = Q(dY) W, dY (t x n) in blocks of 128 outputs, from the stored form of
  * W^T; dW (n x m; F16, BF16 or F32, or NULL) = Qt(dY)^T Qt(X), both in blocks of 128 tokens (the last one smaller); the
- * sums as for Y, by the type of each.  qt and st are not
+ * sums on the e4m3 matrix cores for dX and a 16-bit dW, of 24 bits for an fp32 dW.  qt and st are not
  * read without dX, X not without dW. */
 size_t slim_fp8_linear_backward_workspace(int n, int m, int t, int dx, int dw, slim_dtype dw_dtype, int num_cus);
 slim_status slim_fp8_linear_backward(slim_ctx* ctx, const void* dY, const void* X, slim_dtype x_dtype, int t, int64_t lddy, int64_t ldx,

@@ -162,7 +162,7 @@ slim_status launch(slim_ctx* ctx, const FewArgs& a) {
 namespace slimfp8 {
 
 // Up to 16 tokens; more while the busiest CU has no more than 64 blocks of 16 x 16 x 128 to multiply, where the two launches of the other
-// way cost more than the work.  Of 36 shapes with 1 to 28 blocks a wavefront in a row, host's share included: up to 64 blocks one launch is the
+// way cost more than the work.  Of 37 shapes with 1 to 28 blocks a wavefront in a row, host's share included: up to 64 blocks one launch is the
 // faster by 1 to 6 us (384 x 384, 3000 tokens, 54 blocks: 9.3 and 11.8; 4096 x 4096, 32 tokens, 64: 10.1 and 15.0; 512 x 8192, 128 tokens,
 // 64, the deepest: 13.5 and 14.5; the other way only 2048 x 128, 2000 tokens, 63: 12.5 and 11.7); from 66 to 126 either one is (1000 x 3000, 200
 // tokens, 96: 10.8 and 15.1; 700 x 700, 1000 tokens, 66: 14.3 and 11.5; 2048 x 256, 2000 tokens, 126: 17.4 and 11.7); from 128 on two are, but

@@ -161,3 +161,18 @@ def test_the_one_launch_kernel_keeps_24_bits(slim, n, m, t):  # noqa: F811
     q, s = slim.fp8_quantize_weights(W.cuda(), transposed=False)
     A, B = ref.q_rows(X), ref.quantize(W, ref.B, ref.B)[2]
     close(slim.fp8_linear(X.cuda(), q, s), A @ B.t(), A.abs() @ B.abs().t(), m, True)
+
+
+@pytest.mark.parametrize("n,m,t", [(520, 700, 1500), (300, 9000, 1500), (1000, 700, 2050), (4100, 3000, 2050)])
+@pytest.mark.parametrize("x", [F16, BF16])
+def test_what_the_e4m3_cores_drop(slim, n, m, t, x):  # noqa: F811
+    """Of eight products each loses less than 2^-13 of the largest P, without a bias: in squares 8 2^-26 / 3 P^2 a group, P^2 at most the sum of its
+    eight squares, so in all 8 / 3 2^-26 of the norm of the result, beside its rounding.  (Normal data: a result's norm is that of its products.)"""
+    two_launches(n, m, t, x)
+    g = torch.Generator().manual_seed(n)
+    X, W = torch.randn((t, m), generator=g).to(x), torch.randn((n, m), generator=g)
+    q, s = slim.fp8_quantize_weights(W.cuda(), transposed=False)
+    Y = slim.fp8_linear(X.cuda(), q, s).double()
+    exact = exact_product(ref.q_rows(X), ref.quantize(W, ref.B, ref.B)[2])
+    off, rounding = float((Y - exact).norm() / exact.norm()), float((exact.to(x).double() - exact).norm() / exact.norm())
+    assert off ** 2 - rounding ** 2 <= 8 / 3 * 2.0 ** -26, (off, rounding)
