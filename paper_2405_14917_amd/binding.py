@@ -285,7 +285,7 @@ class Slim:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = torch.cuda.current_stream(self.device)
-        self._index, self._raw_stream = self.device.index or 0, self.stream.cuda_stream
+        self._index, self._raw_stream = self.stream.device.index, self.stream.cuda_stream
         self.workspace = (torch.empty(workspace_bytes + 256, dtype=torch.uint8, device=self.device)
                           if workspace_bytes > 0 else None)
         ws_ptr = None

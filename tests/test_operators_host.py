@@ -386,3 +386,31 @@ def test_a_gradient_is_not_lost_silently(binding):
         for t in (leaf(x), None):
             binding._no_graph(t)
     binding._no_graph(x, w, None)
+
+
+@pytest.mark.parametrize("device,index", [("cuda", 1), ("cuda:0", 0), ("cuda:1", 1)])
+def test_a_context_knows_its_device(binding, monkeypatch, device, index):
+    """"cuda" is the current device, which need not be the first."""
+    class Stream:
+        cuda_stream = 0
+
+    Stream.device = torch.device("cuda", index)
+    monkeypatch.setattr(torch.cuda, "set_device", lambda d: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d: Stream())
+    slim = binding.Slim.__new__(binding.Slim)
+
+    class Library:
+        @staticmethod
+        def slim_create(*args):
+            return binding.SLIM_OK
+
+    monkeypatch.setattr(binding, "load", lambda: Library())
+    slim.__init__(device)
+    slim.ctx = None                                              # (nothing to destroy)
+    monkeypatch.setattr(binding, "_current_stream", lambda i: 0)
+
+    class There:
+        def get_device(self):
+            return index
+
+    slim._ready(There())
