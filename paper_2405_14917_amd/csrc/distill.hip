@@ -35,7 +35,8 @@ struct DistillArgs {
   int64_t lds, ldk, ldds;
   int V, K;
   int index64, t_dtype;
-  double tau;
+  double itau;                       // 1 / tau
+  float c;                           // log2(e) / tau
   // rows in chunks: `chunks` of them, their maxima and sums (rows x chunks), and the slots' sums (5 per row)
   int chunks;
   float2* part;
@@ -69,8 +70,8 @@ template <typename T>
 struct Piece {
   static constexpr int E = 16 / sizeof(T);
   unsigned v[4];
+  static constexpr unsigned NONE = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u;      // minus infinity
   __device__ __forceinline__ void none() {                           // logits whose exponential is zero
-    constexpr unsigned NONE = sizeof(T) == 4 ? 0xff800000u : __is_same(T, __half) ? 0xfc00fc00u : 0xff80ff80u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = NONE;
   }
@@ -85,9 +86,15 @@ struct Piece {
       else v[i] = (unsigned)narrow<T>(f[2 * i]) | (unsigned)narrow<T>(f[2 * i + 1]) << 16;
     }
   }
-  __device__ __forceinline__ void drop(int i) {                      // element i becomes minus infinity
-    if constexpr (sizeof(T) == 4) v[i] = 0xff800000u;
-    else v[i / 2] = (v[i / 2] & (i & 1 ? 0xffffu : 0xffff0000u)) | (__is_same(T, __half) ? 0xfc00u : 0xff80u) << (16 * (i & 1));
+  __device__ __forceinline__ void drop(unsigned m) {                 // the elements whose bit is set become minus infinity
+    auto all = [&](int e) { return (unsigned)((int)(m << (31 - e)) >> 31); };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      unsigned to = 0;
+      if constexpr (sizeof(T) == 4) to = all(i);
+      else to = (all(2 * i) & 0xffffu) | (all(2 * i + 1) & 0xffff0000u);
+      v[i] = (v[i] & ~to) | (NONE & to);
+    }
   }
   // The widened values are not kept from one use to the next: they would take twice the registers.
   __device__ __forceinline__ void narrow_again() {
@@ -101,10 +108,24 @@ struct Piece {
 // 2^-150 of the largest, the least fp32 number; 2^30 classes of 2^LIFT are no overflow.
 constexpr int LIFT = 24;
 constexpr double UNLIFT = 1.0 / (1 << LIFT);
-__device__ __forceinline__ float exp_of(float v, float c, float top) { return __builtin_amdgcn_exp2f(fmaf(v - top, c, (float)LIFT)); }
-// log2(e) / tau; what a maximum is worth as a base (minus infinity, of nothing or of excluded classes alone: 0, against which they stay zero)
-__device__ __forceinline__ float per_tau(double itau) { return (float)fmin(LOG2E * itau, 3e38); }
-__device__ __forceinline__ float base_of(float top) { return top > -INFINITY ? top : 0.f; }
+
+// How they are taken: 2^(v c - off), c = log2(e) / tau, off = top c - LIFT rounded to fp32, is one instruction for the argument; k makes up for
+// that rounding, so that only c's own remains, of v - top.  (From v - top itself: 2048 x 12000 fp16 30.2 us in place of 28.3.)  Where top c is
+// so large that the rounding is no small number, the row itself is shifted to a maximum of 0 (Range::shift).
+struct Scale {
+  float c, top, off, k;
+  bool near;
+  // (a maximum of minus infinity, of nothing or of excluded classes alone, is a base of 0, against which they stay zero)
+  __device__ __forceinline__ Scale(float c_, float top_) : c(c_), top(top_ > -INFINITY ? top_ : 0.f) {
+    const float p = top * c;
+    off = p - (float)LIFT;
+    near = fabsf(p) <= 0x1p22f;
+    // the roundings of the product and of the difference, both exact
+    k = near ? __builtin_amdgcn_exp2f(-(fmaf(top, c, -p) + ((p - off) - (float)LIFT))) : 1.f;
+    if (!near) off = -(float)LIFT;
+  }
+  __device__ __forceinline__ float exp_of(float v) const { return __builtin_amdgcn_exp2f(fmaf(v, c, -off)); }
+};
 
 // A range of a row in the registers of a workgroup: P pieces per thread, and the elements behind the last whole piece, one per thread.
 template <typename T, int THREADS, int P>
@@ -137,41 +158,61 @@ struct Range {
   // the classes whose bit is set become minus infinity
   __device__ __forceinline__ void drop(const uint8_t* bits) {
     if (tid < rest && (bits[(pieces * E + tid) >> 3] >> ((pieces * E + tid) & 7) & 1)) last = -INFINITY;
+    constexpr int PER = 32 / E;                                      // pieces whose bits fill a word
+    unsigned mask[(P + PER - 1) / PER] = {}, any = 0;                // (all read before the first is looked at)
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = min(i * THREADS + tid, max(pieces - 1, 0)) * E, mask = (int)bits[at >> 3] >> (at & 7);
-      if (__builtin_expect(mask & ((1 << E) - 1), 0)) {
+      const int at = min(i * THREADS + tid, max(pieces - 1, 0)) * E;
+      const unsigned m = ((unsigned)bits[at >> 3] >> (at & 7)) & ((1u << E) - 1);
+      mask[i / PER] |= m << (i % PER * E);
+    }
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (mask >> e & 1) x[i].drop(e);
-      }
+    for (unsigned m : mask) any |= m;
+    if (!any) return;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (const unsigned m = mask[i / PER] >> (i % PER * E) & ((1u << E) - 1)) x[i].drop(m);
+  }
+  // Logits so far from zero that top c exceeds 2^22 become their difference from `top`.  In the type of the logits: where the difference
+  // counts (150 / 2^22 of top and less) it is exact in fp32 and zero in 16 bits.
+  __device__ __forceinline__ void shift(const Scale& to) {
+    if (__builtin_expect(to.near, 1)) return;
+    last -= to.top;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      float o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = x[i].get(e) - to.top;
+      x[i].set(o);
     }
   }
-  // sum of the exponentials
-  __device__ __forceinline__ float sum(float c, float top) {
-    float s = exp_of(last, c, top);
+  // sum of the exponentials, lifted
+  __device__ __forceinline__ float sum(const Scale& to) {
+    float s = to.exp_of(last);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       float p = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) p += exp_of(x[i].get(e), c, top);
+      for (int e = 0; e < E; ++e) p += to.exp_of(x[i].get(e));
       s += p;
       x[i].narrow_again();
     }
-    return s;
+    return s * to.k;
   }
-  __device__ __forceinline__ void write(T* dS, float c, float top, float f) {
+  // f times the exponentials, f for lifted ones
+  __device__ __forceinline__ void write(T* dS, const Scale& to, float f) {
+    f *= to.k;
 #pragma unroll
     for (int i = 0; i < P; ++i)
       if (i * THREADS + tid < pieces) {
         float o[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = exp_of(x[i].get(e), c, top) * f;
+        for (int e = 0; e < E; ++e) o[e] = to.exp_of(x[i].get(e)) * f;
         Piece<T> p;
         p.set(o);
         store16_once(dS + (i * THREADS + tid) * E, p.v);
       }
-    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, exp_of(last, c, top) * f);
+    if (tid < rest) put<T>(dS, (int64_t)pieces * E + tid, to.exp_of(last) * f);
   }
   __device__ __forceinline__ void write_zero(T* dS) {
     Piece<T> p = {};
@@ -260,8 +301,7 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
-  const double itau = 1.0 / a.tau;
-  const float c = per_tau(itau);
+  const double itau = a.itau;
 
   Range<T, THREADS, P> x;
   x.load(S, a.V, tid);
@@ -281,15 +321,13 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
       if constexpr (REST) atomicOr(&bits[cls >> 5], 1u << (cls & 31));
     }
   }
-  if constexpr (REST) {
-    __syncthreads();
-    x.drop(reinterpret_cast<const uint8_t*>(bits));
-  }
-  const float top = base_of(group_max<W>(x.top(), red_m));
-  high = group_max<W>(high, red_t);
-  double d[4] = {0.0, 0.0, 0.0, (double)x.sum(c, top) * UNLIFT};
+  high = group_max<W>(high, red_t);                                // (its barrier: the bits are set)
+  if constexpr (REST) x.drop(reinterpret_cast<const uint8_t*>(bits));
+  const Scale to(a.c, group_max<W>(x.top(), red_m));
+  x.shift(to);
+  double d[4] = {0.0, 0.0, 0.0, (double)x.sum(to) * UNLIFT};
   // (teacher: t / tau less its maximum, or less its log-sum-exp)
-  const double t0 = REST ? 0.0 : (double)base_of(high), tl = REST ? (double)a.lse[row] : 0.0, zs = REST && high > -INFINITY ? (double)high : (double)top;
+  const double t0 = REST || high == -INFINITY ? 0.0 : (double)high, tl = REST ? (double)a.lse[row] : 0.0, zs = REST && high > -INFINITY ? (double)high : (double)to.top;
   for (int k = tid; k < a.K; k += THREADS) {
     double p = 0.0, ez = 0.0;
     if (si[k] >= 0) {
@@ -304,12 +342,13 @@ __global__ __launch_bounds__(THREADS) void distill(DistillArgs a) {
     se[k] = ez;
   }
   group_sums<W, 4>(d, red_d);
-  const Row r(d[0], d[1], d[2], d[3], ((double)top - zs) * itau, REST);
+  if (!GRAD && tid < THREADS - 64) return;
+  const Row r(d[0], d[1], d[2], d[3], ((double)to.top - zs) * itau, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
     if (r.live) {
-      x.write(dS, c, top, r.factor(g));
+      x.write(dS, to, r.factor(g));
       __syncthreads();
       const double ge = g * r.slot, gp = REST ? g : g / r.B;
       for (int k = tid; k < a.K; k += THREADS)
@@ -337,8 +376,7 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
   const int64_t row = blockIdx.x / a.chunks;
   const int chunk = (int)(blockIdx.x % a.chunks), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
-  const double itau = 1.0 / a.tau;
-  const float c = per_tau(itau);
+  const double itau = a.itau;
   Range<T, CH_THREADS, CH_P> x;
   x.load(S + c0, n, tid);
   if constexpr (REST) {
@@ -354,7 +392,9 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
     x.drop(reinterpret_cast<const uint8_t*>(bits));
   }
   const float top = group_max<W>(x.top(), red_m);
-  double e[1] = {(double)x.sum(c, base_of(top)) * UNLIFT};
+  const Scale to(a.c, top);
+  x.shift(to);
+  double e[1] = {(double)x.sum(to) * UNLIFT};
   group_sums<W, 1>(e, red_e);
   if (tid == 0) a.part[row * a.chunks + chunk] = make_float2(top, (float)e[0]);
   if (chunk != 0) return;
@@ -368,7 +408,8 @@ __global__ __launch_bounds__(CH_THREADS) void distill_chunks(DistillArgs a) {
   }
   t_top = group_max<W>(t_top, red_t);
   z_top = group_max<W>(z_top, red_z);
-  const double t0 = REST ? 0.0 : (double)base_of(t_top), tl = REST ? (double)a.lse[row] : 0.0, zs = (double)base_of(z_top);
+  const double t0 = REST || t_top == -INFINITY ? 0.0 : (double)t_top, tl = REST ? (double)a.lse[row] : 0.0,
+               zs = z_top > -INFINITY ? (double)z_top : 0.0;
   double d[3] = {0.0, 0.0, 0.0};
   for (int k = tid; k < a.K; k += CH_THREADS) {
     const int cls = class_of(a, row * a.ldk + k);
@@ -399,24 +440,23 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
   const int64_t row = blockIdx.x / per_row;
   const int chunk = (int)(blockIdx.x % per_row), c0 = chunk * CHUNK<T>, n = min(CHUNK<T>, a.V - c0);
   const T* S = static_cast<const T*>(a.S) + row * a.lds;
-  const double itau = 1.0 / a.tau;
-  const float c = per_tau(itau);
+  const double itau = a.itau;
   Range<T, CH_THREADS, CH_P> x;
   if constexpr (GRAD) x.load(S + c0, n, tid);
   const float2* part = a.part + row * a.chunks;
   float top = -INFINITY;
   for (int i = lane; i < a.chunks; i += 64) top = fmaxf(top, part[i].x);
-  top = base_of(wave_max_f32(top));
+  const Scale to(a.c, wave_max_f32(top));
   double es = 0.0;
   for (int i = lane; i < a.chunks; i += 64) {
     const float2 v = part[i];
     // (that of a chunk without a maximum is 0 or NaN)
-    es += v.x == -INFINITY ? (double)v.y : (double)v.y * exp(((double)v.x - (double)top) * itau);
+    es += v.x == -INFINITY ? (double)v.y : (double)v.y * exp(((double)v.x - (double)to.top) * itau);
   }
   es = wave_sum(es);
   const double* s = a.slots + row * 5;
-  const double zs = s[3] > -INFINITY ? s[3] : (double)top, t0 = s[4], tl = REST ? (double)a.lse[row] : 0.0;
-  const Row r(s[0], s[1], s[2], es, ((double)top - zs) * itau, REST);
+  const double zs = s[3] > -INFINITY ? s[3] : (double)to.top, t0 = s[4], tl = REST ? (double)a.lse[row] : 0.0;
+  const Row r(s[0], s[1], s[2], es, ((double)to.top - zs) * itau, REST);
   if constexpr (GRAD) {
     T* dS = static_cast<T*>(a.dS) + row * a.ldds;
     const double g = (double)a.dloss[row] * itau;
@@ -425,7 +465,7 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
       extern __shared__ __align__(16) char smem_dl[];
       float* sv = reinterpret_cast<float*>(smem_dl);
       int* si = reinterpret_cast<int*>(sv + a.K);
-      const double ge = g * r.slot, gp = REST ? g : g / r.B, zb = REST ? zs : (double)top;
+      const double ge = g * r.slot, gp = REST ? g : g / r.B, zb = REST ? zs : (double)to.top;
       for (int k = tid; k < a.K; k += CH_THREADS) {
         const int cls = class_of(a, row * a.ldk + k), at = cls - c0;
         si[k] = cls >= 0 && at >= 0 && at < n ? at : -1;
@@ -433,7 +473,8 @@ __global__ __launch_bounds__(GRAD ? CH_THREADS : 64) void distill_join(DistillAr
           sv[k] = (float)(exp(((double)value<T>(S, cls) - zb) * itau) * ge - exp(((double)teacher_of(a, row * a.ldk + k) - t0) * itau - tl) * gp);
       }
       __syncthreads();
-      x.write(dS + c0, c, top, r.factor(g));
+      x.shift(to);
+      x.write(dS + c0, to, r.factor(g));
       __syncthreads();
       for (int k = tid; k < a.K; k += CH_THREADS)
         if (si[k] >= 0) put<T>(dS, c0 + si[k], sv[k]);
@@ -466,13 +507,14 @@ size_t need(int64_t rows, int V, slim_dtype d) {
 }
 
 // Threads of a row in one workgroup.  Eight pieces per thread up to 2048 pieces: of 4000 x 3000 bf16 one wavefront a row takes 19.9 us, four
-// 24.9; 2048 x 12000 with four 26.6 us, with eight 38.0.  Beyond, more than two rows per CU: four wavefronts of 16 pieces (2048 x 32000 bf16
-// 62.6 us against 66.1 with eight of 8, 2048 x 16000 fp32 56.1 and 60.8; 600 x 32000 22.0 and 22.5, 600 x 16000 16.3 and 19.4); fewer: eight of
-// 8 (400 x 32000 16.3 us against 17.7, 400 x 16000 12.3 and 13.5).
-int threads_of(int pieces, int64_t rows, bool grad, int ncu) {
+// 24.9; 2048 x 12000 with four 26.6 us, with eight 38.0.  Beyond, many rows: four wavefronts of 16 pieces (2048 x 32000 bf16 with 64 slots
+// 61.6 us against 65.3 with eight of 8, with 256 slots 68.1 and 70.7; 1600 x 32000 50.9 and 54.6), but fewer rows, a last round of which
+// leaves CUs idle, and many slots, a thread's share of which is twice as long: eight of 8 (400 x 32000 16.0 us against 17.1, 1200 x 32000
+// 35.3 and 36.3; between them 600 rows 22.3 and 20.6; 2048 x 32000 with 1024 slots 91.5 and 93.9, 3000 130.9 and 141.8).
+int threads_of(int pieces, int64_t rows, int K, bool grad, int ncu) {
   if (pieces <= 512) return 64;
   if (pieces <= 1024) return 128;
-  return pieces <= 2048 || (grad && rows > 2 * ncu) ? 256 : 512;
+  return pieces <= 2048 || (grad && rows > 6 * ncu && K <= 512) ? 256 : 512;
 }
 
 template <typename T, bool REST, bool GRAD>
@@ -489,7 +531,7 @@ slim_status by_size(slim_ctx* ctx, DistillArgs a, int64_t rows) {
                 dim3(GRAD ? CH_THREADS : 64), GRAD ? (size_t)a.K * 8 : 0, a);
     return SLIM_OK;
   }
-  switch (threads_of(pieces, rows, GRAD, ctx->num_cus)) {
+  switch (threads_of(pieces, rows, a.K, GRAD, ctx->num_cus)) {
     case 64: return launch<T, 64, 8, REST, GRAD>(ctx, a, rows);
     case 128: return launch<T, 128, 8, REST, GRAD>(ctx, a, rows);
     case 512: return launch<T, 512, 8, REST, GRAD>(ctx, a, rows);
@@ -505,16 +547,16 @@ slim_status by_form(slim_ctx* ctx, const DistillArgs& a, int64_t rows, bool grad
   return grad ? by_size<T, false, true>(ctx, a, rows) : by_size<T, false, false>(ctx, a, rows);
 }
 
-slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype, int64_t rows, slim_dtype t_dtype, bool grad) {
+slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype, int64_t rows, slim_dtype t_dtype, double tau, bool grad) {
   auto is_float = [](slim_dtype d) { return d == SLIM_F16 || d == SLIM_BF16 || d == SLIM_F32; };
   if (!is_float(s_dtype) || !is_float(t_dtype)) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: logits are F16, BF16 or F32", fn);
   SLIM_REQUIRE(ctx, rows >= 0 && a.V > 0 && a.V < (1 << 30) && a.K >= 0, "%s: rows = %lld, V = %d, K = %d", fn, (long long)rows, a.V, a.K);
   if (a.K > DL_MAX_K) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: up to %d slots a row, got %d", fn, DL_MAX_K, a.K);
   // (a launch has fewer than 2^32 threads)
-  const int chunks = chunks_of(a.V, s_dtype), threads = threads_of(a.V / (s_dtype == SLIM_F32 ? 4 : 8), rows, grad, ctx->num_cus);
+  const int chunks = chunks_of(a.V, s_dtype), threads = threads_of(a.V / (s_dtype == SLIM_F32 ? 4 : 8), rows, a.K, grad, ctx->num_cus);
   if (rows >= (1ll << 31) || rows * (chunks ? (int64_t)chunks * CH_THREADS : threads) >= (1ll << 32))
     return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: %lld rows of %d classes are too many for one call", fn, (long long)rows, a.V);
-  SLIM_REQUIRE(ctx, a.tau > 0.0 && a.tau <= 1e30, "%s: tau = %g", fn, a.tau);
+  SLIM_REQUIRE(ctx, tau > 0.0 && tau <= 1e30, "%s: tau = %g", fn, tau);
   if (rows == 0) return SLIM_OK;
   SLIM_REQUIRE(ctx, a.S && a.loss && (a.K == 0 || (a.index && a.teacher)), "%s: null pointer", fn);
   SLIM_REQUIRE(ctx, a.lds >= a.V && a.ldk >= a.K, "%s: rows shorter than V or K", fn);
@@ -522,6 +564,8 @@ slim_status run(slim_ctx* ctx, const char* fn, DistillArgs a, slim_dtype s_dtype
   if (const size_t bytes = need(rows, a.V, s_dtype))
     if (const slim_status st = slim_ws_reserve(ctx, bytes); st != SLIM_OK) return st;
   a.t_dtype = (int)t_dtype;
+  a.itau = 1.0 / tau;
+  a.c = (float)std::min(LOG2E * a.itau, 3e38);
   if (s_dtype == SLIM_F32) return by_form<float>(ctx, a, rows, grad);
   return s_dtype == SLIM_F16 ? by_form<__half>(ctx, a, rows, grad) : by_form<__hip_bfloat16>(ctx, a, rows, grad);
 }
@@ -536,16 +580,16 @@ slim_status slim_distill_loss(slim_ctx* ctx, const void* S, slim_dtype s_dtype, 
                               int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                               float* loss) {
   if (!ctx) return SLIM_ERR_INVALID_ARG;
-  DistillArgs a = {S, index, teacher, lse, nullptr, loss, nullptr, lds, ldk, 0, V, K, index64 != 0, 0, tau, 0, nullptr, nullptr};
-  return run(ctx, "slim_distill_loss", a, s_dtype, rows, t_dtype, false);
+  DistillArgs a = {S, index, teacher, lse, nullptr, loss, nullptr, lds, ldk, 0, V, K, index64 != 0, 0, 0.0, 0.f, 0, nullptr, nullptr};
+  return run(ctx, "slim_distill_loss", a, s_dtype, rows, t_dtype, tau, false);
 }
 
 slim_status slim_distill_loss_grad(slim_ctx* ctx, const void* S, slim_dtype s_dtype, int64_t rows, int V, int64_t lds, const void* index,
                                    int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                                    const float* dloss, float* loss, void* dS, int64_t ldds) {
   if (!ctx) return SLIM_ERR_INVALID_ARG;
-  DistillArgs a = {S, index, teacher, lse, dloss, loss, dS, lds, ldk, ldds, V, K, index64 != 0, 0, tau, 0, nullptr, nullptr};
-  return run(ctx, "slim_distill_loss_grad", a, s_dtype, rows, t_dtype, true);
+  DistillArgs a = {S, index, teacher, lse, dloss, loss, dS, lds, ldk, ldds, V, K, index64 != 0, 0, 0.0, 0.f, 0, nullptr, nullptr};
+  return run(ctx, "slim_distill_loss_grad", a, s_dtype, rows, t_dtype, tau, true);
 }
 
 }  // extern "C"
