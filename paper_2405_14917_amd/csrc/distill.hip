@@ -117,11 +117,10 @@ struct Scale {
   bool near;
   // (a maximum of minus infinity, of nothing or of excluded classes alone, is a base of 0, against which they stay zero)
   __device__ __forceinline__ Scale(float c_, float top_) : c(c_), top(top_ > -INFINITY ? top_ : 0.f) {
-    const float p = top * c;
-    off = p - (float)LIFT;
-    near = fabsf(p) <= 0x1p22f;
-    // the roundings of the product and of the difference, both exact
-    k = near ? __builtin_amdgcn_exp2f(-(fmaf(top, c, -p) + ((p - off) - (float)LIFT))) : 1.f;
+    const double exact = fma((double)top, (double)c, -(double)LIFT);
+    off = (float)exact;
+    near = fabsf(off) <= 0x1p22f;
+    k = near ? __builtin_amdgcn_exp2f((float)((double)off - exact)) : 1.f;
     if (!near) off = -(float)LIFT;
   }
   __device__ __forceinline__ float exp_of(float v) const { return __builtin_amdgcn_exp2f(fmaf(v, c, -off)); }
