@@ -415,7 +415,7 @@ int parts_of(int tiles, int nk, int ncu) {
 // 1.44 (2.6) a step, of two medium ones per CU 5.4 + 0.82 (1.42), of two small ones 2.7 + 0.34 (0.56), a medium one alone on its CU 0.6 of
 // that a step; 6 for the launch.  So 15872 x 128, 6139 tokens, takes medium tiles (81; large ones 110, small ones 147), as does 14666 x 2048, 2078 tokens,
 // whose 522 large ones are three rounds (78 and 102), 2048 x 2048, 1024 tokens, small ones (17; medium ones 26), and 8192 x 28672, 4096
-// tokens, large ones (790; medium ones above 900).
+// tokens, large ones (790; medium ones above 900).  The bytes of the operands are in the measured step, not a term of their own.
 double tile_cost(const Product& p, int tile, int ncu) {
   static const double round[] = {15.0, 5.4, 2.7}, step[2][3] = {{1.44, 0.82, 0.34}, {2.6, 1.42, 0.56}};
   const int tiles = tiles_of(p, tile), s = parts_of(tiles, p.nk, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
