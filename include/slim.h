@@ -413,6 +413,36 @@ slim_status slim_fp8_linear_backward(slim_ctx* ctx, const void* dY, const void* 
                                      const uint8_t* qt, int64_t ldqt, const uint8_t* st, int64_t ldst, int n, int m, void* dX, int64_t lddx,
                                      void* dW, slim_dtype dw_dtype, int64_t lddw);
 
+/* The same layer with what stands around it in a block: Y = act(Q(X) W^T + bias) + R, computed in fp32 from the sums and rounded once.
+ *   X        t x m as above, or NULL; then xq, xs: its 8-bit form Q(X), as slim_add_norm writes it (rows of whole blocks of 128, padded with zeros;
+ *            t rows of scale bytes, ldxs a multiple of 4)
+ *   bias     n numbers of Y's type or F32, or NULL          act   SLIM_ACT_*: relu, z Phi(z), its tanh form, z / (1 + exp(-z))
+ *   R        t x n of Y's type (ldr >= n), or NULL          Z     t x n of Y's type (ldz >= n), or NULL: takes Q(X) W^T + bias, rounded
+ * Y and Z are distinct; Y may be R.  epilogue NULL: slim_fp8_linear, from either form of X.  Sums as for slim_fp8_linear. */
+enum { SLIM_ACT_NONE = 0, SLIM_ACT_RELU = 1, SLIM_ACT_GELU = 2, SLIM_ACT_GELU_TANH = 3, SLIM_ACT_SILU = 4 };
+typedef struct slim_epilogue {
+  const void* bias;
+  slim_dtype bias_dtype;
+  int act;
+  const void* R;
+  int64_t ldr;
+  void* Z;
+  int64_t ldz;
+} slim_epilogue;
+size_t slim_fp8_linear_act_workspace(int n, int m, int t, int x_8bit, slim_dtype y_dtype, int num_cus);
+slim_status slim_fp8_linear_act(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* xq, int64_t ldxq,
+                                const uint8_t* xs, int64_t ldxs, const uint8_t* q, int64_t ldq, const uint8_t* s, int64_t lds, int n, int m,
+                                const slim_epilogue* epilogue, void* Y, slim_dtype y_dtype, int64_t ldy);
+
+/* Its backward pass: dZ = dY act'(Z), rounded to their type (that of X; without an activation Z is not read), then dX = Q(dZ) W and dW =
+ * Qt(dZ)^T Qt(X) as in slim_fp8_linear_backward, and db (n; F16, BF16 or F32, or NULL) = the sum of dY act'(Z), not rounded, over the tokens: 128 of them
+ * in fp32, these sums in fp64.  The gradient of R is dY. */
+size_t slim_fp8_linear_act_backward_workspace(int n, int m, int t, int dx, int dw, slim_dtype dw_dtype, int db, int num_cus);
+slim_status slim_fp8_linear_act_backward(slim_ctx* ctx, const void* dY, const void* Z, int act, const void* X, slim_dtype x_dtype, int t,
+                                         int64_t lddy, int64_t ldz, int64_t ldx, const uint8_t* qt, int64_t ldqt, const uint8_t* st, int64_t ldst,
+                                         int n, int m, void* dX, int64_t lddx, void* dW, slim_dtype dw_dtype, int64_t lddw, void* db,
+                                         slim_dtype db_dtype);
+
 /* Layer norm of rows: y = (x - mu) r w + b with r = 1 / sqrt(v + eps), mu and v the row's mean and variance; rms != 0: mu = 0 and v the mean
  * of x^2.  X and Y F16, BF16 or F32; w and b (b may be NULL) of the same type or F32.  mean (not written with rms) and rstd: mu and r of
  * the rows for the backward pass, or NULL.  Arithmetic in fp32, rounded once; deviations are taken from the mean.  Y may be X.
@@ -424,6 +454,19 @@ size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, slim_dtype x_d
 slim_status slim_layer_norm_backward(slim_ctx* ctx, const void* dY, const void* X, slim_dtype x_dtype, int64_t rows, int cols, int64_t lddy,
                                      int64_t ldx, const void* w, slim_dtype w_dtype, const float* mean, const float* rstd, void* dX,
                                      int64_t lddx, void* dw, void* db);
+
+/* The norm of the residual stream: H = X + R, rounded to their type, then the norm of H as above.  R NULL: H is X (and is not written); H NULL:
+ * not wanted.  Y: the norm's output; q, s: what the quantiser Q above makes of Y (rounded to X's type), rows of ldq numbers (a multiple of 128, of at
+ * least cols; q 16-byte aligned; the last block of a row is padded with zeros) and of lds scale bytes (a multiple of 4; s 4-byte aligned), as
+ * slim_fp8_linear_act takes them; either may be NULL, not both.  H and Y may be X or R (not both the same).
+ * Backward: dX = dH + the norm's gradient at H, the gradient of X and of R alike; dH (or NULL: none) is the gradient that reaches H past the norm; the e4m3
+ * rounding counts as the identity.  dX may be dY, dH or H.  Workspace: slim_layer_norm_backward_workspace. */
+slim_status slim_add_norm(slim_ctx* ctx, const void* X, const void* R, slim_dtype x_dtype, int64_t rows, int cols, int64_t ldx, int64_t ldr,
+                          const void* w, const void* b, slim_dtype w_dtype, double eps, int rms, void* H, int64_t ldh, void* Y, int64_t ldy,
+                          uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, float* mean, float* rstd);
+slim_status slim_add_norm_backward(slim_ctx* ctx, const void* dY, const void* dH, const void* H, slim_dtype x_dtype, int64_t rows, int cols,
+                                   int64_t lddy, int64_t lddh, int64_t ldh, const void* w, slim_dtype w_dtype, const float* mean,
+                                   const float* rstd, void* dX, int64_t lddx, void* dw, void* db);
 
 /* Divergence of the student's logits S (rows x V; F16, BF16 or F32) from a teacher's top logits, and its gradient.
  *   index    rows x K classes (ld = ldk), int64 (index64 != 0) or int32, distinct within a row (of a class named twice, the gradient of
@@ -442,6 +485,19 @@ slim_status slim_distill_loss(slim_ctx* ctx, const void* S, slim_dtype s_dtype, 
 slim_status slim_distill_loss_grad(slim_ctx* ctx, const void* S, slim_dtype s_dtype, int64_t rows, int V, int64_t lds, const void* index,
                                    int index64, const void* teacher, slim_dtype t_dtype, int K, int64_t ldk, const float* lse, double tau,
                                    const float* dloss, float* loss, void* dS, int64_t ldds);
+
+/* The norm of many tensors together, n = sqrt(sum of all squares) (summed in fp64), and the same tensors scaled down to a limit: g min(1, limit / n),
+ * rounded once.  `tensors`, `out`: host arrays of `count` descriptions (F16, BF16 or F32, mixed at will; rows ld elements apart); out NULL: in place.  An
+ * output is its own input or does not overlap any input or other output.  Where n is at most the limit, or no finite number, the tensors are left (or
+ * copied) bit for bit.  norm: one fp32 number.  slim_grad_norm_workspace: bytes of workspace of both (host only). */
+typedef struct slim_tensor {
+  void* data;
+  int64_t rows, cols, ld;
+  int64_t dtype; /* slim_dtype */
+} slim_tensor;
+size_t slim_grad_norm_workspace(int count, int num_cus);
+slim_status slim_grad_norm(slim_ctx* ctx, const slim_tensor* tensors, int count, float* norm);
+slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const slim_tensor* out, int count, double limit, float* norm);
 
 /* ---------------------------------------------------------------------------------------------
  * Per-kernel timing with HIP events on the context's stream (measurement aid, host only).

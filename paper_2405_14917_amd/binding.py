@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -21,6 +21,7 @@ Q1_SIGN, Q1_AFFINE = 0, 1
 SCOPE_BLOCK, SCOPE_ROW = 0, 1
 SAL_HINV_DIAG, SAL_CHOL_DIAG = 0, 1
 OBJ_KL, OBJ_MSE = 0, 1
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 _DT = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.float64: F64}
 
@@ -34,6 +35,8 @@ EXPORTS = [
     "slim_fp8_quantize_weights", "slim_fp8_linear_workspace", "slim_fp8_linear", "slim_fp8_linear_backward_workspace",
     "slim_fp8_linear_backward", "slim_layer_norm", "slim_layer_norm_backward_workspace", "slim_layer_norm_backward",
     "slim_distill_workspace", "slim_distill_loss", "slim_distill_loss_grad",
+    "slim_fp8_linear_act_workspace", "slim_fp8_linear_act", "slim_fp8_linear_act_backward_workspace", "slim_fp8_linear_act_backward",
+    "slim_add_norm", "slim_add_norm_backward", "slim_grad_norm_workspace", "slim_grad_norm", "slim_clip_gradients",
     "slim_profile_enable", "slim_profile_collect", "slim_profile_entry", "slim_profile_reset",
 ]
 
@@ -46,6 +49,21 @@ class SlimParams(ctypes.Structure):
 class SlimShape(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int), ("m", ctypes.c_int), ("beta", ctypes.c_int), ("t_c", ctypes.c_int64),
                 ("t_s", ctypes.c_int64), ("t_x", ctypes.c_int), ("lwc_steps", ctypes.c_int)]
+
+
+class SlimEpilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int), ("act", ctypes.c_int), ("R", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("Z", ctypes.c_void_p), ("ldz", ctypes.c_int64)]
+
+
+class AddNorm(NamedTuple):
+    """What Slim.add_norm returns; what was not asked for is None."""
+    H: torch.Tensor                  # the residual stream
+    Y: Optional[torch.Tensor]        # its norm
+    q: Optional[torch.Tensor]        # the same in 8 bits: numbers and scales
+    s: Optional[torch.Tensor]
+    mean: Optional[torch.Tensor]     # of the rows, for the backward pass
+    rstd: Optional[torch.Tensor]
 
 
 def workspace_query(n: int, m: int, beta: int, t_c: int = 0, t_s: int = 0, t_x: int = 0, num_cus: int = 0,
@@ -142,7 +160,20 @@ def load() -> ctypes.CDLL:
                                       c_void_p, c_double, c_void_p]
     lib.slim_distill_loss_grad.argtypes = lib.slim_distill_loss.argtypes[:-1] + [c_void_p, c_void_p, c_void_p, c_i64]
     lib.slim_distill_workspace.argtypes = [c_i64, c_int, c_int]
-    for fn in (lib.slim_distill_workspace, lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
+    lib.slim_fp8_linear_act_workspace.argtypes = [c_int] * 6
+    lib.slim_fp8_linear_act.argtypes = [c_void_p, c_void_p, c_int, c_int, c_i64] + [c_void_p, c_i64] * 4 + [c_int, c_int, c_void_p, c_void_p,
+                                                                                                          c_int, c_i64]
+    lib.slim_fp8_linear_act_backward_workspace.argtypes = [c_int] * 8
+    lib.slim_fp8_linear_act_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_i64, c_i64, c_i64, c_void_p, c_i64,
+                                                 c_void_p, c_i64, c_int, c_int, c_void_p, c_i64, c_void_p, c_int, c_i64, c_void_p, c_int]
+    lib.slim_add_norm.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_i64, c_void_p, c_void_p, c_int, c_double, c_int,
+                                  c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_void_p]
+    lib.slim_add_norm_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_i64, c_i64, c_void_p, c_int,
+                                           c_void_p, c_void_p, c_void_p, c_i64, c_void_p, c_void_p]
+    lib.slim_grad_norm_workspace.argtypes = [c_int, c_int]
+    lib.slim_grad_norm.argtypes = [c_void_p, c_void_p, c_int, c_void_p]
+    lib.slim_clip_gradients.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_double, c_void_p]
+    for fn in (lib.slim_fp8_linear_act_workspace, lib.slim_fp8_linear_act_backward_workspace, lib.slim_grad_norm_workspace, lib.slim_distill_workspace, lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
         fn.restype = c_size_t
     lib.slim_profile_enable.argtypes = [c_void_p, c_int]
     lib.slim_profile_collect.argtypes = [c_void_p]
@@ -206,6 +237,53 @@ def distill_workspace(rows: int, V: int, dtype: torch.dtype = torch.bfloat16) ->
     return int(load().slim_distill_workspace(rows, V, _DT[dtype]))
 
 
+def fp8_linear_act_workspace(n: int, m: int, t: int, x_8bit: bool = False, dtype: torch.dtype = torch.bfloat16, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.fp8_linear_act (host only, no GPU needed)."""
+    return int(load().slim_fp8_linear_act_workspace(n, m, t, int(x_8bit), _DT[dtype], num_cus))
+
+
+def fp8_linear_act_backward_workspace(n: int, m: int, t: int, dx: bool = True, dw: bool = True, dw_dtype: torch.dtype = torch.bfloat16,
+                                      db: bool = True, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.fp8_linear_act_backward (host only, no GPU needed)."""
+    return int(load().slim_fp8_linear_act_backward_workspace(n, m, t, int(dx), int(dw), _DT[dw_dtype], int(db), num_cus))
+
+
+def grad_norm_workspace(count: int, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.grad_norm and Slim.clip_gradients for `count` tensors (host only, no GPU needed)."""
+    return int(load().slim_grad_norm_workspace(count, num_cus))
+
+
+def _tensor_list(tensors, what: str):
+    """The descriptions (address, rows, columns, leading dimension, type) that the library takes of a list of tensors."""
+    flat = []
+    for t in tensors:
+        if t.dtype not in (torch.float16, torch.bfloat16, torch.float32):
+            raise ValueError("%s have to be float16, bfloat16 or float32" % what)
+        if t.is_contiguous():
+            n = t.numel()
+            flat += (t.data_ptr(), 1, n, n, _DT[t.dtype])
+        elif t.dim() == 2:
+            flat += (t.data_ptr(), t.shape[0], t.shape[1], _row_stride(t, what), _DT[t.dtype])
+        else:
+            raise ValueError("%s have to be contiguous, or matrices with contiguous rows" % what)
+    return (ctypes.c_int64 * len(flat))(*flat)
+
+
+def _tensor_rows(tensors, what: str):
+    """The same with matrices described by their rows, contiguous or not."""
+    flat = _tensor_list(tensors, what)
+    for i, t in enumerate(tensors):
+        if t.dim() == 2:
+            flat[5 * i + 1], flat[5 * i + 2], flat[5 * i + 3] = t.shape[0], t.shape[1], _row_stride(t, what)
+    return flat
+
+
+def _check_act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError("act has to be one of %s, got %r" % (", ".join(str(a) for a in ACTIVATIONS), act))
+    return ACTIVATIONS[act]
+
+
 def _empty_like(x: torch.Tensor) -> torch.Tensor:
     """A contiguous tensor of x's shape and type."""
     return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
@@ -226,12 +304,13 @@ def _row_stride(x: torch.Tensor, what: str) -> int:
     return ld
 
 
-def _stored_strides(q: torch.Tensor, s: torch.Tensor, what: str):
-    """Leading dimensions of stored 8-bit weights; raises where they are not what Slim.fp8_quantize_weights makes."""
+def _stored_strides(q: torch.Tensor, s: torch.Tensor, what: str, rows: int = 128):
+    """Leading dimensions of stored 8-bit weights, in blocks of 128 x 128, or of activations (`rows` = 1); raises where they are not what
+    Slim.fp8_quantize_weights or Slim.add_norm makes."""
     if q.dtype != _E4M3 or s.dtype != torch.uint8 or q.dim() != 2 or s.dim() != 2:
         raise ValueError("%s has to be a float8_e4m3fn matrix, its scales a uint8 matrix" % what)
     n, m = q.shape
-    nb, mb = (n + 127) // 128, (m + 127) // 128
+    nb, mb = (n + rows - 1) // rows, (m + 127) // 128
     if s.shape != (nb, mb):
         raise ValueError("%s (%d x %d) needs %d x %d scales, got %d x %d" % (what, n, m, nb, mb, s.shape[0], s.shape[1]))
     (ldq, qstep), (lds, sstep) = q.stride(), s.stride()
@@ -640,6 +719,190 @@ class Slim:
         if st:
             self._check(st)
         return (Y, mean, rstd) if stats else Y
+
+    def fp8_linear_act(self, X, W: torch.Tensor, Ws: torch.Tensor, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+                       residual: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None, keep: bool = False):
+        """Y (t, n) = act(Q(X) W^T + bias) + residual.  X: (t, m) float16 / bfloat16, or its 8-bit form (q, s) as add_norm makes it; bias (n,)
+        of Y's type or float32; act: None, "relu", "gelu", "gelu_tanh" or "silu"; residual (t, n) of Y's type.  `dtype`: of Y (default: the
+        residual's, else X's, else bfloat16).  With `keep` (Y, Z): the values before the activation in Y's type, for the backward pass.
+        Records no graph (without `keep` tensors that require a gradient are refused outside torch.no_grad())."""
+        xq = xs = None
+        ldx = ldxq = ldxs = 0
+        if isinstance(X, torch.Tensor):
+            first = X
+        else:
+            xq, xs = X
+            first = xq
+        if not keep:
+            _no_graph(first, bias, residual)
+        self._ready(first, xs, W, Ws, bias, residual)
+        ldq, lds = _stored_strides(W, Ws, "W")
+        n, m = W.shape
+        if first.dim() != 2 or first.shape[1] != m:
+            raise ValueError("X has to be (t, %d), got %s" % (m, tuple(first.shape)))
+        t = first.shape[0]
+        if xq is None:
+            ldx = _row_stride(X, "X")
+        else:
+            ldxq, ldxs = _stored_strides(xq, xs, "X", 1)
+        if dtype is None:
+            dtype = residual.dtype if residual is not None else X.dtype if xq is None else torch.bfloat16
+        Y = W.new_empty((t, n), dtype=dtype)
+        Z = W.new_empty((t, n), dtype=dtype) if keep else None
+        y = _dtype(Y)
+        e = SlimEpilogue(None, y, _check_act(act), None, 0, None, n)
+        if bias is not None:
+            if bias.shape != (n,) or not bias.is_contiguous():
+                raise ValueError("bias has to be a contiguous vector of %d numbers" % n)
+            e.bias, e.bias_dtype = bias.data_ptr(), _dtype(bias)
+        if residual is not None:
+            if residual.shape != (t, n) or residual.dtype != dtype:
+                raise ValueError("residual has to be (%d, %d) of Y's type" % (t, n))
+            e.R, e.ldr = residual.data_ptr(), _row_stride(residual, "residual")
+        if keep:
+            e.Z = Z.data_ptr()
+        st = self.lib.slim_fp8_linear_act(self.ctx, X.data_ptr() if xq is None else None, _dtype(X) if xq is None else F16, t, ldx,
+                                          None if xq is None else xq.data_ptr(), ldxq, None if xs is None else xs.data_ptr(), ldxs,
+                                          W.data_ptr(), ldq, Ws.data_ptr(), lds, n, m, ctypes.byref(e), Y.data_ptr(), y, n)
+        if st:
+            self._check(st)
+        return (Y, Z) if keep else Y
+
+    def fp8_linear_act_backward(self, dY: torch.Tensor, Z: Optional[torch.Tensor], act: Optional[str], X: Optional[torch.Tensor],
+                                Wt: Optional[torch.Tensor], Wts: Optional[torch.Tensor], dw_dtype: Optional[torch.dtype] = None, dx: bool = True,
+                                dw: bool = True, db_dtype: Optional[torch.dtype] = None):
+        """(dX (t, m), dW (n, m), db (n,)) for dY and Z (t, n) and X (t, m) of one 16-bit type; Z is what fp8_linear_act kept (not
+        needed without an activation); dw_dtype: of dW (default: X's); db_dtype: of db, None: not wanted.  Without `dx` Wt and Wts may be
+        None, without `dw` X; the gradient that is not wanted is None.  That of the residual is dY."""
+        a = _check_act(act)
+        Z = Z if a else None
+        self._ready(dY, Z, X, Wt, Wts)
+        if not (dx or dw or db_dtype):
+            raise ValueError("no gradient is wanted")
+        if dY.dim() != 2:
+            raise ValueError("dY has to be a matrix")
+        t, n = dY.shape
+        if a and (Z is None or Z.shape != dY.shape or Z.dtype != dY.dtype):
+            raise ValueError("Z has to be of dY's shape and type")
+        ldqt = ldst = 0
+        m = 1
+        if dw:
+            if X is None or X.dim() != 2 or X.shape[0] != t or X.dtype != dY.dtype:
+                raise ValueError("X has to be a matrix of dY's tokens and type")
+            m = X.shape[1]
+        if dx:
+            if Wt is None or Wts is None:
+                raise ValueError("dX needs the stored weights of W^T")
+            ldqt, ldst = _stored_strides(Wt, Wts, "Wt")
+            if Wt.shape[1] != n or dw and Wt.shape[0] != m:
+                raise ValueError("Wt has to be (m, n) = (%s, %d), got %s" % (m if dw else "m", n, tuple(Wt.shape)))
+            m = Wt.shape[0]
+        dX = dY.new_empty((t, m)) if dx else None
+        dW = dY.new_empty((n, m), dtype=dw_dtype) if dw else None
+        db = dY.new_empty(n, dtype=db_dtype) if db_dtype else None
+        st = self.lib.slim_fp8_linear_act_backward(
+            self.ctx, dY.data_ptr(), None if Z is None else Z.data_ptr(), a, X.data_ptr() if dw else None, _dtype(dY), t, _row_stride(dY, "dY"),
+            0 if Z is None else _row_stride(Z, "Z"), _row_stride(X, "X") if dw else 0, Wt.data_ptr() if dx else None, ldqt,
+            Wts.data_ptr() if dx else None, ldst, n, m, dX.data_ptr() if dx else None, m, dW.data_ptr() if dw else None, _dtype(dW) if dw else F32, m,
+            None if db is None else db.data_ptr(), F32 if db is None else _dtype(db))
+        if st:
+            self._check(st)
+        return dX, dW, db
+
+    def add_norm(self, X: torch.Tensor, R: Optional[torch.Tensor], w: torch.Tensor, b: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                 rms: bool = False, y: bool = True, e4m3: bool = False, stats: bool = False, H: Optional[torch.Tensor] = None) -> AddNorm:
+        """The residual stream H = X + R (rounded to their type; R None: X) and its norm Y, as layer_norm's.  y: Y in X's type is wanted; e4m3:
+        its 8-bit form (q, s), which fp8_linear_act takes; stats: mean (None with `rms`) and rstd for the backward pass.  H may be given, X or R
+        among others.  Records no graph: without `stats` tensors that require a gradient are refused outside torch.no_grad()."""
+        if not stats:
+            _no_graph(X, R, w, b)
+        self._ready(X, R, w, b, H)
+        rows, cols = self._norm_shape(X, w, b)
+        if not (y or e4m3):
+            raise ValueError("neither form of the norm is wanted")
+        for v in (R, H):
+            if v is not None and (v.shape != X.shape or v.dtype != X.dtype):
+                raise ValueError("R and H have to be of X's shape and type")
+        if R is None:
+            if H is not None and H.data_ptr() != X.data_ptr():
+                raise ValueError("without R the stream is X itself")
+            H = X
+        elif H is None:
+            H = _empty_like(X)
+        Y = _empty_like(X) if y else None
+        q = s = mean = rstd = None
+        ldq = lds = 0
+        if e4m3:
+            blocks = (cols + 127) // 128
+            ldq, lds = (blocks | 1) * 128, (blocks + 3) // 4 * 4     # (rows an odd number of blocks apart: they spread over the channels of the L2)
+            q = X.new_empty((rows, ldq), dtype=_E4M3)[:, :cols]
+            s = X.new_empty((rows, lds), dtype=torch.uint8)[:, :blocks]
+        if stats:
+            mean = None if rms else X.new_empty(rows, dtype=torch.float32)
+            rstd = X.new_empty(rows, dtype=torch.float32)
+        p = lambda v: None if v is None else v.data_ptr()
+        st = self.lib.slim_add_norm(self.ctx, X.data_ptr(), p(R), _dtype(X), rows, cols, _row_stride(X, "X"), 0 if R is None else _row_stride(R, "R"),
+                                    w.data_ptr(), p(b), _dtype(w), eps, rms, H.data_ptr(), _row_stride(H, "H"), p(Y), cols, p(q), ldq, p(s), lds,
+                                    p(mean), p(rstd))
+        if st:
+            self._check(st)
+        return AddNorm(H, Y, q, s, mean, rstd)
+
+    def add_norm_backward(self, dY: torch.Tensor, dH: Optional[torch.Tensor], H: torch.Tensor, w: torch.Tensor, mean: Optional[torch.Tensor],
+                          rstd: torch.Tensor, bias: bool = False):
+        """(dX, dw, db): the gradient of X and of R alike, of weight and bias, from those of Y and, past the norm, of H (None: none); db is None
+        without `bias`."""
+        self._ready(dY, dH, H, w, mean, rstd)
+        rows, cols = self._norm_shape(H, w, None)
+        for v in (dY, dH):
+            if v is not None and (v.shape != H.shape or v.dtype != H.dtype):
+                raise ValueError("dY and dH have to be of H's shape and type")
+        for v in (mean, rstd):
+            if v is not None and (v.dtype != torch.float32 or v.shape != (rows,) or not v.is_contiguous()):
+                raise ValueError("mean and rstd have to be float32 vectors of H's rows")
+        dX, dw = _empty_like(H), torch.empty_like(w)
+        db = torch.empty_like(w) if bias else None
+        st = self.lib.slim_add_norm_backward(self.ctx, dY.data_ptr(), None if dH is None else dH.data_ptr(), H.data_ptr(), _dtype(H), rows, cols,
+                                             _row_stride(dY, "dY"), 0 if dH is None else _row_stride(dH, "dH"), _row_stride(H, "H"), w.data_ptr(),
+                                             _dtype(w), None if mean is None else mean.data_ptr(), rstd.data_ptr(), dX.data_ptr(), cols,
+                                             dw.data_ptr(), None if db is None else db.data_ptr())
+        if st:
+            self._check(st)
+        return dX, dw, db
+
+    def grad_norm(self, tensors: Sequence[torch.Tensor]) -> torch.Tensor:
+        """The norm of all of the tensors together: one float32 number on the device."""
+        tensors = list(tensors)
+        self._ready(*tensors)
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        st = self.lib.slim_grad_norm(self.ctx, _tensor_list(tensors, "tensors"), len(tensors), norm.data_ptr())
+        if st:
+            self._check(st)
+        return norm
+
+    def clip_gradients(self, tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+        """Scales the tensors by min(1, limit / norm), in place or into `out` (tensors of their shapes and types, which do not overlap them or one
+        another); returns their norm before that, one float32 number on the device.  A norm that is not finite leaves the values as they are."""
+        tensors = list(tensors)
+        self._ready(*tensors)
+        into = None
+        if out is not None:
+            out = list(out)
+            self._ready(*out)
+            if len(out) != len(tensors) or any(o.shape != t.shape or o.dtype != t.dtype for o, t in zip(out, tensors)):
+                raise ValueError("out has to hold tensors of the same shapes and types")
+            # (one description of rows for both: an output of other strides is described by its rows too)
+            if any(o.is_contiguous() != t.is_contiguous() for o, t in zip(out, tensors)):
+                into, tensors = _tensor_rows(out, "out"), _tensor_rows(tensors, "tensors")
+            else:
+                into, tensors = _tensor_list(out, "out"), _tensor_list(tensors, "tensors")
+        else:
+            tensors = _tensor_list(tensors, "tensors")
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        st = self.lib.slim_clip_gradients(self.ctx, tensors, into, len(tensors) // 5, float(limit), norm.data_ptr())
+        if st:
+            self._check(st)
+        return norm
 
     @staticmethod
     def _norm_shape(X, w, b):

@@ -1,0 +1,263 @@
+// The norm of many tensors together, and their scaling to a limit: n = sqrt(sum of all squares), g <- g min(1, limit / n).
+//
+// Bound by memory: everything is read twice, since the factor depends on all of it, and written once.  The tensors are one row of chunks of
+// 16 KiB; a launch takes up to 60 tensors (their addresses are its arguments, so that a captured call needs no table in memory).  First kernel:
+// a workgroup takes chunks blockIdx, blockIdx + gridDim, ... and leaves one sum of squares, in fp64: no square of an fp32 or bf16 number leaves its
+// range, and 10^9 of them added one after another in fp32 would lose their digits.  Second kernel: every workgroup adds these sums, in their
+// order, and scales its chunks, the last ones first: the end of what the first kernel read is still in the cache behind the L2.
+#include <memory>
+
+#include "piece_device.h"
+#include "slim_internal.h"
+
+namespace {
+
+using namespace slimnorm;
+
+constexpr int CL_TENSORS = 60, CL_THREADS = 256, CL_PIECES = 4, CL_BYTES = 16 * CL_THREADS * CL_PIECES, CL_PER_CU = 4;
+
+struct ClipTensor {
+  const void* in;
+  void* out;
+  int64_t n, cols, ldi, ldo;             // elements; ldi == ldo == 0: one after another
+  int64_t first;                         // chunks in front of it
+  int dtype;
+};
+struct ClipArgs {
+  ClipTensor t[CL_TENSORS];
+  int count;
+  int64_t chunks;
+};
+static_assert(sizeof(ClipArgs) <= 4096 - 64, "the arguments of a launch");
+
+// the tensor of a chunk (the same in every lane)
+__device__ __forceinline__ int tensor_of(const ClipArgs& a, int64_t chunk) {
+  int lo = 0, hi = a.count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.t[mid].first <= chunk) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+template <typename T, typename F>
+__device__ __forceinline__ void each_element(const ClipTensor& t, int64_t e0, F use) {
+  for (int i = threadIdx.x; i < CL_BYTES / (int)sizeof(T); i += CL_THREADS) {
+    const int64_t e = e0 + i;
+    if (e >= t.n) break;
+    const int64_t row = e / t.cols, col = e - row * t.cols;
+    use(row * t.ldi + col, row * t.ldo + col);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ double squares(const ClipTensor& t, int64_t chunk) {
+  constexpr int E = Piece<T>::E;
+  const int64_t e0 = chunk * (CL_BYTES / (int64_t)sizeof(T));
+  double s = 0.0;
+  if (t.ldi == 0) {
+    Piece<T> p[CL_PIECES];
+    const T* in = static_cast<const T*>(t.in) + e0;
+    const int64_t left = t.n - e0;
+#pragma unroll
+    for (int i = 0; i < CL_PIECES; ++i) {
+      const int c = (i * CL_THREADS + threadIdx.x) * E;
+      p[i].load(in + c, (int)min((int64_t)E, left - c));
+    }
+#pragma unroll
+    for (int i = 0; i < CL_PIECES; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const double v = (double)p[i].get(e);
+        s = fma(v, v, s);
+      }
+  } else {
+    each_element<T>(t, e0, [&](int64_t i, int64_t) {
+      const double v = (double)value<T>(t.in, i);
+      s = fma(v, v, s);
+    });
+  }
+  return s;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, float factor, bool copy) {
+  constexpr int E = Piece<T>::E;
+  const int64_t e0 = chunk * (CL_BYTES / (int64_t)sizeof(T));
+  if (t.ldi == 0) {
+    Piece<T> p[CL_PIECES];
+    const T* in = static_cast<const T*>(t.in) + e0;
+    T* out = static_cast<T*>(t.out) + e0;
+    const int64_t left = t.n - e0;
+#pragma unroll
+    for (int i = 0; i < CL_PIECES; ++i) {
+      const int c = (i * CL_THREADS + threadIdx.x) * E;
+      p[i].load(in + c, (int)min((int64_t)E, left - c));
+    }
+#pragma unroll
+    for (int i = 0; i < CL_PIECES; ++i) {
+      const int c = (i * CL_THREADS + threadIdx.x) * E;
+      if (!copy) {
+        float f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = p[i].get(e) * factor;
+        p[i].set(f);
+      }
+      p[i].store(out + c, (int)min((int64_t)E, left - c));
+    }
+  } else {
+    each_element<T>(t, e0, [&](int64_t i, int64_t o) {
+      if (copy) static_cast<T*>(t.out)[o] = static_cast<const T*>(t.in)[i];
+      else put<T>(t.out, o, value<T>(t.in, i) * factor);
+    });
+  }
+}
+
+__global__ __launch_bounds__(CL_THREADS) void clip_squares(ClipArgs a, double* __restrict__ sums) {
+  __shared__ double red[CL_THREADS / 64];
+  double s = 0.0;
+  for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const ClipTensor& t = a.t[tensor_of(a, chunk)];
+    const int64_t c = chunk - t.first;
+    s += t.dtype == SLIM_F32 ? squares<float>(t, c) : t.dtype == SLIM_F16 ? squares<__half>(t, c) : squares<__hip_bfloat16>(t, c);
+  }
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) sums[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ __launch_bounds__(CL_THREADS) void clip_scale(ClipArgs a, const double* __restrict__ sums, int parts, double limit, float* norm) {
+  __shared__ double red[CL_THREADS / 64];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += CL_THREADS) s += sums[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  const double n = sqrt((red[0] + red[1]) + (red[2] + red[3]));
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+  // a norm that is no finite number leaves everything as it is: the caller sees it and drops the step
+  const bool copy = !(n > limit) || !(n < __longlong_as_double(0x7ff0000000000000ll));
+  const float factor = copy ? 1.f : (float)(limit / n);
+  for (int64_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
+    const int64_t chunk = a.chunks - 1 - k;
+    const ClipTensor& t = a.t[tensor_of(a, chunk)];
+    if (copy && t.in == t.out) continue;
+    const int64_t c = chunk - t.first;
+    if (t.dtype == SLIM_F32) scale<float>(t, c, factor, copy);
+    else if (t.dtype == SLIM_F16) scale<__half>(t, c, factor, copy);
+    else scale<__hip_bfloat16>(t, c, factor, copy);
+  }
+}
+
+int64_t elements(const slim_tensor& t) { return t.rows * t.cols; }
+int64_t chunks_of(const slim_tensor& t) {
+  const int64_t per = CL_BYTES / (t.dtype == SLIM_F32 ? 4 : 2);
+  return (elements(t) + per - 1) / per;
+}
+
+slim_status check(slim_ctx* ctx, const char* fn, const slim_tensor* t, int count) {
+  SLIM_REQUIRE(ctx, count >= 0 && (t || count == 0), "%s: null list of %d tensors", fn, count);
+  for (int i = 0; i < count; ++i) {
+    SLIM_REQUIRE(ctx, t[i].rows >= 0 && t[i].cols >= 0, "%s: tensor %d is %lld x %lld", fn, i, (long long)t[i].rows, (long long)t[i].cols);
+    SLIM_REQUIRE(ctx, t[i].cols == 0 || t[i].rows <= (INT64_MAX >> 8) / t[i].cols, "%s: tensor %d is %lld x %lld", fn, i, (long long)t[i].rows,
+                 (long long)t[i].cols);
+    if (elements(t[i]) == 0) continue;
+    SLIM_REQUIRE(ctx, t[i].data && (t[i].rows == 1 || t[i].ld >= t[i].cols), "%s: null tensor %d, or rows that overlap (ld = %lld)", fn, i,
+                 (long long)t[i].ld);
+    if (t[i].dtype != SLIM_F16 && t[i].dtype != SLIM_BF16 && t[i].dtype != SLIM_F32)
+      return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: tensor %d is not F16, BF16 or F32", fn, i);
+  }
+  return SLIM_OK;
+}
+
+int grid_of(int64_t chunks, int ncu) { return (int)std::max<int64_t>(1, std::min<int64_t>(chunks, (int64_t)CL_PER_CU * ncu)); }
+size_t need(int count, int ncu) { return slim_ws_round(sizeof(double) * (size_t)std::max(1, slim_cdiv(count, CL_TENSORS)) * CL_PER_CU * ncu); }
+
+// the tensors from `at` on as arguments of one launch; returns the first one that did not fit
+int fill(ClipArgs& a, const slim_tensor* in, const slim_tensor* out, int at, int count) {
+  a.count = 0;
+  a.chunks = 0;
+  for (; at < count && a.count < CL_TENSORS; ++at) {
+    if (elements(in[at]) == 0) continue;
+    const slim_tensor &t = in[at], &o = out ? out[at] : in[at];
+    ClipTensor& c = a.t[a.count++];
+    c.in = t.data;
+    c.out = o.data;
+    c.n = elements(t);
+    c.cols = t.cols;
+    const bool dense = t.rows == 1 || (t.ld == t.cols && o.ld == o.cols);
+    c.ldi = dense ? 0 : t.ld;
+    c.ldo = dense ? 0 : o.ld;
+    c.first = a.chunks;
+    c.dtype = (int)t.dtype;
+    a.chunks += chunks_of(t);
+  }
+  return at;
+}
+
+slim_status norm_and_scale(slim_ctx* ctx, const char* fn, const slim_tensor* in, const slim_tensor* out, int count, double limit, float* norm) {
+  if (const slim_status st = slim_ws_reserve(ctx, need(count, ctx->num_cus)); st != SLIM_OK) return st;
+  double* sums = static_cast<double*>(slim_ws_alloc(ctx, need(count, ctx->num_cus)));
+  if (!sums) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
+  ClipArgs a;
+  int parts = 0;
+  for (int at = 0; at < count;) {
+    at = fill(a, in, out, at, count);
+    if (a.count == 0) break;
+    const int grid = grid_of(a.chunks, ctx->num_cus);
+    SLIM_LAUNCH(ctx, "clip_squares", clip_squares, dim3(grid), dim3(CL_THREADS), 0, a, sums + parts);
+    parts += grid;
+  }
+  if (!out) {
+    a.count = 0;
+    a.chunks = 0;
+    SLIM_LAUNCH(ctx, "clip_scale", clip_scale, dim3(1), dim3(CL_THREADS), 0, a, sums, parts, limit, norm);
+    return SLIM_OK;
+  }
+  for (int at = 0; at < count || norm;) {
+    if (at > 0 || count > CL_TENSORS || parts == 0) at = fill(a, in, out, at, count);
+    else at = count;                          // (one launch: the arguments are there)
+    SLIM_LAUNCH(ctx, "clip_scale", clip_scale, dim3(grid_of(a.chunks, ctx->num_cus)), dim3(CL_THREADS), 0, a, sums, parts, limit, norm);
+    norm = nullptr;
+  }
+  return SLIM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t slim_grad_norm_workspace(int count, int num_cus) { return count < 0 ? 0 : need(count, num_cus > 0 ? num_cus : 256); }
+
+slim_status slim_grad_norm(slim_ctx* ctx, const slim_tensor* tensors, int count, float* norm) {
+  if (!ctx) return SLIM_ERR_INVALID_ARG;
+  const char* fn = "slim_grad_norm";
+  if (const slim_status st = check(ctx, fn, tensors, count); st != SLIM_OK) return st;
+  SLIM_REQUIRE(ctx, norm, "%s: null norm", fn);
+  return norm_and_scale(ctx, fn, tensors, nullptr, count, 0.0, norm);
+}
+
+slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const slim_tensor* out, int count, double limit, float* norm) {
+  if (!ctx) return SLIM_ERR_INVALID_ARG;
+  const char* fn = "slim_clip_gradients";
+  if (const slim_status st = check(ctx, fn, tensors, count); st != SLIM_OK) return st;
+  SLIM_REQUIRE(ctx, norm, "%s: null norm", fn);
+  SLIM_REQUIRE(ctx, limit >= 0.0, "%s: limit = %g", fn, limit);
+  if (!out) out = tensors;
+  if (const slim_status st = check(ctx, fn, out, count); st != SLIM_OK) return st;
+  const std::unique_ptr<const void*[]> written(new (std::nothrow) const void*[(size_t)count + 1]);
+  if (!written) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: host memory", fn);
+  const void** end = written.get();
+  for (int i = 0; i < count; ++i) {
+    SLIM_REQUIRE(ctx, out[i].rows == tensors[i].rows && out[i].cols == tensors[i].cols && out[i].dtype == tensors[i].dtype,
+                 "%s: output %d is of another shape or type", fn, i);
+    if (elements(out[i])) *end++ = out[i].data;
+  }
+  std::sort(written.get(), end);
+  SLIM_REQUIRE(ctx, std::adjacent_find(written.get(), const_cast<const void**>(end)) == end, "%s: a tensor is written twice", fn);
+  return norm_and_scale(ctx, fn, tensors, out, count, limit, norm);
+}
+
+}  // extern "C"

@@ -89,6 +89,21 @@ __device__ __forceinline__ unsigned to_e4m3(unsigned a, unsigned b, float scale)
   return __builtin_bit_cast(unsigned, r);
 }
 
+// over a row of 16 lanes
+__device__ __forceinline__ unsigned row_max_x2(unsigned m) {
+  m = max_u16x2(m, (unsigned)dpp_b32<DPP_XOR1>((int)m));
+  m = max_u16x2(m, (unsigned)dpp_b32<DPP_XOR2>((int)m));
+  m = max_u16x2(m, (unsigned)dpp_b32<DPP_HALF_MIRROR>((int)m));
+  return max_u16x2(m, (unsigned)dpp_b32<DPP_MIRROR>((int)m));
+}
+// the scale byte of a block of 16 lanes x 8 elements
+template <typename T>
+__device__ __forceinline__ unsigned block_scale(const unsigned (&v)[4]) {
+  unsigned m = larger_half(row_max_x2(amax_x2(v)));
+  if (__builtin_expect(__any(m >= Half16<T>::INF), 0)) m = larger_half(row_max_x2(amax_finite_x2<T>(v)));
+  return scale_byte(Half16<T>::float_bits(m));
+}
+
 // Eight stored numbers times their scale as bf16, which holds them exactly (four significant bits, the exponents of fp32; what is below
 // 2^-126 may count as zero): the operand of the products whose sums keep 24 bits.  The matrix cores' own e4m3 products are summed in
 // groups of eight in which only about 13 bits below the largest product are kept (measured: of 2^16 - 2^16 + 2^k they lose 2^2 and less;
@@ -133,6 +148,14 @@ struct Operand {
   int64_t ld, lds;
   int rows, shift;
 };
+// What becomes of a sum before it is stored: y = act(sum + bias[a]) + R[b][a]; Z takes the sum with the bias.  R and Z are of C's type; any of
+// bias, R and Z may be null.
+struct Epilogue {
+  const void *bias, *R;
+  void* Z;
+  int64_t ldr, ldz;
+  int bias_dtype, act;
+};
 // C[b][a] = sum over nk blocks of A[a] . B[b]
 struct Product {
   Operand a, b;
@@ -140,6 +163,7 @@ struct Product {
   int64_t ldc;
   slim_dtype c_dtype;
   int nk;
+  const Epilogue* e;               // of a product that is alone in its launch, or null
 };
 // bytes of workspace of a set of products, enough too for those of fewer rows and shorter contractions; 256-byte multiples
 size_t gemm_workspace(const Product* p, int count, int num_cus);
@@ -154,17 +178,39 @@ struct Activations {
   int rows, cols;
   uint8_t *rows_q, *rows_s, *cols_q, *cols_s;
 };
+// The gradient of the values before an activation, X act'(Z) rounded to X's type, in the place of X; sums: X act'(Z) summed over every 128 rows (rows of
+// cols numbers) or null
+struct ActGradient {
+  const void* Z;
+  int64_t ldz;
+  int act;
+  float* sums;
+};
 slim_status quantize(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const Activations* a, int count);
+// the same of two matrices (the second may have no rows), of which the first is such a gradient; its forms may both be null
+slim_status quantize_gradient(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const Activations (&a)[2], const ActGradient& g);
+// out = the sums of `parts` rows of cols numbers, in fp64, of one of the float types
+slim_status join_columns(slim_ctx* ctx, const char* name, const float* sums, int parts, int cols, void* out, slim_dtype dtype);
 
 // ---- and fp8_few.hip: few tokens, or little work, in one launch -----------------------------------------------------
 bool takes_few_tokens(int n, int m, int t, int ncu);
-slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, void* Y,
-                       slim_dtype y_dtype, int64_t ldy);
+// X (t x m, 16 bits), or, where it is null, its 8-bit form xq; e may be null for the former
+slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& xq, const Operand& w, int m,
+                       const Epilogue* e, void* Y, slim_dtype y_dtype, int64_t ldy);
 
 // value to one of the output types, rounded to nearest even
 __device__ __forceinline__ unsigned short to_16(float v, bool bf16) {
   if (bf16) return __builtin_bit_cast(unsigned short, (__bf16)v);
   return __builtin_bit_cast(unsigned short, (_Float16)v);
+}
+__device__ __forceinline__ float from_any(const void* p, int dtype, int64_t i) {
+  if (dtype == SLIM_F32) return static_cast<const float*>(p)[i];
+  const unsigned h = static_cast<const unsigned short*>(p)[i];
+  return __uint_as_float(dtype == SLIM_BF16 ? Half16<__hip_bfloat16>::float_bits(h) : Half16<__half>::float_bits(h));
+}
+__device__ __forceinline__ void to_any(void* p, int dtype, int64_t i, float v) {
+  if (dtype == SLIM_F32) static_cast<float*>(p)[i] = v;
+  else static_cast<unsigned short*>(p)[i] = to_16(v, dtype == SLIM_BF16);
 }
 
 }  // namespace slimfp8

@@ -9,6 +9,7 @@
 // products end and after its registers are free: with eight wavefronts on a CU deeper rings of registers gained nothing (46.6 and 44.4 us).
 //
 // 28672 x 8192: 44 us for 16 tokens, 43 for one (5.4 and 5.5 TB/s; a kernel that only reads reaches 6.3 to 7.0).
+#include "act_device.h"
 #include "fp8_device.h"
 
 namespace {
@@ -25,17 +26,24 @@ struct FewArgs {
   int64_t ldx, ldq, lds, ldy;
   int t, n, m, mb;                  // mb: blocks of channels
   int y_dtype;
+  const uint8_t *xq, *xs;           // the activations' 8-bit form (T = uint8_t)
+  int64_t ldxq, ldxs;
+  Epilogue e;                       // (EPI)
 };
 
-template <typename T, int RT>
+// T = uint8_t: the activations come in 8 bits (rows of whole blocks).  EPI: bias, activation, residual, before the outputs are stored.
+template <typename T, int RT, bool EPI>
 __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   constexpr int ROWS = 16 * RT, LD = ROWS + 4;                 // floats per token of a wavefront's sums
+  constexpr bool Q8 = sizeof(T) == 1;
   extern __shared__ __align__(16) float part[];                // [wavefront][token][row]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), nw = blockDim.x >> 6;
   const int l16 = lane & 15, c = lane >> 4;
   const int row0 = blockIdx.x * ROWS, tok0 = blockIdx.y * 16, tn = min(16, a.t - tok0);
   // (tokens that do not exist are the last one again: their columns of the product are not stored)
-  const T* xrow = static_cast<const T*>(a.X) + (int64_t)min(tok0 + l16, a.t - 1) * a.ldx + c * 16;
+  const T* xrow = Q8 ? (const T*)(a.xq + (int64_t)min(tok0 + l16, a.t - 1) * a.ldxq + c * 16)
+                     : static_cast<const T*>(a.X) + (int64_t)min(tok0 + l16, a.t - 1) * a.ldx + c * 16;
+  const uint8_t* xsrow = Q8 ? a.xs + (int64_t)min(tok0 + l16, a.t - 1) * a.ldxs : nullptr;
   const uint8_t* wrow[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) wrow[r] = a.q + (int64_t)min(row0 + r * 16 + l16, a.n - 1) * a.ldq + c * 16;
@@ -47,11 +55,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   for (int r = 0; r < RT; ++r) acc[r] = v4f{0.f, 0.f, 0.f, 0.f};
 
   const int per = (a.mb + nw - 1) / nw, first = wave * per, end = min(a.mb, first + per);
-  unsigned x[16];
+  unsigned x[Q8 ? 8 : 16];
   uint4 w[RT][2];
   auto load = [&](int kb) {
     const int ch = kb * BLOCK;
-    if (ch + BLOCK <= a.m) {
+    if constexpr (Q8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) __builtin_memcpy(&x[4 * h], xrow + ch + h * 64, 16);
+    } else if (ch + BLOCK <= a.m) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) __builtin_memcpy(&x[4 * h], xrow + ch + (h >> 1) * 64 + (h & 1) * 8, 16);
     } else {                                                    // (behind the last channel everything reads as zero)
@@ -68,27 +79,34 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   };
   auto block = [&](int kb) {
     const int ch = kb * BLOCK;
-    if (ch + BLOCK > a.m && a.m >= 8)
+    if (!Q8 && ch + BLOCK > a.m && a.m >= 8)
 #pragma unroll
-      for (int h = 0; h < 4; ++h) row_end_shift<8>(*reinterpret_cast<unsigned(*)[4]>(&x[4 * h]), a.m - ch - (h >> 1) * 64 - (h & 1) * 8 - c * 16);
+      for (int h = 0; h < (Q8 ? 0 : 4); ++h) row_end_shift<8>(*reinterpret_cast<unsigned(*)[4]>(&x[4 * h]), a.m - ch - (h >> 1) * 64 - (h & 1) * 8 - c * 16);
     float sw[2];
 #pragma unroll
     for (int i = 0; i < (128 % (16 * RT) ? 2 : 1); ++i)
       sw[i] = __uint_as_float(((*reinterpret_cast<const unsigned*>(srow[i] + (kb & ~3)) >> (8 * (kb & 3))) & 255u) << 23);
-    unsigned mx = amax_x2(x);
-    mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
-    mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
-    unsigned top = larger_half(mx);
-    if (__builtin_expect(__any(top >= Half16<T>::INF), 0)) {
-      mx = amax_finite_x2<T>(x);
+    float sx;
+    if constexpr (Q8) {
+      sx = __uint_as_float((unsigned)xsrow[kb] << 23);
+    } else {
+      unsigned mx = amax_x2(x);
       mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
       mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
-      top = larger_half(mx);
+      unsigned top = larger_half(mx);
+      if (__builtin_expect(__any(top >= Half16<T>::INF), 0)) {
+        mx = amax_finite_x2<T>(x);
+        mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 16, 64));
+        mx = max_u16x2(mx, (unsigned)__shfl_xor((int)mx, 32, 64));
+        top = larger_half(mx);
+      }
+      sx = __uint_as_float(scale_byte(Half16<T>::float_bits(top)) << 23);
     }
-    const float sx = __uint_as_float(scale_byte(Half16<T>::float_bits(top)) << 23);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const v8bf xb = dequantized((int)to_e4m3<T>(x[4 * i], x[4 * i + 1], sx), (int)to_e4m3<T>(x[4 * i + 2], x[4 * i + 3], sx), sx);
+      v8bf xb;
+      if constexpr (Q8) xb = dequantized((int)x[2 * i], (int)x[2 * i + 1], sx);
+      else xb = dequantized((int)to_e4m3<T>(x[4 * i], x[4 * i + 1], sx), (int)to_e4m3<T>(x[4 * i + 2], x[4 * i + 3], sx), sx);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const uint4 wv = w[r][i >> 1];
@@ -111,18 +129,24 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
     float sum = 0.f;
     for (int i = 0; i < nw; ++i) sum += part[(i * 16 + tok) * LD + r];
     if (r < last) {
-      const int64_t at = (int64_t)(tok0 + tok) * a.ldy + row0 + r;
-      if (a.y_dtype == SLIM_F32) static_cast<float*>(a.Y)[at] = sum;
-      else static_cast<unsigned short*>(a.Y)[at] = to_16(sum, a.y_dtype == SLIM_BF16);
+      if constexpr (EPI) {
+        const int64_t row = tok0 + tok;
+        const int col = row0 + r;
+        if (a.e.bias) sum += from_any(a.e.bias, a.e.bias_dtype, col);
+        if (a.e.Z) to_any(a.e.Z, a.y_dtype, row * a.e.ldz + col, sum);
+        sum = slimact::activated(sum, a.e.act);
+        if (a.e.R) sum += from_any(a.e.R, a.y_dtype, row * a.e.ldr + col);
+      }
+      to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
     }
   }
 }
 
-template <typename T, int RT>
+template <typename T, bool EPI, int RT>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
   constexpr int ROWS = 16 * RT;
   const int nw = std::min(FEW_WAVES, a.mb);
-  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT>), dim3(slim_cdiv(a.n, ROWS), slim_cdiv(a.t, 16)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
+  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT, EPI>), dim3(slim_cdiv(a.n, ROWS), slim_cdiv(a.t, 16)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
   return SLIM_OK;
 }
 
@@ -144,16 +168,16 @@ int sixteens(int n, int t, int ncu) {
   return rt;
 }
 
-template <typename T>
+template <typename T, bool EPI>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
   switch (sixteens(a.n, a.t, ctx->num_cus)) {
-    case 1: return launch<T, 1>(ctx, a);
-    case 2: return launch<T, 2>(ctx, a);
-    case 3: return launch<T, 3>(ctx, a);
-    case 4: return launch<T, 4>(ctx, a);
-    case 5: return launch<T, 5>(ctx, a);
-    case 6: return launch<T, 6>(ctx, a);
-    default: return launch<T, FEW_RT>(ctx, a);
+    case 1: return launch<T, EPI, 1>(ctx, a);
+    case 2: return launch<T, EPI, 2>(ctx, a);
+    case 3: return launch<T, EPI, 3>(ctx, a);
+    case 4: return launch<T, EPI, 4>(ctx, a);
+    case 5: return launch<T, EPI, 5>(ctx, a);
+    case 6: return launch<T, EPI, 6>(ctx, a);
+    default: return launch<T, EPI, FEW_RT>(ctx, a);
   }
 }
 
@@ -171,10 +195,13 @@ bool takes_few_tokens(int n, int m, int t, int ncu) {
   return t <= 16 || (t <= 65535 * 16 && least_busiest(n, t, ncu) * slim_cdiv(m, BLOCK) <= 64);
 }
 
-slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, void* Y,
-                       slim_dtype y_dtype, int64_t ldy) {
-  const FewArgs a = {X, w.q, w.s, Y, ldx, w.ld, w.lds, ldy, t, w.rows, m, slim_cdiv(m, BLOCK), (int)y_dtype};
-  return x_dtype == SLIM_F16 ? launch<__half>(ctx, a) : launch<__hip_bfloat16>(ctx, a);
+slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& xq, const Operand& w, int m,
+                       const Epilogue* e, void* Y, slim_dtype y_dtype, int64_t ldy) {
+  FewArgs a = {X, w.q, w.s, Y, ldx, w.ld, w.lds, ldy, t, w.rows, m, slim_cdiv(m, BLOCK), (int)y_dtype, xq.q, xq.s, xq.ld, xq.lds, {}};
+  if (e) a.e = *e;
+  if (!X) return launch<uint8_t, true>(ctx, a);
+  if (e) return x_dtype == SLIM_F16 ? launch<__half, true>(ctx, a) : launch<__hip_bfloat16, true>(ctx, a);
+  return x_dtype == SLIM_F16 ? launch<__half, false>(ctx, a) : launch<__hip_bfloat16, false>(ctx, a);
 }
 
 }  // namespace slimfp8

@@ -20,6 +20,7 @@
 // cores at the clock the power allows).
 #include <atomic>
 
+#include "act_device.h"
 #include "fp8_device.h"
 
 namespace {
@@ -39,6 +40,7 @@ struct ProductArgs {
 struct GemmArgs {
   ProductArgs p[2];
   int first;                               // workgroups of the first product
+  Epilogue e;                              // (EPI)
 };
 
 // Direct loads, if step `k` is below `n` (the branch is in here so that the code around it stays one block for the scheduler).
@@ -118,6 +120,70 @@ __device__ __forceinline__ void store4(void* row, int dtype, int col, int left, 
   }
 }
 
+// four values of a row from column `col` on as floats, of which `left` exist (the others are zero)
+__device__ __forceinline__ float4 load_any4(const void* row, int dtype, int col, int left) {
+  float f[4] = {0.f, 0.f, 0.f, 0.f};
+  if (dtype == SLIM_F32) {
+    const float* p = static_cast<const float*>(row) + col;
+    if (left >= 4) {
+      __builtin_memcpy(f, p, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < left) f[i] = p[i];
+    }
+  } else {
+    const unsigned short* p = static_cast<const unsigned short*>(row) + col;
+    unsigned short h[4] = {0, 0, 0, 0};
+    if (left >= 4) {
+      __builtin_memcpy(h, p, 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < left) h[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      f[i] = __uint_as_float(dtype == SLIM_BF16 ? Half16<__hip_bfloat16>::float_bits(h[i]) : Half16<__half>::float_bits(h[i]));
+  }
+  return make_float4(f[0], f[1], f[2], f[3]);
+}
+
+// N quads of sums through the epilogue, quad i of row `row[i]` of C from column `col` on, of which `left` exist: the residuals first, so that their
+// loads are under way together (Z and C are stored here; rows behind the last one are left out)
+template <int N>
+__device__ __forceinline__ void finish(const Epilogue& e, char* c, int64_t ldc, int dtype, int row, int step, int rows, int col, int left, float (&v)[4 * N]) {
+  const int64_t size = dtype == SLIM_F32 ? 4 : 2;
+  float4 r[N];
+  if (e.R)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (row + i * step < rows) r[i] = load_any4(static_cast<const char*>(e.R) + (row + i * step) * e.ldr * size, dtype, col, left);
+  if (e.bias) {
+    const float4 b = load_any4(e.bias, e.bias_dtype, col, left);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[4 * i] += b.x;
+      v[4 * i + 1] += b.y;
+      v[4 * i + 2] += b.z;
+      v[4 * i + 3] += b.w;
+    }
+  }
+  if (e.Z)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (row + i * step < rows)
+        store4(static_cast<char*>(e.Z) + (row + i * step) * e.ldz * size, dtype, col, left, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+  slimact::activate(v, e.act);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (row + i * step < rows) {
+      float4 y = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      if (e.R) y = make_float4(y.x + r[i].x, y.y + r[i].y, y.z + r[i].z, y.w + r[i].w);
+      store4(c + (row + i * step) * ldc * size, dtype, col, left, y);
+    }
+}
+
 // The operands of half a step (64 of the contraction) in registers: 32 bytes per lane and 32 rows
 template <typename T>
 struct Half {
@@ -147,8 +213,8 @@ __device__ __forceinline__ void read_operand(Half<T>& f, const char* st, const P
 template <int M>
 __device__ __forceinline__ constexpr int share_from(int m, int n) { return m * 2 >= M ? n : m * 2 * n / M; }
 
-// EXACT: products of the numbers in bf16 (fp32 outputs)
-template <typename T, bool EXACT>
+// EXACT: products of the numbers in bf16 (fp32 outputs).  EPI: one product, with an epilogue.
+template <typename T, bool EXACT, bool EPI>
 __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_gemm(GemmArgs ga) {
   constexpr int MA = T::MA, MB = T::MB, M = MA * MB, READS = 2 * (MA + MB), S = T::STAGES;
   extern __shared__ __align__(16) char smem_fg[];
@@ -363,22 +429,35 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(out + l32 * T::OUT_LD + i * 32 + q * 8 + h * 4) =
             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    if constexpr (EPI) {
+      constexpr int N = 4;
+      const int col = (lane % QUADS) * 4, ca = a0 + wa * T::MA * 32 + col;
+#pragma unroll 1
+      for (int r = lane / QUADS; r < 32; r += N * RPI) {
+        float v[4 * N];
 #pragma unroll
-    for (int r = 0; r < 32; r += RPI) {
-      const int rr = r + lane / QUADS, col = (lane % QUADS) * 4;
-      const float4 v = *reinterpret_cast<const float4*>(out + rr * T::OUT_LD + col);
-      const int row = b0 + (wb * T::MB + j) * 32 + rr, ca = a0 + wa * T::MA * 32 + col;
-      if (row < p.b.rows) store4(cbase + (int64_t)row * p.ldc * esize, p.c_dtype, ca, p.a.rows - ca, v);
+        for (int i = 0; i < N; ++i) *reinterpret_cast<float4*>(&v[4 * i]) = *reinterpret_cast<const float4*>(out + (r + i * RPI) * T::OUT_LD + col);
+        if (ca < p.a.rows) finish<N>(ga.e, cbase, p.ldc, p.c_dtype, b0 + (wb * T::MB + j) * 32 + r, RPI, p.b.rows, ca, p.a.rows - ca, v);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 32; r += RPI) {
+        const int rr = r + lane / QUADS, col = (lane % QUADS) * 4;
+        const float4 v = *reinterpret_cast<const float4*>(out + rr * T::OUT_LD + col);
+        const int row = b0 + (wb * T::MB + j) * 32 + rr, ca = a0 + wa * T::MA * 32 + col;
+        if (row < p.b.rows) store4(cbase + (int64_t)row * p.ldc * esize, p.c_dtype, ca, p.a.rows - ca, v);
+      }
     }
   }
 }
 
 // C = the sum of a product's parts, in their order
-__global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __restrict__ parts, int64_t ldp, void* c, int64_t ldc, int dtype) {
+template <bool EPI>
+__global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __restrict__ parts, int64_t ldp, void* c, int64_t ldc, int dtype, Epilogue e) {
   const int quads = (p.a.rows + 3) / 4;
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= (int64_t)quads * p.b.rows) return;
-  const int row = (int)(e / quads), col = (int)(e % quads) * 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)quads * p.b.rows) return;
+  const int row = (int)(id / quads), col = (int)(id % quads) * 4;
   const float* src = parts + (int64_t)row * ldp + col;
   float4 s = *reinterpret_cast<const float4*>(src);
   for (int i = 1; i < p.splits; ++i) {
@@ -387,6 +466,10 @@ __global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __re
     s.y += v.y;
     s.z += v.z;
     s.w += v.w;
+  }
+  if constexpr (EPI) {
+    float v[4] = {s.x, s.y, s.z, s.w};
+    return finish<1>(e, static_cast<char*>(c), ldc, dtype, row, 1, p.b.rows, col, p.a.rows - col, v);
   }
   store4(static_cast<char*>(c) + (int64_t)row * ldc * (dtype == SLIM_F32 ? 4 : 2), dtype, col, p.a.rows - col, s);
 }
@@ -456,21 +539,27 @@ size_t parts_bytes(const Product& p, int ncu) {
   return most < 2 ? 0 : slim_ws_round(sizeof(float) * (size_t)std::min((int64_t)ncu * Large::TA * Large::TB, most * ldp * p.b.rows));
 }
 
-template <typename T, bool EXACT>
+template <typename T, bool EXACT, bool EPI>
 slim_status launch(slim_ctx* ctx, const char* name, const GemmArgs& ga, int grid) {
   // (an attribute of the function on the device, asked for once: it costs a call as much as a third of the launch)
   static std::atomic<uint64_t> allowed{0};
   const uint64_t bit = ctx->device < 64 ? 1ull << ctx->device : 0;
   if (T::LDS > 64 * 1024 && !(allowed.load(std::memory_order_relaxed) & bit)) {
-    SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_gemm<T, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+    SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_gemm<T, EXACT, EPI>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
     allowed.fetch_or(bit, std::memory_order_relaxed);
   }
-  SLIM_LAUNCH(ctx, name, (fp8_gemm<T, EXACT>), dim3(grid), dim3(T::THREADS), T::LDS, ga);
+  SLIM_LAUNCH(ctx, name, (fp8_gemm<T, EXACT, EPI>), dim3(grid), dim3(T::THREADS), T::LDS, ga);
   return SLIM_OK;
 }
-template <bool EXACT>
+template <bool EXACT, bool EPI>
 slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid) {
-  return tile == TILE_LARGE ? launch<Large, EXACT>(ctx, name, ga, grid) : tile == TILE_MEDIUM ? launch<Medium, EXACT>(ctx, name, ga, grid) : launch<Small, EXACT>(ctx, name, ga, grid);
+  return tile == TILE_LARGE    ? launch<Large, EXACT, EPI>(ctx, name, ga, grid)
+         : tile == TILE_MEDIUM ? launch<Medium, EXACT, EPI>(ctx, name, ga, grid)
+                               : launch<Small, EXACT, EPI>(ctx, name, ga, grid);
+}
+template <bool EXACT>
+slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid, bool epilogue) {
+  return epilogue ? launch<EXACT, true>(ctx, name, tile, ga, grid) : launch<EXACT, false>(ctx, name, tile, ga, grid);
 }
 
 slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count) {
@@ -502,13 +591,17 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
     if (i == 0) ga.first = q.tiles_a * q.tiles_b * q.splits;
     grid += q.tiles_a * q.tiles_b * q.splits;
   }
-  const slim_status st = p[0].c_dtype == SLIM_F32 ? launch<true>(ctx, name, tile, ga, grid) : launch<false>(ctx, name, tile, ga, grid);
+  const Epilogue* const e = p[0].e;          // (where the product is cut, the parts' sum goes through it)
+  if (e) ga.e = *e;
+  const bool whole = e && !parts[0];
+  const slim_status st = p[0].c_dtype == SLIM_F32 ? launch<true>(ctx, name, tile, ga, grid, whole) : launch<false>(ctx, name, tile, ga, grid, whole);
   if (st != SLIM_OK) return st;
   for (int i = 0; i < count; ++i)
     if (parts[i]) {
       const int64_t quads = (int64_t)slim_cdiv(p[i].a.rows, 4) * p[i].b.rows;
-      SLIM_LAUNCH(ctx, "fp8_join", fp8_join, dim3(slim_cdiv(quads, 256)), dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc,
-                  (int)p[i].c_dtype);
+      const dim3 g(slim_cdiv(quads, 256));
+      if (e) SLIM_LAUNCH(ctx, "fp8_join", fp8_join<true>, g, dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc, (int)p[i].c_dtype, ga.e);
+      else SLIM_LAUNCH(ctx, "fp8_join", fp8_join<false>, g, dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc, (int)p[i].c_dtype, ga.e);
     }
   return SLIM_OK;
 }

@@ -5,6 +5,7 @@
 // above infinity's, and only then is the search done again without it.  The transposed form (blocks of 128 tokens, for the gradient of
 // the weights) takes a tile of 128 x 128 through LDS once, in bytes; the gradient of the outputs needs both forms and is read once for
 // them.
+#include "act_device.h"
 #include "fp8_device.h"
 
 namespace {
@@ -12,20 +13,6 @@ namespace {
 using namespace slimfp8;
 
 constexpr int RQ_THREADS = 256, RQ_UNITS = 2;     // units of 512 elements a wavefront holds at a time
-
-__device__ __forceinline__ unsigned row_max_x2(unsigned m) {
-  m = max_u16x2(m, (unsigned)dpp_b32<DPP_XOR1>((int)m));
-  m = max_u16x2(m, (unsigned)dpp_b32<DPP_XOR2>((int)m));
-  m = max_u16x2(m, (unsigned)dpp_b32<DPP_HALF_MIRROR>((int)m));
-  return max_u16x2(m, (unsigned)dpp_b32<DPP_MIRROR>((int)m));
-}
-// the scale byte of a block of 16 lanes x 8 elements
-template <typename T>
-__device__ __forceinline__ unsigned block_scale(const unsigned (&v)[4]) {
-  unsigned m = larger_half(row_max_x2(amax_x2(v)));
-  if (__builtin_expect(__any(m >= Half16<T>::INF), 0)) m = larger_half(row_max_x2(amax_finite_x2<T>(v)));
-  return scale_byte(Half16<T>::float_bits(m));
-}
 
 // Rows: a wavefront takes units of 512 elements (four blocks) of one row.
 template <typename T>
@@ -58,12 +45,15 @@ __global__ __launch_bounds__(RQ_THREADS) void fp8_rows(const T* __restrict__ X, 
 struct TileArgs {
   Activations a[2];
   int tiles[2], tiles_c[2];        // tiles of 128 x 128, and along the columns
+  ActGradient g;                   // (ACT: of the first matrix)
 };
 
-// Tiles of 128 x 128: thread t holds rows 8 (t / 16) .. + 7 of columns 8 (t % 16) .. + 7.
-template <typename T>
+// Tiles of 128 x 128: thread t holds rows 8 (t / 16) .. + 7 of columns 8 (t % 16) .. + 7.  ACT: the first matrix is the gradient behind an
+// activation; it is formed in fp32 and rounded in its place, and its columns' sums are taken before the rounding.
+template <typename T, bool ACT>
 __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
   __shared__ __align__(16) unsigned colmax[4][64];         // per wavefront, pairs of columns
+  __shared__ __align__(16) float colsum[ACT ? 4 : 1][BLOCK];
   __shared__ __align__(16) uint8_t tile[BLOCK * BLOCK];    // [column][row], units of 8 bytes at unit ^ (column / 8)
   const int p = (int)blockIdx.x >= ta.tiles[0];
   const Activations& a = ta.a[p];
@@ -80,6 +70,43 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
     row_end_shift<8>(v[i], a.cols < 8 ? 8 : a.cols - c0);
     if (r0 + i >= a.rows) v[i][0] = v[i][1] = v[i][2] = v[i][3] = 0u;
   }
+  if constexpr (ACT)
+    if (p == 0) {
+      float cs[8] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        unsigned z[4];
+        if (ta.g.Z) {
+          fetch8(static_cast<const T*>(ta.g.Z) + (int64_t)min(r0 + i, a.rows - 1) * ta.g.ldz + c0, a.cols - c0, a.cols, z);
+          row_end_shift<8>(z, a.cols < 8 ? 8 : a.cols - c0);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float d[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            d[h] = __uint_as_float(Half16<T>::float_bits((v[i][j] >> (16 * h)) & 0xffffu));
+            if (ta.g.Z && r0 + i < a.rows) d[h] *= slimact::slope(__uint_as_float(Half16<T>::float_bits((z[j] >> (16 * h)) & 0xffffu)), ta.g.act);
+            cs[2 * j + h] += d[h];
+          }
+          v[i][j] = (unsigned)to_16(d[0], Half16<T>::INF == 0x7f80u) | (unsigned)to_16(d[1], Half16<T>::INF == 0x7f80u) << 16;
+        }
+      }
+      if (ta.g.sums) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          cs[e] += __shfl_xor(cs[e], 16, 64);
+          cs[e] += __shfl_xor(cs[e], 32, 64);
+        }
+        if (lane < 16) {
+          *reinterpret_cast<float4*>(&colsum[wave][cg * 8]) = make_float4(cs[0], cs[1], cs[2], cs[3]);
+          *reinterpret_cast<float4*>(&colsum[wave][cg * 8 + 4]) = make_float4(cs[4], cs[5], cs[6], cs[7]);
+        }
+        __syncthreads();
+        if (tid < BLOCK && tc * BLOCK + tid < a.cols)
+          ta.g.sums[(int64_t)tr * a.cols + tc * BLOCK + tid] = (colsum[0][tid] + colsum[1][tid]) + (colsum[2][tid] + colsum[3][tid]);
+      }
+    }
   // Largest magnitudes.  Rows: of the lane's eight numbers, two rows to a word, then over the 16 lanes of a row; columns: of the lane's
   // eight rows, the four groups of 16 lanes, the four wavefronts.
   unsigned rm[4], m[4];
@@ -162,6 +189,20 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
     uint4 w = *reinterpret_cast<const uint4*>(tile + c * BLOCK + ((2 * u) ^ (x & 14)) * 8);
     if (x & 1) w = make_uint4(w.z, w.w, w.x, w.y);
     if (tc * BLOCK + c < a.cols) *reinterpret_cast<uint4*>(a.cols_q + (int64_t)(tc * BLOCK + c) * ldq + tr * BLOCK + u * 16) = w;
+  }
+}
+
+// out = the columns' sums of `parts` rows: 32 columns x 32 ranges of rows, in fp64
+__global__ __launch_bounds__(1024) void fp8_join_columns(const float* __restrict__ sums, int parts, int cols, void* out, int dtype) {
+  __shared__ double red[32][33];
+  const int x = threadIdx.x & 31, c = blockIdx.x * 32 + x, k = threadIdx.x >> 5;
+  double s = 0.0;
+  for (int i = k; i < parts; i += 32) s += (double)sums[(int64_t)i * cols + min(c, cols - 1)];
+  red[k][x] = s;
+  __syncthreads();
+  if (k == 0 && c < cols) {
+    for (int i = 1; i < 32; ++i) s += red[i][x];
+    to_any(out, dtype, c, (float)s);
   }
 }
 
@@ -254,9 +295,31 @@ slim_status quantize(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const 
     tiles += ta.tiles[i];
   }
   if (x_dtype == SLIM_F16)
-    SLIM_LAUNCH(ctx, name, fp8_tiles<__half>, dim3(tiles), dim3(256), 0, ta);
+    SLIM_LAUNCH(ctx, name, (fp8_tiles<__half, false>), dim3(tiles), dim3(256), 0, ta);
   else
-    SLIM_LAUNCH(ctx, name, fp8_tiles<__hip_bfloat16>, dim3(tiles), dim3(256), 0, ta);
+    SLIM_LAUNCH(ctx, name, (fp8_tiles<__hip_bfloat16, false>), dim3(tiles), dim3(256), 0, ta);
+  return SLIM_OK;
+}
+
+slim_status quantize_gradient(slim_ctx* ctx, const char* name, slim_dtype x_dtype, const Activations (&a)[2], const ActGradient& g) {
+  TileArgs ta = {};
+  ta.g = g;
+  int tiles = 0;
+  for (int i = 0; i < 2; ++i) {
+    ta.a[i] = a[i];
+    ta.tiles_c[i] = slim_cdiv(a[i].cols, BLOCK);
+    ta.tiles[i] = ta.tiles_c[i] * slim_cdiv(a[i].rows, BLOCK);
+    tiles += ta.tiles[i];
+  }
+  if (x_dtype == SLIM_F16)
+    SLIM_LAUNCH(ctx, name, (fp8_tiles<__half, true>), dim3(tiles), dim3(256), 0, ta);
+  else
+    SLIM_LAUNCH(ctx, name, (fp8_tiles<__hip_bfloat16, true>), dim3(tiles), dim3(256), 0, ta);
+  return SLIM_OK;
+}
+
+slim_status join_columns(slim_ctx* ctx, const char* name, const float* sums, int parts, int cols, void* out, slim_dtype dtype) {
+  SLIM_LAUNCH(ctx, name, fp8_join_columns, dim3(slim_cdiv(cols, 32)), dim3(1024), 0, sums, parts, cols, out, (int)dtype);
   return SLIM_OK;
 }
 
