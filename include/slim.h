@@ -499,6 +499,24 @@ size_t slim_grad_norm_workspace(int count, int num_cus);
 slim_status slim_grad_norm(slim_ctx* ctx, const slim_tensor* tensors, int count, float* norm);
 slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const slim_tensor* out, int count, double limit, float* norm);
 
+/* The cross entropy of labels in the softmax of an 8-bit head's outputs, and its gradients, without these outputs (t x V logits) in memory.
+ *   X        t x m, F16 or BF16, quantised along the channels as in slim_fp8_linear;  q, s: the head W (V x m) as slim_fp8_quantize_weights writes it
+ *   labels   t classes, int64 (labels64 != 0) or int32; what lies outside 0 .. V - 1, -100 say, is no label: loss 0, no gradient
+ *   loss     t: ln sum exp z - z[label] for z = Q(X) W^T, whose sums keep 24 bits
+ *   dloss    t: the gradients of the losses (not read where there is no label)
+ *   dX       t x m of X's type, or NULL: Q(dz) W for dz = dloss (softmax z - [label]), in e4m3 in blocks of 128 classes, from the stored form qt, st of
+ *            W^T (not read without dX); sums on the e4m3 matrix cores, between pieces of the vocabulary in fp32
+ *   dW       V x m, F16, BF16 or F32, or NULL: Qt(dz)^T Qt(X), both in blocks of 128 tokens, sums as in slim_fp8_linear_backward.  A row of X without a
+ *            label adds nothing to dW if it is finite.
+ * The gradients take the logits a second time, a piece of the vocabulary after another: 16 Mi of them, or 1024 classes, at a time. */
+size_t slim_head_loss_workspace(int V, int m, int t, int num_cus);
+slim_status slim_head_loss(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
+                           int64_t lds, int V, int m, const void* labels, int labels64, float* loss);
+size_t slim_head_loss_grad_workspace(int V, int m, int t, int dx, int dw, slim_dtype dw_dtype, int num_cus);
+slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
+                                int64_t lds, const uint8_t* qt, int64_t ldqt, const uint8_t* st, int64_t ldst, int V, int m, const void* labels,
+                                int labels64, const float* dloss, float* loss, void* dX, int64_t lddx, void* dW, slim_dtype dw_dtype, int64_t lddw);
+
 /* ---------------------------------------------------------------------------------------------
  * Per-kernel timing with HIP events on the context's stream (measurement aid, host only).
  * While enabled, every kernel launch of the library is bracketed by an event pair.

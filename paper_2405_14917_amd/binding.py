@@ -36,6 +36,7 @@ EXPORTS = [
     "slim_fp8_linear_backward", "slim_layer_norm", "slim_layer_norm_backward_workspace", "slim_layer_norm_backward",
     "slim_distill_workspace", "slim_distill_loss", "slim_distill_loss_grad",
     "slim_fp8_linear_act_workspace", "slim_fp8_linear_act", "slim_fp8_linear_act_backward_workspace", "slim_fp8_linear_act_backward",
+    "slim_head_loss_workspace", "slim_head_loss", "slim_head_loss_grad_workspace", "slim_head_loss_grad",
     "slim_add_norm", "slim_add_norm_backward", "slim_grad_norm_workspace", "slim_grad_norm", "slim_clip_gradients",
     "slim_profile_enable", "slim_profile_collect", "slim_profile_entry", "slim_profile_reset",
 ]
@@ -170,10 +171,15 @@ def load() -> ctypes.CDLL:
                                   c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_void_p]
     lib.slim_add_norm_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_i64, c_i64, c_i64, c_void_p, c_int,
                                            c_void_p, c_void_p, c_void_p, c_i64, c_void_p, c_void_p]
+    lib.slim_head_loss_workspace.argtypes = [c_int] * 4
+    lib.slim_head_loss.argtypes = [c_void_p, c_void_p, c_int, c_int, c_i64, c_void_p, c_i64, c_void_p, c_i64, c_int, c_int, c_void_p, c_int, c_void_p]
+    lib.slim_head_loss_grad_workspace.argtypes = [c_int] * 7
+    lib.slim_head_loss_grad.argtypes = [c_void_p, c_void_p, c_int, c_int, c_i64] + [c_void_p, c_i64] * 4 + [c_int, c_int, c_void_p, c_int, c_void_p,
+                                                                                                          c_void_p, c_void_p, c_i64, c_void_p, c_int, c_i64]
     lib.slim_grad_norm_workspace.argtypes = [c_int, c_int]
     lib.slim_grad_norm.argtypes = [c_void_p, c_void_p, c_int, c_void_p]
     lib.slim_clip_gradients.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_double, c_void_p]
-    for fn in (lib.slim_fp8_linear_act_workspace, lib.slim_fp8_linear_act_backward_workspace, lib.slim_grad_norm_workspace, lib.slim_distill_workspace, lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
+    for fn in (lib.slim_head_loss_workspace, lib.slim_head_loss_grad_workspace, lib.slim_fp8_linear_act_workspace, lib.slim_fp8_linear_act_backward_workspace, lib.slim_grad_norm_workspace, lib.slim_distill_workspace, lib.slim_fp8_linear_workspace, lib.slim_fp8_linear_backward_workspace, lib.slim_layer_norm_backward_workspace):
         fn.restype = c_size_t
     lib.slim_profile_enable.argtypes = [c_void_p, c_int]
     lib.slim_profile_collect.argtypes = [c_void_p]
@@ -246,6 +252,16 @@ def fp8_linear_act_backward_workspace(n: int, m: int, t: int, dx: bool = True, d
                                       db: bool = True, num_cus: int = 0) -> int:
     """Bytes of workspace of Slim.fp8_linear_act_backward (host only, no GPU needed)."""
     return int(load().slim_fp8_linear_act_backward_workspace(n, m, t, int(dx), int(dw), _DT[dw_dtype], int(db), num_cus))
+
+
+def head_loss_workspace(V: int, m: int, t: int, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.head_loss (host only, no GPU needed)."""
+    return int(load().slim_head_loss_workspace(V, m, t, num_cus))
+
+
+def head_loss_grad_workspace(V: int, m: int, t: int, dx: bool = True, dw: bool = True, dw_dtype: torch.dtype = torch.bfloat16, num_cus: int = 0) -> int:
+    """Bytes of workspace of Slim.head_loss_grad (host only, no GPU needed)."""
+    return int(load().slim_head_loss_grad_workspace(V, m, t, int(dx), int(dw), _DT[dw_dtype], num_cus))
 
 
 def grad_norm_workspace(count: int, num_cus: int = 0) -> int:
@@ -973,6 +989,54 @@ class Slim:
         if st:
             self._check(st)
         return loss, dS
+
+    def _head_shape(self, X, W, Ws, labels):
+        ldq, lds = _stored_strides(W, Ws, "W")
+        V, m = W.shape
+        if X.dim() != 2 or X.shape[1] != m:
+            raise ValueError("X has to be (t, %d), got %s" % (m, tuple(X.shape)))
+        if labels.shape != X.shape[:1] or labels.dtype not in (torch.int64, torch.int32) or not labels.is_contiguous():
+            raise ValueError("labels have to be a contiguous int64 or int32 vector of the tokens")
+        return V, m, X.shape[0], ldq, lds
+
+    def head_loss(self, X: torch.Tensor, W: torch.Tensor, Ws: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
+        """loss float32 (t,): the cross entropy of the labels (t,) in the softmax of fp8_linear(X, W, Ws), whose outputs are not kept; 0 for a label
+        that is no class, -100 say.  Records no graph: X that requires a gradient is refused outside torch.no_grad() (head_loss_grad gives it)."""
+        _no_graph(X, W)
+        self._ready(X, W, Ws, labels)
+        V, m, t, ldq, lds = self._head_shape(X, W, Ws, labels)
+        loss = X.new_empty(t, dtype=torch.float32)
+        st = self.lib.slim_head_loss(self.ctx, X.data_ptr(), _dtype(X), t, _row_stride(X, "X"), W.data_ptr(), ldq, Ws.data_ptr(), lds, V, m,
+                                     labels.data_ptr(), int(labels.dtype == torch.int64), loss.data_ptr())
+        if st:
+            self._check(st)
+        return loss
+
+    def head_loss_grad(self, X: torch.Tensor, W: torch.Tensor, Ws: torch.Tensor, Wt: Optional[torch.Tensor], Wts: Optional[torch.Tensor],
+                       labels: torch.Tensor, dloss: torch.Tensor, dw_dtype: Optional[torch.dtype] = None, dx: bool = True, dw: bool = True):
+        """(loss, dX (t, m), dW (V, m)): head_loss and the gradients of sum(dloss * loss); dw_dtype: of dW (default: X's).  Without `dx` Wt and Wts may be
+        None; the gradient that is not wanted is None."""
+        self._ready(X, W, Ws, Wt, Wts, labels, dloss)
+        if not (dx or dw):
+            raise ValueError("neither gradient is wanted")
+        V, m, t, ldq, lds = self._head_shape(X, W, Ws, labels)
+        if dloss.dtype != torch.float32 or dloss.shape != (t,) or not dloss.is_contiguous():
+            raise ValueError("dloss has to be a float32 vector of the tokens")
+        ldqt = ldst = 0
+        if dx:
+            if Wt is None or Wts is None or Wt.shape != (m, V):
+                raise ValueError("dX needs the stored weights of W^T, (%d, %d)" % (m, V))
+            ldqt, ldst = _stored_strides(Wt, Wts, "Wt")
+        loss = X.new_empty(t, dtype=torch.float32)
+        dX = X.new_empty((t, m)) if dx else None
+        dW = X.new_empty((V, m), dtype=dw_dtype) if dw else None
+        st = self.lib.slim_head_loss_grad(self.ctx, X.data_ptr(), _dtype(X), t, _row_stride(X, "X"), W.data_ptr(), ldq, Ws.data_ptr(), lds,
+                                          Wt.data_ptr() if dx else None, ldqt, Wts.data_ptr() if dx else None, ldst, V, m, labels.data_ptr(),
+                                          int(labels.dtype == torch.int64), dloss.data_ptr(), loss.data_ptr(), dX.data_ptr() if dx else None, m,
+                                          dW.data_ptr() if dw else None, _dtype(dW) if dw else F32, m)
+        if st:
+            self._check(st)
+        return loss, dX, dW
 
     # ---- measurement aid
     def profile_enable(self, on: bool = True):

@@ -16,7 +16,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["ctx.hip", "util.hip", "dgemm.hip", "rgemm.hip", "gram.hip", "inverse.hip", "salience.hip", "sba.hip", "quant.hip",
            "pack.hip", "dequant.hip", "dequant_few.hip", "dequant_gemm.hip", "handover.hip", "int8_products.hip", "lwc.hip",
-           "fp8_quant.hip", "fp8_few.hip", "fp8_gemm.hip", "fp8_linear.hip", "norm.hip", "add_norm.hip", "clip.hip", "distill.hip"]
+           "fp8_quant.hip", "fp8_few.hip", "fp8_gemm.hip", "fp8_linear.hip", "head_loss.hip", "norm.hip", "add_norm.hip", "clip.hip", "distill.hip"]
 
 # packed-fp32 code generation is switched off for all device code (a device-compiler option; the host
 # pass does not know the feature and says so, which is harmless)

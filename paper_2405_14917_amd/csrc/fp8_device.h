@@ -148,13 +148,21 @@ struct Operand {
   int64_t ld, lds;
   int rows, shift;
 };
-// What becomes of a sum before it is stored: y = act(sum + bias[a]) + R[b][a]; Z takes the sum with the bias.  R and Z are of C's type; any of
-// bias, R and Z may be null.
+// What becomes of a sum before it is stored: y = act(sum + bias[a]) + R[b][a]; Z takes the sum with the bias.  Z is of C's type, R of
+// r_dtype; any of bias, R and Z may be null.
 struct Epilogue {
   const void *bias, *R;
   void* Z;
   int64_t ldr, ldz;
-  int bias_dtype, act;
+  int bias_dtype, act, r_dtype;
+};
+// Or, in the place of C, what the softmax of the rows of B over those of A needs: of every tile of A the maximum and the sum of the exponentials of the
+// differences from it (rows of `parts` pairs), and the sum of the row's label.
+struct Softmax {
+  float2* part;
+  float* z;
+  const void* labels;
+  int labels64, parts;
 };
 // C[b][a] = sum over nk blocks of A[a] . B[b]
 struct Product {
@@ -164,7 +172,11 @@ struct Product {
   slim_dtype c_dtype;
   int nk;
   const Epilogue* e;               // of a product that is alone in its launch, or null
+  bool coarse;                     // fp32 C from the e4m3 matrix cores
+  const Softmax* sm;               // of a product that is alone in its launch, or null
 };
+// tiles of A of such a product: the `parts` of its Softmax
+int softmax_parts(const Product& p, int num_cus);
 // bytes of workspace of a set of products, enough too for those of fewer rows and shorter contractions; 256-byte multiples
 size_t gemm_workspace(const Product* p, int count, int num_cus);
 slim_status gemm(slim_ctx* ctx, const char* name, const Product* p, int count);
@@ -194,7 +206,10 @@ slim_status join_columns(slim_ctx* ctx, const char* name, const float* sums, int
 
 // ---- and fp8_few.hip: few tokens, or little work, in one launch -----------------------------------------------------
 bool takes_few_tokens(int n, int m, int t, int ncu);
-// X (t x m, 16 bits), or, where it is null, its 8-bit form xq; e may be null for the former
+// X (t x m, 16 bits), or, where it is null, its 8-bit form xq; e may be null for the former.  softmax_few: the same with what the softmax needs in the
+// place of Y; its parts
+int softmax_parts_few(int n, int t, int ncu);
+slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm);
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& xq, const Operand& w, int m,
                        const Epilogue* e, void* Y, slim_dtype y_dtype, int64_t ldy);
 
@@ -207,6 +222,9 @@ __device__ __forceinline__ float from_any(const void* p, int dtype, int64_t i) {
   if (dtype == SLIM_F32) return static_cast<const float*>(p)[i];
   const unsigned h = static_cast<const unsigned short*>(p)[i];
   return __uint_as_float(dtype == SLIM_BF16 ? Half16<__hip_bfloat16>::float_bits(h) : Half16<__half>::float_bits(h));
+}
+__device__ __forceinline__ int64_t label_at(const void* labels, int labels64, int64_t i) {
+  return labels64 ? static_cast<const int64_t*>(labels)[i] : (int64_t)static_cast<const int*>(labels)[i];
 }
 __device__ __forceinline__ void to_any(void* p, int dtype, int64_t i, float v) {
   if (dtype == SLIM_F32) static_cast<float*>(p)[i] = v;

@@ -28,11 +28,13 @@ struct FewArgs {
   int y_dtype;
   const uint8_t *xq, *xs;           // the activations' 8-bit form (T = uint8_t)
   int64_t ldxq, ldxs;
-  Epilogue e;                       // (EPI)
+  Epilogue e;                       // (FINISH)
+  Softmax sm;                       // (SOFTMAX)
 };
+enum { PLAIN, FINISH, SOFTMAX };    // what becomes of the sums: stored, stored through the epilogue, or what the softmax needs of them
 
-// T = uint8_t: the activations come in 8 bits (rows of whole blocks).  EPI: bias, activation, residual, before the outputs are stored.
-template <typename T, int RT, bool EPI>
+// T = uint8_t: the activations come in 8 bits (rows of whole blocks).
+template <typename T, int RT, int MODE>
 __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   constexpr int ROWS = 16 * RT, LD = ROWS + 4;                 // floats per token of a wavefront's sums
   constexpr bool Q8 = sizeof(T) == 1;
@@ -128,25 +130,41 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
     const int tok = e / ROWS, r = e % ROWS;
     float sum = 0.f;
     for (int i = 0; i < nw; ++i) sum += part[(i * 16 + tok) * LD + r];
-    if (r < last) {
-      if constexpr (EPI) {
+    if constexpr (MODE == SOFTMAX) {
+      part[tok * LD + r] = r < last ? sum : -__builtin_inff();   // (the place of the first wavefront's sum, which nobody else reads)
+    } else if (r < last) {
+      if constexpr (MODE == FINISH) {
         const int64_t row = tok0 + tok;
         const int col = row0 + r;
         if (a.e.bias) sum += from_any(a.e.bias, a.e.bias_dtype, col);
         if (a.e.Z) to_any(a.e.Z, a.y_dtype, row * a.e.ldz + col, sum);
         sum = slimact::activated(sum, a.e.act);
-        if (a.e.R) sum += from_any(a.e.R, a.y_dtype, row * a.e.ldr + col);
+        if (a.e.R) sum += from_any(a.e.R, a.e.r_dtype, row * a.e.ldr + col);
       }
       to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
     }
   }
+  if constexpr (MODE == SOFTMAX) {
+    __syncthreads();
+    for (int tok = wave; tok < tn; tok += nw) {
+      const float* z = part + tok * LD;
+      const float z0 = lane < ROWS ? z[lane] : -__builtin_inff(), z1 = lane + 64 < ROWS ? z[lane + 64] : -__builtin_inff();
+      const float top = wave_max_f32(fmaxf(z0, z1));
+      const float sum = wave_sum_f32(__builtin_amdgcn_exp2f((z0 - top) * slimact::LOG2E_HI) + __builtin_amdgcn_exp2f((z1 - top) * slimact::LOG2E_HI));
+      if (lane == 0) {
+        const int64_t row = tok0 + tok, at = label_at(a.sm.labels, a.sm.labels64, row) - row0;
+        a.sm.part[row * a.sm.parts + blockIdx.x] = make_float2(top, sum);
+        if (at >= 0 && at < last) a.sm.z[row] = z[at];
+      }
+    }
+  }
 }
 
-template <typename T, bool EPI, int RT>
+template <typename T, int MODE, int RT>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
   constexpr int ROWS = 16 * RT;
   const int nw = std::min(FEW_WAVES, a.mb);
-  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT, EPI>), dim3(slim_cdiv(a.n, ROWS), slim_cdiv(a.t, 16)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
+  SLIM_LAUNCH(ctx, "fp8_linear_few", (fp8_few<T, RT, MODE>), dim3(slim_cdiv(a.n, ROWS), slim_cdiv(a.t, 16)), dim3(64 * nw), sizeof(float) * (size_t)nw * 16 * (ROWS + 4), a);
   return SLIM_OK;
 }
 
@@ -168,16 +186,16 @@ int sixteens(int n, int t, int ncu) {
   return rt;
 }
 
-template <typename T, bool EPI>
+template <typename T, int MODE>
 slim_status launch(slim_ctx* ctx, const FewArgs& a) {
   switch (sixteens(a.n, a.t, ctx->num_cus)) {
-    case 1: return launch<T, EPI, 1>(ctx, a);
-    case 2: return launch<T, EPI, 2>(ctx, a);
-    case 3: return launch<T, EPI, 3>(ctx, a);
-    case 4: return launch<T, EPI, 4>(ctx, a);
-    case 5: return launch<T, EPI, 5>(ctx, a);
-    case 6: return launch<T, EPI, 6>(ctx, a);
-    default: return launch<T, EPI, FEW_RT>(ctx, a);
+    case 1: return launch<T, MODE, 1>(ctx, a);
+    case 2: return launch<T, MODE, 2>(ctx, a);
+    case 3: return launch<T, MODE, 3>(ctx, a);
+    case 4: return launch<T, MODE, 4>(ctx, a);
+    case 5: return launch<T, MODE, 5>(ctx, a);
+    case 6: return launch<T, MODE, 6>(ctx, a);
+    default: return launch<T, MODE, FEW_RT>(ctx, a);
   }
 }
 
@@ -197,11 +215,18 @@ bool takes_few_tokens(int n, int m, int t, int ncu) {
 
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& xq, const Operand& w, int m,
                        const Epilogue* e, void* Y, slim_dtype y_dtype, int64_t ldy) {
-  FewArgs a = {X, w.q, w.s, Y, ldx, w.ld, w.lds, ldy, t, w.rows, m, slim_cdiv(m, BLOCK), (int)y_dtype, xq.q, xq.s, xq.ld, xq.lds, {}};
+  FewArgs a = {X, w.q, w.s, Y, ldx, w.ld, w.lds, ldy, t, w.rows, m, slim_cdiv(m, BLOCK), (int)y_dtype, xq.q, xq.s, xq.ld, xq.lds, {}, {}};
   if (e) a.e = *e;
-  if (!X) return launch<uint8_t, true>(ctx, a);
-  if (e) return x_dtype == SLIM_F16 ? launch<__half, true>(ctx, a) : launch<__hip_bfloat16, true>(ctx, a);
-  return x_dtype == SLIM_F16 ? launch<__half, false>(ctx, a) : launch<__hip_bfloat16, false>(ctx, a);
+  if (!X) return launch<uint8_t, FINISH>(ctx, a);
+  if (e) return x_dtype == SLIM_F16 ? launch<__half, FINISH>(ctx, a) : launch<__hip_bfloat16, FINISH>(ctx, a);
+  return x_dtype == SLIM_F16 ? launch<__half, PLAIN>(ctx, a) : launch<__hip_bfloat16, PLAIN>(ctx, a);
+}
+
+int softmax_parts_few(int n, int t, int ncu) { return slim_cdiv(n, 16 * sixteens(n, t, ncu)); }
+
+slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm) {
+  FewArgs a = {X, w.q, w.s, nullptr, ldx, w.ld, w.lds, 0, t, w.rows, m, slim_cdiv(m, BLOCK), (int)SLIM_F32, nullptr, nullptr, 0, 0, {}, sm};
+  return x_dtype == SLIM_F16 ? launch<__half, SOFTMAX>(ctx, a) : launch<__hip_bfloat16, SOFTMAX>(ctx, a);
 }
 
 }  // namespace slimfp8

@@ -40,8 +40,10 @@ struct ProductArgs {
 struct GemmArgs {
   ProductArgs p[2];
   int first;                               // workgroups of the first product
-  Epilogue e;                              // (EPI)
+  Epilogue e;                              // (FINISH)
+  Softmax sm;                              // (SOFTMAX)
 };
+enum { PLAIN, FINISH, SOFTMAX };           // what becomes of the sums: stored, stored through the epilogue, or what the softmax needs of them
 
 // Direct loads, if step `k` is below `n` (the branch is in here so that the code around it stays one block for the scheduler).
 // load_lds16x4: four times 16 bytes per lane, to 4 KiB of LDS one after another, from gbase + off[i]; the instruction's offset counts
@@ -158,7 +160,8 @@ __device__ __forceinline__ void finish(const Epilogue& e, char* c, int64_t ldc, 
   if (e.R)
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (row + i * step < rows) r[i] = load_any4(static_cast<const char*>(e.R) + (row + i * step) * e.ldr * size, dtype, col, left);
+      if (row + i * step < rows)
+        r[i] = load_any4(static_cast<const char*>(e.R) + (row + i * step) * e.ldr * (e.r_dtype == SLIM_F32 ? 4 : 2), e.r_dtype, col, left);
   if (e.bias) {
     const float4 b = load_any4(e.bias, e.bias_dtype, col, left);
 #pragma unroll
@@ -213,8 +216,8 @@ __device__ __forceinline__ void read_operand(Half<T>& f, const char* st, const P
 template <int M>
 __device__ __forceinline__ constexpr int share_from(int m, int n) { return m * 2 >= M ? n : m * 2 * n / M; }
 
-// EXACT: products of the numbers in bf16 (fp32 outputs).  EPI: one product, with an epilogue.
-template <typename T, bool EXACT, bool EPI>
+// EXACT: products of the numbers in bf16 (fp32 outputs).  MODE other than PLAIN: of one product that is not cut.
+template <typename T, bool EXACT, int MODE>
 __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_gemm(GemmArgs ga) {
   constexpr int MA = T::MA, MB = T::MB, M = MA * MB, READS = 2 * (MA + MB), S = T::STAGES;
   extern __shared__ __align__(16) char smem_fg[];
@@ -413,9 +416,55 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
     }
   }
 
-  // A lane holds column b = lane % 32 of an MFMA tile and rows 8 (q / 4) + 4 h + q % 4.  32 rows of C at a time through a
-  // part of LDS of the wavefront's own.
+  // A lane holds column b = lane % 32 of an MFMA tile and rows 8 (q / 4) + 4 h + q % 4.
   __syncthreads();
+  if constexpr (MODE == SOFTMAX) {
+    // So the rows of A that a lane holds of a row of B are joined in its registers, then with the lane 32 on and with the other wavefronts.
+    float2* const share = reinterpret_cast<float2*>(smem_fg);        // [part of A][row of B]
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      const int first = a0 + wa * MA * 32 + h * 4, in_b = (wb * MB + j) * 32 + l32, row = b0 + in_b;
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          if (first + i * 32 + 8 * (q / 4) + q % 4 >= p.a.rows) acc[i][j][q] = -__builtin_inff();
+          top = fmaxf(top, acc[i][j][q]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float from = top == -__builtin_inff() ? 0.f : top;       // (rows behind the last one alone)
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f((acc[i][j][q] - from) * slimact::LOG2E_HI);
+      sum += __shfl_xor(sum, 32, 64);
+      if (h == 0) share[wa * T::TB + in_b] = make_float2(top, sum);
+      const int64_t label = row < p.b.rows ? label_at(ga.sm.labels, ga.sm.labels64, row) : -1;
+      const int at = label >= first && label < min(p.a.rows, first + MA * 32) ? (int)(label - first) : -1;
+      if (__any(at >= 0)) {
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (at == i * 32 + 8 * (q / 4) + q % 4) ga.sm.z[row] = acc[i][j][q];
+      }
+    }
+    __syncthreads();
+    for (int r = tid; r < T::TB && b0 + r < p.b.rows; r += T::THREADS) {
+      float2 s = share[r];
+#pragma unroll
+      for (int w = 1; w < T::WA; ++w) {
+        const float2 o = share[w * T::TB + r];
+        const float top = fmaxf(s.x, o.x);
+        s = make_float2(top, s.y * __builtin_amdgcn_exp2f((s.x - top) * slimact::LOG2E_HI) + o.y * __builtin_amdgcn_exp2f((o.x - top) * slimact::LOG2E_HI));
+      }
+      ga.sm.part[(int64_t)(b0 + r) * ga.sm.parts + a0 / T::TA] = s;
+    }
+    return;
+  }
+  // 32 rows of C at a time through a part of LDS of the wavefront's own.
   float* out = reinterpret_cast<float*>(smem_fg) + wave * 32 * T::OUT_LD;
   constexpr int QUADS = T::MA * 8, RPI = 64 / QUADS;           // lanes per row of C, rows per instruction
   static_assert(QUADS <= 64, "a row of a wavefront's part is read by one instruction");
@@ -429,7 +478,7 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(out + l32 * T::OUT_LD + i * 32 + q * 8 + h * 4) =
             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    if constexpr (EPI) {
+    if constexpr (MODE == FINISH) {
       constexpr int N = 4;
       const int col = (lane % QUADS) * 4, ca = a0 + wa * T::MA * 32 + col;
 #pragma unroll 1
@@ -452,7 +501,7 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
 }
 
 // C = the sum of a product's parts, in their order
-template <bool EPI>
+template <bool FINISH_>
 __global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __restrict__ parts, int64_t ldp, void* c, int64_t ldc, int dtype, Epilogue e) {
   const int quads = (p.a.rows + 3) / 4;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -467,7 +516,7 @@ __global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __re
     s.z += v.z;
     s.w += v.w;
   }
-  if constexpr (EPI) {
+  if constexpr (FINISH_) {
     float v[4] = {s.x, s.y, s.z, s.w};
     return finish<1>(e, static_cast<char*>(c), ldc, dtype, row, 1, p.b.rows, col, p.a.rows - col, v);
   }
@@ -485,10 +534,13 @@ struct Plan {
 };
 constexpr int TILE_A[] = {Large::TA, Medium::TA, Small::TA}, TILE_B[] = {Large::TB, Medium::TB, Small::TB};
 
+bool exact(const Product& p) { return p.sm || (p.c_dtype == SLIM_F32 && !p.coarse); }
 int tiles_of(const Product& p, int tile) { return slim_cdiv(p.a.rows, TILE_A[tile]) * slim_cdiv(p.b.rows, TILE_B[tile]); }
 
-// Parts along the contraction, where `tiles` do not fill the chip; eight steps a part at least.
-int parts_of(int tiles, int nk, int ncu) {
+// Parts along the contraction, where `tiles` do not fill the chip; eight steps a part at least.  (A softmax needs the whole sums.)
+int parts_of(const Product& p, int tiles, int ncu) {
+  if (p.sm) return 1;
+  const int nk = p.nk;
   const int s = std::max(1, std::min(ncu / std::max(1, tiles), nk / 8));
   const int per = slim_cdiv(slim_cdiv(std::max(1, nk), s), 4) * 4;
   return std::max(1, slim_cdiv(nk, per));
@@ -501,8 +553,8 @@ int parts_of(int tiles, int nk, int ncu) {
 // tokens, large ones (790; medium ones above 900).  The bytes of the operands are in the measured step, not a term of their own.
 double tile_cost(const Product& p, int tile, int ncu) {
   static const double round[] = {15.0, 5.4, 2.7}, step[2][3] = {{1.44, 0.82, 0.34}, {2.6, 1.42, 0.56}};
-  const int tiles = tiles_of(p, tile), s = parts_of(tiles, p.nk, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
-  double one = step[p.c_dtype == SLIM_F32][tile];
+  const int tiles = tiles_of(p, tile), s = parts_of(p, tiles, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
+  double one = step[exact(p)][tile];
   if (tile == TILE_MEDIUM && tiles * s <= ncu) one *= 0.6;
   const double join = s > 1 ? 4.0 + 8.0 * s * p.a.rows * (double)p.b.rows / 4.85e6 : 0.0;
   return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + one * slim_cdiv(p.nk, s)) + join;
@@ -516,7 +568,7 @@ int tile_of(const Product& p, int ncu) {
 
 // Products of one launch: all, or one where they differ in their kind or tile (a gradient of long contraction and few tiles beside one of many).
 int in_one_launch(const Product* p, int count, int ncu) {
-  return count == 2 && ((p[0].c_dtype == SLIM_F32) != (p[1].c_dtype == SLIM_F32) || tile_of(p[0], ncu) != tile_of(p[1], ncu)) ? 1 : count;
+  return count == 2 && (exact(p[0]) != exact(p[1]) || tile_of(p[0], ncu) != tile_of(p[1], ncu)) ? 1 : count;
 }
 
 // Each product's parts as if it were alone: beside another one of many tiles, few of long contraction would be what the launch waits for
@@ -524,7 +576,7 @@ int in_one_launch(const Product* p, int count, int ncu) {
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
   for (int i = 0; i < count; ++i) {
-    pl.splits[i] = parts_of(tiles_of(p[i], tile_of(p[i], ncu)), p[i].nk, ncu);
+    pl.splits[i] = parts_of(p[i], tiles_of(p[i], tile_of(p[i], ncu)), ncu);
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
   }
   return pl;
@@ -539,27 +591,28 @@ size_t parts_bytes(const Product& p, int ncu) {
   return most < 2 ? 0 : slim_ws_round(sizeof(float) * (size_t)std::min((int64_t)ncu * Large::TA * Large::TB, most * ldp * p.b.rows));
 }
 
-template <typename T, bool EXACT, bool EPI>
+template <typename T, bool EXACT, int MODE>
 slim_status launch(slim_ctx* ctx, const char* name, const GemmArgs& ga, int grid) {
   // (an attribute of the function on the device, asked for once: it costs a call as much as a third of the launch)
   static std::atomic<uint64_t> allowed{0};
   const uint64_t bit = ctx->device < 64 ? 1ull << ctx->device : 0;
   if (T::LDS > 64 * 1024 && !(allowed.load(std::memory_order_relaxed) & bit)) {
-    SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_gemm<T, EXACT, EPI>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
+    SLIM_HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_gemm<T, EXACT, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS));
     allowed.fetch_or(bit, std::memory_order_relaxed);
   }
-  SLIM_LAUNCH(ctx, name, (fp8_gemm<T, EXACT, EPI>), dim3(grid), dim3(T::THREADS), T::LDS, ga);
+  SLIM_LAUNCH(ctx, name, (fp8_gemm<T, EXACT, MODE>), dim3(grid), dim3(T::THREADS), T::LDS, ga);
   return SLIM_OK;
 }
-template <bool EXACT, bool EPI>
+template <bool EXACT, int MODE>
 slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid) {
-  return tile == TILE_LARGE    ? launch<Large, EXACT, EPI>(ctx, name, ga, grid)
-         : tile == TILE_MEDIUM ? launch<Medium, EXACT, EPI>(ctx, name, ga, grid)
-                               : launch<Small, EXACT, EPI>(ctx, name, ga, grid);
+  return tile == TILE_LARGE    ? launch<Large, EXACT, MODE>(ctx, name, ga, grid)
+         : tile == TILE_MEDIUM ? launch<Medium, EXACT, MODE>(ctx, name, ga, grid)
+                               : launch<Small, EXACT, MODE>(ctx, name, ga, grid);
 }
-template <bool EXACT>
-slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid, bool epilogue) {
-  return epilogue ? launch<EXACT, true>(ctx, name, tile, ga, grid) : launch<EXACT, false>(ctx, name, tile, ga, grid);
+slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid, bool exact, int mode) {
+  if (mode == SOFTMAX) return launch<true, SOFTMAX>(ctx, name, tile, ga, grid);
+  if (mode == FINISH) return exact ? launch<true, FINISH>(ctx, name, tile, ga, grid) : launch<false, FINISH>(ctx, name, tile, ga, grid);
+  return exact ? launch<true, PLAIN>(ctx, name, tile, ga, grid) : launch<false, PLAIN>(ctx, name, tile, ga, grid);
 }
 
 slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count) {
@@ -593,8 +646,8 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
   }
   const Epilogue* const e = p[0].e;          // (where the product is cut, the parts' sum goes through it)
   if (e) ga.e = *e;
-  const bool whole = e && !parts[0];
-  const slim_status st = p[0].c_dtype == SLIM_F32 ? launch<true>(ctx, name, tile, ga, grid, whole) : launch<false>(ctx, name, tile, ga, grid, whole);
+  if (p[0].sm) ga.sm = *p[0].sm;
+  const slim_status st = launch(ctx, name, tile, ga, grid, exact(p[0]), p[0].sm ? SOFTMAX : e && !parts[0] ? FINISH : PLAIN);
   if (st != SLIM_OK) return st;
   for (int i = 0; i < count; ++i)
     if (parts[i]) {
@@ -609,6 +662,8 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
 }  // namespace
 
 namespace slimfp8 {
+
+int softmax_parts(const Product& p, int num_cus) { return slim_cdiv(p.a.rows, TILE_A[tile_of(p, num_cus)]); }
 
 size_t gemm_workspace(const Product* p, int count, int num_cus) {
   size_t bytes = 0;

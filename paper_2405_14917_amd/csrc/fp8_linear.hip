@@ -7,24 +7,11 @@
 // With an epilogue the same kernels add bias and residual and apply the activation before the outputs are stored (where a product is cut along
 // its contraction, the kernel that adds the parts does), and the activations may come in 8 bits; in its backward pass the launch that quantises the
 // gradient of the outputs first multiplies it by the activation's derivative, and leaves the sums of 128 rows for the bias.
-#include "fp8_device.h"
+#include "fp8_entry.h"
 
 namespace {
 
 using namespace slimfp8;
-
-constexpr int FL_MAX = 1 << 23;            // rows and leading dimensions: offsets inside a tile of 256 rows fit 32 bits
-
-bool is_16(slim_dtype d) { return d == SLIM_F16 || d == SLIM_BF16; }
-
-size_t activation_bytes(int64_t rows, int64_t contraction) {
-  return slim_ws_round((size_t)rows * quantized_ld(contraction)) + slim_ws_round((size_t)rows * scales_ld(contraction));
-}
-bool carve(slim_ctx* ctx, int64_t rows, int64_t contraction, uint8_t*& q, uint8_t*& s) {
-  q = static_cast<uint8_t*>(slim_ws_alloc(ctx, (size_t)rows * quantized_ld(contraction)));
-  s = static_cast<uint8_t*>(slim_ws_alloc(ctx, (size_t)rows * scales_ld(contraction)));
-  return q && s;
-}
 
 Product forward_product(int n, int m, int t, slim_dtype y_dtype) {
   Product p = {};
@@ -64,18 +51,6 @@ size_t backward_need(int n, int m, int t, bool dx, bool dw, slim_dtype dw_dtype,
   Product p[2];
   const int count = backward_products(n, m, t, dx, dw, dw_dtype, p);
   return (dx ? activation_bytes(t, n) : 0) + (dw ? activation_bytes(n, t) + activation_bytes(m, t) : 0) + gemm_workspace(p, count, ncu);
-}
-
-slim_status check_stored(slim_ctx* ctx, const char* fn, const char* what, const uint8_t* q, int64_t ldq, const uint8_t* s, int64_t lds,
-                         int rows, int cols) {
-  SLIM_REQUIRE(ctx, q && s, "%s: null %s", fn, what);
-  SLIM_REQUIRE(ctx, rows > 0 && cols > 0 && rows <= FL_MAX && cols <= FL_MAX, "%s: %s is %d x %d", fn, what, rows, cols);
-  SLIM_REQUIRE(ctx, slim_aligned16(q) && ((uintptr_t)s & 3u) == 0, "%s: %s has to be 16-byte aligned, its scales 4-byte", fn, what);
-  SLIM_REQUIRE(ctx, ldq >= padded(cols) && ldq % BLOCK == 0 && ldq <= FL_MAX, "%s: rows of %s are whole blocks of 128 (ld = %lld)", fn, what,
-               (long long)ldq);
-  SLIM_REQUIRE(ctx, lds >= slim_cdiv(cols, BLOCK) && lds % 4 == 0 && lds <= FL_MAX, "%s: rows of the scales of %s are whole words (ld = %lld)", fn, what,
-               (long long)lds);
-  return SLIM_OK;
 }
 
 // dX and dW (either may be null) from the quantised gradient of the outputs and activations
@@ -187,7 +162,7 @@ slim_status slim_fp8_linear_act(slim_ctx* ctx, const void* X, slim_dtype x_dtype
   if (!is_16(y_dtype) && y_dtype != SLIM_F32) return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: Y is F16, BF16 or F32", fn);
   Epilogue e = {};
   if (epilogue) {
-    e = Epilogue{epilogue->bias, epilogue->R, epilogue->Z, epilogue->ldr, epilogue->ldz, (int)epilogue->bias_dtype, epilogue->act};
+    e = Epilogue{epilogue->bias, epilogue->R, epilogue->Z, epilogue->ldr, epilogue->ldz, (int)epilogue->bias_dtype, epilogue->act, (int)y_dtype};
     SLIM_REQUIRE(ctx, e.act >= SLIM_ACT_NONE && e.act <= SLIM_ACT_SILU, "%s: act = %d", fn, e.act);
     if (e.bias && e.bias_dtype != (int)y_dtype && e.bias_dtype != SLIM_F32)
       return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: the bias is of Y's type or F32", fn);
