@@ -16,8 +16,16 @@ __device__ __forceinline__ float exp_of(float x) {
   const float h = x * LOG2E_HI, l = fmaf(x, LOG2E_LO, fmaf(x, LOG2E_HI, -h));
   return __builtin_amdgcn_exp2f(h) * fmaf(l, LN2, 1.f);
 }
-// 1 / (1 + exp(-v)); at the ends 0 and 1
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp_of(fminf(fmaxf(-v, -126.f), 126.f))); }
+// 1 / (1 + exp(-v)); at the ends 0 and 1.  rest: what is missing to 1 (in the upper half not as a difference: it is multiplied by numbers like v)
+__device__ __forceinline__ float sigmoid(float v, float& rest) {
+  const float e = exp_of(fminf(fmaxf(-v, -126.f), 126.f)), s = __builtin_amdgcn_rcpf(1.f + e);
+  rest = v > 0.f ? e * s : 1.f - s;
+  return s;
+}
+__device__ __forceinline__ float sigmoid(float v) {
+  float rest;
+  return sigmoid(v, rest);
+}
 
 // Phi(-|z|) = exp(-z^2 / 2) P(u) u / 2 with u = 1 / (1 + 0.45 |z| / sqrt 2): P of degree 9 is fitted to exp(x^2) erfc(x) / u by least squares, the
 // weights raised where the error was large (relative error 3.2e-8); e: exp(-z^2 / 2), its exponent in two parts
@@ -64,12 +72,15 @@ __device__ __forceinline__ float slope(float z, int act) {
       return fmaf(z * 0.398942280f, e, z > 0.f ? 1.f - q : q);
     }
     case SLIM_ACT_GELU_TANH: {
-      const float c = fminf(fmaxf(z, -1e4f), 1e4f), s = sigmoid(c * fmaf(TANH_B, c * c, TANH_A));
-      return z == z ? fmaf(c * s * (1.f - s), fmaf(3.f * TANH_B, c * c, TANH_A), s) : z;
+      const float c = fminf(fmaxf(z, -1e4f), 1e4f);
+      float rest;
+      const float s = sigmoid(c * fmaf(TANH_B, c * c, TANH_A), rest);
+      return z == z ? fmaf(c * s * rest, fmaf(3.f * TANH_B, c * c, TANH_A), s) : z;
     }
     case SLIM_ACT_SILU: {
-      const float s = sigmoid(z);
-      return s * fmaf(z, 1.f - s, 1.f);
+      float rest;
+      const float s = sigmoid(z, rest);
+      return s * fmaf(z, rest, 1.f);
     }
     default: return 1.f;
   }

@@ -137,8 +137,8 @@ __global__ __launch_bounds__(CL_THREADS) void clip_scale(ClipArgs a, const doubl
   __syncthreads();
   const double n = sqrt((red[0] + red[1]) + (red[2] + red[3]));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-  // a norm that is no finite number leaves everything as it is: the caller sees it and drops the step
-  const bool copy = !(n > limit) || !(n < __longlong_as_double(0x7ff0000000000000ll));
+  // a norm that is no finite fp32 number leaves everything as it is: the caller sees it and drops the step
+  const bool copy = !(n > limit) || !((float)n < __builtin_inff());
   const float factor = copy ? 1.f : (float)(limit / n);
   for (int64_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
     const int64_t chunk = a.chunks - 1 - k;
