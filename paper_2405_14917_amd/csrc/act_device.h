@@ -86,20 +86,24 @@ __device__ __forceinline__ float slope(float z, int act) {
   }
 }
 
-// the same of several values, one branch for all
+// f with the activation as a constant: one branch for many values
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+  switch (act) {
+    case SLIM_ACT_RELU: return f(std::integral_constant<int, SLIM_ACT_RELU>());
+    case SLIM_ACT_GELU: return f(std::integral_constant<int, SLIM_ACT_GELU>());
+    case SLIM_ACT_GELU_TANH: return f(std::integral_constant<int, SLIM_ACT_GELU_TANH>());
+    case SLIM_ACT_SILU: return f(std::integral_constant<int, SLIM_ACT_SILU>());
+    default: return f(std::integral_constant<int, SLIM_ACT_NONE>());
+  }
+}
 template <int N>
 __device__ __forceinline__ void activate(float (&v)[N], int act) {
-  auto each = [&](auto a) {
+  if (act == SLIM_ACT_NONE) return;
+  with_act(act, [&](auto a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = activated(v[i], decltype(a)::value);
-  };
-  switch (act) {
-    case SLIM_ACT_RELU: return each(std::integral_constant<int, SLIM_ACT_RELU>());
-    case SLIM_ACT_GELU: return each(std::integral_constant<int, SLIM_ACT_GELU>());
-    case SLIM_ACT_GELU_TANH: return each(std::integral_constant<int, SLIM_ACT_GELU_TANH>());
-    case SLIM_ACT_SILU: return each(std::integral_constant<int, SLIM_ACT_SILU>());
-    default: return;
-  }
+  });
 }
 
 }  // namespace slimact

@@ -164,6 +164,20 @@ struct Softmax {
   const void* labels;
   int labels64, parts;
 };
+// Or the gradient of a cross entropy: of a token (a row of B) the largest logit, the gradient g of its loss, g over the sum of the exponentials of the
+// differences from the largest, and its label (-1: none; g is 0 then) ...
+struct TokenStat {
+  float top, g, scaled;
+  int label;
+};
+// ... for dz[b][a] = scaled exp(C[b][a] - top) - [first + a = label] g, quantised in blocks of 128 of A (rows_q, as activations are) and of 128 of B (cols_q,
+// transposed); either may be null.
+struct SoftmaxGradient {
+  const TokenStat* stat;
+  uint8_t *rows_q, *rows_s, *cols_q, *cols_s;
+  int64_t ldrq, ldrs, ldcq, ldcs;
+  int first;
+};
 // C[b][a] = sum over nk blocks of A[a] . B[b]
 struct Product {
   Operand a, b;
@@ -174,6 +188,7 @@ struct Product {
   const Epilogue* e;               // of a product that is alone in its launch, or null
   bool coarse;                     // fp32 C from the e4m3 matrix cores
   const Softmax* sm;               // of a product that is alone in its launch, or null
+  const SoftmaxGradient* sg;       // the same
 };
 // tiles of A of such a product: the `parts` of its Softmax
 int softmax_parts(const Product& p, int num_cus);

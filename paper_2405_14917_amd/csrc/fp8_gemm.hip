@@ -42,8 +42,10 @@ struct GemmArgs {
   int first;                               // workgroups of the first product
   Epilogue e;                              // (FINISH)
   Softmax sm;                              // (SOFTMAX)
+  SoftmaxGradient sg;                      // (GRADIENT)
 };
-enum { PLAIN, FINISH, SOFTMAX };           // what becomes of the sums: stored, stored through the epilogue, or what the softmax needs of them
+// what becomes of the sums: stored, stored through the epilogue, what the softmax needs of them, or the quantised gradient of its logarithm
+enum { PLAIN, FINISH, SOFTMAX, GRADIENT };
 
 // Direct loads, if step `k` is below `n` (the branch is in here so that the code around it stays one block for the scheduler).
 // load_lds16x4: four times 16 bytes per lane, to 4 KiB of LDS one after another, from gbase + off[i]; the instruction's offset counts
@@ -215,6 +217,157 @@ __device__ __forceinline__ void read_operand(Half<T>& f, const char* st, const P
 // the share of n things that belongs beside product m of M, all of them beside the first half of the products
 template <int M>
 __device__ __forceinline__ constexpr int share_from(int m, int n) { return m * 2 >= M ? n : m * 2 * n / M; }
+
+// The sums of a tile as logits: dz in their place, then its two 8-bit forms.  A lane holds, of 32 tokens l32 of each j, the classes 32 i + 8 (q / 4) + 4 h + q % 4:
+// a token's block of 128 classes is in two lanes (and two wavefronts, where a wavefront's part is 64 wide), a class's block of 128 tokens in
+// the 32 lanes of a half (and two wavefronts).  What is not finite fills a token's whole row (the sum it is divided by, or g, is not), so that one flag a
+// token is enough.  Both forms leave through a part of LDS of the wavefront's own, in rows of the block.
+template <typename T>
+__device__ __forceinline__ void quantize_gradient(v16f (&acc)[T::MA][T::MB], const SoftmaxGradient& sg, const ProductArgs& p, char* smem, int a0, int b0, int wa,
+                                                  int wb, int wave, int lane) {
+  constexpr int MA = T::MA, MB = T::MB, PA = 32 * MA, PB = 32 * MB, LD = 16;      // LD: bytes between the rows of a part
+  static_assert(BLOCK % PA == 0 && BLOCK % PB == 0 && T::TA % BLOCK == 0 && T::TB % BLOCK == 0, "a tile is made of whole blocks");
+  const int l32 = lane & 31, h = lane >> 5;
+  const int first = a0 + wa * PA + h * 4, tok0 = b0 + wb * PB;
+  unsigned* const row_max = reinterpret_cast<unsigned*>(smem);                    // [part of A][token], [part of B][class]
+  unsigned* const col_max = row_max + T::WA * T::TB;
+  constexpr int PART = PA > PB ? PA * (PB + LD) : PB * (PA + LD);
+  uint8_t* const scale = reinterpret_cast<uint8_t*>(col_max + T::WB * T::TA) + wave * PA;
+  char* const part = smem + 4 * (T::WA * T::TB + T::WB * T::TA) + T::WAVES * PA + wave * PART;
+  static_assert(PA % 16 == 0 && 4 * (T::WA * T::TB + T::WB * T::TA) + T::WAVES * (PA + PART) <= T::LDS, "the stages' place is enough");
+  TokenStat st[MB];
+#pragma unroll
+  for (int j = 0; j < MB; ++j) st[j] = sg.stat[min(tok0 + j * 32 + l32, p.b.rows - 1)];
+  unsigned rmax[MB], fine[MB];                       // fine: all ones where the token's gradients are finite
+#pragma unroll
+  for (int j = 0; j < MB; ++j) {
+    const bool live = tok0 + j * 32 + l32 < p.b.rows && st[j].label >= 0;
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = __builtin_amdgcn_exp2f((acc[i][j][q] - st[j].top) * slimact::LOG2E_HI) * st[j].scaled;
+    const int label = st[j].label - sg.first - first, at = live && label >= 0 && label < PA ? label : -1;
+    if (__any(at >= 0)) {
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (at == i * 32 + 8 * (q / 4) + q % 4) acc[i][j][q] -= st[j].g;
+    }
+    if (__any(!live)) {
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] = live ? acc[i][j][q] : 0.f;
+    }
+    if (a0 + T::TA > p.a.rows) {                     // (the last tile: classes that do not exist)
+      int left = p.a.rows - first;
+#if defined(__HIP_DEVICE_COMPILE__)
+      asm volatile("" : "+v"(left));                 // (or 64 results of comparisons are kept from one j for the next, and spilled)
+#endif
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (i * 32 + 8 * (q / 4) + q % 4 >= left) acc[i][j][q] = 0.f;
+    }
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) m = max(m, __float_as_uint(acc[i][j][q]) & 0x7fffffffu);
+    m = max(m, (unsigned)__shfl_xor((int)m, 32, 64));
+    fine[j] = m < 0x7f800000u ? ~0u : 0u;            // (patterns order like the values, NaN above infinity)
+    rmax[j] = m & fine[j];
+    if (PA < BLOCK && h == 0) row_max[wa * T::TB + wb * PB + j * 32 + l32] = rmax[j];
+  }
+  unsigned cmax[MA][16];
+  if (sg.cols_q) {
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        unsigned m = 0;
+#pragma unroll
+        for (int j = 0; j < MB; ++j) m = max(m, __float_as_uint(acc[i][j][q]) & 0x7fffffffu & fine[j]);
+        m = max(m, (unsigned)dpp_b32<DPP_XOR1>((int)m));
+        m = max(m, (unsigned)dpp_b32<DPP_XOR2>((int)m));
+        m = max(m, (unsigned)dpp_b32<DPP_HALF_MIRROR>((int)m));
+        m = max(m, (unsigned)dpp_b32<DPP_MIRROR>((int)m));
+        const auto both = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+        cmax[i][q] = max(both[0], both[1]);
+        if (PB < BLOCK && l32 == 0) col_max[wb * T::TA + wa * PA + h * 4 + i * 32 + 8 * (q / 4) + q % 4] = cmax[i][q];
+      }
+  }
+  if constexpr (PA < BLOCK || PB < BLOCK) __syncthreads();
+  // the other wavefront's half of a block
+  auto joined = [&](unsigned own, const unsigned* shared, int w, int width, int at) { return max(own, shared[(w ^ 1) * width + at]); };
+  if (sg.rows_q) {
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      const int in_b = wb * PB + j * 32 + l32;
+      const unsigned b = scale_byte(PA < BLOCK ? joined(rmax[j], row_max, wa, T::TB, in_b) : rmax[j]);
+      const float inv = __uint_as_float((254u - b) << 23);
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][4 * q] * inv, acc[i][j][4 * q + 1] * inv, 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][4 * q + 2] * inv, acc[i][j][4 * q + 3] * inv, w, true);
+          *reinterpret_cast<int*>(part + (j * 32 + l32) * (PA + LD) + i * 32 + q * 8 + h * 4) = w;
+        }
+      if (h == 0 && b0 + in_b < p.b.rows && first < p.a.rows && (PA == BLOCK || wa % 2 == 0)) sg.rows_s[(int64_t)(b0 + in_b) * sg.ldrs + first / BLOCK] = (uint8_t)b;
+    }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LANES = PA / 16;                   // of a row
+    if ((a0 + wa * PA) / BLOCK * BLOCK < p.a.rows)   // (a block that exists: its end behind the last class is zeros)
+#pragma unroll
+      for (int r = 0; r < PB; r += 64 / LANES) {
+        const int row = r + lane / LANES, c = lane % LANES * 16;
+        const uint4 v = *reinterpret_cast<const uint4*>(part + row * (PA + LD) + c);
+        if (tok0 + row < p.b.rows) *reinterpret_cast<uint4*>(sg.rows_q + (int64_t)(tok0 + row) * sg.ldrq + a0 + wa * PA + c) = v;
+      }
+  }
+  if (sg.cols_q) {
+    // four lanes' words (four classes of a token each) become four words of a class: bytes change places with the lane beside, then pairs of bytes with
+    // the lane two on
+    __builtin_amdgcn_wave_barrier();
+    const unsigned sel1 = lane & 1 ? 0x03070105u : 0x06020400u, sel2 = lane & 2 ? 0x03020706u : 0x05040100u;
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float inv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int in_a = wa * PA + h * 4 + i * 32 + 8 * q + k;
+          const unsigned b = scale_byte(PB < BLOCK ? joined(cmax[i][4 * q + k], col_max, wb, T::TA, in_a) : cmax[i][4 * q + k]);
+          inv[k] = __uint_as_float((254u - b) << 23);
+          if (l32 == 0) scale[h * 4 + i * 32 + 8 * q + k] = (uint8_t)b;
+        }
+#pragma unroll
+        for (int j = 0; j < MB; ++j) {
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][4 * q] * inv[0], acc[i][j][4 * q + 1] * inv[1], 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(acc[i][j][4 * q + 2] * inv[2], acc[i][j][4 * q + 3] * inv[3], w, true);
+          w = (int)__builtin_amdgcn_perm((unsigned)dpp_b32<DPP_XOR1>(w), (unsigned)w, sel1);
+          w = (int)__builtin_amdgcn_perm((unsigned)dpp_b32<DPP_XOR2>(w), (unsigned)w, sel2);
+          *reinterpret_cast<int*>(part + (i * 32 + 8 * q + h * 4 + (lane & 3)) * (PB + LD) + j * 32 + (l32 & ~3)) = w;
+        }
+      }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LANES = PB / 16;
+    for (int c = lane; c < PA; c += 64)
+      if (a0 + wa * PA + c < p.a.rows && tok0 < p.b.rows && (PB == BLOCK || wb % 2 == 0))
+        sg.cols_s[(int64_t)(a0 + wa * PA + c) * sg.ldcs + tok0 / BLOCK] = scale[c];
+    if (tok0 / BLOCK * BLOCK < p.b.rows)
+#pragma unroll
+      for (int r = 0; r < PA; r += 64 / LANES) {
+        const int row = r + lane / LANES, c = lane % LANES * 16, cls = a0 + wa * PA + row;
+        const uint4 v = *reinterpret_cast<const uint4*>(part + row * (PB + LD) + c);
+        if (cls < p.a.rows) *reinterpret_cast<uint4*>(sg.cols_q + (int64_t)cls * sg.ldcq + tok0 + c) = v;
+      }
+  }
+}
 
 // EXACT: products of the numbers in bf16 (fp32 outputs).  MODE other than PLAIN: of one product that is not cut.
 template <typename T, bool EXACT, int MODE>
@@ -424,14 +577,22 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
 #pragma unroll
     for (int j = 0; j < MB; ++j) {
       const int first = a0 + wa * MA * 32 + h * 4, in_b = (wb * MB + j) * 32 + l32, row = b0 + in_b;
+      if (a0 + T::TA > p.a.rows) {                                   // (the last tile: classes that do not exist)
+        int left = p.a.rows - first;
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(left));                               // (or 64 results of comparisons are kept from one j for the next, and spilled)
+#endif
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (i * 32 + 8 * (q / 4) + q % 4 >= left) acc[i][j][q] = -__builtin_inff();
+      }
       float top = -__builtin_inff();
 #pragma unroll
       for (int i = 0; i < MA; ++i)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          if (first + i * 32 + 8 * (q / 4) + q % 4 >= p.a.rows) acc[i][j][q] = -__builtin_inff();
-          top = fmaxf(top, acc[i][j][q]);
-        }
+        for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float from = top == -__builtin_inff() ? 0.f : top;       // (rows behind the last one alone)
       float sum = 0.f;
@@ -444,12 +605,19 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       const int64_t label = row < p.b.rows ? label_at(ga.sm.labels, ga.sm.labels64, row) : -1;
       const int at = label >= first && label < min(p.a.rows, first + MA * 32) ? (int)(label - first) : -1;
       if (__any(at >= 0)) {
+        float z = 0.f;
+        bool mine = false;                                           // (the other half of the lanes holds four classes in eight)
 #pragma unroll
         for (int i = 0; i < MA; ++i)
 #pragma unroll
           for (int q = 0; q < 16; ++q)
-            if (at == i * 32 + 8 * (q / 4) + q % 4) ga.sm.z[row] = acc[i][j][q];
+            if (at == i * 32 + 8 * (q / 4) + q % 4) {
+              z = acc[i][j][q];
+              mine = true;
+            }
+        if (mine) ga.sm.z[row] = z;
       }
+      __builtin_amdgcn_sched_barrier(0);                             // (one j at a time in the registers)
     }
     __syncthreads();
     for (int r = tid; r < T::TB && b0 + r < p.b.rows; r += T::THREADS) {
@@ -462,6 +630,10 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       }
       ga.sm.part[(int64_t)(b0 + r) * ga.sm.parts + a0 / T::TA] = s;
     }
+    return;
+  }
+  if constexpr (MODE == GRADIENT) {
+    quantize_gradient<T>(acc, ga.sg, p, smem_fg, a0, b0, wa, wb, wave, lane);
     return;
   }
   // 32 rows of C at a time through a part of LDS of the wavefront's own.
@@ -534,12 +706,12 @@ struct Plan {
 };
 constexpr int TILE_A[] = {Large::TA, Medium::TA, Small::TA}, TILE_B[] = {Large::TB, Medium::TB, Small::TB};
 
-bool exact(const Product& p) { return p.sm || (p.c_dtype == SLIM_F32 && !p.coarse); }
+bool exact(const Product& p) { return p.sm || p.sg || (p.c_dtype == SLIM_F32 && !p.coarse); }
 int tiles_of(const Product& p, int tile) { return slim_cdiv(p.a.rows, TILE_A[tile]) * slim_cdiv(p.b.rows, TILE_B[tile]); }
 
 // Parts along the contraction, where `tiles` do not fill the chip; eight steps a part at least.  (A softmax needs the whole sums.)
 int parts_of(const Product& p, int tiles, int ncu) {
-  if (p.sm) return 1;
+  if (p.sm || p.sg) return 1;
   const int nk = p.nk;
   const int s = std::max(1, std::min(ncu / std::max(1, tiles), nk / 8));
   const int per = slim_cdiv(slim_cdiv(std::max(1, nk), s), 4) * 4;
@@ -560,7 +732,7 @@ double tile_cost(const Product& p, int tile, int ncu) {
   return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + one * slim_cdiv(p.nk, s)) + join;
 }
 int tile_of(const Product& p, int ncu) {
-  int best = TILE_SMALL;
+  int best = p.sg ? TILE_MEDIUM : TILE_SMALL;                       // (a gradient's tile holds whole blocks of 128)
   for (int t : {TILE_MEDIUM, TILE_LARGE})
     if (tile_cost(p, t, ncu) < tile_cost(p, best, ncu)) best = t;
   return best;
@@ -610,6 +782,7 @@ slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga
                                : launch<Small, EXACT, MODE>(ctx, name, ga, grid);
 }
 slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga, int grid, bool exact, int mode) {
+  if (mode == GRADIENT) return tile == TILE_LARGE ? launch<Large, true, GRADIENT>(ctx, name, ga, grid) : launch<Medium, true, GRADIENT>(ctx, name, ga, grid);
   if (mode == SOFTMAX) return launch<true, SOFTMAX>(ctx, name, tile, ga, grid);
   if (mode == FINISH) return exact ? launch<true, FINISH>(ctx, name, tile, ga, grid) : launch<false, FINISH>(ctx, name, tile, ga, grid);
   return exact ? launch<true, PLAIN>(ctx, name, tile, ga, grid) : launch<false, PLAIN>(ctx, name, tile, ga, grid);
@@ -647,7 +820,8 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
   const Epilogue* const e = p[0].e;          // (where the product is cut, the parts' sum goes through it)
   if (e) ga.e = *e;
   if (p[0].sm) ga.sm = *p[0].sm;
-  const slim_status st = launch(ctx, name, tile, ga, grid, exact(p[0]), p[0].sm ? SOFTMAX : e && !parts[0] ? FINISH : PLAIN);
+  if (p[0].sg) ga.sg = *p[0].sg;
+  const slim_status st = launch(ctx, name, tile, ga, grid, exact(p[0]), p[0].sg ? GRADIENT : p[0].sm ? SOFTMAX : e && !parts[0] ? FINISH : PLAIN);
   if (st != SLIM_OK) return st;
   for (int i = 0; i < count; ++i)
     if (parts[i]) {

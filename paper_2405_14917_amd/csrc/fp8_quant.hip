@@ -65,6 +65,12 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
   for (int i = 0; i < 8; ++i) {
     fetch8(static_cast<const T*>(a.X) + (int64_t)min(r0 + i, a.rows - 1) * a.ldx + c0, a.cols - c0, a.cols, v[i]);
   }
+  unsigned z[ACT ? 8 : 1][4] = {};
+  if constexpr (ACT)
+    if (p == 0 && ta.g.Z)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        fetch8(static_cast<const T*>(ta.g.Z) + (int64_t)min(r0 + i, a.rows - 1) * ta.g.ldz + c0, a.cols - c0, a.cols, z[i]);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     row_end_shift<8>(v[i], a.cols < 8 ? 8 : a.cols - c0);
@@ -73,25 +79,27 @@ __global__ __launch_bounds__(256) void fp8_tiles(TileArgs ta) {
   if constexpr (ACT)
     if (p == 0) {
       float cs[8] = {};
+      slimact::with_act(ta.g.act, [&](auto act) {
+        constexpr int A = decltype(act)::value;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        unsigned z[4];
-        if (ta.g.Z) {
-          fetch8(static_cast<const T*>(ta.g.Z) + (int64_t)min(r0 + i, a.rows - 1) * ta.g.ldz + c0, a.cols - c0, a.cols, z);
-          row_end_shift<8>(z, a.cols < 8 ? 8 : a.cols - c0);
-        }
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (A != SLIM_ACT_NONE) row_end_shift<8>(z[i], a.cols < 8 ? 8 : a.cols - c0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float d[2];
+          for (int j = 0; j < 4; ++j) {
+            float d[2];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            d[h] = __uint_as_float(Half16<T>::float_bits((v[i][j] >> (16 * h)) & 0xffffu));
-            if (ta.g.Z && r0 + i < a.rows) d[h] *= slimact::slope(__uint_as_float(Half16<T>::float_bits((z[j] >> (16 * h)) & 0xffffu)), ta.g.act);
-            cs[2 * j + h] += d[h];
+            for (int h = 0; h < 2; ++h) {
+              d[h] = __uint_as_float(Half16<T>::float_bits((v[i][j] >> (16 * h)) & 0xffffu));
+              if constexpr (A != SLIM_ACT_NONE) {
+                const float f = slimact::slope(__uint_as_float(Half16<T>::float_bits((z[i][j] >> (16 * h)) & 0xffffu)), A);
+                d[h] = r0 + i < a.rows ? d[h] * f : 0.f;               // (behind the last row: the last one's, which need not be finite)
+              }
+              cs[2 * j + h] += d[h];
+            }
+            if constexpr (A != SLIM_ACT_NONE) v[i][j] = (unsigned)to_16(d[0], Half16<T>::INF == 0x7f80u) | (unsigned)to_16(d[1], Half16<T>::INF == 0x7f80u) << 16;
           }
-          v[i][j] = (unsigned)to_16(d[0], Half16<T>::INF == 0x7f80u) | (unsigned)to_16(d[1], Half16<T>::INF == 0x7f80u) << 16;
         }
-      }
+      });
       if (ta.g.sums) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

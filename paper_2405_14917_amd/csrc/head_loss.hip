@@ -14,15 +14,9 @@ namespace {
 
 using namespace slimfp8;
 
-// A token's softmax: exp(z - top) inv is a probability; g: the gradient of its loss, 0 where its label is no class
-struct Stat {
-  float top, inv, g;
-  int label;
-};
-
 // One wavefront per token.  Pairs in a fixed order; loss or stat may be null.
 __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part, int parts, const float* __restrict__ z, const void* labels, int labels64,
-                                                 const float* __restrict__ dloss, int t, int V, float* __restrict__ loss, Stat* __restrict__ stat) {
+                                                 const float* __restrict__ dloss, int t, int V, float* __restrict__ loss, TokenStat* __restrict__ stat) {
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= t) return;
@@ -37,122 +31,10 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
     const int64_t label = label_at(labels, labels64, row);
     const bool live = label >= 0 && label < V;
     loss[row] = live ? (float)((double)top + log(sum) - (double)z[row]) : 0.f;
-    if (stat) stat[row] = Stat{top, (float)(1.0 / sum), live ? dloss[row] : 0.f, live ? (int)label : -1};
-  }
-}
-
-struct GradientArgs {
-  const float* z;                  // t x classes logits of this piece
-  const Stat* stat;
-  uint8_t *rows_q, *rows_s;        // dz in blocks of 128 classes (may be null)
-  uint8_t *cols_q, *cols_s;        // and, transposed, of 128 tokens (may be null)
-  int64_t ldz, ldrq, ldrs, ldcq, ldcs;
-  int t, classes, first;           // first class of the piece
-  int tiles_c;
-};
-
-__device__ __forceinline__ unsigned row_max(unsigned m) {
-  m = max(m, (unsigned)dpp_b32<DPP_XOR1>((int)m));
-  m = max(m, (unsigned)dpp_b32<DPP_XOR2>((int)m));
-  m = max(m, (unsigned)dpp_b32<DPP_HALF_MIRROR>((int)m));
-  return max(m, (unsigned)dpp_b32<DPP_MIRROR>((int)m));
-}
-// the magnitude's pattern, zero for what is not finite (patterns order like the values)
-__device__ __forceinline__ unsigned finite(float v) {
-  const unsigned u = __float_as_uint(v) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
-__device__ __forceinline__ unsigned four_e4m3(float a, float b, float c, float d, float inv) {
-  auto s = [&](float v) { return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u ? v * inv : __uint_as_float(0x7fc00000u); };
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(s(a), s(b), 0, false);
-  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(s(c), s(d), w, true);
-}
-
-// Tiles of 128 tokens x 128 classes: thread t holds tokens 8 (t / 16) .. + 7 of classes 8 (t % 16) .. + 7.
-__global__ __launch_bounds__(256) void head_gradient(GradientArgs a) {
-  __shared__ __align__(16) unsigned colmax[4][BLOCK];
-  __shared__ __align__(16) uint8_t tile[BLOCK * BLOCK];    // [class][token], units of 8 bytes at unit ^ (class / 8)
-  const int tr = blockIdx.x / a.tiles_c, tc = blockIdx.x % a.tiles_c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid & 15, rg = tid >> 4;
-  const int r0 = tr * BLOCK + rg * 8, c0 = tc * BLOCK + cg * 8;
-  float v[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    // (rows of the logits are padded to whole quads: ldz)
-    const float* p = a.z + (int64_t)min(r0 + i, a.t - 1) * a.ldz;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int c = c0 + 4 * h;
-      const float4 q = *reinterpret_cast<const float4*>(p + (c < a.classes ? c : 0));
-      v[i][4 * h] = q.x;
-      v[i][4 * h + 1] = q.y;
-      v[i][4 * h + 2] = q.z;
-      v[i][4 * h + 3] = q.w;
+    if (stat) {
+      const float g = live ? dloss[row] : 0.f, fine = g - g == 0.f ? g : __builtin_nanf("");      // (an infinite one is NaN in 8 bits in any case)
+      stat[row] = TokenStat{top, fine, (float)((double)fine / sum), live ? (int)label : -1};
     }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const Stat s = a.stat[min(r0 + i, a.t - 1)];
-    const bool live = r0 + i < a.t && s.label >= 0;
-    const int at = s.label - a.first - c0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = slimact::exp_of(fmaxf(v[i][j] - s.top, -126.f)) * s.inv;
-      v[i][j] = live && c0 + j < a.classes ? s.g * (v[i][j] != v[i][j] ? v[i][j] : at == j ? p - 1.f : p) : 0.f;
-    }
-  }
-  unsigned rm[8], m[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const unsigned u = finite(v[i][j]);
-      rm[i] = j ? max(rm[i], u) : u;
-      m[j] = i ? max(m[j], u) : u;
-    }
-  if (a.rows_q) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const unsigned b = scale_byte(row_max(rm[i]));
-      const float inv = __uint_as_float((254u - b) << 23);
-      if (r0 + i < a.t) {
-        const int64_t row = r0 + i;
-        *reinterpret_cast<uint2*>(a.rows_q + row * a.ldrq + c0) =
-            make_uint2(four_e4m3(v[i][0], v[i][1], v[i][2], v[i][3], inv), four_e4m3(v[i][4], v[i][5], v[i][6], v[i][7], inv));
-        if (cg == 0) a.rows_s[row * a.ldrs + tc] = (uint8_t)b;
-      }
-    }
-  }
-  if (!a.cols_q) return;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const auto a32 = __builtin_amdgcn_permlane32_swap(m[j], m[j], false, false);
-    const unsigned h = max(a32[0], a32[1]);
-    const auto a16 = __builtin_amdgcn_permlane16_swap(h, h, false, false);
-    m[j] = max(a16[0], a16[1]);
-  }
-  if (lane < 16) {
-    *reinterpret_cast<uint4*>(&colmax[wave][cg * 8]) = make_uint4(m[0], m[1], m[2], m[3]);
-    *reinterpret_cast<uint4*>(&colmax[wave][cg * 8 + 4]) = make_uint4(m[4], m[5], m[6], m[7]);
-  }
-  __syncthreads();
-  uint8_t* const tile0 = tile + cg * 8 * BLOCK + ((rg ^ cg) * 8);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int c = cg * 8 + j;
-    const unsigned b = scale_byte(max(max(colmax[0][c], colmax[1][c]), max(colmax[2][c], colmax[3][c])));
-    const float inv = __uint_as_float((254u - b) << 23);
-    *reinterpret_cast<uint2*>(tile0 + j * BLOCK) =
-        make_uint2(four_e4m3(v[0][j], v[1][j], v[2][j], v[3][j], inv), four_e4m3(v[4][j], v[5][j], v[6][j], v[7][j], inv));
-    if (rg == 0 && tc * BLOCK + c < a.classes) a.cols_s[(int64_t)(tc * BLOCK + c) * a.ldcs + tr] = (uint8_t)b;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = i * 32 + (tid >> 3), u = tid & 7, x = c >> 3;      // 16 bytes: units 2 u and 2 u + 1
-    uint4 w = *reinterpret_cast<const uint4*>(tile + c * BLOCK + ((2 * u) ^ (x & 14)) * 8);
-    if (x & 1) w = make_uint4(w.z, w.w, w.x, w.y);
-    if (tc * BLOCK + c < a.classes) *reinterpret_cast<uint4*>(a.cols_q + (int64_t)(tc * BLOCK + c) * a.ldcq + tr * BLOCK + u * 16) = w;
   }
 }
 
@@ -190,7 +72,7 @@ size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int
   if (t <= 0) return 0;
   const int64_t Vp = (int64_t)(V + HL_STEP - 1) / HL_STEP * HL_STEP;
   const int64_t logits = std::min(t * Vp, std::max(HL_LOGITS, (int64_t)HL_LEAST * t));
-  size_t bytes = loss_need(V, m, t, ncu) + slim_ws_round(sizeof(Stat) * (size_t)t) + slim_ws_round(sizeof(float) * (size_t)logits);
+  size_t bytes = loss_need(V, m, t, ncu) + slim_ws_round(sizeof(TokenStat) * (size_t)t);
   size_t parts = 0;                               // of the products that are cut, one after another
   Product p = {};
   if (dx) {
@@ -208,8 +90,7 @@ size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int
     p.nk = slim_cdiv(t, BLOCK);
     parts = std::max(parts, gemm_workspace(&p, 1, ncu));
   }
-  p = logits_product((int)Vp, m, t, nullptr);
-  return bytes + std::max(parts, gemm_workspace(&p, 1, ncu));
+  return bytes + parts;
 }
 
 slim_status check_head(slim_ctx* ctx, const char* fn, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
@@ -225,7 +106,7 @@ slim_status check_head(slim_ctx* ctx, const char* fn, const void* X, slim_dtype 
 
 // Losses and, with `stat`, the tokens' sums; x: the quantised activations (not looked at where a few tokens are multiplied in one launch)
 slim_status losses(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& x, const Operand& w, int m, const void* labels,
-                   int labels64, const float* dloss, float* loss, Stat* stat) {
+                   int labels64, const float* dloss, float* loss, TokenStat* stat) {
   const int V = w.rows, ncu = ctx->num_cus;
   const bool few = takes_few_tokens(V, m, t, ncu);
   Softmax sm = {nullptr, nullptr, labels, labels64, 0};
@@ -296,7 +177,7 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
   Activations a = {X, ldx, t, m, nullptr, nullptr, nullptr, nullptr};
   bool ok = carve(ctx, t, m, a.rows_q, a.rows_s);
   if (dW) ok = ok && carve(ctx, m, t, a.cols_q, a.cols_s);
-  Stat* const stat = static_cast<Stat*>(slim_ws_alloc(ctx, sizeof(Stat) * (size_t)t));
+  TokenStat* const stat = static_cast<TokenStat*>(slim_ws_alloc(ctx, sizeof(TokenStat) * (size_t)t));
   if (!ok || !stat) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
   if (const slim_status e = quantize(ctx, "fp8_quantize_x", x_dtype, &a, 1); e != SLIM_OK) return e;
   const Operand x = {a.rows_q, a.rows_s, quantized_ld(m), scales_ld(m), t, 0}, xt = {a.cols_q, a.cols_s, quantized_ld(t), scales_ld(t), m, 0};
@@ -305,14 +186,9 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
 
   const int piece = piece_of(V, t);
   const int64_t ldacc = (m + 3) / 4 * 4;
-  GradientArgs g = {};
+  SoftmaxGradient g = {};
   g.stat = stat;
-  g.t = t;
-  g.ldz = piece;
-  float* const z = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)t * piece));
   float* acc = nullptr;
-  g.z = z;
-  ok = z != nullptr;
   if (dX) {
     g.ldrq = quantized_ld(piece);
     g.ldrs = scales_ld(piece);
@@ -331,19 +207,14 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
     Product p = logits_product(n, m, t, nullptr);
     p.a = Operand{q + v0 * ldq, s + v0 / BLOCK * lds, ldq, lds, n, 7};
     p.b = x;
-    p.c = z;
-    p.ldc = piece;
-    ctx->ws_off = mark;                           // (the parts of a product that is cut are done with once it is enqueued)
-    if (const slim_status e = gemm(ctx, "head_logits", &p, 1); e != SLIM_OK) return e;
-    g.classes = n;
+    p.sg = &g;
     g.first = v0;
-    g.tiles_c = slim_cdiv(n, BLOCK);
-    SLIM_LAUNCH(ctx, "head_gradient", head_gradient, dim3(g.tiles_c * slim_cdiv(t, BLOCK)), dim3(256), 0, g);
+    if (const slim_status e = gemm(ctx, "head_gradient", &p, 1); e != SLIM_OK) return e;
     if (dX) {
       Product d = {};
       d.a = Operand{qt + v0, st + v0 / BLOCK, ldqt, ldst, m, 7};
       d.b = Operand{g.rows_q, g.rows_s, g.ldrq, g.ldrs, t, 0};
-      d.nk = g.tiles_c;
+      d.nk = slim_cdiv(n, BLOCK);
       d.coarse = true;
       const bool last = v0 + n == V;
       d.c = last ? dX : acc;
@@ -354,7 +225,7 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
       sum.ldr = ldacc;
       sum.r_dtype = SLIM_F32;
       if (v0 > 0) d.e = &sum;
-      ctx->ws_off = mark;
+      ctx->ws_off = mark;                         // (the parts of a product that is cut are done with once it is enqueued)
       if (const slim_status e = gemm(ctx, "head_dx", &d, 1); e != SLIM_OK) return e;
     }
     if (dW) {
