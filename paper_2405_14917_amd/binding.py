@@ -269,17 +269,21 @@ def grad_norm_workspace(count: int, num_cus: int = 0) -> int:
     return int(load().slim_grad_norm_workspace(count, num_cus))
 
 
+_FLOATS = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
 def _tensor_list(tensors, what: str):
     """The descriptions (address, rows, columns, leading dimension, type) that the library takes of a list of tensors."""
     flat = []
     for t in tensors:
-        if t.dtype not in (torch.float16, torch.bfloat16, torch.float32):
+        d = _FLOATS.get(t.dtype)
+        if d is None:
             raise ValueError("%s have to be float16, bfloat16 or float32" % what)
         if t.is_contiguous():
             n = t.numel()
-            flat += (t.data_ptr(), 1, n, n, _DT[t.dtype])
+            flat += (t.data_ptr(), 1, n, n, d)
         elif t.dim() == 2:
-            flat += (t.data_ptr(), t.shape[0], t.shape[1], _row_stride(t, what), _DT[t.dtype])
+            flat += (t.data_ptr(), t.shape[0], t.shape[1], _row_stride(t, what), d)
         else:
             raise ValueError("%s have to be contiguous, or matrices with contiguous rows" % what)
     return (ctypes.c_int64 * len(flat))(*flat)
@@ -836,30 +840,40 @@ class Slim:
         rows, cols = self._norm_shape(X, w, b)
         if not (y or e4m3):
             raise ValueError("neither form of the norm is wanted")
-        for v in (R, H):
-            if v is not None and (v.shape != X.shape or v.dtype != X.dtype):
-                raise ValueError("R and H have to be of X's shape and type")
+        shape, dtype = X.shape, X.dtype
+        if R is not None and (R.shape != shape or R.dtype != dtype) or H is not None and (H.shape != shape or H.dtype != dtype):
+            raise ValueError("R and H have to be of X's shape and type")
+        ldx = _row_stride(X, "X")
+        ldr = ldh = cols
         if R is None:
             if H is not None and H.data_ptr() != X.data_ptr():
                 raise ValueError("without R the stream is X itself")
             H = X
-        elif H is None:
-            H = _empty_like(X)
+        else:
+            ldr = _row_stride(R, "R")
+            if H is None:
+                H = _empty_like(X)
+            else:
+                ldh = _row_stride(H, "H")
         Y = _empty_like(X) if y else None
         q = s = mean = rstd = None
         ldq = lds = 0
         if e4m3:
+            # (rows of many an odd number of blocks apart: they spread over the channels of the L2; a few next to one another: no view to be made)
             blocks = (cols + 127) // 128
-            ldq, lds = (blocks | 1) * 128, (blocks + 3) // 4 * 4     # (rows an odd number of blocks apart: they spread over the channels of the L2)
-            q = X.new_empty((rows, ldq), dtype=_E4M3)[:, :cols]
-            s = X.new_empty((rows, lds), dtype=torch.uint8)[:, :blocks]
+            ldq, lds = (blocks if rows <= 16 else blocks | 1) * 128, (blocks + 3) // 4 * 4
+            q, s = X.new_empty((rows, ldq), dtype=_E4M3), X.new_empty((rows, lds), dtype=torch.uint8)
+            if ldq != cols:
+                q = q[:, :cols]
+            if lds != blocks:
+                s = s[:, :blocks]
         if stats:
             mean = None if rms else X.new_empty(rows, dtype=torch.float32)
             rstd = X.new_empty(rows, dtype=torch.float32)
-        p = lambda v: None if v is None else v.data_ptr()
-        st = self.lib.slim_add_norm(self.ctx, X.data_ptr(), p(R), _dtype(X), rows, cols, _row_stride(X, "X"), 0 if R is None else _row_stride(R, "R"),
-                                    w.data_ptr(), p(b), _dtype(w), eps, rms, H.data_ptr(), _row_stride(H, "H"), p(Y), cols, p(q), ldq, p(s), lds,
-                                    p(mean), p(rstd))
+        st = self.lib.slim_add_norm(self.ctx, X.data_ptr(), None if R is None else R.data_ptr(), _dtype(X), rows, cols, ldx, ldr, w.data_ptr(),
+                                    None if b is None else b.data_ptr(), _dtype(w), eps, rms, H.data_ptr(), ldh, None if Y is None else Y.data_ptr(),
+                                    cols, None if q is None else q.data_ptr(), ldq, None if s is None else s.data_ptr(), lds,
+                                    None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr())
         if st:
             self._check(st)
         return AddNorm(H, Y, q, s, mean, rstd)
@@ -905,17 +919,19 @@ class Slim:
         if out is not None:
             out = list(out)
             self._ready(*out)
-            if len(out) != len(tensors) or any(o.shape != t.shape or o.dtype != t.dtype for o, t in zip(out, tensors)):
-                raise ValueError("out has to hold tensors of the same shapes and types")
-            # (one description of rows for both: an output of other strides is described by its rows too)
-            if any(o.is_contiguous() != t.is_contiguous() for o, t in zip(out, tensors)):
-                into, tensors = _tensor_rows(out, "out"), _tensor_rows(tensors, "tensors")
-            else:
-                into, tensors = _tensor_list(out, "out"), _tensor_list(tensors, "tensors")
+            if len(out) != len(tensors):
+                raise ValueError("out has to hold as many tensors")
+            into, flat = _tensor_list(out, "out"), _tensor_list(tensors, "tensors")
+            for o, t in zip(out, tensors):
+                if o.shape != t.shape or o.dtype != t.dtype:
+                    raise ValueError("out has to hold tensors of the same shapes and types")
+            if into[1::5] != flat[1::5]:
+                # (of a tensor and its output one is contiguous, described as one row, and the other is not: both by their rows)
+                into, flat = _tensor_rows(out, "out"), _tensor_rows(tensors, "tensors")
         else:
-            tensors = _tensor_list(tensors, "tensors")
+            flat = _tensor_list(tensors, "tensors")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
-        st = self.lib.slim_clip_gradients(self.ctx, tensors, into, len(tensors) // 5, float(limit), norm.data_ptr())
+        st = self.lib.slim_clip_gradients(self.ctx, flat, into, len(tensors), limit, norm.data_ptr())
         if st:
             self._check(st)
         return norm

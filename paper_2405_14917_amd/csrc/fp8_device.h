@@ -185,7 +185,7 @@ struct Product {
   int64_t ldc;
   slim_dtype c_dtype;
   int nk;
-  const Epilogue* e;               // of a product that is alone in its launch, or null
+  const Epilogue* e;               // of the first product of a launch, or null
   bool coarse;                     // fp32 C from the e4m3 matrix cores
   const Softmax* sm;               // of a product that is alone in its launch, or null
   const SoftmaxGradient* sg;       // the same

@@ -124,25 +124,49 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   // a lane holds rows 4 c .. + 3 of its token
 #pragma unroll
   for (int r = 0; r < RT; ++r) *reinterpret_cast<v4f*>(part + (wave * 16 + l16) * LD + r * 16 + c * 4) = acc[r];
-  __syncthreads();
   const int last = min(ROWS, a.n - row0);
+  // element e of the tile's: row e % ROWS of token e / ROWS
+  auto sum_of = [&](int e) {
+    const float* p = part + (e / ROWS) * LD + e % ROWS;
+    float sum = 0.f;
+    for (int i = 0; i < nw; ++i) sum += p[i * 16 * LD];
+    return sum;
+  };
+  if constexpr (MODE == FINISH) {
+    // Bias and residual of a thread's elements are fetched before the wavefronts' sums are waited for, and there is one branch for the activation
+    // (1000 x 1504, 301 tokens, 8-bit activations, gelu, kept sums: 9.5 -> 9.1 us).
+    constexpr int EACH = (16 * ROWS + 64 * FEW_WAVES - 1) / (64 * FEW_WAVES);      // elements of a thread, with all the wavefronts
+    for (int e0 = threadIdx.x, first = 1; first || e0 - (int)threadIdx.x < tn * ROWS; e0 += EACH * blockDim.x, first = 0) {
+      float v[EACH], b[EACH], res[EACH];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const int e = e0 + i * blockDim.x, tok = e / ROWS, r = e % ROWS;
+        const bool there = tok < tn && r < last;
+        b[i] = there && a.e.bias ? from_any(a.e.bias, a.e.bias_dtype, row0 + r) : 0.f;
+        res[i] = there && a.e.R ? from_any(a.e.R, a.e.r_dtype, (int64_t)(tok0 + tok) * a.e.ldr + row0 + r) : 0.f;
+      }
+      if (first) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const int e = e0 + i * blockDim.x, tok = e / ROWS, r = e % ROWS;
+        v[i] = tok < tn ? sum_of(e) + b[i] : 0.f;
+        if (a.e.Z && tok < tn && r < last) to_any(a.e.Z, a.y_dtype, (int64_t)(tok0 + tok) * a.e.ldz + row0 + r, v[i]);
+      }
+      slimact::activate(v, a.e.act);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const int e = e0 + i * blockDim.x, tok = e / ROWS, r = e % ROWS;
+        if (tok < tn && r < last) to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, a.e.R ? v[i] + res[i] : v[i]);
+      }
+    }
+    return;
+  }
+  __syncthreads();
   for (int e = threadIdx.x; e < tn * ROWS; e += blockDim.x) {
     const int tok = e / ROWS, r = e % ROWS;
-    float sum = 0.f;
-    for (int i = 0; i < nw; ++i) sum += part[(i * 16 + tok) * LD + r];
-    if constexpr (MODE == SOFTMAX) {
-      part[tok * LD + r] = r < last ? sum : -__builtin_inff();   // (the place of the first wavefront's sum, which nobody else reads)
-    } else if (r < last) {
-      if constexpr (MODE == FINISH) {
-        const int64_t row = tok0 + tok;
-        const int col = row0 + r;
-        if (a.e.bias) sum += from_any(a.e.bias, a.e.bias_dtype, col);
-        if (a.e.Z) to_any(a.e.Z, a.y_dtype, row * a.e.ldz + col, sum);
-        sum = slimact::activated(sum, a.e.act);
-        if (a.e.R) sum += from_any(a.e.R, a.e.r_dtype, row * a.e.ldr + col);
-      }
-      to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
-    }
+    const float sum = sum_of(e);
+    if constexpr (MODE == SOFTMAX) part[tok * LD + r] = r < last ? sum : -__builtin_inff();      // (the first wavefront's sum, which nobody else reads)
+    else if (r < last) to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
   }
   if constexpr (MODE == SOFTMAX) {
     __syncthreads();

@@ -124,48 +124,67 @@ __device__ __forceinline__ void store4(void* row, int dtype, int col, int left, 
   }
 }
 
-// four values of a row from column `col` on as floats, of which `left` exist (the others are zero)
-__device__ __forceinline__ float4 load_any4(const void* row, int dtype, int col, int left) {
-  float f[4] = {0.f, 0.f, 0.f, 0.f};
+// Four values of a row from column `col` on as they lie there, of which `left` exist (the others are zero), and as floats
+struct alignas(16) Quad {
+  unsigned v[4];
+};
+__device__ __forceinline__ Quad load_quad(const void* row, int dtype, int col, int left) {
+  Quad r = {{0u, 0u, 0u, 0u}};
   if (dtype == SLIM_F32) {
-    const float* p = static_cast<const float*>(row) + col;
+    const unsigned* p = static_cast<const unsigned*>(row) + col;
     if (left >= 4) {
-      __builtin_memcpy(f, p, 16);
+      __builtin_memcpy(r.v, p, 16);
     } else {
 #pragma unroll
       for (int i = 0; i < 3; ++i)
-        if (i < left) f[i] = p[i];
+        if (i < left) r.v[i] = p[i];
     }
   } else {
     const unsigned short* p = static_cast<const unsigned short*>(row) + col;
-    unsigned short h[4] = {0, 0, 0, 0};
     if (left >= 4) {
-      __builtin_memcpy(h, p, 8);
+      __builtin_memcpy(r.v, p, 8);
     } else {
 #pragma unroll
       for (int i = 0; i < 3; ++i)
-        if (i < left) h[i] = p[i];
+        if (i < left) r.v[i / 2] |= (unsigned)p[i] << (16 * (i & 1));
     }
+  }
+  return r;
+}
+__device__ __forceinline__ float4 widen(const Quad& r, int dtype) {
+  if (dtype == SLIM_F32) return make_float4(__uint_as_float(r.v[0]), __uint_as_float(r.v[1]), __uint_as_float(r.v[2]), __uint_as_float(r.v[3]));
+  float f[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      f[i] = __uint_as_float(dtype == SLIM_BF16 ? Half16<__hip_bfloat16>::float_bits(h[i]) : Half16<__half>::float_bits(h[i]));
+  for (int i = 0; i < 4; ++i) {
+    const unsigned h = (r.v[i / 2] >> (16 * (i & 1))) & 0xffffu;
+    f[i] = __uint_as_float(dtype == SLIM_BF16 ? Half16<__hip_bfloat16>::float_bits(h) : Half16<__half>::float_bits(h));
   }
   return make_float4(f[0], f[1], f[2], f[3]);
 }
 
-// N quads of sums through the epilogue, quad i of row `row[i]` of C from column `col` on, of which `left` exist: the residuals first, so that their
-// loads are under way together (Z and C are stored here; rows behind the last one are left out)
+// f of 0 .. N - 1 as constants (a loop whose body is too long to be unrolled would keep the accumulators in memory)
+template <int I, int N, typename F>
+__device__ __forceinline__ void static_for(const F& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>());
+    static_for<I + 1, N>(f);
+  }
+}
+
+// The residuals of N quads, quad i in row `row + i step` from column `col` on (rows behind the last one: what is there is not used)
 template <int N>
-__device__ __forceinline__ void finish(const Epilogue& e, char* c, int64_t ldc, int dtype, int row, int step, int rows, int col, int left, float (&v)[4 * N]) {
-  const int64_t size = dtype == SLIM_F32 ? 4 : 2;
-  float4 r[N];
-  if (e.R)
+__device__ __forceinline__ void load_residuals(const Epilogue& e, int row, int step, int rows, int col, int left, Quad (&r)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (row + i * step < rows)
-        r[i] = load_any4(static_cast<const char*>(e.R) + (row + i * step) * e.ldr * (e.r_dtype == SLIM_F32 ? 4 : 2), e.r_dtype, col, left);
+  for (int i = 0; i < N; ++i)
+    if (row + i * step < rows) r[i] = load_quad(static_cast<const char*>(e.R) + (row + i * step) * e.ldr * (int64_t)(e.r_dtype == SLIM_F32 ? 4 : 2), e.r_dtype, col, left);
+}
+// These quads' sums through the epilogue (Z and C are stored here)
+template <int N>
+__device__ __forceinline__ void finish(const Epilogue& e, char* c, int64_t ldc, int dtype, int row, int step, int rows, int col, int left, float (&v)[4 * N],
+                                       const Quad (&r)[N]) {
+  const int64_t size = dtype == SLIM_F32 ? 4 : 2;
   if (e.bias) {
-    const float4 b = load_any4(e.bias, e.bias_dtype, col, left);
+    const float4 b = widen(load_quad(e.bias, e.bias_dtype, col, left), e.bias_dtype);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       v[4 * i] += b.x;
@@ -184,7 +203,10 @@ __device__ __forceinline__ void finish(const Epilogue& e, char* c, int64_t ldc, 
   for (int i = 0; i < N; ++i)
     if (row + i * step < rows) {
       float4 y = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-      if (e.R) y = make_float4(y.x + r[i].x, y.y + r[i].y, y.z + r[i].z, y.w + r[i].w);
+      if (e.R) {
+        const float4 s = widen(r[i], e.r_dtype);
+        y = make_float4(y.x + s.x, y.y + s.y, y.z + s.z, y.w + s.w);
+      }
       store4(c + (row + i * step) * ldc * size, dtype, col, left, y);
     }
 }
@@ -369,7 +391,8 @@ __device__ __forceinline__ void quantize_gradient(v16f (&acc)[T::MA][T::MB], con
   }
 }
 
-// EXACT: products of the numbers in bf16 (fp32 outputs).  MODE other than PLAIN: of one product that is not cut.
+// EXACT: products of the numbers in bf16 (fp32 outputs).  MODE other than PLAIN: of the first product, which is not cut; SOFTMAX and GRADIENT have
+// no second one.
 template <typename T, bool EXACT, int MODE>
 __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_gemm(GemmArgs ga) {
   constexpr int MA = T::MA, MB = T::MB, M = MA * MB, READS = 2 * (MA + MB), S = T::STAGES;
@@ -642,6 +665,53 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
   static_assert(QUADS <= 64, "a row of a wavefront's part is read by one instruction");
   char* cbase = static_cast<char*>(p.c) + (int64_t)split * p.part * 4;
   const int esize = p.c_dtype == SLIM_F32 ? 4 : 2;
+  if (MODE == FINISH && !second) {
+    // N quads of a lane at a time.  Residuals are fetched many at a time and ahead of their use, not one round of loads after another: where N is all
+    // of a j, those of every j first (4096 x 11008, 2048 tokens, 16-bit activations: 120 -> 110 us), else those of the j to come, which wait in a
+    // part of LDS, since a loop of several rounds cannot count through registers (8192 x 4096, 4096 tokens: 223 -> 168).
+    constexpr int N = RPI >= 4 ? 32 / RPI : 4, ALL = 32 / RPI;
+    constexpr bool AHEAD = N * RPI == 32 && MB <= 2;
+    static_assert(AHEAD || T::OUT + T::THREADS * ALL * 16 <= T::LDS, "the stages' place is enough");
+    uint4* const waiting = reinterpret_cast<uint4*>(smem_fg + T::OUT) + tid;      // quad i of this lane at i T::THREADS
+    const int col = (lane % QUADS) * 4, ca = a0 + wa * T::MA * 32 + col, row0 = b0 + wb * T::MB * 32 + lane / QUADS;
+    const bool some = ca < p.a.rows;
+    Quad ahead[AHEAD ? MB : 1][ALL];
+    if (some && ga.e.R)
+#pragma unroll
+      for (int j = 0; j < (AHEAD ? MB : 1); ++j) load_residuals<ALL>(ga.e, row0 + j * 32, RPI, p.b.rows, ca, p.a.rows - ca, ahead[j]);
+    static_for<0, MB>([&](auto block) __attribute__((always_inline)) {
+      constexpr int j = decltype(block)::value;
+#pragma unroll
+      for (int i = 0; i < T::MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(out + l32 * T::OUT_LD + i * 32 + q * 8 + h * 4) =
+              make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      if (!AHEAD && some && ga.e.R) {
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) waiting[i * T::THREADS] = *reinterpret_cast<const uint4*>(ahead[0][i].v);
+        if (j + 1 < MB) load_residuals<ALL>(ga.e, row0 + (j + 1) * 32, RPI, p.b.rows, ca, p.a.rows - ca, ahead[0]);
+      }
+#pragma unroll 1
+      for (int r = 0; r < 32; r += N * RPI) {
+        const int row = row0 + j * 32 + r;
+        float v[4 * N];
+        Quad res[N] = {};
+        if (AHEAD) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) res[i] = ahead[AHEAD ? j : 0][i];
+        } else if (some && ga.e.R) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(res[i].v) = waiting[(r / RPI + i) * T::THREADS];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          *reinterpret_cast<float4*>(&v[4 * i]) = *reinterpret_cast<const float4*>(out + (r + lane / QUADS + i * RPI) * T::OUT_LD + col);
+        if (some) finish<N>(ga.e, cbase, p.ldc, p.c_dtype, row, RPI, p.b.rows, ca, p.a.rows - ca, v, res);
+      }
+    });
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < T::MB; ++j) {
 #pragma unroll
@@ -650,24 +720,12 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(out + l32 * T::OUT_LD + i * 32 + q * 8 + h * 4) =
             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    if constexpr (MODE == FINISH) {
-      constexpr int N = 4;
-      const int col = (lane % QUADS) * 4, ca = a0 + wa * T::MA * 32 + col;
-#pragma unroll 1
-      for (int r = lane / QUADS; r < 32; r += N * RPI) {
-        float v[4 * N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<float4*>(&v[4 * i]) = *reinterpret_cast<const float4*>(out + (r + i * RPI) * T::OUT_LD + col);
-        if (ca < p.a.rows) finish<N>(ga.e, cbase, p.ldc, p.c_dtype, b0 + (wb * T::MB + j) * 32 + r, RPI, p.b.rows, ca, p.a.rows - ca, v);
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 32; r += RPI) {
-        const int rr = r + lane / QUADS, col = (lane % QUADS) * 4;
-        const float4 v = *reinterpret_cast<const float4*>(out + rr * T::OUT_LD + col);
-        const int row = b0 + (wb * T::MB + j) * 32 + rr, ca = a0 + wa * T::MA * 32 + col;
-        if (row < p.b.rows) store4(cbase + (int64_t)row * p.ldc * esize, p.c_dtype, ca, p.a.rows - ca, v);
-      }
+    for (int r = 0; r < 32; r += RPI) {
+      const int rr = r + lane / QUADS, col = (lane % QUADS) * 4;
+      const float4 v = *reinterpret_cast<const float4*>(out + rr * T::OUT_LD + col);
+      const int row = b0 + (wb * T::MB + j) * 32 + rr, ca = a0 + wa * T::MA * 32 + col;
+      if (row < p.b.rows) store4(cbase + (int64_t)row * p.ldc * esize, p.c_dtype, ca, p.a.rows - ca, v);
     }
   }
 }
@@ -690,7 +748,9 @@ __global__ __launch_bounds__(256) void fp8_join(ProductArgs p, const float* __re
   }
   if constexpr (FINISH_) {
     float v[4] = {s.x, s.y, s.z, s.w};
-    return finish<1>(e, static_cast<char*>(c), ldc, dtype, row, 1, p.b.rows, col, p.a.rows - col, v);
+    Quad r[1] = {};
+    if (e.R) load_residuals<1>(e, row, 1, p.b.rows, col, p.a.rows - col, r);
+    return finish<1>(e, static_cast<char*>(c), ldc, dtype, row, 1, p.b.rows, col, p.a.rows - col, v, r);
   }
   store4(static_cast<char*>(c) + (int64_t)row * ldc * (dtype == SLIM_F32 ? 4 : 2), dtype, col, p.a.rows - col, s);
 }
@@ -710,10 +770,10 @@ bool exact(const Product& p) { return p.sm || p.sg || (p.c_dtype == SLIM_F32 && 
 int tiles_of(const Product& p, int tile) { return slim_cdiv(p.a.rows, TILE_A[tile]) * slim_cdiv(p.b.rows, TILE_B[tile]); }
 
 // Parts along the contraction, where `tiles` do not fill the chip; eight steps a part at least.  (A softmax needs the whole sums.)
-int parts_of(const Product& p, int tiles, int ncu) {
+int parts_of(const Product& p, int tile, int ncu) {
   if (p.sm || p.sg) return 1;
   const int nk = p.nk;
-  const int s = std::max(1, std::min(ncu / std::max(1, tiles), nk / 8));
+  const int s = std::max(1, std::min(ncu / std::max(1, tiles_of(p, tile)), nk / 8));
   const int per = slim_cdiv(slim_cdiv(std::max(1, nk), s), 4) * 4;
   return std::max(1, slim_cdiv(nk, per));
 }
@@ -723,13 +783,16 @@ int parts_of(const Product& p, int tiles, int ncu) {
 // that a step; 6 for the launch.  So 15872 x 128, 6139 tokens, takes medium tiles (81; large ones 110, small ones 147), as does 14666 x 2048, 2078 tokens,
 // whose 522 large ones are three rounds (78 and 102), 2048 x 2048, 1024 tokens, small ones (17; medium ones 26), and 8192 x 28672, 4096
 // tokens, large ones (790; medium ones above 900).  The bytes of the operands are in the measured step, not a term of their own.
+// With residuals or kept sums a round of large tiles costs 3 more than one of medium ones, whose epilogues run beside another workgroup's products: 8192 x
+// 4096, 4096 tokens, residual 168 and 164, with gelu and kept sums too 225 and 202; 8192 x 28672 792 and 985.
 double tile_cost(const Product& p, int tile, int ncu) {
   static const double round[] = {15.0, 5.4, 2.7}, step[2][3] = {{1.44, 0.82, 0.34}, {2.6, 1.42, 0.56}};
-  const int tiles = tiles_of(p, tile), s = parts_of(p, tiles, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
+  const int tiles = tiles_of(p, tile), s = parts_of(p, tile, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
   double one = step[exact(p)][tile];
   if (tile == TILE_MEDIUM && tiles * s <= ncu) one *= 0.6;
+  const double epilogue = tile == TILE_LARGE && p.e && (p.e->R || p.e->Z) ? 3.0 : 0.0;
   const double join = s > 1 ? 4.0 + 8.0 * s * p.a.rows * (double)p.b.rows / 4.85e6 : 0.0;
-  return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + one * slim_cdiv(p.nk, s)) + join;
+  return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + epilogue + one * slim_cdiv(p.nk, s)) + join;
 }
 int tile_of(const Product& p, int ncu) {
   int best = p.sg ? TILE_MEDIUM : TILE_SMALL;                       // (a gradient's tile holds whole blocks of 128)
@@ -748,7 +811,7 @@ int in_one_launch(const Product* p, int count, int ncu) {
 Plan make_plan(const Product* p, int count, int ncu) {
   Plan pl = {};
   for (int i = 0; i < count; ++i) {
-    pl.splits[i] = parts_of(p[i], tiles_of(p[i], tile_of(p[i], ncu)), ncu);
+    pl.splits[i] = parts_of(p[i], tile_of(p[i], ncu), ncu);
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
   }
   return pl;
@@ -827,7 +890,7 @@ slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int coun
     if (parts[i]) {
       const int64_t quads = (int64_t)slim_cdiv(p[i].a.rows, 4) * p[i].b.rows;
       const dim3 g(slim_cdiv(quads, 256));
-      if (e) SLIM_LAUNCH(ctx, "fp8_join", fp8_join<true>, g, dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc, (int)p[i].c_dtype, ga.e);
+      if (e && i == 0) SLIM_LAUNCH(ctx, "fp8_join", fp8_join<true>, g, dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc, (int)p[i].c_dtype, ga.e);
       else SLIM_LAUNCH(ctx, "fp8_join", fp8_join<false>, g, dim3(256), 0, ga.p[i], parts[i], pl.ldp[i], p[i].c, p[i].ldc, (int)p[i].c_dtype, ga.e);
     }
   return SLIM_OK;

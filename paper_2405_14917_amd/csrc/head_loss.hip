@@ -81,14 +81,14 @@ size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int
     p.a.rows = m;
     p.b.rows = t;
     p.nk = (int)(Vp / BLOCK);
-    parts = std::max(parts, gemm_workspace(&p, 1, ncu));
+    parts += gemm_workspace(&p, 1, ncu);
   }
   if (dw) {
     bytes += activation_bytes(m, t) + slim_ws_round((size_t)(logits + 2 * BLOCK * Vp)) + slim_ws_round((size_t)(logits / BLOCK + 8 * Vp));
     p.a.rows = m;
     p.b.rows = (int)Vp;
     p.nk = slim_cdiv(t, BLOCK);
-    parts = std::max(parts, gemm_workspace(&p, 1, ncu));
+    parts += gemm_workspace(&p, 1, ncu);
   }
   return bytes + parts;
 }
@@ -210,8 +210,11 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
     p.sg = &g;
     g.first = v0;
     if (const slim_status e = gemm(ctx, "head_gradient", &p, 1); e != SLIM_OK) return e;
+    Product both[2] = {};                         // dX's share, and the piece's rows of dW
+    int count = 0;
+    Epilogue sum = {};
     if (dX) {
-      Product d = {};
+      Product& d = both[count++];
       d.a = Operand{qt + v0, st + v0 / BLOCK, ldqt, ldst, m, 7};
       d.b = Operand{g.rows_q, g.rows_s, g.ldrq, g.ldrs, t, 0};
       d.nk = slim_cdiv(n, BLOCK);
@@ -220,25 +223,22 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
       d.c = last ? dX : acc;
       d.ldc = last ? lddx : ldacc;
       d.c_dtype = last ? x_dtype : SLIM_F32;
-      Epilogue sum = {};
       sum.R = acc;
       sum.ldr = ldacc;
       sum.r_dtype = SLIM_F32;
       if (v0 > 0) d.e = &sum;
-      ctx->ws_off = mark;                         // (the parts of a product that is cut are done with once it is enqueued)
-      if (const slim_status e = gemm(ctx, "head_dx", &d, 1); e != SLIM_OK) return e;
     }
     if (dW) {
-      Product d = {};
+      Product& d = both[count++];
       d.a = xt;
       d.b = Operand{g.cols_q, g.cols_s, g.ldcq, g.ldcs, n, 0};
       d.nk = slim_cdiv(t, BLOCK);
       d.c = static_cast<char*>(dW) + (int64_t)v0 * lddw * (dw_dtype == SLIM_F32 ? 4 : 2);
       d.ldc = lddw;
       d.c_dtype = dw_dtype;
-      ctx->ws_off = mark;
-      if (const slim_status e = gemm(ctx, "head_dw", &d, 1); e != SLIM_OK) return e;
     }
+    ctx->ws_off = mark;                           // (the parts of products that are cut are done with once these are enqueued)
+    if (const slim_status e = gemm(ctx, "head_dx_dw", both, count); e != SLIM_OK) return e;
   }
   return SLIM_OK;
 }

@@ -159,7 +159,8 @@ extern "C" {
 
 size_t slim_layer_norm_backward_workspace(int64_t rows, int cols, slim_dtype x_dtype, int bias, int num_cus) {
   if (rows <= 0 || cols <= 0) return 0;
-  const size_t one = slim_ws_round(sizeof(float) * (size_t)parts_of(rows, cols, x_dtype, num_cus > 0 ? num_cus : 256) * cols);
+  const int ncu = num_cus > 0 ? num_cus : 256;
+  const size_t one = slim_ws_round(sizeof(float) * (size_t)std::max(parts_of(rows, cols, x_dtype, ncu, false), parts_of(rows, cols, x_dtype, ncu, true)) * cols);
   return bias ? 2 * one : one;
 }
 

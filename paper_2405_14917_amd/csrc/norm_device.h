@@ -235,25 +235,26 @@ __global__ __launch_bounds__(1024) void norm_join(const float* __restrict__ pw, 
 struct Shape {
   int w, p, g, per_cu;
 };
-Shape shape_of(int64_t rows, int cols, int e) {
+Shape shape_of(int64_t rows, int cols, int e, bool add) {
   const int pieces = slim_cdiv(cols, e);
   if (pieces <= 64) return rows <= 64 ? Shape{1, 1, 16, 0} : Shape{1, 1, 4, 4};
   if (pieces <= 128) return rows <= 32 ? Shape{1, 2, 8, 0} : Shape{1, 2, 4, 3};
   if (pieces <= 256) return rows <= 16 ? Shape{4, 1, 4, 0} : Shape{4, 1, 2, 2};
+  if (add && pieces > 256 && pieces <= 512 && rows > 8 && e == 8) return {4, 2, 1, 2};
   if (pieces <= 512) return rows <= 8 ? Shape{4, 2, 2, 0} : e == 8 ? Shape{4, 2, 1, 3} : Shape{4, 2, 2, 2};
   if (pieces <= 1024) return {8, 2, 1, rows <= 4 ? 0 : 2};
   if (pieces <= 2048) return {16, 2, 1, rows <= 4 ? 0 : 1};
   return {0, 0, 1, 2};
 }
 // workgroups, and with them partial sums, of the backward pass; 0: one for all rows, without partial sums
-int parts_of(int64_t rows, int cols, slim_dtype d, int ncu) {
-  const Shape s = shape_of(rows, cols, d == SLIM_F32 ? 4 : 8);
+int parts_of(int64_t rows, int cols, slim_dtype d, int ncu, bool add) {
+  const Shape s = shape_of(rows, cols, d == SLIM_F32 ? 4 : 8, add);
   return (int)std::min<int64_t>((rows + s.g - 1) / s.g, (int64_t)s.per_cu * ncu);
 }
 
 template <typename T, typename TW, bool ADD = false>
 slim_status backward(slim_ctx* ctx, const NormArgs& a, void* dw, void* db, int parts) {
-  const Shape s = shape_of(a.rows, a.cols, Piece<T>::E);
+  const Shape s = shape_of(a.rows, a.cols, Piece<T>::E, ADD);
   const char* name = "norm_backward";
   const dim3 grid(std::max(1, parts)), block(64 * s.w * s.g);
   const size_t smem = s.g > 1 ? sizeof(float) * (db ? 2 : 1) * (size_t)a.cols : 0;
@@ -303,7 +304,7 @@ slim_status backward_args(slim_ctx* ctx, const char* fn, NormArgs& a, const void
   SLIM_REQUIRE(ctx, w && dw, "%s: null weight or dw", fn);
   SLIM_REQUIRE(ctx, rows == 0 || (dY && X && dX && rstd && lddy >= cols && ldx >= cols && lddx >= cols),
                "%s: null pointer, or rows shorter than cols", fn);
-  parts = rows ? parts_of(rows, cols, x_dtype, ctx->num_cus) : 0;
+  parts = rows ? parts_of(rows, cols, x_dtype, ctx->num_cus, a.dH != nullptr) : 0;
   if (const slim_status st = slim_ws_reserve(ctx, slim_layer_norm_backward_workspace(rows, cols, x_dtype, db != nullptr, ctx->num_cus)); st != SLIM_OK)
     return st;
   a.X = X;

@@ -75,7 +75,7 @@ def test_gradients(slim, V, m, t, x, dw):
     gradient_check(slim, V, m, t, x, dw)
 
 
-@pytest.mark.parametrize("V,m,t", [(4100, 96, 700), (2050, 512, 1030), (33000, 64, 40), (40000, 128, 3), (5000, 130, 9000)])
+@pytest.mark.parametrize("V,m,t", [(4100, 96, 700), (2050, 512, 1030), (33000, 64, 40), (40000, 128, 3), (8200, 3000, 1030), (5000, 130, 9000)])
 def test_every_tile_and_several_pieces(slim, V, m, t):
     """Sizes that reach the tiles of both passes; the last one takes its vocabulary in several pieces."""
     X, labels, dloss, W, loss, dX, dW = gradient_check(slim, V, m, t, torch.bfloat16, torch.float32)

@@ -112,7 +112,7 @@ def test_forward(slim, n, m, t, x, y, name, bias, residual):
     forward(slim, n, m, t, x, y, name, bias, residual)
 
 
-TILES = [(1024, 512, 1100), (2304, 384, 2100), (1000, 1504, 301), (4096, 1030, 90), (4100, 1030, 70), (520, 9000, 96), (128, 20000, 40), (9000, 700, 16)]
+TILES = [(1024, 512, 1100), (2304, 384, 2100), (1000, 1504, 301), (4096, 1030, 90), (4100, 1030, 70), (520, 9000, 96), (128, 20000, 40), (9000, 700, 16), (4000, 6000, 2100)]
 
 
 @pytest.mark.parametrize("n,m,t", TILES)
