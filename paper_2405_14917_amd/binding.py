@@ -836,6 +836,7 @@ class Slim:
         among others.  Records no graph: without `stats` tensors that require a gradient are refused outside torch.no_grad()."""
         if not stats:
             _no_graph(X, R, w, b)
+        _no_graph(H)                         # (written over)
         self._ready(X, R, w, b, H)
         rows, cols = self._norm_shape(X, w, b)
         if not (y or e4m3):
@@ -901,10 +902,12 @@ class Slim:
         return dX, dw, db
 
     def grad_norm(self, tensors: Sequence[torch.Tensor]) -> torch.Tensor:
-        """The norm of all of the tensors together: one float32 number on the device."""
+        """The norm of all of the tensors together: one float32 number on the device.  Records no graph: tensors that require a gradient are
+        refused outside torch.no_grad()."""
         tensors = list(tensors)
+        _no_graph(*tensors)
         self._ready(*tensors)
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        norm = torch.empty((), dtype=torch.float32, device=self.stream.device)
         st = self.lib.slim_grad_norm(self.ctx, _tensor_list(tensors, "tensors"), len(tensors), norm.data_ptr())
         if st:
             self._check(st)
@@ -912,13 +915,17 @@ class Slim:
 
     def clip_gradients(self, tensors: Sequence[torch.Tensor], limit: float, out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
         """Scales the tensors by min(1, limit / norm), in place or into `out` (tensors of their shapes and types, which do not overlap them or one
-        another); returns their norm before that, one float32 number on the device.  A norm that is not finite leaves the values as they are."""
+        another); returns their norm before that, one float32 number on the device.  A norm that is not finite leaves the values as they are.
+        Records no graph, as grad_norm."""
         tensors = list(tensors)
+        _no_graph(*tensors)
+        if out is not None:
+            out = list(out)
+            _no_graph(*out)
+            self._ready(*out)
         self._ready(*tensors)
         into = None
         if out is not None:
-            out = list(out)
-            self._ready(*out)
             if len(out) != len(tensors):
                 raise ValueError("out has to hold as many tensors")
             into, flat = _tensor_list(out, "out"), _tensor_list(tensors, "tensors")
@@ -930,7 +937,7 @@ class Slim:
                 into, flat = _tensor_rows(out, "out"), _tensor_rows(tensors, "tensors")
         else:
             flat = _tensor_list(tensors, "tensors")
-        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        norm = torch.empty((), dtype=torch.float32, device=self.stream.device)
         st = self.lib.slim_clip_gradients(self.ctx, flat, into, len(tensors), limit, norm.data_ptr())
         if st:
             self._check(st)

@@ -239,6 +239,11 @@ slim_status forward(slim_ctx* ctx, const NormArgs& a) {
   return SLIM_OK;
 }
 
+// (columns are counted in 32 bits, several thousand beyond the last)
+slim_status check_columns(slim_ctx* ctx, const char* fn, int cols) {
+  return cols <= 1 << 30 ? SLIM_OK : slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: rows of %d numbers are too long", fn, cols);
+}
+
 }  // namespace
 
 extern "C" {
@@ -249,6 +254,7 @@ slim_status slim_add_norm(slim_ctx* ctx, const void* X, const void* R, slim_dtyp
   if (!ctx) return SLIM_ERR_INVALID_ARG;
   const char* fn = "slim_add_norm";
   if (const slim_status st = check(ctx, fn, x_dtype, w_dtype, rows, cols); st != SLIM_OK) return st;
+  if (const slim_status st = check_columns(ctx, fn, cols); st != SLIM_OK) return st;
   SLIM_REQUIRE(ctx, w, "%s: null weight", fn);
   SLIM_REQUIRE(ctx, eps >= 0.0, "%s: eps = %g", fn, eps);
   SLIM_REQUIRE(ctx, !q == !s && (Y || q || rows == 0), "%s: neither Y nor its 8-bit form, or half of that", fn);
@@ -288,9 +294,10 @@ slim_status slim_add_norm_backward(slim_ctx* ctx, const void* dY, const void* dH
                                    int64_t lddy, int64_t lddh, int64_t ldh, const void* w, slim_dtype w_dtype, const float* mean,
                                    const float* rstd, void* dX, int64_t lddx, void* dw, void* db) {
   if (!ctx) return SLIM_ERR_INVALID_ARG;
+  const char* fn = "slim_add_norm_backward";
+  if (const slim_status st = check_columns(ctx, fn, cols); st != SLIM_OK) return st;
   if (!dH || rows == 0)
     return slim_layer_norm_backward(ctx, dY, H, x_dtype, rows, cols, lddy, ldh, w, w_dtype, mean, rstd, dX, lddx, dw, db);
-  const char* fn = "slim_add_norm_backward";
   NormArgs a = {};
   a.dH = dH;
   a.lddh = lddh;

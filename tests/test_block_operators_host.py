@@ -46,6 +46,9 @@ int main() {
   say("bad", norm(3, 200, B, F, 1e-5, 200, p, 200, p, 200, nullptr, 200, nullptr, 256, nullptr, 4));
   say("unsupported", norm(3, 200, D, F, 1e-5, 200, p, 200, p, 200, p, 200, u, 256, u, 4));
   say("unsupported", norm(3, 200, B, SLIM_F16, 1e-5, 200, p, 200, p, 200, p, 200, u, 256, u, 4));
+  const int far = (1 << 30) + 1;
+  say("unsupported", norm(3, far, B, F, 1e-5, far, p, far, p, far, p, far, nullptr, 0, nullptr, 0));
+  say("unsupported", slim_add_norm_backward(&c, p, p, p, B, 3, far, far, far, far, p, F, nullptr, f, p, far, p, nullptr));
   auto back = [&](int64_t rows, const void* dY, const void* dH, const void* H, int64_t lddy, int64_t lddh, int64_t ldh, void* dX, int64_t lddx, void* dw) {
     return slim_add_norm_backward(&c, dY, dH, H, B, rows, 200, lddy, lddh, ldh, p, F, nullptr, f, dX, lddx, dw, nullptr);
   };
@@ -317,7 +320,9 @@ def test_a_gradient_is_not_lost_silently(binding):
     leaf = lambda t: t.clone().requires_grad_()
     for call in (lambda: slim.add_norm(leaf(x), None, w), lambda: slim.add_norm(x, leaf(x), w), lambda: slim.add_norm(x, x, leaf(w)),
                  lambda: slim.add_norm(x, x, w, leaf(w)), lambda: slim.fp8_linear_act(leaf(x), w, w), lambda: slim.fp8_linear_act(x, w, w, leaf(w)),
-                 lambda: slim.fp8_linear_act(x, w, w, residual=leaf(x)), lambda: slim.head_loss(leaf(x), w, w, w)):
+                 lambda: slim.fp8_linear_act(x, w, w, residual=leaf(x)), lambda: slim.head_loss(leaf(x), w, w, w),
+                 lambda: slim.add_norm(x, x, w, stats=True, H=leaf(x)), lambda: slim.grad_norm([x, leaf(x)]), lambda: slim.clip_gradients([x, leaf(x)], 1.0),
+                 lambda: slim.clip_gradients([x], 1.0, out=[leaf(x)])):
         with pytest.raises(ValueError, match="graph"):
             call()
     with pytest.raises(ValueError, match="act"):
