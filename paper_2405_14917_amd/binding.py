@@ -3,8 +3,10 @@ marshalling only.  PyTorch supplies device memory and the HIP stream; every step
 in the library's kernels.  There is no fallback: if the library is missing, `load()` raises."""
 from __future__ import annotations
 
+import array
 import ctypes
 import os
+import struct
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
@@ -55,6 +57,9 @@ class SlimShape(ctypes.Structure):
 class SlimEpilogue(ctypes.Structure):
     _fields_ = [("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int), ("act", ctypes.c_int), ("R", ctypes.c_void_p), ("ldr", ctypes.c_int64),
                 ("Z", ctypes.c_void_p), ("ldz", ctypes.c_int64)]
+
+
+_EPILOGUE = struct.Struct("PiiPqPq")          # the same as bytes, which are made in a fifth of the time
 
 
 class AddNorm(NamedTuple):
@@ -286,7 +291,11 @@ def _tensor_list(tensors, what: str):
             flat += (t.data_ptr(), t.shape[0], t.shape[1], _row_stride(t, what), d)
         else:
             raise ValueError("%s have to be contiguous, or matrices with contiguous rows" % what)
-    return (ctypes.c_int64 * len(flat))(*flat)
+    return array.array("q", flat)
+
+
+def _address(a: array.array) -> int:
+    return a.buffer_info()[0]
 
 
 def _tensor_rows(tensors, what: str):
@@ -770,20 +779,20 @@ class Slim:
         Y = W.new_empty((t, n), dtype=dtype)
         Z = W.new_empty((t, n), dtype=dtype) if keep else None
         y = _dtype(Y)
-        e = SlimEpilogue(None, y, _check_act(act), None, 0, None, n)
+        b = r = ldr = 0
+        b_dtype = y
         if bias is not None:
             if bias.shape != (n,) or not bias.is_contiguous():
                 raise ValueError("bias has to be a contiguous vector of %d numbers" % n)
-            e.bias, e.bias_dtype = bias.data_ptr(), _dtype(bias)
+            b, b_dtype = bias.data_ptr(), _dtype(bias)
         if residual is not None:
             if residual.shape != (t, n) or residual.dtype != dtype:
                 raise ValueError("residual has to be (%d, %d) of Y's type" % (t, n))
-            e.R, e.ldr = residual.data_ptr(), _row_stride(residual, "residual")
-        if keep:
-            e.Z = Z.data_ptr()
+            r, ldr = residual.data_ptr(), _row_stride(residual, "residual")
+        e = _EPILOGUE.pack(b, b_dtype, _check_act(act), r, ldr, Z.data_ptr() if keep else 0, n)
         st = self.lib.slim_fp8_linear_act(self.ctx, X.data_ptr() if xq is None else None, _dtype(X) if xq is None else F16, t, ldx,
                                           None if xq is None else xq.data_ptr(), ldxq, None if xs is None else xs.data_ptr(), ldxs,
-                                          W.data_ptr(), ldq, Ws.data_ptr(), lds, n, m, ctypes.byref(e), Y.data_ptr(), y, n)
+                                          W.data_ptr(), ldq, Ws.data_ptr(), lds, n, m, e, Y.data_ptr(), y, n)
         if st:
             self._check(st)
         return (Y, Z) if keep else Y
@@ -907,8 +916,9 @@ class Slim:
         tensors = list(tensors)
         _no_graph(*tensors)
         self._ready(*tensors)
+        flat = _tensor_list(tensors, "tensors")
         norm = torch.empty((), dtype=torch.float32, device=self.stream.device)
-        st = self.lib.slim_grad_norm(self.ctx, _tensor_list(tensors, "tensors"), len(tensors), norm.data_ptr())
+        st = self.lib.slim_grad_norm(self.ctx, _address(flat), len(tensors), norm.data_ptr())
         if st:
             self._check(st)
         return norm
@@ -938,7 +948,7 @@ class Slim:
         else:
             flat = _tensor_list(tensors, "tensors")
         norm = torch.empty((), dtype=torch.float32, device=self.stream.device)
-        st = self.lib.slim_clip_gradients(self.ctx, flat, into, len(tensors), limit, norm.data_ptr())
+        st = self.lib.slim_clip_gradients(self.ctx, _address(flat), None if into is None else _address(into), len(tensors), limit, norm.data_ptr())
         if st:
             self._check(st)
         return norm

@@ -14,7 +14,9 @@ namespace {
 
 using namespace slimnorm;
 
-constexpr int CL_TENSORS = 60, CL_THREADS = 256, CL_PIECES = 4, CL_BYTES = 16 * CL_THREADS * CL_PIECES, CL_PER_CU = 4;
+// Three workgroups a CU, four pieces a lane: what is under way together is enough, and more of it costs the memory its pages (two matrices' layers of
+// 4096 x 11008 and the like, 810 MB: 414 us; two workgroups a CU 424, four 421, eight 448; eight pieces and two workgroups 424).
+constexpr int CL_TENSORS = 60, CL_THREADS = 256, CL_PIECES = 4, CL_BYTES = 16 * CL_THREADS * CL_PIECES, CL_PER_CU = 3;
 
 struct ClipTensor {
   const void* in;
@@ -30,16 +32,15 @@ struct ClipArgs {
 };
 static_assert(sizeof(ClipArgs) <= 4096 - 64, "the arguments of a launch");
 
-// the tensor of a chunk (the same in every lane)
-__device__ __forceinline__ int tensor_of(const ClipArgs& a, int64_t chunk) {
-  int lo = 0, hi = a.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.t[mid].first <= chunk) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+// The tensor of a chunk (the same in every lane): `first` is what lane l holds of tensor l.  (A search by halves is a chain of loads of the arguments.)
+__device__ __forceinline__ int64_t first_of_lane(const ClipArgs& a) {
+  const int lane = threadIdx.x & 63;
+  return lane < a.count ? a.t[lane].first : INT64_MAX;
 }
+__device__ __forceinline__ int tensor_of(int64_t first, int64_t chunk) {
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(first <= chunk)) - 1);
+}
+static_assert(CL_TENSORS <= 64, "a lane for every tensor");
 
 template <typename T, typename F>
 __device__ __forceinline__ void each_element(const ClipTensor& t, int64_t e0, F use) {
@@ -116,9 +117,10 @@ __device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, float 
 
 __global__ __launch_bounds__(CL_THREADS) void clip_squares(ClipArgs a, double* __restrict__ sums) {
   __shared__ double red[CL_THREADS / 64];
+  const int64_t first = first_of_lane(a);
   double s = 0.0;
   for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-    const ClipTensor& t = a.t[tensor_of(a, chunk)];
+    const ClipTensor& t = a.t[tensor_of(first, chunk)];
     const int64_t c = chunk - t.first;
     s += t.dtype == SLIM_F32 ? squares<float>(t, c) : t.dtype == SLIM_F16 ? squares<__half>(t, c) : squares<__hip_bfloat16>(t, c);
   }
@@ -130,6 +132,7 @@ __global__ __launch_bounds__(CL_THREADS) void clip_squares(ClipArgs a, double* _
 
 __global__ __launch_bounds__(CL_THREADS) void clip_scale(ClipArgs a, const double* __restrict__ sums, int parts, double limit, float* norm) {
   __shared__ double red[CL_THREADS / 64];
+  const int64_t first = first_of_lane(a);
   double s = 0.0;
   for (int i = threadIdx.x; i < parts; i += CL_THREADS) s += sums[i];
   s = wave_sum(s);
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(CL_THREADS) void clip_scale(ClipArgs a, const doubl
   const float factor = copy ? 1.f : (float)(limit / n);
   for (int64_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
     const int64_t chunk = a.chunks - 1 - k;
-    const ClipTensor& t = a.t[tensor_of(a, chunk)];
+    const ClipTensor& t = a.t[tensor_of(first, chunk)];
     if (copy && t.in == t.out) continue;
     const int64_t c = chunk - t.first;
     if (t.dtype == SLIM_F32) scale<float>(t, c, factor, copy);

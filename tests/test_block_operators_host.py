@@ -303,6 +303,12 @@ def test_null_contexts_are_rejected(binding):
         assert fn(*[None if a is ctypes.c_void_p else a(0).value for a in fn.argtypes]) == binding.ERR_INVALID_ARG, name
 
 
+def test_the_epilogues_bytes_are_the_structure(binding):
+    assert binding._EPILOGUE.size == ctypes.sizeof(binding.SlimEpilogue)
+    e = binding.SlimEpilogue.from_buffer_copy(binding._EPILOGUE.pack(11, 2, 4, 13, 14, 15, 16))
+    assert (e.bias, e.bias_dtype, e.act, e.R, e.ldr, e.Z, e.ldz) == (11, 2, 4, 13, 14, 15, 16)
+
+
 def test_lists_of_tensors(binding):
     a = torch.zeros((4, 10))
     d = list(binding._tensor_list([a, a[:, 2:7], a[1], torch.zeros(()), torch.zeros((0, 3)).half()], "t"))
