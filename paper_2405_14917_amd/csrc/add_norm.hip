@@ -13,6 +13,30 @@ namespace {
 using namespace slimnorm;
 using slimfp8::BLOCK;
 
+// Sums over the W wavefronts of a row, of the lanes' sums in fp64: what is off in a row's factor is off in all of its numbers, and moves those next
+// to a border of the 8-bit form to its other side (fp32 outputs are 4.6e-8 to 5.1e-8 off, with these sums in fp32 6.0e-8 to 6.6e-8; one rounding is 2.5e-8; with deviations and
+// outputs in fp64 as well 16384 x 4096 took 102 us in place of 87)
+template <int W>
+__device__ __forceinline__ double row_sum(double v, double (*red)[W], int& slot) {
+  v = wave_sum(v);
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) red[slot][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v += red[slot][i];
+    slot ^= 1;
+  }
+  return v;
+}
+// 1 / sqrt(v): the hardware's estimate of some 26 bits and two of Newton's steps
+__device__ __forceinline__ double inverse_root(double v) {
+  const double r0 = __builtin_amdgcn_rsq(v);
+  double r = r0 * fma(-0.5 * v * r0, r0, 1.5);
+  r = r * fma(-0.5 * v * r, r, 1.5);
+  return v > 0.0 && v < __longlong_as_double(0x7ff0000000000000ll) ? r : r0;
+}
+
 // h of one piece: the sum, rounded (pairs of elements stay packed)
 template <typename T>
 __device__ __forceinline__ void add(Piece<T>& x, const Piece<T>& r) {
@@ -62,10 +86,10 @@ __device__ __forceinline__ void store_e4m3(const NormArgs& a, int64_t row, int c
 template <typename T, typename TW, int W, int P>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_norm_forward(NormArgs a) {
   constexpr int E = Piece<T>::E, LANES = 64 * W, RPW = W == 1 ? 4 : 1;
-  __shared__ float red[2][W][1];
+  __shared__ double red[2][W];
   const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * RPW + (W == 1 ? threadIdx.x >> 6 : 0), step = (int64_t)gridDim.x * RPW;
-  const float inv_n = 1.f / (float)a.cols;
+  const double inv_n = 1.0 / (double)a.cols;
   int slot = 0;
   Piece<T> x[P], r[P];
   auto fetch = [&](int64_t row) {
@@ -92,8 +116,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_norm_forward(NormAr
 #pragma unroll
     for (int i = 0; i < P; ++i) affine(wk[i], bk[i], (i * LANES + lane) * E);
   for (int64_t row = row0; row < a.rows; row += step) {
-    float s[1] = {0.f};
-    float mean = 0.f;
+    float s = 0.f, mean = 0.f;
     if (a.R)
 #pragma unroll
       for (int i = 0; i < P; ++i) {
@@ -105,10 +128,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_norm_forward(NormAr
 #pragma unroll
       for (int i = 0; i < P; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[0] += x[i].get(e);
-      row_sums<W, 1>(s, red, slot);
-      mean = s[0] * inv_n;
-      s[0] = 0.f;
+        for (int e = 0; e < E; ++e) s += x[i].get(e);
+      mean = (float)(row_sum<W>((double)s, red, slot) * inv_n);
+      s = 0.f;
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -116,11 +138,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_norm_forward(NormAr
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float d = e < left ? x[i].get(e) - mean : 0.f;
-        s[0] = fmaf(d, d, s[0]);
+        s = fmaf(d, d, s);
       }
     }
-    row_sums<W, 1>(s, red, slot);
-    const float rs = 1.f / sqrtf(fmaf(s[0], inv_n, a.eps));
+    const float rs = (float)inverse_root(fma(row_sum<W>((double)s, red, slot), inv_n, (double)a.eps));
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int c = (i * LANES + lane) * E;
@@ -153,9 +174,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void add_norm_forward(NormAr
 template <typename T, typename TW>
 __global__ __launch_bounds__(1024) void add_norm_forward_long(NormArgs a) {
   constexpr int E = Piece<T>::E;
-  __shared__ float red[2][16][1];
+  __shared__ double red[2][16];
   int slot = 0;
-  const float inv_n = 1.f / (float)a.cols;
+  const double inv_n = 1.0 / (double)a.cols;
   const int padded = (a.cols + BLOCK - 1) / BLOCK * BLOCK, lane0 = threadIdx.x * E;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     auto sum = [&](int c) {                   // h, from where it still is
@@ -173,30 +194,28 @@ __global__ __launch_bounds__(1024) void add_norm_forward_long(NormArgs a) {
       h.load(static_cast<const T*>(a.H) + row * a.ldh + c, a.cols - c);
       return h;
     };
-    float s[1] = {0.f};
+    float s = 0.f;
     for (int c = lane0; c < a.cols; c += 1024 * E) {
       const Piece<T> h = sum(c);
       if (a.H && a.R) h.store(static_cast<T*>(a.H) + row * a.ldh + c, a.cols - c);
       if (!a.rms)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[0] += h.get(e);
+        for (int e = 0; e < E; ++e) s += h.get(e);
     }
     float mean = 0.f;
     if (!a.rms) {
-      row_sums<16, 1>(s, red, slot);
-      mean = s[0] * inv_n;
-      s[0] = 0.f;
+      mean = (float)(row_sum<16>((double)s, red, slot) * inv_n);
+      s = 0.f;
     }
     for (int c = lane0; c < a.cols; c += 1024 * E) {
       const Piece<T> h = again(c);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float d = e < a.cols - c ? h.get(e) - mean : 0.f;
-        s[0] = fmaf(d, d, s[0]);
+        s = fmaf(d, d, s);
       }
     }
-    row_sums<16, 1>(s, red, slot);
-    const float rs = 1.f / sqrtf(fmaf(s[0], inv_n, a.eps));
+    const float rs = (float)inverse_root(fma(row_sum<16>((double)s, red, slot), inv_n, (double)a.eps));
     for (int c = lane0; c - lane0 < padded; c += 1024 * E) {       // (whole wavefronts, for the blocks' maxima)
       const Piece<T> h = again(c);
       float y[E];
