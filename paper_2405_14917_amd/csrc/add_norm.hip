@@ -5,6 +5,9 @@
 // Bound by memory: x and r are read, h and the output written, once each.  As in norm.hip a row lives in the registers of a group of
 // wavefronts; a block of 128 channels is 16 (16-bit types) or 32 lanes one after another, so that its largest magnitude takes a few moves
 // inside the wavefront, on packed 16-bit patterns where the type has 16 bits.
+//
+// 16384 x 4096 bf16 without the mean, the output in both forms: forward 107 us (5.6 TB/s), backward
+// 108 to 111 (4.9 TB/s), the second kernel 5.
 #include "fp8_device.h"
 #include "norm_device.h"
 

@@ -4,9 +4,14 @@
 //
 // One product over the whole vocabulary leaves, of every tile, the maximum and the sum of exponentials of its classes for each token (fp8_gemm.hip,
 // fp8_few.hip); `head_join` puts a token's tiles together in fp64.  The gradients need the logits a second time, once the sums are known: a piece
-// of the vocabulary at a time, so that what is in memory is a piece's and not t x V numbers.  A piece is multiplied again, `head_gradient` turns its
-// logits into dz in e4m3, in blocks of 128 classes and of 128 tokens, and the two products of the backward pass follow; dx is summed over
+// of the vocabulary at a time, so that what is in memory is a piece's and not t x V numbers.  A piece is multiplied again, the end of that product turns its
+// logits into dz in e4m3, in blocks of 128 classes and of 128 tokens (fp8_gemm.hip; with the logits through memory and a launch of its own
+// 32000 x 4096 with 2048 tokens took 1786 us in place of 1470), and the two products of the backward pass follow in one launch; dx is summed over
 // the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
+//
+// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1470 to 1550 us, of them the logits' first product 390
+// (1.38 PFLOP/s), the second one with dz 460 in four pieces (1.17), dx and dw 620 (1.73); one token, the loss alone: 27 us, the weights'
+// read (5.0 TB/s), and 3 for `head_join`.
 #include "act_device.h"
 #include "fp8_entry.h"
 
@@ -14,19 +19,32 @@ namespace {
 
 using namespace slimfp8;
 
-// One wavefront per token.  Pairs in a fixed order; loss or stat may be null.
+// One wavefront per token.  Pairs in a fixed order, eight a lane under way at a time with the sum carried along to the new maximum (one token and
+// 2000 pairs: the loss took 2 us more with two passes of one load after another); stat may be null.
 __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part, int parts, const float* __restrict__ z, const void* labels, int labels64,
                                                  const float* __restrict__ dloss, int t, int V, float* __restrict__ loss, TokenStat* __restrict__ stat) {
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= t) return;
   const float2* p = part + row * parts;
-  float top = -__builtin_inff();
-  for (int i = lane; i < parts; i += 64) top = fmaxf(top, p[i].x);
-  top = wave_max_f32(top);
+  auto e = [](float x) { return slimact::exp_of(fmaxf(x, -126.f)); };
+  constexpr int DEEP = 8;                          // pairs of a lane that are fetched together
+  float own = -__builtin_inff();
   double sum = 0.0;
-  for (int i = lane; i < parts; i += 64) sum += (double)(p[i].y * slimact::exp_of(fmaxf(p[i].x - top, -126.f)));
-  sum = wave_sum(sum);
+  for (int i0 = lane; i0 < parts; i0 += 64 * DEEP) {
+    float2 v[DEEP];
+    float most = own;
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) v[d] = i0 + 64 * d < parts ? p[i0 + 64 * d] : make_float2(-__builtin_inff(), 0.f);
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) most = fmaxf(most, v[d].x);
+    sum *= (double)e(own - most);
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) sum += (double)(v[d].y * e(v[d].x - most));
+    own = most;
+  }
+  const float top = wave_max_f32(own);
+  sum = wave_sum(sum * (double)e(own - top));
   if (lane == 0) {
     const int64_t label = label_at(labels, labels64, row);
     const bool live = label >= 0 && label < V;
@@ -38,8 +56,8 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
   }
 }
 
-// Pieces: as many classes as make 16 Mi logits (64 MB and their e4m3 forms: they stay in the cache behind the L2 between the kernels), 1024 at
-// least; whole words of four scales.
+// Pieces: as many classes as make 16 Mi logits, in e4m3 twice (32 MB: they stay in the cache behind the L2 between the kernels), 1024 at
+// least; whole words of four scales.  32000 x 4096 with 2048 tokens: 16, 32 and 64 Mi take 1470, 1465 and 1500 us, so the smallest.
 constexpr int64_t HL_LOGITS = 1 << 24;
 constexpr int HL_LEAST = 1024, HL_STEP = 4 * BLOCK;
 int piece_of(int V, int t) {

@@ -231,6 +231,7 @@ __global__ __launch_bounds__(1024) void norm_join(const float* __restrict__ pw, 
 // more partial sums than that takes.  With the forward pass: 16384 x 4096 bf16, one row at a time, three workgroups per CU 128 us, two 135,
 // two rows at a time 142 (too few registers); 3001 x 1501 fp32 the other way, 28.5 (four) and 26.0; 30000 x 640 bf16 one wavefront per row 52,
 // four 68.
+// With a gradient that joins dX (`add`) two workgroups per CU: 16384 x 4096 bf16 one row at a time, forward and backward, two 216, three 220.
 // Up to four rounds of rows: one workgroup, which needs no second kernel (52 x 64: 24 -> 20 us with the forward pass, most of it the host's).
 struct Shape {
   int w, p, g, per_cu;
