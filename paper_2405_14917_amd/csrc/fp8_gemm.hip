@@ -12,8 +12,8 @@
 //    across steps: the one barrier of a step is in its middle, behind it the step's stage is free for the loads of the step STAGES on.
 //  * The rows of A are the rows of an MFMA tile, so a lane ends up with 4 consecutive outputs of one row of C at a time; the tile goes through
 //    LDS, wavefront by wavefront, and leaves in rows.
-//  * What becomes of a tile's sums (MODE): they are stored; bias, residual and activation first (FINISH, the residuals fetched before
-//    the last steps' products: 4096 x 11008 with 2048 tokens 110 us, fetched after them 120); of a tile of logits the maximum and the sum of exponentials
+//  * What becomes of a tile's sums (MODE): they are stored; bias, residual and activation first (FINISH, the residuals fetched many at a
+//    time: 4096 x 11008 with 2048 tokens 110 us, one round of loads after another 120); of a tile of logits the maximum and the sum of exponentials
 //    of every token (SOFTMAX); or the logits' gradients, quantised in both directions for the products behind them (GRADIENT).
 //  * Several products share a launch (the two gradients, where their outputs are of one kind).  A product whose tiles do not fill the chip
 //    is cut along the contraction; the parts go to the workspace in fp32 and are added in a fixed order by a second kernel.
@@ -788,14 +788,15 @@ int parts_of(const Product& p, int tile, int ncu) {
 // tokens, large ones (790; medium ones above 900).  The bytes of the operands are in the measured step, not a term of their own.
 // With residuals or kept sums a round of large tiles costs 3 more than one of medium ones, whose epilogues run beside another workgroup's products: 8192 x
 // 4096, 4096 tokens, residual 168 and 164, with gelu and kept sums too 225 and 202; 8192 x 28672 792 and 985.
-double tile_cost(const Product& p, int tile, int ncu) {
+double tile_time(const Product& p, int tile, int parts = 1, bool alone = false) {
   static const double round[] = {15.0, 5.4, 2.7}, step[2][3] = {{1.44, 0.82, 0.34}, {2.6, 1.42, 0.56}};
-  const int tiles = tiles_of(p, tile), s = parts_of(p, tile, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
-  double one = step[exact(p)][tile];
-  if (tile == TILE_MEDIUM && tiles * s <= ncu) one *= 0.6;
   const double epilogue = tile == TILE_LARGE && p.e && (p.e->R || p.e->Z) ? 3.0 : 0.0;
+  return round[tile] + epilogue + step[exact(p)][tile] * (alone ? 0.6 : 1.0) * slim_cdiv(p.nk, parts);
+}
+double tile_cost(const Product& p, int tile, int ncu) {
+  const int tiles = tiles_of(p, tile), s = parts_of(p, tile, ncu), at_once = tile == TILE_LARGE ? ncu : 2 * ncu;
   const double join = s > 1 ? 4.0 + 8.0 * s * p.a.rows * (double)p.b.rows / 4.85e6 : 0.0;
-  return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * (round[tile] + epilogue + one * slim_cdiv(p.nk, s)) + join;
+  return 6.0 + slim_cdiv((int64_t)tiles * s, at_once) * tile_time(p, tile, s, tile == TILE_MEDIUM && tiles * s <= ncu) + join;
 }
 int tile_of(const Product& p, int ncu) {
   int best = p.sg ? TILE_MEDIUM : TILE_SMALL;                       // (a gradient's tile holds whole blocks of 128)
@@ -804,17 +805,50 @@ int tile_of(const Product& p, int ncu) {
   return best;
 }
 
+// Two products' tiles in one launch, none of them cut, the first one's first: a CU that is done with a tile takes the next.  `sum`: if no CU waited
+// at the end.
+double joint_cost(const Product* p, int tile, int ncu, double& sum) {
+  const int slots = tile == TILE_LARGE ? ncu : 2 * ncu, count = tiles_of(p[0], tile), more = count % slots;
+  const double t0 = tile_time(p[0], tile), t1 = tile_time(p[1], tile);
+  sum = (count * t0 + tiles_of(p[1], tile) * t1) / slots;
+  double least = count / slots * t0, most = least + t0, end = more ? most : least;      // slots - more of them are done with the first, and more
+  for (int left = tiles_of(p[1], tile); left > 0;) {
+    const bool early = !more || least <= most;
+    double& done = early ? least : most;
+    left -= early ? slots - more : more;
+    done += t1;
+    end = std::max(end, done);
+  }
+  return end;
+}
 // Products of one launch: all, or one where they differ in their kind or tile (a gradient of long contraction and few tiles beside one of many).
-int in_one_launch(const Product* p, int count, int ncu) {
-  return count == 2 && (exact(p[0]) != exact(p[1]) || tile_of(p[0], ncu) != tile_of(p[1], ncu)) ? 1 : count;
+// Two whose tiles differ, or are medium, take large ones together where they fill each other's last rounds.  Measured (16-bit gradients of n x m, t tokens):
+// where the costs say so, two launches -> one 8 % less on average (8192 x 8192, 2048 tokens: 322 -> 304 us; 25053 x 2798, 3193: 542 -> 432; at most 8 %
+// more, 5364 x 2008, 3148), medium -> large 5 % (8192 x 4096, 2048: 148 -> 139; 16384 x 4096, 2048: 308 -> 266; at 8192 x 4096, 1536, where large ones
+// would end unevenly, 118 and 128).  Large ones move half the operands' bytes, which the costs leave out: hence the eighth.
+int in_one_launch(const Product* p, int count, int ncu, int& tile) {
+  tile = tile_of(p[0], ncu);
+  if (count != 2 || exact(p[0]) != exact(p[1])) return 1;
+  const int other = tile_of(p[1], ncu);
+  if ((tile == TILE_LARGE && other == TILE_LARGE) || tile == TILE_SMALL || other == TILE_SMALL || parts_of(p[0], tile, ncu) > 1 || parts_of(p[1], other, ncu) > 1)
+    return tile == other ? 2 : 1;
+  double sum, of_medium;
+  const double large = joint_cost(p, TILE_LARGE, ncu, sum);
+  if (tile != other) {
+    if (6.0 + large >= tile_cost(p[0], tile, ncu) + tile_cost(p[1], other, ncu)) return 1;
+    tile = TILE_LARGE;
+  } else if (large <= 1.125 * joint_cost(p, tile, ncu, of_medium) && sum <= 1.04 * of_medium) {
+    tile = TILE_LARGE;
+  }
+  return 2;
 }
 
 // Each product's parts as if it were alone: beside another one of many tiles, few of long contraction would be what the launch waits for
 // (gradients of 14666 x 2078, 88 tokens: 17 tiles of 115 steps took 82 us beside 1955 of one).
-Plan make_plan(const Product* p, int count, int ncu) {
+Plan make_plan(const Product* p, int count, int tile, int ncu) {
   Plan pl = {};
   for (int i = 0; i < count; ++i) {
-    pl.splits[i] = parts_of(p[i], tile_of(p[i], ncu), ncu);
+    pl.splits[i] = tile == tile_of(p[i], ncu) ? parts_of(p[i], tile, ncu) : 1;
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
   }
   return pl;
@@ -854,9 +888,8 @@ slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga
   return exact ? launch<true, PLAIN>(ctx, name, tile, ga, grid) : launch<false, PLAIN>(ctx, name, tile, ga, grid);
 }
 
-slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count) {
-  const Plan pl = make_plan(p, count, ctx->num_cus);
-  const int tile = tile_of(p[0], ctx->num_cus);
+slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count, int tile) {
+  const Plan pl = make_plan(p, count, tile, ctx->num_cus);
   GemmArgs ga = {};
   float* parts[2] = {};
   int grid = 0;
@@ -912,8 +945,17 @@ size_t gemm_workspace(const Product* p, int count, int num_cus) {
 }
 
 slim_status gemm(slim_ctx* ctx, const char* name, const Product* p, int count) {
-  for (int i = 0, c = in_one_launch(p, count, ctx->num_cus); i < count; i += c)
-    if (const slim_status st = multiply(ctx, name, p + i, c); st != SLIM_OK) return st;
+  // (tiles of the longer contraction first: those of the shorter one fill what they leave; 525 x 3810, 7784 tokens: 81 -> 64 us, 2560 x 2048, 6000: 88 -> 72)
+  Product longest_first[2];
+  if (count == 2 && p[1].nk > p[0].nk && !p[0].e) {
+    longest_first[0] = p[1];
+    longest_first[1] = p[0];
+    p = longest_first;
+  }
+  for (int i = 0, c, tile; i < count; i += c) {
+    c = in_one_launch(p + i, count - i, ctx->num_cus, tile);
+    if (const slim_status st = multiply(ctx, name, p + i, c, tile); st != SLIM_OK) return st;
+  }
   return SLIM_OK;
 }
 

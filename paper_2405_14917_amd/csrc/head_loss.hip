@@ -9,8 +9,8 @@
 // 32000 x 4096 with 2048 tokens took 1786 us in place of 1470), and the two products of the backward pass follow in one launch; dx is summed over
 // the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
 //
-// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1470 to 1550 us, of them the logits' first product 390
-// (1.38 PFLOP/s), the second one with dz 460 in four pieces (1.17), dx and dw 620 (1.73); one token, the loss alone: 27 us, the weights'
+// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1440 us, of them the logits' first product 390
+// (1.38 PFLOP/s), the second one with dz 460 in four pieces (1.17), dx and dw 575 (1.87); one token, the loss alone: 27 us, the weights'
 // read (5.0 TB/s), and 3 for `head_join`.
 #include "act_device.h"
 #include "fp8_entry.h"

@@ -260,6 +260,22 @@ def test_without_an_activation_it_is_the_plain_backward_pass(slim):
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("n,m,t", [(8192, 2304, 2048), (3576, 4083, 2453), (6462, 2356, 2000), (525, 3810, 5000), (2048, 2304, 5000), (1503, 2000, 97)])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_gradients_together_are_those_alone(slim, n, m, t, dtype):
+    """The tiles of two products of one launch depend on both; the order of a sum does not."""
+    W = (numbers(n, m, torch.float32, 3) * 0.05).cuda()
+    X, dY = numbers(t, m, torch.float16, 4).cuda(), numbers(t, n, torch.float16, 5).cuda()
+    q, s, qt, st = slim.fp8_quantize_weights(W)
+    dX, dW = slim.fp8_linear_backward(dY, X, qt, st, dtype)
+    assert torch.equal(dX, slim.fp8_linear_backward(dY, None, qt, st, dw=False)[0])
+    assert torch.equal(dW, slim.fp8_linear_backward(dY, X, None, None, dtype, dx=False)[1])
+    rows = torch.randperm(t, generator=torch.Generator().manual_seed(1))[:40].cuda()
+    A, B = ref.q_rows(dY[rows].cpu()), ref.quantize(W.cpu(), ref.B, ref.B)[2]
+    size = A.abs() @ B.abs()
+    check(dX[rows], A @ B, ((2 * n / 8 + 16) * 2.0 ** -23 + 2.0 ** -10) * size)
+
+
 @pytest.mark.parametrize("name", ACTS[1:])
 def test_slopes_are_differences_of_the_activations(slim, name):
     """The bias gradient of one token is the slope itself; differences of the formula in 64 bits."""
