@@ -499,7 +499,7 @@ size_t slim_grad_norm_workspace(int count, int num_cus);
 slim_status slim_grad_norm(slim_ctx* ctx, const slim_tensor* tensors, int count, float* norm);
 slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const slim_tensor* out, int count, double limit, float* norm);
 
-/* The cross entropy of labels in the softmax of an 8-bit head's outputs, and its gradients, without these outputs (t x V logits) in memory.
+/* The cross entropy of labels in the softmax of an 8-bit head's outputs, and its gradients; of these outputs (t x V logits) no more than 64 Mi are in memory.
  *   X        t x m, F16 or BF16, quantised along the channels as in slim_fp8_linear;  q, s: the head W (V x m) as slim_fp8_quantize_weights writes it
  *   labels   t classes, int64 (labels64 != 0) or int32; what lies outside 0 .. V - 1, -100 say, is no label: loss 0, no gradient
  *   loss     t: ln sum exp z - z[label] for z = Q(X) W^T, whose sums keep 24 bits
@@ -508,7 +508,8 @@ slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const
  *            W^T (not read without dX); sums on the e4m3 matrix cores, between pieces of the vocabulary in fp32
  *   dW       V x m, F16, BF16 or F32, or NULL: Qt(dz)^T Qt(X), both in blocks of 128 tokens, sums as in slim_fp8_linear_backward.  A row of X without a
  *            label adds nothing to dW if it is finite.
- * The gradients take the logits a second time, a piece of the vocabulary after another: 16 Mi of them, or 1024 classes, at a time. */
+ * The loss alone keeps no logits.  The gradients need them twice: up to 64 Mi (256 MB of the workspace, in fp32) are kept, those of the classes behind are
+ * computed again; from there on a piece of the vocabulary at a time, 16 Mi logits or 1024 classes. */
 size_t slim_head_loss_workspace(int V, int m, int t, int num_cus);
 slim_status slim_head_loss(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
                            int64_t lds, int V, int m, const void* labels, int labels64, float* loss);

@@ -157,12 +157,12 @@ struct Epilogue {
   int bias_dtype, act, r_dtype;
 };
 // Or, in the place of C, what the softmax of the rows of B over those of A needs: of every tile of A the maximum and the sum of the exponentials of the
-// differences from it (rows of `parts` pairs), and the sum of the row's label.
+// differences from it (rows of `parts` pairs), and the sum of the row's label.  C of the first `keep` rows of A (whole large tiles) is stored beside.
 struct Softmax {
   float2* part;
   float* z;
   const void* labels;
-  int labels64, parts;
+  int labels64, parts, keep;
 };
 // Or the gradient of a cross entropy: of a token (a row of B) the largest logit, the gradient g of its loss, g over the sum of the exponentials of the
 // differences from the largest, and its label (-1: none; g is 0 then) ...
@@ -224,7 +224,7 @@ bool takes_few_tokens(int n, int m, int t, int ncu);
 // X (t x m, 16 bits), or, where it is null, its 8-bit form xq; e may be null for the former.  softmax_few: the same with what the softmax needs in the
 // place of Y; its parts
 int softmax_parts_few(int n, int t, int ncu);
-slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm);
+slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm, float* kept, int64_t ldk);
 slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& xq, const Operand& w, int m,
                        const Epilogue* e, void* Y, slim_dtype y_dtype, int64_t ldy);
 

@@ -165,8 +165,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
   for (int e = threadIdx.x; e < tn * ROWS; e += blockDim.x) {
     const int tok = e / ROWS, r = e % ROWS;
     const float sum = sum_of(e);
-    if constexpr (MODE == SOFTMAX) part[tok * LD + r] = r < last ? sum : -__builtin_inff();      // (the first wavefront's sum, which nobody else reads)
-    else if (r < last) to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
+    if constexpr (MODE == SOFTMAX) {
+      part[tok * LD + r] = r < last ? sum : -__builtin_inff();      // (the first wavefront's sum, which nobody else reads)
+      if (row0 + r < a.sm.keep && r < last) static_cast<float*>(a.Y)[(int64_t)(tok0 + tok) * a.ldy + row0 + r] = sum;
+    } else if (r < last) to_any(a.Y, a.y_dtype, (int64_t)(tok0 + tok) * a.ldy + row0 + r, sum);
   }
   if constexpr (MODE == SOFTMAX) {
     __syncthreads();
@@ -248,8 +250,8 @@ slim_status few_tokens(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, 
 
 int softmax_parts_few(int n, int t, int ncu) { return slim_cdiv(n, 16 * sixteens(n, t, ncu)); }
 
-slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm) {
-  FewArgs a = {X, w.q, w.s, nullptr, ldx, w.ld, w.lds, 0, t, w.rows, m, slim_cdiv(m, BLOCK), (int)SLIM_F32, nullptr, nullptr, 0, 0, {}, sm};
+slim_status softmax_few(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& w, int m, const Softmax& sm, float* kept, int64_t ldk) {
+  FewArgs a = {X, w.q, w.s, kept, ldx, w.ld, w.lds, ldk, t, w.rows, m, slim_cdiv(m, BLOCK), (int)SLIM_F32, nullptr, nullptr, 0, 0, {}, sm};
   return x_dtype == SLIM_F16 ? launch<__half, SOFTMAX>(ctx, a) : launch<__hip_bfloat16, SOFTMAX>(ctx, a);
 }
 

@@ -14,7 +14,7 @@
 //    LDS, wavefront by wavefront, and leaves in rows.
 //  * What becomes of a tile's sums (MODE): they are stored; bias, residual and activation first (FINISH, the residuals fetched many at a
 //    time: 4096 x 11008 with 2048 tokens 110 us, one round of loads after another 120); of a tile of logits the maximum and the sum of exponentials
-//    of every token (SOFTMAX); or the logits' gradients, quantised in both directions for the products behind them (GRADIENT).
+//    of every token, with or without the logits themselves (SOFTMAX); or the logits' gradients, quantised in both directions for the products behind them (GRADIENT).
 //  * Several products share a launch (the two gradients, where their outputs are of one kind).  A product whose tiles do not fill the chip
 //    is cut along the contraction; the parts go to the workspace in fp32 and are added in a fixed order by a second kernel.
 //
@@ -656,7 +656,8 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
       }
       ga.sm.part[(int64_t)(b0 + r) * ga.sm.parts + a0 / T::TA] = s;
     }
-    return;
+    if (a0 >= ga.sm.keep) return;
+    __syncthreads();
   }
   if constexpr (MODE == GRADIENT) {
     quantize_gradient<T>(acc, ga.sg, p, smem_fg, a0, b0, wa, wb, wave, lane);

@@ -1,17 +1,17 @@
-// The cross entropy of labels in the softmax of an 8-bit head's outputs, and its gradients, without the outputs (the logits) in memory:
+// The cross entropy of labels in the softmax of an 8-bit head's outputs (the logits), and its gradients:
 //
 //   z = Q(x) W^T,  loss = ln sum exp z - z[label];   dz = dloss (softmax z - [label]),  dx = Q(dz) W,  dW = Qt(dz)^T Qt(x)
 //
 // One product over the whole vocabulary leaves, of every tile, the maximum and the sum of exponentials of its classes for each token (fp8_gemm.hip,
-// fp8_few.hip); `head_join` puts a token's tiles together in fp64.  The gradients need the logits a second time, once the sums are known: a piece
-// of the vocabulary at a time, so that what is in memory is a piece's and not t x V numbers.  A piece is multiplied again, the end of that product turns its
-// logits into dz in e4m3, in blocks of 128 classes and of 128 tokens (fp8_gemm.hip; with the logits through memory and a launch of its own
-// 32000 x 4096 with 2048 tokens took 1786 us in place of 1470), and the two products of the backward pass follow in one launch; dx is summed over
-// the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
+// fp8_few.hip); `head_join` puts a token's tiles together in fp64.  The loss alone needs no more: no logit is in memory.  The gradients need the logits a
+// second time, once the sums are known.  Up to 64 Mi of them wait in memory in fp32, and `head_gradient` turns them into dz in e4m3, in blocks of 128
+// classes and of 128 tokens; of the classes behind those the product is made again, and its end does the same.  It goes a piece of the vocabulary
+// at a time, so that the 8-bit forms stay small, and the two products of the backward pass follow each piece in one launch; dx is
+// summed over the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
 //
-// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1440 us, of them the logits' first product 390
-// (1.38 PFLOP/s), the second one with dz 460 in four pieces (1.17), dx and dw 575 (1.87); one token, the loss alone: 27 us, the weights'
-// read (5.0 TB/s), and 3 for `head_join`.
+// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1130 to 1180 us, of them the logits 437 (1.23 PFLOP/s; without
+// storing them 394), dz 113 in four pieces (3.5 TB/s; made again 466), dx and dw 575 (1.87).  One token, the loss alone: 27 us, the weights' read
+// (5.0 TB/s), and 3 for `head_join`.
 #include "act_device.h"
 #include "fp8_entry.h"
 
@@ -56,14 +56,117 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
   }
 }
 
+struct GradientArgs {
+  const float* z;                  // t x classes logits of this piece
+  SoftmaxGradient g;
+  int64_t ldz;
+  int t, classes, tiles_c;
+};
+
+__device__ __forceinline__ unsigned four_e4m3(float a, float b, float c, float d, float inv) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+}
+
+// Kept logits to dz in e4m3, as the end of the product does it (fp8_gemm.hip: quantize_gradient): tiles of 128 tokens x 128 classes, a thread holds
+// tokens 8 (tid / 16) .. + 7 of classes 8 (tid % 16) .. + 7; the transposed form goes through LDS in bytes.  Bound by memory.
+__global__ __launch_bounds__(256) void head_gradient(GradientArgs a) {
+  __shared__ __align__(16) unsigned colmax[4][BLOCK];
+  __shared__ __align__(16) uint8_t tile[BLOCK * BLOCK];    // [class][token], units of 8 bytes at unit ^ (class / 8 % 16)
+  const int tr = blockIdx.x / a.tiles_c, tc = blockIdx.x % a.tiles_c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid & 15, rg = tid >> 4;
+  const int r0 = tr * BLOCK + rg * 8, c0 = tc * BLOCK + cg * 8;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // (rows of kept logits have whole blocks of 128 classes: those behind the last class are not looked at)
+    const float* p = a.z + (int64_t)min(r0 + i, a.t - 1) * a.ldz + c0;
+    *reinterpret_cast<float4*>(&v[i][0]) = *reinterpret_cast<const float4*>(p);
+    *reinterpret_cast<float4*>(&v[i][4]) = *reinterpret_cast<const float4*>(p + 4);
+  }
+  unsigned rm[8], m[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const TokenStat s = a.g.stat[min(r0 + i, a.t - 1)];
+    const bool live = r0 + i < a.t && s.label >= 0;
+    const int at = s.label - a.g.first - c0;
+    rm[i] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float d = __builtin_amdgcn_exp2f((v[i][j] - s.top) * slimact::LOG2E_HI) * s.scaled;
+      if (at == j) d -= s.g;
+      v[i][j] = live && c0 + j < a.classes ? d : 0.f;
+      unsigned u = __float_as_uint(v[i][j]) & 0x7fffffffu;           // (patterns order like the values)
+      u = u < 0x7f800000u ? u : 0u;
+      rm[i] = max(rm[i], u);
+      m[j] = max(m[j], u);
+    }
+  }
+  if (a.g.rows_q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      unsigned u = rm[i];                                            // of the 16 lanes of a row
+      u = max(u, (unsigned)dpp_b32<DPP_XOR1>((int)u));
+      u = max(u, (unsigned)dpp_b32<DPP_XOR2>((int)u));
+      u = max(u, (unsigned)dpp_b32<DPP_HALF_MIRROR>((int)u));
+      u = max(u, (unsigned)dpp_b32<DPP_MIRROR>((int)u));
+      const unsigned b = scale_byte(u);
+      const float inv = __uint_as_float((254u - b) << 23);
+      if (r0 + i < a.t) {
+        const int64_t row = r0 + i;
+        *reinterpret_cast<uint2*>(a.g.rows_q + row * a.g.ldrq + c0) =
+            make_uint2(four_e4m3(v[i][0], v[i][1], v[i][2], v[i][3], inv), four_e4m3(v[i][4], v[i][5], v[i][6], v[i][7], inv));
+        if (cg == 0) a.g.rows_s[row * a.g.ldrs + tc] = (uint8_t)b;
+      }
+    }
+  }
+  if (!a.g.cols_q) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const auto a32 = __builtin_amdgcn_permlane32_swap(m[j], m[j], false, false);
+    const unsigned h = max(a32[0], a32[1]);
+    const auto a16 = __builtin_amdgcn_permlane16_swap(h, h, false, false);
+    m[j] = max(a16[0], a16[1]);
+  }
+  if (lane < 16) {
+    *reinterpret_cast<uint4*>(&colmax[wave][cg * 8]) = make_uint4(m[0], m[1], m[2], m[3]);
+    *reinterpret_cast<uint4*>(&colmax[wave][cg * 8 + 4]) = make_uint4(m[4], m[5], m[6], m[7]);
+  }
+  __syncthreads();
+  uint8_t* const tile0 = tile + cg * 8 * BLOCK + ((rg ^ cg) * 8);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int c = cg * 8 + j;
+    const unsigned b = scale_byte(max(max(colmax[0][c], colmax[1][c]), max(colmax[2][c], colmax[3][c])));
+    const float inv = __uint_as_float((254u - b) << 23);
+    *reinterpret_cast<uint2*>(tile0 + j * BLOCK) =
+        make_uint2(four_e4m3(v[0][j], v[1][j], v[2][j], v[3][j], inv), four_e4m3(v[4][j], v[5][j], v[6][j], v[7][j], inv));
+    if (rg == 0 && tc * BLOCK + c < a.classes) a.g.cols_s[(int64_t)(tc * BLOCK + c) * a.g.ldcs + tr] = (uint8_t)b;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = i * 32 + (tid >> 3), u = tid & 7, x = c >> 3;      // 16 bytes: units 2 u and 2 u + 1
+    uint4 w = *reinterpret_cast<const uint4*>(tile + c * BLOCK + ((2 * u) ^ (x & 14)) * 8);
+    if (x & 1) w = make_uint4(w.z, w.w, w.x, w.y);
+    if (tc * BLOCK + c < a.classes) *reinterpret_cast<uint4*>(a.g.cols_q + (int64_t)(tc * BLOCK + c) * a.g.ldcq + tr * BLOCK + u * 16) = w;
+  }
+}
+
 // Pieces: as many classes as make 16 Mi logits, in e4m3 twice (32 MB: they stay in the cache behind the L2 between the kernels), 1024 at
 // least; whole words of four scales.  32000 x 4096 with 2048 tokens: 16, 32 and 64 Mi take 1470, 1465 and 1500 us, so the smallest.
-constexpr int64_t HL_LOGITS = 1 << 24;
+// Kept are up to 64 Mi logits (256 MB of workspace, whole steps of classes).  32000 x 4096 with 2048 tokens, 62.5 Mi logits: none kept 1436 us, 16, 32
+// and 64 Mi 1391, 1313 and 1148; 50257 x 1501 with 301 tokens 274 and 242, 32000 x 4096 with 16 tokens 209 and 182, 1000 x 300 with 100 34 and 29.
+// More would cost memory that grows with the batch, which is what this operator is there to spare.
+constexpr int64_t HL_LOGITS = 1 << 24, HL_KEPT = 1 << 26;
 constexpr int HL_LEAST = 1024, HL_STEP = 4 * BLOCK;
 int piece_of(int V, int t) {
   const int64_t c = std::max<int64_t>(HL_LEAST, HL_LOGITS / std::max(1, t) / HL_STEP * HL_STEP);
   return (int)std::min<int64_t>(c, (V + HL_STEP - 1) / HL_STEP * HL_STEP);
 }
+
+int kept_of(int V, int t) { return (int)std::min<int64_t>(HL_KEPT / std::max(1, t) / HL_STEP * HL_STEP, (V + HL_STEP - 1) / HL_STEP * HL_STEP); }
+constexpr int HL_APART = 32;                       // numbers between the rows of kept logits (at a multiple of 4 KiB they share few of the L2's channels)
 
 Product logits_product(int V, int m, int t, const Softmax* sm) {
   Product p = {};
@@ -82,15 +185,17 @@ size_t pair_bytes(int V, int t, int ncu) {
   const int64_t few = std::min((int64_t)t * slim_cdiv(V, 16), std::max((int64_t)16 * slim_cdiv(V, 16), (int64_t)70 * 16 * ncu));
   return slim_ws_round(sizeof(float2) * (size_t)std::max(few, (int64_t)t * slim_cdiv(V, 64)));
 }
-size_t loss_need(int V, int m, int t, int ncu) {
-  return pair_bytes(V, t, ncu) + slim_ws_round(sizeof(float) * (size_t)t) + activation_bytes(t, m);
-}
-// In the pieces' terms: t times a piece is no more than `logits`, which grows with t, and a piece no more than the vocabulary.
+size_t sums_need(int V, int t, int ncu) { return pair_bytes(V, t, ncu) + slim_ws_round(sizeof(float) * (size_t)t); }
+size_t loss_need(int V, int m, int t, int ncu) { return sums_need(V, t, ncu) + activation_bytes(t, m); }
+// What the pieces need lies where the tokens' pairs were.  In the pieces' terms: t times a piece is no more than `logits`, which grows with t, and a
+// piece no more than the vocabulary.
 size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int ncu) {
   if (t <= 0) return 0;
   const int64_t Vp = (int64_t)(V + HL_STEP - 1) / HL_STEP * HL_STEP;
   const int64_t logits = std::min(t * Vp, std::max(HL_LOGITS, (int64_t)HL_LEAST * t));
-  size_t bytes = loss_need(V, m, t, ncu) + slim_ws_round(sizeof(TokenStat) * (size_t)t);
+  size_t stay = activation_bytes(t, m) + slim_ws_round(sizeof(TokenStat) * (size_t)t) +
+                slim_ws_round(sizeof(float) * (size_t)(std::min(t * Vp, HL_KEPT) + HL_APART * (int64_t)t));
+  size_t bytes = 0;
   size_t parts = 0;                               // of the products that are cut, one after another
   Product p = {};
   if (dx) {
@@ -102,13 +207,14 @@ size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int
     parts += gemm_workspace(&p, 1, ncu);
   }
   if (dw) {
-    bytes += activation_bytes(m, t) + slim_ws_round((size_t)(logits + 2 * BLOCK * Vp)) + slim_ws_round((size_t)(logits / BLOCK + 8 * Vp));
+    stay += activation_bytes(m, t);
+    bytes += slim_ws_round((size_t)(logits + 2 * BLOCK * Vp)) + slim_ws_round((size_t)(logits / BLOCK + 8 * Vp));
     p.a.rows = m;
     p.b.rows = (int)Vp;
     p.nk = slim_cdiv(t, BLOCK);
     parts += gemm_workspace(&p, 1, ncu);
   }
-  return bytes + parts;
+  return stay + std::max(sums_need(V, t, ncu), bytes + parts);
 }
 
 slim_status check_head(slim_ctx* ctx, const char* fn, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
@@ -122,20 +228,23 @@ slim_status check_head(slim_ctx* ctx, const char* fn, const void* X, slim_dtype 
   return SLIM_OK;
 }
 
-// Losses and, with `stat`, the tokens' sums; x: the quantised activations (not looked at where a few tokens are multiplied in one launch)
+// Losses and, with `stat`, the tokens' sums; x: the quantised activations (not looked at where a few tokens are multiplied in one launch).  The
+// logits of the first `keep` classes go to `kept`.
 slim_status losses(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const Operand& x, const Operand& w, int m, const void* labels,
-                   int labels64, const float* dloss, float* loss, TokenStat* stat) {
+                   int labels64, const float* dloss, float* loss, TokenStat* stat, float* kept, int64_t ldk, int keep) {
   const int V = w.rows, ncu = ctx->num_cus;
   const bool few = takes_few_tokens(V, m, t, ncu);
-  Softmax sm = {nullptr, nullptr, labels, labels64, 0};
+  Softmax sm = {nullptr, nullptr, labels, labels64, 0, keep};
   Product p = logits_product(V, m, t, &sm);
   p.a = w;
   p.b = x;
+  p.c = kept;
+  p.ldc = ldk;
   sm.parts = few ? softmax_parts_few(V, t, ncu) : softmax_parts(p, ncu);
   sm.part = static_cast<float2*>(slim_ws_alloc(ctx, sizeof(float2) * (size_t)sm.parts * t));
   sm.z = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)t));
   if (!sm.part || !sm.z) return slim_fail(ctx, SLIM_ERR_ALLOC, "head_loss: workspace");
-  if (const slim_status st = few ? softmax_few(ctx, X, x_dtype, t, ldx, w, m, sm) : gemm(ctx, "head_logits", &p, 1); st != SLIM_OK) return st;
+  if (const slim_status st = few ? softmax_few(ctx, X, x_dtype, t, ldx, w, m, sm, kept, ldk) : gemm(ctx, "head_logits", &p, 1); st != SLIM_OK) return st;
   SLIM_LAUNCH(ctx, "head_join", head_join, dim3(slim_cdiv(t, 4)), dim3(256), 0, sm.part, sm.parts, sm.z, labels, labels64, dloss, t, V, loss, stat);
   return SLIM_OK;
 }
@@ -166,7 +275,7 @@ slim_status slim_head_loss(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int
     if (const slim_status st = quantize(ctx, "fp8_quantize_x", x_dtype, &a, 1); st != SLIM_OK) return st;
   }
   const Operand x = {a.rows_q, a.rows_s, quantized_ld(m), scales_ld(m), t, 0};
-  return losses(ctx, X, x_dtype, t, ldx, x, Operand{q, s, ldq, lds, V, 7}, m, labels, labels64, nullptr, loss, nullptr);
+  return losses(ctx, X, x_dtype, t, ldx, x, Operand{q, s, ldq, lds, V, 7}, m, labels, labels64, nullptr, loss, nullptr, nullptr, 0, 0);
 }
 
 slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
@@ -196,12 +305,16 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
   bool ok = carve(ctx, t, m, a.rows_q, a.rows_s);
   if (dW) ok = ok && carve(ctx, m, t, a.cols_q, a.cols_s);
   TokenStat* const stat = static_cast<TokenStat*>(slim_ws_alloc(ctx, sizeof(TokenStat) * (size_t)t));
-  if (!ok || !stat) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
+  const int keep = kept_of(V, t);
+  const int64_t ldk = keep + HL_APART;
+  float* const kept = static_cast<float*>(slim_ws_alloc(ctx, sizeof(float) * (size_t)t * ldk));
+  if (!ok || !stat || !kept) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
   if (const slim_status e = quantize(ctx, "fp8_quantize_x", x_dtype, &a, 1); e != SLIM_OK) return e;
   const Operand x = {a.rows_q, a.rows_s, quantized_ld(m), scales_ld(m), t, 0}, xt = {a.cols_q, a.cols_s, quantized_ld(t), scales_ld(t), m, 0};
   const Operand w = {q, s, ldq, lds, V, 7};
-  if (const slim_status e = losses(ctx, X, x_dtype, t, ldx, x, w, m, labels, labels64, dloss, loss, stat); e != SLIM_OK) return e;
-
+  const size_t stay = ctx->ws_off;
+  if (const slim_status e = losses(ctx, X, x_dtype, t, ldx, x, w, m, labels, labels64, dloss, loss, stat, kept, ldk, keep); e != SLIM_OK) return e;
+  ctx->ws_off = stay;
   const int piece = piece_of(V, t);
   const int64_t ldacc = (m + 3) / 4 * 4;
   SoftmaxGradient g = {};
@@ -220,14 +333,19 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
   }
   if (!ok) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
   const size_t mark = ctx->ws_off;
-  for (int v0 = 0; v0 < V; v0 += piece) {
-    const int n = std::min(piece, V - v0);
-    Product p = logits_product(n, m, t, nullptr);
-    p.a = Operand{q + v0 * ldq, s + v0 / BLOCK * lds, ldq, lds, n, 7};
-    p.b = x;
-    p.sg = &g;
+  for (int v0 = 0, n; v0 < V; v0 += n) {
+    n = std::min(piece, (v0 < keep ? std::min(keep, V) : V) - v0);
     g.first = v0;
-    if (const slim_status e = gemm(ctx, "head_gradient", &p, 1); e != SLIM_OK) return e;
+    if (v0 < keep) {
+      const GradientArgs ga = {kept + v0, g, ldk, t, n, slim_cdiv(n, BLOCK)};
+      SLIM_LAUNCH(ctx, "head_gradient_kept", head_gradient, dim3(ga.tiles_c * slim_cdiv(t, BLOCK)), dim3(256), 0, ga);
+    } else {
+      Product p = logits_product(n, m, t, nullptr);
+      p.a = Operand{q + v0 * ldq, s + v0 / BLOCK * lds, ldq, lds, n, 7};
+      p.b = x;
+      p.sg = &g;
+      if (const slim_status e = gemm(ctx, "head_gradient", &p, 1); e != SLIM_OK) return e;
+    }
     Product both[2] = {};                         // dX's share, and the piece's rows of dW
     int count = 0;
     Epilogue sum = {};

@@ -92,6 +92,11 @@ def test_several_pieces_with_odd_ends(slim):
     gradient_check(slim, 2049, 65, 17000, torch.float16, torch.float16, labels_type=torch.int32)
 
 
+def test_more_logits_than_are_kept(slim):
+    """More than 64 Mi: the last classes' are computed again, and a piece ends where the kept ones do."""
+    gradient_check(slim, 17001, 40, 4200, torch.float16, torch.float32)
+
+
 @pytest.mark.parametrize("t", [1, 16, 40, 300, 2000])
 @pytest.mark.parametrize("V", [700, 5003])
 def test_losses(slim, t, V):
