@@ -509,7 +509,7 @@ slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const
  *   dW       V x m, F16, BF16 or F32, or NULL: Qt(dz)^T Qt(X), both in blocks of 128 tokens, sums as in slim_fp8_linear_backward.  A row of X without a
  *            label adds nothing to dW if it is finite.
  * The loss alone keeps no logits.  The gradients need them twice: up to 64 Mi (256 MB of the workspace, in fp32) are kept, those of the classes behind are
- * computed again; from there on a piece of the vocabulary at a time, 16 Mi logits or 1024 classes. */
+ * computed again, 64 Mi logits or 1024 classes at a time. */
 size_t slim_head_loss_workspace(int V, int m, int t, int num_cus);
 slim_status slim_head_loss(slim_ctx* ctx, const void* X, slim_dtype x_dtype, int t, int64_t ldx, const uint8_t* q, int64_t ldq, const uint8_t* s,
                            int64_t lds, int V, int m, const void* labels, int labels64, float* loss);

@@ -9,8 +9,8 @@
 // at a time, so that the 8-bit forms stay small, and the two products of the backward pass follow each piece in one launch; dx is
 // summed over the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
 //
-// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1130 to 1180 us, of them the logits 437 (1.23 PFLOP/s; without
-// storing them 394), dz 113 in four pieces (3.5 TB/s; made again 466), dx and dw 575 (1.87).  One token, the loss alone: 27 us, the weights' read
+// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1070 to 1090 us, of them the logits 437 (1.23 PFLOP/s; without
+// storing them 394), dz 78 (5.0 TB/s; made again 466), dx and dw 537 (2.00).  One token, the loss alone: 27 us, the weights' read
 // (5.0 TB/s), and 3 for `head_join`.
 #include "act_device.h"
 #include "fp8_entry.h"
@@ -153,19 +153,20 @@ __global__ __launch_bounds__(256) void head_gradient(GradientArgs a) {
   }
 }
 
-// Pieces: as many classes as make 16 Mi logits, in e4m3 twice (32 MB: they stay in the cache behind the L2 between the kernels), 1024 at
-// least; whole words of four scales.  32000 x 4096 with 2048 tokens: 16, 32 and 64 Mi take 1470, 1465 and 1500 us, so the smallest.
-// Kept are up to 64 Mi logits (256 MB of workspace, whole steps of classes).  32000 x 4096 with 2048 tokens, 62.5 Mi logits: none kept 1436 us, 16, 32
-// and 64 Mi 1391, 1313 and 1148; 50257 x 1501 with 301 tokens 274 and 242, 32000 x 4096 with 16 tokens 209 and 182, 1000 x 300 with 100 34 and 29.
-// More would cost memory that grows with the batch, which is what this operator is there to spare.
-constexpr int64_t HL_LOGITS = 1 << 24, HL_KEPT = 1 << 26;
+// Pieces: as many classes as make 64 Mi logits (in e4m3, twice, 128 MB of workspace), 1024 at least; whole words of four scales.  The first one's
+// are kept (256 MB, in fp32).  Measured: 32000 x 4096 with 2048 tokens, 62.5 Mi logits: none kept 1436 us, 16, 32 and 64 Mi in pieces of 16 Mi 1391,
+// 1313 and 1143, in pieces of 32 and 64 Mi 1085 and 1068 (fewer rounds that end unevenly, dx once through memory); pieces of 16, 32 and 64 Mi behind 64 Mi kept:
+// 131072 x 1024, 2000 tokens 2298, 2218 and 1883, 100000 x 300, 8000 tokens 3942, 3973 and 2997.  With fewer logits than that, without and with keeping
+// them: 50257 x 1501, 301 tokens 274 and 242, 32000 x 4096, 16 tokens 209 and 182, 1000 x 300, 100 tokens 34 and 29.  More would cost
+// memory that grows with the batch, which is what this operator is there to spare.
+constexpr int64_t HL_LOGITS = 1 << 26;
 constexpr int HL_LEAST = 1024, HL_STEP = 4 * BLOCK;
 int piece_of(int V, int t) {
   const int64_t c = std::max<int64_t>(HL_LEAST, HL_LOGITS / std::max(1, t) / HL_STEP * HL_STEP);
   return (int)std::min<int64_t>(c, (V + HL_STEP - 1) / HL_STEP * HL_STEP);
 }
 
-int kept_of(int V, int t) { return (int)std::min<int64_t>(HL_KEPT / std::max(1, t) / HL_STEP * HL_STEP, (V + HL_STEP - 1) / HL_STEP * HL_STEP); }
+int kept_of(int V, int t) { return (int)std::min<int64_t>(HL_LOGITS / std::max(1, t) / HL_STEP * HL_STEP, (V + HL_STEP - 1) / HL_STEP * HL_STEP); }
 constexpr int HL_APART = 32;                       // numbers between the rows of kept logits (at a multiple of 4 KiB they share few of the L2's channels)
 
 Product logits_product(int V, int m, int t, const Softmax* sm) {
@@ -194,7 +195,7 @@ size_t grad_need(int V, int m, int t, bool dx, bool dw, slim_dtype dw_dtype, int
   const int64_t Vp = (int64_t)(V + HL_STEP - 1) / HL_STEP * HL_STEP;
   const int64_t logits = std::min(t * Vp, std::max(HL_LOGITS, (int64_t)HL_LEAST * t));
   size_t stay = activation_bytes(t, m) + slim_ws_round(sizeof(TokenStat) * (size_t)t) +
-                slim_ws_round(sizeof(float) * (size_t)(std::min(t * Vp, HL_KEPT) + HL_APART * (int64_t)t));
+                slim_ws_round(sizeof(float) * (size_t)(std::min(t * Vp, HL_LOGITS) + HL_APART * (int64_t)t));
   size_t bytes = 0;
   size_t parts = 0;                               // of the products that are cut, one after another
   Product p = {};

@@ -77,7 +77,7 @@ def test_gradients(slim, V, m, t, x, dw):
 
 @pytest.mark.parametrize("V,m,t", [(4100, 96, 700), (2050, 512, 1030), (33000, 64, 40), (40000, 128, 3), (8200, 3000, 1030), (5000, 130, 9000)])
 def test_every_tile_and_several_pieces(slim, V, m, t):
-    """Sizes that reach the tiles of both passes; the last one takes its vocabulary in several pieces."""
+    """Sizes that reach the tiles of both passes."""
     X, labels, dloss, W, loss, dX, dW = gradient_check(slim, V, m, t, torch.bfloat16, torch.float32)
     again = slim.head_loss_grad(X.cuda(), *W, labels.cuda(), dloss.cuda(), torch.float32)
     assert all(torch.equal(a, b) for a, b in zip(again, (loss, dX, dW)))
@@ -88,13 +88,39 @@ def test_every_tile_and_several_pieces(slim, V, m, t):
 
 
 def test_several_pieces_with_odd_ends(slim):
-    """More than 16 Mi logits, an odd vocabulary: pieces that start inside the stored matrix, the last one of a few classes."""
+    """Many tokens, an odd vocabulary."""
     gradient_check(slim, 2049, 65, 17000, torch.float16, torch.float16, labels_type=torch.int32)
 
 
 def test_more_logits_than_are_kept(slim):
     """More than 64 Mi: the last classes' are computed again, and a piece ends where the kept ones do."""
     gradient_check(slim, 17001, 40, 4200, torch.float16, torch.float32)
+
+
+def test_several_pieces_of_many_tokens(slim):
+    """Three pieces, of 3584 classes and the rest: all losses, the gradients of some tokens and, at the pieces' ends, of some classes."""
+    V, m, t = 8300, 65, 17000
+    W, X, labels, dloss = problem(V, m, t, torch.float16, 5)
+    q, s, qt, st = slim.fp8_quantize_weights(W.cuda())
+    loss, dX, dW = slim.head_loss_grad(X.cuda(), q, s, qt, st, labels.cuda(), dloss.cuda(), torch.float32)
+    classes = torch.tensor([0, 1, 127, 128, 3583, 3584, 3585, 7167, 7168, V - 1, int(labels[5]), int(labels[t - 1])])
+    rows, cols = [], []
+    for i in range(0, t, 2000):
+        part = slice(i, min(t, i + 2000))
+        B, z, e, live, at, lse, want, e_lse, e_loss = expected(W, X[part], labels[part])
+        check(loss[part], want, e_loss)
+        p = torch.exp(z - lse[:, None])
+        off = p - torch.zeros_like(p).scatter_(1, at, 1.0)
+        g = torch.where(live, dloss[part].double(), 0.0)[:, None]
+        dz, e_dz = g * off, g * (p * (e + e_lse[:, None] + 8 * U) + 3 * U * off.abs())
+        lo, hi = dz - e_dz, dz + e_dz
+        some = torch.arange(0, len(lo), 397)
+        rows.append((some + i, lo[some], hi[some]))
+        cols.append((lo[:, classes], hi[:, classes]))
+    at, lo, hi = (torch.cat(v) for v in zip(*rows))
+    product_of_range(*gradient_range(lo, hi, "rows"), B, dX[at.cuda()], False)
+    least, most = gradient_range(*(torch.cat(v) for v in zip(*cols)), "cols")
+    product_of_range(least.t().contiguous(), most.t().contiguous(), ref.q_cols(X), dW[classes.cuda()], True)
 
 
 @pytest.mark.parametrize("t", [1, 16, 40, 300, 2000])
