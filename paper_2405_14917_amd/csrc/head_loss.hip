@@ -166,7 +166,7 @@ int piece_of(int V, int t) {
   return (int)std::min<int64_t>(c, (V + HL_STEP - 1) / HL_STEP * HL_STEP);
 }
 
-int kept_of(int V, int t) { return (int)std::min<int64_t>(HL_LOGITS / std::max(1, t) / HL_STEP * HL_STEP, (V + HL_STEP - 1) / HL_STEP * HL_STEP); }
+int kept_of(int V, int t) { return (int64_t)piece_of(V, t) * t <= HL_LOGITS ? piece_of(V, t) : 0; }     // (1024 classes may be more)
 constexpr int HL_APART = 32;                       // numbers between the rows of kept logits (at a multiple of 4 KiB they share few of the L2's channels)
 
 Product logits_product(int V, int m, int t, const Softmax* sm) {
@@ -334,8 +334,8 @@ slim_status slim_head_loss_grad(slim_ctx* ctx, const void* X, slim_dtype x_dtype
   }
   if (!ok) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: workspace", fn);
   const size_t mark = ctx->ws_off;
-  for (int v0 = 0, n; v0 < V; v0 += n) {
-    n = std::min(piece, (v0 < keep ? std::min(keep, V) : V) - v0);
+  for (int v0 = 0; v0 < V; v0 += piece) {
+    const int n = std::min(piece, V - v0);
     g.first = v0;
     if (v0 < keep) {
       const GradientArgs ga = {kept + v0, g, ldk, t, n, slim_cdiv(n, BLOCK)};

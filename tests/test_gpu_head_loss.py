@@ -97,13 +97,14 @@ def test_more_logits_than_are_kept(slim):
     gradient_check(slim, 17001, 40, 4200, torch.float16, torch.float32)
 
 
-def test_several_pieces_of_many_tokens(slim):
-    """Three pieces, of 3584 classes and the rest: all losses, the gradients of some tokens and, at the pieces' ends, of some classes."""
-    V, m, t = 8300, 65, 17000
+@pytest.mark.parametrize("V,m,t", [(8300, 65, 17000), (601, 20, 66000), (1100, 20, 70000), (513, 20, 132000)])
+def test_many_tokens(slim, V, m, t):
+    """Three pieces, of 3584 classes and the rest; fewer logits kept than make a piece, in one piece and two: all losses, the gradients of some tokens and, at the
+    pieces' ends, of some classes."""
     W, X, labels, dloss = problem(V, m, t, torch.float16, 5)
     q, s, qt, st = slim.fp8_quantize_weights(W.cuda())
     loss, dX, dW = slim.head_loss_grad(X.cuda(), q, s, qt, st, labels.cuda(), dloss.cuda(), torch.float32)
-    classes = torch.tensor([0, 1, 127, 128, 3583, 3584, 3585, 7167, 7168, V - 1, int(labels[5]), int(labels[t - 1])])
+    classes = torch.tensor([c for c in (0, 1, 127, 128, 511, 512, 1023, 1024, 3583, 3584, 3585, 7167, 7168) if c < V] + [V - 1, int(labels[5]), int(labels[t - 1])])
     rows, cols = [], []
     for i in range(0, t, 2000):
         part = slice(i, min(t, i + 2000))
