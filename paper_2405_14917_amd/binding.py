@@ -1048,7 +1048,7 @@ class Slim:
     def head_loss_grad(self, X: torch.Tensor, W: torch.Tensor, Ws: torch.Tensor, Wt: Optional[torch.Tensor], Wts: Optional[torch.Tensor],
                        labels: torch.Tensor, dloss: torch.Tensor, dw_dtype: Optional[torch.dtype] = None, dx: bool = True, dw: bool = True):
         """(loss, dX (t, m), dW (V, m)): head_loss and the gradients of sum(dloss * loss); dw_dtype: of dW (default: X's).  Without `dx` Wt and Wts may be
-        None; the gradient that is not wanted is None."""
+        None; the gradient that is not wanted is None.  The workspace keeps up to 64 Mi of the t x V outputs in between, 256 MB."""
         self._ready(X, W, Ws, Wt, Wts, labels, dloss)
         if not (dx or dw):
             raise ValueError("neither gradient is wanted")

@@ -6,8 +6,7 @@
 // wavefronts; a block of 128 channels is 16 (16-bit types) or 32 lanes one after another, so that its largest magnitude takes a few moves
 // inside the wavefront, on packed 16-bit patterns where the type has 16 bits.
 //
-// 16384 x 4096 bf16 without the mean, the output in both forms: forward 107 us (5.6 TB/s), backward
-// 108 to 111 (4.9 TB/s), the second kernel 5.
+// 16384 x 4096 bf16 without the mean, the output in both forms: forward 107 us (5.6 TB/s), backward 108 to 111 (4.9 TB/s), the second kernel 5.
 #include "fp8_device.h"
 #include "norm_device.h"
 
@@ -17,8 +16,8 @@ using namespace slimnorm;
 using slimfp8::BLOCK;
 
 // Sums over the W wavefronts of a row, of the lanes' sums in fp64: what is off in a row's factor is off in all of its numbers, and moves those next
-// to a border of the 8-bit form to its other side (fp32 outputs are 4.6e-8 to 5.1e-8 off, with these sums in fp32 6.0e-8 to 6.6e-8; one rounding is 2.5e-8; with deviations and
-// outputs in fp64 as well 16384 x 4096 took 102 us in place of 87)
+// to a border of the 8-bit form to its other side (fp32 outputs are 4.6e-8 to 5.1e-8 off, with these sums in fp32 6.0e-8 to 6.6e-8; one rounding is
+// 2.5e-8; with deviations and outputs in fp64 as well 16384 x 4096 took 102 us in place of 87)
 template <int W>
 __device__ __forceinline__ double row_sum(double v, double (*red)[W], int& slot) {
   v = wave_sum(v);
@@ -242,6 +241,8 @@ __global__ __launch_bounds__(1024) void add_norm_forward_long(NormArgs a) {
   }
 }
 
+// Workgroups a CU (forward passes, bf16, weight and bias fp32): one piece a lane six (12000 x 1504 27.6 -> 25.8 us, 16384 x 512 13.9 -> 12.7), four pieces
+// four (9000 x 8192 115 -> 108, 2100 x 8192 32.5 -> 27.9; fp32 9000 x 4096 112 and 114), between them eight (16384 x 4000 98, with six 102, with five 112).
 template <typename T, typename TW>
 slim_status forward(slim_ctx* ctx, const NormArgs& a) {
   constexpr int E = Piece<T>::E;
@@ -250,11 +251,11 @@ slim_status forward(slim_ctx* ctx, const NormArgs& a) {
   const char* name = "add_norm_forward";
   auto grid = [&](int64_t groups, int per_cu) { return dim3((unsigned)std::min<int64_t>(groups, (int64_t)per_cu * ctx->num_cus)); };
   const bool few = a.rows < many;              // rows that do not fill the chip: more lanes per row
-  if (pieces <= 64) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 1, 1>), grid((a.rows + 3) / 4, 8), dim3(256), 0, a);
-  else if (pieces <= 256 && (few || pieces > 128)) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 4, 1>), grid(a.rows, 8), dim3(256), 0, a);
+  if (pieces <= 64) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 1, 1>), grid((a.rows + 3) / 4, 6), dim3(256), 0, a);
+  else if (pieces <= 256 && (few || pieces > 128)) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 4, 1>), grid(a.rows, 6), dim3(256), 0, a);
   else if (pieces <= 128) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 1, 2>), grid((a.rows + 3) / 4, 8), dim3(256), 0, a);
   else if (pieces <= 512) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 4, 2>), grid(a.rows, 8), dim3(256), 0, a);
-  else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 4, 4>), grid(a.rows, 8), dim3(256), 0, a);
+  else if (pieces <= 1024) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 4, 4>), grid(a.rows, 4), dim3(256), 0, a);
   else if (pieces <= 2048) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 16, 2>), grid(a.rows, 2), dim3(1024), 0, a);
   else if (pieces <= 4096) SLIM_LAUNCH(ctx, name, (add_norm_forward<T, TW, 16, 4>), grid(a.rows, 2), dim3(1024), 0, a);
   else SLIM_LAUNCH(ctx, name, (add_norm_forward_long<T, TW>), grid(a.rows, 2), dim3(1024), 0, a);
