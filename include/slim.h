@@ -504,7 +504,8 @@ slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const
  *   labels   t classes, int64 (labels64 != 0) or int32; what lies outside 0 .. V - 1, -100 say, is no label: loss 0, no gradient
  *   loss     t: ln sum exp z - z[label] for z = Q(X) W^T, whose sums keep 24 bits
  *   dloss    t: the gradients of the losses (not read where there is no label)
- *   dX       t x m of X's type, or NULL: Q(dz) W for dz = dloss (softmax z - [label]), in e4m3 in blocks of 128 classes, from the stored form qt, st of
+ *   dX       t x m of X's type, or NULL: Q(dz) W for dz = dloss (softmax z - [label]) (at the label -dloss times the other classes' share, not a difference
+ *            from one), in e4m3 in blocks of 128 classes, from the stored form qt, st of
  *            W^T (not read without dX); sums on the e4m3 matrix cores, between pieces of the vocabulary in fp32
  *   dW       V x m, F16, BF16 or F32, or NULL: Qt(dz)^T Qt(X), both in blocks of 128 tokens, sums as in slim_fp8_linear_backward.  A row of X without a
  *            label adds nothing to dW if it is finite.

@@ -156,21 +156,22 @@ struct Epilogue {
   int64_t ldr, ldz;
   int bias_dtype, act, r_dtype;
 };
-// Or, in the place of C, what the softmax of the rows of B over those of A needs: of every tile of A the maximum and the sum of the exponentials of the
-// differences from it (rows of `parts` pairs), and the sum of the row's label.  C of the first `keep` rows of A (whole large tiles) is stored beside.
+// Or, in the place of C, what the softmax of the rows of B over those of A needs: the row's C at its label (z), and of every tile of A the maximum of the
+// others and the sum of the exponentials of their differences from it (rows of `parts` pairs).  Apart, since what a confident row lacks to a probability of
+// one is that sum, and lost as a difference.  C of the first `keep` rows of A (whole large tiles) is stored beside.
 struct Softmax {
   float2* part;
   float* z;
   const void* labels;
   int labels64, parts, keep;
 };
-// Or the gradient of a cross entropy: of a token (a row of B) the largest logit, the gradient g of its loss, g over the sum of the exponentials of the
-// differences from the largest, and its label (-1: none; g is 0 then) ...
+// Or the gradient of a cross entropy: of a token (a row of B) the largest logit, the gradient of its loss over the sum of the exponentials of the
+// differences from the largest, its label (-1: none; the gradient is 0 then), and dz there, the gradient times what its probability lacks to one, negated ...
 struct TokenStat {
-  float top, g, scaled;
+  float top, own, scaled;
   int label;
 };
-// ... for dz[b][a] = scaled exp(C[b][a] - top) - [first + a = label] g, quantised in blocks of 128 of A (rows_q, as activations are) and of 128 of B (cols_q,
+// ... for dz[b][a] = scaled exp(C[b][a] - top), `own` where first + a = label, quantised in blocks of 128 of A (rows_q, as activations are) and of 128 of B (cols_q,
 // transposed); either may be null.
 struct SoftmaxGradient {
   const TokenStat* stat;

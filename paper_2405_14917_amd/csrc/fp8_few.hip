@@ -174,11 +174,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few(FewArgs a) {
     __syncthreads();
     for (int tok = wave; tok < tn; tok += nw) {
       const float* z = part + tok * LD;
-      const float z0 = lane < ROWS ? z[lane] : -__builtin_inff(), z1 = lane + 64 < ROWS ? z[lane + 64] : -__builtin_inff();
-      const float top = wave_max_f32(fmaxf(z0, z1));
-      const float sum = wave_sum_f32(__builtin_amdgcn_exp2f((z0 - top) * slimact::LOG2E_HI) + __builtin_amdgcn_exp2f((z1 - top) * slimact::LOG2E_HI));
+      const int64_t row = tok0 + tok, at = label_at(a.sm.labels, a.sm.labels64, row) - row0;
+      // (the label's own logit counts in neither the maximum nor the sum)
+      const float z0 = lane < ROWS && lane != at ? z[lane] : -__builtin_inff(), z1 = lane + 64 < ROWS && lane + 64 != at ? z[lane + 64] : -__builtin_inff();
+      const float top = wave_max_f32(fmaxf(z0, z1)), from = top == -__builtin_inff() ? 0.f : top;
+      const float sum = wave_sum_f32(__builtin_amdgcn_exp2f((z0 - from) * slimact::LOG2E_HI) + __builtin_amdgcn_exp2f((z1 - from) * slimact::LOG2E_HI));
       if (lane == 0) {
-        const int64_t row = tok0 + tok, at = label_at(a.sm.labels, a.sm.labels64, row) - row0;
         a.sm.part[row * a.sm.parts + blockIdx.x] = make_float2(top, sum);
         if (at >= 0 && at < last) a.sm.z[row] = z[at];
       }

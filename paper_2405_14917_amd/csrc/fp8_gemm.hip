@@ -245,8 +245,8 @@ __device__ __forceinline__ constexpr int share_from(int m, int n) { return m * 2
 
 // The sums of a tile as logits: dz in their place, then its two 8-bit forms.  A lane holds, of 32 tokens l32 of each j, the classes 32 i + 8 (q / 4) + 4 h + q % 4:
 // a token's block of 128 classes is in two lanes (and two wavefronts, where a wavefront's part is 64 wide), a class's block of 128 tokens in
-// the 32 lanes of a half (and two wavefronts).  What is not finite fills a token's whole row (the sum it is divided by, or g, is not), so that one flag a
-// token is enough.  Both forms leave through a part of LDS of the wavefront's own, in rows of the block.
+// the 32 lanes of a half (and two wavefronts).  What is not finite fills a token's whole row (`scaled` and `own` are not), so that one flag a
+// token is enough.  Exponentials with log2(e) in one part: exp(-x) is off by x 7.5e-8 of itself, where e4m3's half step is 2^-4.  Both forms leave through a part of LDS of the wavefront's own, in rows of the block.
 template <typename T>
 __device__ __forceinline__ void quantize_gradient(v16f (&acc)[T::MA][T::MB], const SoftmaxGradient& sg, const ProductArgs& p, char* smem, int a0, int b0, int wa,
                                                   int wb, int wave, int lane) {
@@ -277,7 +277,7 @@ __device__ __forceinline__ void quantize_gradient(v16f (&acc)[T::MA][T::MB], con
       for (int i = 0; i < MA; ++i)
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          if (at == i * 32 + 8 * (q / 4) + q % 4) acc[i][j][q] -= st[j].g;
+          if (at == i * 32 + 8 * (q / 4) + q % 4) acc[i][j][q] = fmaf(acc[i][j][q], 0.f, st[j].own);      // (`own`; as a move it spilled 68 registers)
     }
     if (__any(!live)) {
 #pragma unroll
@@ -614,22 +614,10 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
           for (int q = 0; q < 16; ++q)
             if (i * 32 + 8 * (q / 4) + q % 4 >= left) acc[i][j][q] = -__builtin_inff();
       }
-      float top = -__builtin_inff();
-#pragma unroll
-      for (int i = 0; i < MA; ++i)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float from = top == -__builtin_inff() ? 0.f : top;       // (rows behind the last one alone)
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < MA; ++i)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f((acc[i][j][q] - from) * slimact::LOG2E_HI);
-      sum += __shfl_xor(sum, 32, 64);
-      if (h == 0) share[wa * T::TB + in_b] = make_float2(top, sum);
+      // the label's logit goes its own way, and counts in neither the maximum nor the sum: -inf in its place (NaN if it is not finite), also among
+      // the kept ones, where nobody looks at it
       const int64_t label = row < p.b.rows ? label_at(ga.sm.labels, ga.sm.labels64, row) : -1;
-      const int at = label >= first && label < min(p.a.rows, first + MA * 32) ? (int)(label - first) : -1;
+      int at = label >= first && label < min(p.a.rows, first + MA * 32) ? (int)(label - first) : -1;
       if (__any(at >= 0)) {
         float z = 0.f;
         bool mine = false;                                           // (the other half of the lanes holds four classes in eight)
@@ -642,7 +630,29 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
               mine = true;
             }
         if (mine) ga.sm.z[row] = z;
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(at));                                 // (compared again: kept, or in one loop, 81 registers are spilled)
+#endif
+#pragma unroll
+        for (int i = 0; i < MA; ++i)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (at == i * 32 + 8 * (q / 4) + q % 4) acc[i][j][q] = fmaf(acc[i][j][q], 0.f, -__builtin_inff());
       }
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float from = top == -__builtin_inff() ? 0.f : top;       // (classes behind the last one, or the label, alone)
+      float sum = 0.f;                                               // (log2(e) in one part: exp(-x) is off by x 7.5e-8 of itself, 2.8e-8 of the sum at most)
+#pragma unroll
+      for (int i = 0; i < MA; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f((acc[i][j][q] - from) * slimact::LOG2E_HI);
+      sum += __shfl_xor(sum, 32, 64);
+      if (h == 0) share[wa * T::TB + in_b] = make_float2(top, sum);
       __builtin_amdgcn_sched_barrier(0);                             // (one j at a time in the registers)
     }
     __syncthreads();
@@ -651,8 +661,8 @@ __global__ __launch_bounds__(T::THREADS, T::MA * T::MB >= 8 ? 1 : 2) void fp8_ge
 #pragma unroll
       for (int w = 1; w < T::WA; ++w) {
         const float2 o = share[w * T::TB + r];
-        const float top = fmaxf(s.x, o.x);
-        s = make_float2(top, s.y * __builtin_amdgcn_exp2f((s.x - top) * slimact::LOG2E_HI) + o.y * __builtin_amdgcn_exp2f((o.x - top) * slimact::LOG2E_HI));
+        const float top = fmaxf(s.x, o.x), from = top == -__builtin_inff() ? 0.f : top;
+        s = make_float2(top, s.y * __builtin_amdgcn_exp2f((s.x - from) * slimact::LOG2E_HI) + o.y * __builtin_amdgcn_exp2f((o.x - from) * slimact::LOG2E_HI));
       }
       ga.sm.part[(int64_t)(b0 + r) * ga.sm.parts + a0 / T::TA] = s;
     }

@@ -2,8 +2,9 @@
 //
 //   z = Q(x) W^T,  loss = ln sum exp z - z[label];   dz = dloss (softmax z - [label]),  dx = Q(dz) W,  dW = Qt(dz)^T Qt(x)
 //
-// One product over the whole vocabulary leaves, of every tile, the maximum and the sum of exponentials of its classes for each token (fp8_gemm.hip,
-// fp8_few.hip); `head_join` puts a token's tiles together in fp64.  The loss alone needs no more: no logit is in memory.  The gradients need the logits a
+// One product over the whole vocabulary leaves, of every tile, the maximum and the sum of exponentials of its classes for each token, its label's apart
+// (fp8_gemm.hip, fp8_few.hip); `head_join` puts a token's tiles together in fp64.  dz at the label is -dloss times the others' share of the sum: as a difference
+// of the probability and one it is off by 6 % at 1 - p = 1e-6 and by a third at 1e-7.  The loss alone needs no more: no logit is in memory.  The gradients need the logits a
 // second time, once the sums are known.  Up to 64 Mi of them wait in memory in fp32, and `head_gradient` turns them into dz in e4m3, in blocks of 128
 // classes and of 128 tokens; of the classes behind those the product is made again, and its end does the same.  It goes a piece of the vocabulary
 // at a time, so that the 8-bit forms stay small, and the two products of the backward pass follow each piece in one launch; dx is
@@ -27,6 +28,9 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= t) return;
   const float2* p = part + row * parts;
+  const int64_t label = label_at(labels, labels64, row);
+  const bool live = label >= 0 && label < V;
+  const float at_label = live ? z[row] : 0.f;
   auto e = [](float x) { return slimact::exp_of(fmaxf(x, -126.f)); };
   constexpr int DEEP = 8;                          // pairs of a lane that are fetched together
   float own = -__builtin_inff();
@@ -43,15 +47,16 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
     for (int d = 0; d < DEEP; ++d) sum += (double)(v[d].y * e(v[d].x - most));
     own = most;
   }
-  const float top = wave_max_f32(own);
-  sum = wave_sum(sum * (double)e(own - top));
+  const float most = wave_max_f32(own);
+  sum = wave_sum(sum * (double)e(own - most));
   if (lane == 0) {
-    const int64_t label = label_at(labels, labels64, row);
-    const bool live = label >= 0 && label < V;
-    loss[row] = live ? (float)((double)top + log(sum) - (double)z[row]) : 0.f;
+    const float zl = live ? at_label : most, top = fmaxf(most, zl);
+    const double lead = (double)zl - (double)most, less = exp(-fabs(lead));      // (one of the two is 1; without a label: most, and no term of its own)
+    const double others = lead > 0.0 ? sum * less : sum, all = others + (!live ? 0.0 : lead > 0.0 ? 1.0 : less);
+    loss[row] = live ? (float)((double)top - (double)zl + log(all)) : 0.f;
     if (stat) {
       const float g = live ? dloss[row] : 0.f, fine = g - g == 0.f ? g : __builtin_nanf("");      // (an infinite one is NaN in 8 bits in any case)
-      stat[row] = TokenStat{top, fine, (float)((double)fine / sum), live ? (int)label : -1};
+      stat[row] = TokenStat{top, (float)(-(double)fine * (others / all)), (float)((double)fine / all), live ? (int)label : -1};
     }
   }
 }
@@ -94,7 +99,7 @@ __global__ __launch_bounds__(256) void head_gradient(GradientArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       float d = __builtin_amdgcn_exp2f((v[i][j] - s.top) * slimact::LOG2E_HI) * s.scaled;
-      if (at == j) d -= s.g;
+      if (at == j) d = s.own;
       v[i][j] = live && c0 + j < a.classes ? d : 0.f;
       unsigned u = __float_as_uint(v[i][j]) & 0x7fffffffu;           // (patterns order like the values)
       u = u < 0x7f800000u ? u : 0u;
