@@ -82,8 +82,22 @@ __device__ __forceinline__ double squares(const ClipTensor& t, int64_t chunk) {
   return s;
 }
 
+// A factor below 1 in two fp32 parts and, where fp32 has no room for it (gradients of 1e38 and a limit of 1e-6, say), an exponent: a product is rounded once
+// to fp32.  (In fp64 204 MB in fp16 took 158 us in place of 97, 810 MB in bf16 439 in place of 410.)
+struct Factor {
+  float hi, lo;
+  int exponent;
+  __device__ explicit Factor(double f) {
+    exponent = 0;
+    if (f < 0x1p-64) f = frexp(f, &exponent);
+    hi = (float)f;
+    lo = (float)(f - (double)hi);
+  }
+  __device__ __forceinline__ float times(float v) const { return ldexpf(fmaf(v, hi, v * lo), exponent); }
+};
+
 template <typename T>
-__device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, float factor, bool copy) {
+__device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, const Factor& factor, bool copy) {
   constexpr int E = Piece<T>::E;
   const int64_t e0 = chunk * (CL_BYTES / (int64_t)sizeof(T));
   if (t.ldi == 0) {
@@ -102,7 +116,7 @@ __device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, float 
       if (!copy) {
         float f[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = p[i].get(e) * factor;
+        for (int e = 0; e < E; ++e) f[e] = factor.times(p[i].get(e));
         p[i].set(f);
       }
       p[i].store(out + c, (int)min((int64_t)E, left - c));
@@ -110,7 +124,7 @@ __device__ __forceinline__ void scale(const ClipTensor& t, int64_t chunk, float 
   } else {
     each_element<T>(t, e0, [&](int64_t i, int64_t o) {
       if (copy) static_cast<T*>(t.out)[o] = static_cast<const T*>(t.in)[i];
-      else put<T>(t.out, o, value<T>(t.in, i) * factor);
+      else put<T>(t.out, o, factor.times(value<T>(t.in, i)));
     });
   }
 }
@@ -142,7 +156,7 @@ __global__ __launch_bounds__(CL_THREADS) void clip_scale(ClipArgs a, const doubl
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
   // a norm that is no finite fp32 number leaves everything as it is: the caller sees it and drops the step
   const bool copy = !(n > limit) || !((float)n < __builtin_inff());
-  const float factor = copy ? 1.f : (float)(limit / n);
+  const Factor factor(copy ? 1.0 : limit / n);
   for (int64_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
     const int64_t chunk = a.chunks - 1 - k;
     const ClipTensor& t = a.t[tensor_of(first, chunk)];
