@@ -181,11 +181,62 @@ slim_status check(slim_ctx* ctx, const char* fn, const slim_tensor* t, int count
     SLIM_REQUIRE(ctx, t[i].cols == 0 || t[i].rows <= (INT64_MAX >> 8) / t[i].cols, "%s: tensor %d is %lld x %lld", fn, i, (long long)t[i].rows,
                  (long long)t[i].cols);
     if (elements(t[i]) == 0) continue;
-    SLIM_REQUIRE(ctx, t[i].data && (t[i].rows == 1 || t[i].ld >= t[i].cols), "%s: null tensor %d, or rows that overlap (ld = %lld)", fn, i,
-                 (long long)t[i].ld);
+    SLIM_REQUIRE(ctx, t[i].data && (t[i].rows == 1 || (t[i].ld >= t[i].cols && t[i].ld <= (INT64_MAX >> 8) / t[i].rows)),
+                 "%s: null tensor %d, or rows that overlap (ld = %lld)", fn, i, (long long)t[i].ld);
     if (t[i].dtype != SLIM_F16 && t[i].dtype != SLIM_BF16 && t[i].dtype != SLIM_F32)
       return slim_fail(ctx, SLIM_ERR_UNSUPPORTED, "%s: tensor %d is not F16, BF16 or F32", fn, i);
   }
+  return SLIM_OK;
+}
+
+// A tensor's bytes: rows of `width`, `step` apart (no less); of tensor `index`, or of the norm (-1)
+struct Span {
+  uintptr_t begin, end, step, width;
+  int64_t rows;
+  int index;
+  bool written;
+};
+Span span_of(const slim_tensor& t, int index, bool written) {
+  const uintptr_t size = t.dtype == SLIM_F32 ? 4 : 2, begin = reinterpret_cast<uintptr_t>(t.data);
+  const bool dense = t.rows == 1 || t.ld == t.cols;
+  const uintptr_t width = (uintptr_t)(dense ? elements(t) : t.cols) * size, step = dense ? width : (uintptr_t)t.ld * size;
+  const int64_t rows = dense ? 1 : t.rows;
+  return {begin, begin + (uintptr_t)(rows - 1) * step + width, step, width, rows, index, written};
+}
+// whether any row of b meets one of a, which begins no later: of a's rows that begin before the end of a row of b the last one reaches farthest.  With
+// one step b's first row tells; else the rows of the one with fewer are gone through.
+bool meet(const Span& a, const Span& b) {
+  auto row_meets = [](const Span& s, uintptr_t from, uintptr_t to) {
+    if (to <= s.begin) return false;
+    const uintptr_t k = std::min<uintptr_t>((uintptr_t)s.rows - 1, (to - 1 - s.begin) / s.step);
+    return s.begin + k * s.step + s.width > from;
+  };
+  if (b.begin >= a.end) return false;
+  if (a.step == b.step) return row_meets(a, b.begin, b.begin + b.width);
+  const Span &few = a.rows < b.rows ? a : b, &many = a.rows < b.rows ? b : a;
+  for (int64_t i = 0; i < few.rows; ++i)
+    if (row_meets(many, few.begin + (uintptr_t)i * few.step, few.begin + (uintptr_t)i * few.step + few.width)) return true;
+  return false;
+}
+// Workgroups read and write in no order: an output is its own input, or in memory that nothing else here lies in.
+slim_status check_outputs(slim_ctx* ctx, const char* fn, const slim_tensor* in, const slim_tensor* out, int count, const float* norm) {
+  const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * (size_t)count + 1]);
+  if (!spans) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: host memory", fn);
+  Span* end = spans.get();
+  const uintptr_t place = reinterpret_cast<uintptr_t>(norm);
+  *end++ = {place, place + 4, 4, 4, 1, -1, true};
+  for (int i = 0; i < count; ++i) {
+    if (elements(out[i]) == 0) continue;
+    *end++ = span_of(out[i], i, true);
+    if (in != out && !(in[i].data == out[i].data && (in[i].rows == 1 || in[i].ld == out[i].ld))) *end++ = span_of(in[i], i, false);
+  }
+  std::sort(spans.get(), end, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  for (const Span* a = spans.get(); a != end; ++a)
+    for (const Span* b = a + 1; b != end && b->begin < a->end; ++b)
+      if ((a->written || b->written) && meet(*a, *b)) {
+        const Span &w = a->written && a->index >= 0 ? *a : *b, &o = &w == a ? *b : *a;
+        SLIM_REQUIRE(ctx, false, o.index < 0 ? "%s: output %d overlaps the norm" : o.written ? "%s: outputs %d and %d overlap" : "%s: output %d overlaps input %d", fn, w.index, o.index);
+      }
   return SLIM_OK;
 }
 
@@ -264,16 +315,10 @@ slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const
   SLIM_REQUIRE(ctx, limit >= 0.0, "%s: limit = %g", fn, limit);
   if (!out) out = tensors;
   if (const slim_status st = check(ctx, fn, out, count); st != SLIM_OK) return st;
-  const std::unique_ptr<const void*[]> written(new (std::nothrow) const void*[(size_t)count + 1]);
-  if (!written) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: host memory", fn);
-  const void** end = written.get();
-  for (int i = 0; i < count; ++i) {
+  for (int i = 0; i < count; ++i)
     SLIM_REQUIRE(ctx, out[i].rows == tensors[i].rows && out[i].cols == tensors[i].cols && out[i].dtype == tensors[i].dtype,
                  "%s: output %d is of another shape or type", fn, i);
-    if (elements(out[i])) *end++ = out[i].data;
-  }
-  std::sort(written.get(), end);
-  SLIM_REQUIRE(ctx, std::adjacent_find(written.get(), const_cast<const void**>(end)) == end, "%s: a tensor is written twice", fn);
+  if (const slim_status st = check_outputs(ctx, fn, tensors, out, count, norm); st != SLIM_OK) return st;
   return norm_and_scale(ctx, fn, tensors, out, count, limit, norm);
 }
 
