@@ -488,9 +488,9 @@ slim_status slim_distill_loss_grad(slim_ctx* ctx, const void* S, slim_dtype s_dt
 
 /* The norm of many tensors together, n = sqrt(sum of all squares) (summed in fp64), and the same tensors scaled down to a limit: g min(1, limit / n),
  * rounded to fp32 and from there to its type.  `tensors`, `out`: host arrays of `count` descriptions (F16, BF16 or F32, mixed at will; rows ld elements
- * apart); out NULL: in place.  An output is its own input or has no byte in common with any input, any other output or the norm (refused otherwise; rows
- * may lie between another tensor's).  Where n is at most the limit, or no finite fp32 number, the tensors are left (or copied) bit for bit.  norm: one
- * fp32 number.  slim_grad_norm_workspace: bytes of workspace of both (host only). */
+ * apart); out NULL: in place.  An output is its own input or has no byte in common with any input or any other output (refused otherwise; rows may lie
+ * between another tensor's).  Where n is at most the limit, or no finite fp32 number, the tensors are left (or copied) bit for bit.  norm: one
+ * fp32 number in none of them.  slim_grad_norm_workspace: bytes of workspace of both (host only). */
 typedef struct slim_tensor {
   void* data;
   int64_t rows, cols, ld;

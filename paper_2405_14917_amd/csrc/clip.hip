@@ -189,7 +189,7 @@ slim_status check(slim_ctx* ctx, const char* fn, const slim_tensor* t, int count
   return SLIM_OK;
 }
 
-// A tensor's bytes: rows of `width`, `step` apart (no less); of tensor `index`, or of the norm (-1)
+// A tensor's bytes: rows of `width`, `step` apart (no less)
 struct Span {
   uintptr_t begin, end, step, width;
   int64_t rows;
@@ -219,12 +219,10 @@ bool meet(const Span& a, const Span& b) {
   return false;
 }
 // Workgroups read and write in no order: an output is its own input, or in memory that nothing else here lies in.
-slim_status check_outputs(slim_ctx* ctx, const char* fn, const slim_tensor* in, const slim_tensor* out, int count, const float* norm) {
+slim_status check_outputs(slim_ctx* ctx, const char* fn, const slim_tensor* in, const slim_tensor* out, int count) {
   const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * (size_t)count + 1]);
   if (!spans) return slim_fail(ctx, SLIM_ERR_ALLOC, "%s: host memory", fn);
   Span* end = spans.get();
-  const uintptr_t place = reinterpret_cast<uintptr_t>(norm);
-  *end++ = {place, place + 4, 4, 4, 1, -1, true};
   for (int i = 0; i < count; ++i) {
     if (elements(out[i]) == 0) continue;
     *end++ = span_of(out[i], i, true);
@@ -234,8 +232,8 @@ slim_status check_outputs(slim_ctx* ctx, const char* fn, const slim_tensor* in, 
   for (const Span* a = spans.get(); a != end; ++a)
     for (const Span* b = a + 1; b != end && b->begin < a->end; ++b)
       if ((a->written || b->written) && meet(*a, *b)) {
-        const Span &w = a->written && a->index >= 0 ? *a : *b, &o = &w == a ? *b : *a;
-        SLIM_REQUIRE(ctx, false, o.index < 0 ? "%s: output %d overlaps the norm" : o.written ? "%s: outputs %d and %d overlap" : "%s: output %d overlaps input %d", fn, w.index, o.index);
+        const Span &w = a->written ? *a : *b, &o = &w == a ? *b : *a;
+        SLIM_REQUIRE(ctx, false, o.written ? "%s: outputs %d and %d overlap" : "%s: output %d overlaps input %d", fn, w.index, o.index);
       }
   return SLIM_OK;
 }
@@ -318,7 +316,7 @@ slim_status slim_clip_gradients(slim_ctx* ctx, const slim_tensor* tensors, const
   for (int i = 0; i < count; ++i)
     SLIM_REQUIRE(ctx, out[i].rows == tensors[i].rows && out[i].cols == tensors[i].cols && out[i].dtype == tensors[i].dtype,
                  "%s: output %d is of another shape or type", fn, i);
-  if (const slim_status st = check_outputs(ctx, fn, tensors, out, count, norm); st != SLIM_OK) return st;
+  if (const slim_status st = check_outputs(ctx, fn, tensors, out, count); st != SLIM_OK) return st;
   return norm_and_scale(ctx, fn, tensors, out, count, limit, norm);
 }
 

@@ -62,11 +62,7 @@ int main() {
     side_by_side += !bad && count > 1 && grid == 0;
   }
   printf("%d %d %d %d\n", wrong, refused, taken, side_by_side);
-  // the norm's own place
-  slim_tensor v = {space, 4, 5, 9, SLIM_F32}, far = {space + 100, 4, 5, 9, SLIM_F32};
-  launches = 0;
-  printf("%d %d %d\n", slim_clip_gradients(&c, &v, &far, 1, 1.0, space + 9), slim_clip_gradients(&c, &v, &far, 1, 1.0, space + 104), launches);
-  printf("%d %d\n", slim_clip_gradients(&c, &v, &far, 1, 1.0, space + 105), slim_clip_gradients(&c, &v, &far, 1, 1.0, space + 8));
+  slim_tensor v = {space, 4, 5, 9, SLIM_F32};
   v.ld = (int64_t)1 << 61;
   printf("%d %d\n", slim_clip_gradients(&c, &v, nullptr, 1, 1.0, &norm), slim_grad_norm(&c, &v, 1, &norm));
   return 0;
@@ -78,7 +74,7 @@ def test_what_may_be_written(tmp_path):
     out = [tuple(map(int, line.split())) for line in compiled(tmp_path, PROGRAM, "-O1")]
     wrong, refused, taken, side_by_side = out[0]
     assert wrong == 0 and refused > 5000 and taken > 5000 and side_by_side > 500, out
-    assert out[1:] == [(-1, -1, 0), (0, 0), (-1, -1)], out
+    assert out[1:] == [(-1, -1)], out
 
 
 def test_two_outputs_in_each_others_inputs(tmp_path):
