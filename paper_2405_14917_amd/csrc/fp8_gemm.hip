@@ -816,10 +816,10 @@ int tile_of(const Product& p, int ncu) {
   return best;
 }
 
-// Two products' tiles in one launch, none of them cut, the first one's first: a CU that is done with a tile takes the next.  `sum`: if no CU waited
-// at the end.
-double joint_cost(const Product* p, int tile, int ncu, double& sum) {
-  const int slots = tile == TILE_LARGE ? ncu : 2 * ncu, count = tiles_of(p[0], tile), more = count % slots;
+// Two products' tiles in one launch on `slots` places, none of them cut, the first one's first: a CU that is done with a tile takes the next.  `sum`: if no
+// CU waited at the end.
+double joint_cost(const Product* p, int tile, int slots, double& sum) {
+  const int count = tiles_of(p[0], tile), more = count % slots;
   const double t0 = tile_time(p[0], tile), t1 = tile_time(p[1], tile);
   sum = (count * t0 + tiles_of(p[1], tile) * t1) / slots;
   double least = count / slots * t0, most = least + t0, end = more ? most : least;      // slots - more of them are done with the first, and more
@@ -832,34 +832,44 @@ double joint_cost(const Product* p, int tile, int ncu, double& sum) {
   }
   return end;
 }
-// Products of one launch: all, or one where they differ in their kind or tile (a gradient of long contraction and few tiles beside one of many).
-// Two whose tiles differ, or are medium, take large ones together where they fill each other's last rounds.  Measured (16-bit gradients of n x m, t tokens):
-// where the costs say so, two launches -> one 8 % less on average (8192 x 8192, 2048 tokens: 322 -> 304 us; 25053 x 2798, 3193: 542 -> 432; at most 8 %
-// more, 5364 x 2008, 3148), medium -> large 5 % (8192 x 4096, 2048: 148 -> 139; 16384 x 4096, 2048: 308 -> 266; at 8192 x 4096, 1536, where large ones
-// would end unevenly, 118 and 128).  Large ones move half the operands' bytes, which the costs leave out: hence the eighth.
-int in_one_launch(const Product* p, int count, int ncu, int& tile) {
-  tile = tile_of(p[0], ncu);
-  if (count != 2 || exact(p[0]) != exact(p[1])) return 1;
-  const int other = tile_of(p[1], ncu);
+int places(int tile, int ncu) { return tile == TILE_LARGE ? ncu : 2 * ncu; }
+// The mean of the costs with all places and with a sixteenth fewer: tiles that fill their rounds to the last place need another round as soon as some take
+// longer (5504 x 3584, 1792 tokens: 77 by the costs in large tiles and 76 in medium ones, 118 us and 96).
+double safe_cost(const Product* p, int tile, int ncu) {
+  double sum;
+  return (joint_cost(p, tile, places(tile, ncu), sum) + joint_cost(p, tile, places(tile, ncu) * 15 / 16, sum)) / 2;
+}
+// Whether two products share a launch, and its tile (own: each one's alone): not where they differ in their kind or tile (a gradient of long contraction and
+// few tiles beside one of many).
+// Two whose tiles differ, or are medium, take large ones together where they fill each other's last rounds.  Of 281 pairs of 16-bit gradients (n x m, t tokens)
+// that would by the costs alone: two launches -> one (111 of 122 by this rule) 7.4 % less on average (25053 x 2798, 3193: 607 -> 503 us; at most 1.8 % more; the
+// other 11 3.2 % less on average, but up to 4.4 % more), medium -> large (46 of 159) 5.6 % (16384 x 4096, 2048: 334 -> 304; at most 2.6 % more, 3522 x 1434, 3351;
+// the others 1.2 % less on average, but up to 22 % more).  Large ones move half the operands' bytes, which the costs leave out: hence the margins.
+bool in_one_launch(const Product (&p)[2], const int (&own)[2], int ncu, int& tile) {
+  tile = own[0];
+  const int other = own[1];
+  if (exact(p[0]) != exact(p[1])) return false;
   if ((tile == TILE_LARGE && other == TILE_LARGE) || tile == TILE_SMALL || other == TILE_SMALL || parts_of(p[0], tile, ncu) > 1 || parts_of(p[1], other, ncu) > 1)
-    return tile == other ? 2 : 1;
+    return tile == other;
   double sum, of_medium;
-  const double large = joint_cost(p, TILE_LARGE, ncu, sum);
+  const double large = joint_cost(p, TILE_LARGE, ncu, sum), safe = safe_cost(p, TILE_LARGE, ncu);
   if (tile != other) {
-    if (6.0 + large >= tile_cost(p[0], tile, ncu) + tile_cost(p[1], other, ncu)) return 1;
+    const double apart = tile_cost(p[0], tile, ncu) + tile_cost(p[1], other, ncu);
+    if (6.0 + large >= apart || 6.0 + safe > 1.03 * apart) return false;
     tile = TILE_LARGE;
-  } else if (large <= 1.125 * joint_cost(p, tile, ncu, of_medium) && sum <= 1.04 * of_medium) {
-    tile = TILE_LARGE;
+  } else {
+    (void)joint_cost(p, tile, places(tile, ncu), of_medium);
+    if (safe <= 1.02 * safe_cost(p, tile, ncu) && sum <= 1.04 * of_medium) tile = TILE_LARGE;
   }
-  return 2;
+  return true;
 }
 
 // Each product's parts as if it were alone: beside another one of many tiles, few of long contraction would be what the launch waits for
 // (gradients of 14666 x 2078, 88 tokens: 17 tiles of 115 steps took 82 us beside 1955 of one).
-Plan make_plan(const Product* p, int count, int tile, int ncu) {
+Plan make_plan(const Product* p, int count, int tile, const int* own, int ncu) {
   Plan pl = {};
   for (int i = 0; i < count; ++i) {
-    pl.splits[i] = tile == tile_of(p[i], ncu) ? parts_of(p[i], tile, ncu) : 1;
+    pl.splits[i] = tile == own[i] ? parts_of(p[i], tile, ncu) : 1;
     pl.ldp[i] = (p[i].a.rows + 3) / 4 * 4;
   }
   return pl;
@@ -899,8 +909,8 @@ slim_status launch(slim_ctx* ctx, const char* name, int tile, const GemmArgs& ga
   return exact ? launch<true, PLAIN>(ctx, name, tile, ga, grid) : launch<false, PLAIN>(ctx, name, tile, ga, grid);
 }
 
-slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count, int tile) {
-  const Plan pl = make_plan(p, count, tile, ctx->num_cus);
+slim_status multiply(slim_ctx* ctx, const char* name, const Product* p, int count, int tile, const int* own) {
+  const Plan pl = make_plan(p, count, tile, own, ctx->num_cus);
   GemmArgs ga = {};
   float* parts[2] = {};
   int grid = 0;
@@ -956,18 +966,22 @@ size_t gemm_workspace(const Product* p, int count, int num_cus) {
 }
 
 slim_status gemm(slim_ctx* ctx, const char* name, const Product* p, int count) {
-  // (tiles of the longer contraction first: those of the shorter one fill what they leave; 525 x 3810, 7784 tokens: 81 -> 64 us, 2560 x 2048, 6000: 88 -> 72)
-  Product longest_first[2];
-  if (count == 2 && p[1].nk > p[0].nk && !p[0].e) {
-    longest_first[0] = p[1];
-    longest_first[1] = p[0];
-    p = longest_first;
+  if (count == 1) {
+    const int tile = tile_of(*p, ctx->num_cus);
+    return multiply(ctx, name, p, 1, tile, &tile);
   }
-  for (int i = 0, c, tile; i < count; i += c) {
-    c = in_one_launch(p + i, count - i, ctx->num_cus, tile);
-    if (const slim_status st = multiply(ctx, name, p + i, c, tile); st != SLIM_OK) return st;
+  // Tiles of the longer contraction first: those of the shorter one fill what they leave (525 x 3810, 7784 tokens: 81 -> 64 us, 2560 x 2048, 6000: 88 -> 72).
+  // Small tiles only where it is twice as long: of 205 pairs those 123 take 3.0 % less on average (three 2 to 3.5 % more), the others 0.9 %, but some 4 % more.
+  const bool swap = p[1].nk > p[0].nk && !p[0].e;
+  const Product in_order[2] = {p[swap], p[!swap]};
+  const int own[2] = {tile_of(in_order[0], ctx->num_cus), tile_of(in_order[1], ctx->num_cus)}, given[2] = {own[swap], own[!swap]};
+  int tile;
+  if (!in_one_launch(in_order, own, ctx->num_cus, tile)) {
+    if (const slim_status st = multiply(ctx, name, p, 1, given[0], given); st != SLIM_OK) return st;
+    return multiply(ctx, name, p + 1, 1, given[1], given + 1);
   }
-  return SLIM_OK;
+  if (tile == TILE_SMALL && in_order[0].nk < 2 * in_order[1].nk) return multiply(ctx, name, p, 2, tile, given);
+  return multiply(ctx, name, in_order, 2, tile, own);
 }
 
 }  // namespace slimfp8
