@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void head_join(const float2* __restrict__ part
     const float zl = live ? at_label : most, top = fmaxf(most, zl);
     const double lead = (double)zl - (double)most, less = exp(-fabs(lead));      // (one of the two is 1; without a label: most, and no term of its own)
     const double others = lead > 0.0 ? sum * less : sum, all = others + (!live ? 0.0 : lead > 0.0 ? 1.0 : less);
-    loss[row] = live ? (float)((double)top - (double)zl + log(all)) : 0.f;
+    loss[row] = live ? (float)((double)top - (double)zl + (lead > 0.0 ? log1p(others) : log(all))) : 0.f;
     if (stat) {
       const float g = live ? dloss[row] : 0.f, fine = g - g == 0.f ? g : __builtin_nanf("");      // (an infinite one is NaN in 8 bits in any case)
       stat[row] = TokenStat{top, (float)(-(double)fine * (others / all)), (float)((double)fine / all), live ? (int)label : -1};

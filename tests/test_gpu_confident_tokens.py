@@ -108,3 +108,18 @@ def test_labels_alone_in_their_tile(slim, V, t):
     product_of_range(*gradient_range(dz - e, dz + e, "rows"), B, dX, False)
     if V == 1:
         assert not loss.any() and not dX.any() and not dW.any()
+
+
+@pytest.mark.parametrize("t", [5, 300])
+def test_losses_below_the_last_digit_of_one(slim, t):
+    """Losses down to fp32's smallest numbers, not zero."""
+    V, m = 900, 64
+    W, X, labels, dloss = confident(V, m, t, torch.float16, 4)
+    w = W[labels]
+    X = (w / (w * w).sum(1, keepdim=True) * torch.linspace(70.0, 130.0, t)[:, None]).half()
+    q, s, qt, st = slim.fp8_quantize_weights(W.cuda())
+    loss = slim.head_loss_grad(X.cuda(), q, s, qt, st, labels.cuda(), dloss.cuda(), dw=False)[0]
+    assert torch.equal(loss, slim.head_loss(X.cuda(), q, s, labels.cuda()))
+    want, _, _, rel, _, _ = expected(W, X, labels)
+    assert float(want.max()) < 2.0 ** -24 and float(want.min()) < 1e-25
+    assert bool(((loss.double().cpu() - want).abs() <= (rel + U) * want + 2.0 ** -149).all()) and bool((loss > 0).all())
