@@ -47,3 +47,29 @@ def test_large_tiles_together_only_with_room(tmp_path):
             assert grids == [large], ((n, m, t), grids)
         else:
             assert grids == [medium] or len(grids) == 2, ((n, m, t), grids)
+
+
+HEAD_PROGRAM = PROGRAM[:PROGRAM.index("  for (auto [n, m, t]")] + r"""
+  for (auto [V, m, t] : {SHAPES}) {
+    calls = 0;
+    const int64_t ld = (V + 127) / 128 * 128 + 4096;
+    const slim_status st = slim_head_loss_grad(&c, p, SLIM_BF16, t, ld, u, ld, u, 4096, u, ld, u, 4096, V, m, p, 1, reinterpret_cast<const float*>(p),
+                                               reinterpret_cast<float*>(p), p, ld, nullptr, SLIM_F32, ld);
+    printf("%d", st);
+    for (int i = 0; i < calls; ++i) printf(" %u", grids[i]);
+    printf("\n");
+  }
+  return 0;
+}
+"""
+
+
+def test_logits_made_again_in_large_tiles(tmp_path):
+    """Of the sizes of test_gpu_head_pieces.py: X quantised, the logits, their sums, then of every piece the gradients (kept, or made again) and dX."""
+    sizes = [(40000, 2560, 2048, (32768,)), (16500, 2600, 8200, (7680, 15360))]
+    source = HEAD_PROGRAM.replace("SHAPES", ", ".join("std::tuple<int, int, int>(%d, %d, %d)" % s[:3] for s in sizes))
+    for (V, m, t, ends), line in zip(sizes, compiled(tmp_path, source, "-O1")):
+        status, x, logits, sums, *grids = map(int, line.split())
+        assert status == 0 and logits in (tiles(V, t, 256), tiles(V, t, 128)) and grids[0] == tiles(ends[0], t, 128), line
+        for first, end in zip(ends, (*ends[1:], V)):
+            assert tiles(end - first, t, 256) in grids[2:], (first, grids)
