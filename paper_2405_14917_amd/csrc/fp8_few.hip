@@ -235,7 +235,12 @@ namespace slimfp8 {
 // faster by 1 to 6 us (384 x 384, 3000 tokens, 54 blocks: 9.3 and 11.8; 4096 x 4096, 32 tokens, 64: 10.1 and 15.0; 512 x 8192, 128 tokens,
 // 64, the deepest: 13.5 and 14.5; the other way only 2048 x 128, 2000 tokens, 63: 12.5 and 11.7); from 66 to 126 either one is (1000 x 3000, 200
 // tokens, 96: 10.8 and 15.1; 700 x 700, 1000 tokens, 66: 14.3 and 11.5; 2048 x 256, 2000 tokens, 126: 17.4 and 11.7); from 128 on two are, but
-// for one shape.
+// for one shape.  Activations in 8 bits, whose other way is one launch too unless the product is cut, with gelu and kept sums: of 54 shapes up to 64 blocks one is at
+// most 1.3 % slower and 26 % faster (1000 x 1504, 301 tokens, 60 blocks: 11.6 and 11.7; 4096 x 4096, 32 tokens: 11.3 and 14.3) but for 636 x 153, 1952 tokens, 40:
+// 13.9 and 12.0; from 84 on either one (1000 x 1504, 600 tokens, 120: 12.6 and 11.7).  The head's loss: up to 16 tokens 10 to 59 % faster (32000 x 4096: 23.3 to 28.8
+// and 29.8 to 31.6), above them up to 64 blocks up to 51 %, but 19464 x 199, 76 tokens, 48 16.0 and 14.4 and 4169 x 770, 116, 63 17.3 and 13.7.  With its gradients, whose
+// activations are quantised anyway: up to 16 tokens 1 to 19 % faster, above them between 13 % faster (728 x 2316, 197 tokens, 57: 34 and 39) and 12 % slower
+// (4169 x 770, 116: 52 and 45).
 bool takes_few_tokens(int n, int m, int t, int ncu) {
   return t <= 16 || (t <= 65535 * 16 && least_busiest(n, t, ncu) * slim_cdiv(m, BLOCK) <= 64);
 }

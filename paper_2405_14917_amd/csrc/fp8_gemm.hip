@@ -13,7 +13,7 @@
 //  * The rows of A are the rows of an MFMA tile, so a lane ends up with 4 consecutive outputs of one row of C at a time; the tile goes through
 //    LDS, wavefront by wavefront, and leaves in rows.
 //  * What becomes of a tile's sums (MODE): they are stored; bias, residual and activation first (FINISH, the residuals fetched many at a
-//    time: 4096 x 11008 with 2048 tokens 110 us, one round of loads after another 120); of a tile of logits the maximum and the sum of exponentials
+//    time: 4096 x 11008 with 2048 tokens, on one card, 110 us, one round of loads after another 120); of a tile of logits the maximum and the sum of exponentials
 //    of every token, with or without the logits themselves (SOFTMAX); or the logits' gradients, quantised in both directions for the products behind them (GRADIENT).
 //  * Several products share a launch (the two gradients, where their outputs are of one kind).  A product whose tiles do not fill the chip
 //    is cut along the contraction; the parts go to the workspace in fp32 and are added in a fixed order by a second kernel.

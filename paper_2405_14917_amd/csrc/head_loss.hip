@@ -10,9 +10,9 @@
 // at a time, so that the 8-bit forms stay small, and the two products of the backward pass follow each piece in one launch; dx is
 // summed over the pieces in fp32.  Both products of logits keep 24 bits (the bf16 matrix cores): a difference of large logits is a probability's exponent.
 //
-// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1070 to 1090 us, of them the logits 437 (1.23 PFLOP/s; without
-// storing them 394), dz 78 (5.0 TB/s; made again 466), dx and dw 537 (2.00).  One token, the loss alone: 27 us, the weights' read
-// (5.0 TB/s), and 3 for `head_join`.
+// Bound by the matrix cores.  32000 x 4096, 2048 tokens, bf16, both gradients: 1075 to 1097 us, of them the logits 437 to 450 (1.2 PFLOP/s; without
+// storing them 394 to 405), dz 79 (5.0 TB/s; made again 466), dx and dw 537 (2.00).  One token, the loss alone: 23.5 to 27 us, the weights' read
+// (5.7 TB/s), and 4 for `head_join`.
 #include "act_device.h"
 #include "fp8_entry.h"
 
